@@ -298,6 +298,206 @@ seedq_status seedq_pack_stream(const seedq_layer *layer, const uint32_t *seed, c
 seedq_status seedq_fp64_fma_probe(int64_t iters, int32_t blocks_per_sm, double *out,
                                   void *cuda_stream, int64_t *fmas);
 
+/* ---------------------------------------------------------------- serving
+ * What stands between the compressed products of a decode step: which page of
+ * an 8-bit key/value cache each new token goes to (seedq_batch_plan), the
+ * cache write and its inverse (seedq_kv_append, seedq_kv_gather), the
+ * attention that reads the cache (seedq_kv_attend), and what a row of logits
+ * says about a token (seedq_token_logprobs).  No paper counterpart: the paper
+ * covers the weights only.
+ *
+ * All calls are hot calls: they validate on the host, enqueue one or two
+ * launches, allocate nothing and do not synchronize; every length, slot and
+ * page number stays on the device, so a step can be captured in a CUDA graph.
+ * Kernels check what they read from device memory (pages, slots, offsets)
+ * against the sizes given here and skip what is out of range. */
+
+/* Element types of activations and logits. */
+enum { SEEDQ_F32 = 0, SEEDQ_BF16 = 1, SEEDQ_F16 = 2 };
+
+/* Request states that seedq_batch_plan reports. */
+enum {
+  SEEDQ_REQ_OK = 0,
+  SEEDQ_REQ_NO_PAGES = 1,  /* the free stack ran out at or before this request */
+  SEEDQ_REQ_BAD = 2,       /* negative length, n_new < -1, or more pages than a table row holds */
+  SEEDQ_REQ_NO_ROOM = 3    /* its tokens pass max_tokens, or its returned pages pass free_capacity */
+};
+#define SEEDQ_MAX_REQUESTS 8192
+
+/* Page bookkeeping of one step, from request lengths alone.  For request i
+ * with L = seq_lens[i] tokens in the cache and n = n_new[i]:
+ *   n >= 0   it gets ceil((L+n)/P) - ceil(L/P) new pages (P = page_size) and
+ *            its tokens the positions L .. L+n-1;
+ *   n == -1  it is finished: its ceil(L/P) pages go back to the free stack.
+ * Returned pages are pushed first, in request order; new pages are then popped
+ * off the end of the stack in request order.  A request whose pages the stack
+ * cannot cover, counting those of all requests before it, gets none and its
+ * status says so; requests that need no page are still served.
+ *
+ * In:  seq_lens, n_new: n_requests int32.  block_table: n_requests rows of
+ *      table_width int32 at table_stride; row i lists its pages in order.
+ *      free_pages: free_capacity int32, the first *free_count of them free.
+ * Out: block_table and free_pages are updated in place (popped entries stay
+ *      behind).  free_count_out: entries left.  seq_lens_out: L+n if served,
+ *      0 if finished, else L.  starts: n_requests+1 token offsets (exclusive
+ *      sum of max(n, 0), at most max_tokens, whatever the status).  status:
+ *      SEEDQ_REQ_*.  Per token (max_tokens entries, the rest marked unused):
+ *      slots = page * P + offset, -1 for unused tokens and for those of
+ *      requests that were not served; positions, 0 where unused; requests, -1
+ *      where unused.
+ * All device memory; the outputs must not alias seq_lens, n_new or free_count.
+ * Errors: INVALID_ARG (NULL or aliased pointer, n_requests outside
+ * 1..SEEDQ_MAX_REQUESTS, max_tokens or page_size < 1, table_width outside
+ * 1..2^20 or above table_stride, free_capacity < 0), CUDA. */
+seedq_status seedq_batch_plan(int32_t n_requests, const int32_t *seq_lens, const int32_t *n_new,
+                              int32_t page_size, int32_t *block_table, int64_t table_stride,
+                              int32_t table_width, int32_t *free_pages, int32_t free_capacity,
+                              const int32_t *free_count, int32_t max_tokens, int64_t *slots,
+                              int32_t *positions, int32_t *requests, int32_t *seq_lens_out,
+                              int32_t *starts, int32_t *status, int32_t *free_count_out,
+                              void *cuda_stream);
+
+/* A paged key/value cache in 8 bits: n_pages pages of page_size tokens, and
+ * per page and key-value head one float32 scale for the keys and one for the
+ * values; a cached number is code * scale.  Codes are two's complement
+ * (SEEDQ_KV_INT8) or OCP E4M3 (SEEDQ_KV_E4M3; its two NaN codes are never
+ * written and read as +-480).  Token t of page p of head h begins at
+ * k + p * page_stride + h * head_stride + t * token_stride (bytes, multiples
+ * of 16, each at least head_dim), head_dim codes in a row; the same for v.
+ * k, v: device, 16-byte aligned.  k_scale, v_scale: device, n_pages x
+ * n_kv_heads, row-major.  head_dim: a multiple of 16, 16..256.  page_size: a
+ * multiple of 16, 16..256. */
+enum { SEEDQ_KV_INT8 = 0, SEEDQ_KV_E4M3 = 1 };
+typedef struct {
+  int32_t kind;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t page_size;
+  int64_t n_pages;
+  void *k;
+  void *v;
+  float *k_scale;
+  float *v_scale;
+  int64_t page_stride;
+  int64_t head_stride;
+  int64_t token_stride;
+} seedq_kv_cache;
+
+/* Write the keys and values of n_tokens new tokens at their slots (page *
+ * page_size + offset; a slot that is negative or past the cache is skipped).
+ * k, v: device, token t of head h at k + t * token_stride + h * head_stride
+ * (elements), head_dim elements in a row, of type dtype.  The tokens of one
+ * page must follow one another, as seedq_batch_plan lays them out; each run of
+ * consecutive slots among them is written as if by a call of its own, in order.
+ *
+ * Per page, head and tensor the scale is the smallest power of two s (at least
+ * 2^-126) with max|x| <= 127 s (448 s for E4M3), 0 where all x are 0, and a
+ * code is x / s rounded to nearest even.  If a run begins at the page's first
+ * token, s comes from its tokens alone (a reused page needs no
+ * clearing); otherwise s = max(scale of the page, s of the new tokens), and if
+ * that is larger than the page's scale, the codes before the first new one are
+ * rounded again under it.  With powers of two that is a shift, so all rounding
+ * of a value, however often its page's scale grows, stays below one step of the
+ * final scale.  A page that receives an infinity or a NaN gets the scale NaN:
+ * whatever reads it is NaN.
+ * Errors: INVALID_ARG (NULL pointer, n_tokens < 0, unknown dtype), UNSUPPORTED
+ * (head_dim, page_size, strides or alignment outside the above), CUDA.
+ * n_tokens = 0 is a no-op. */
+seedq_status seedq_kv_append(const seedq_kv_cache *cache, const void *k, const void *v,
+                             int32_t dtype, int64_t token_stride, int64_t head_stride,
+                             const int64_t *slots, int64_t n_tokens, void *cuda_stream);
+
+/* The inverse: k[t], v[t] = the cached numbers at slots[t] for every head,
+ * rounded once to dtype (strides as in seedq_kv_append); zeros for a slot that
+ * is negative or past the cache. */
+seedq_status seedq_kv_gather(const seedq_kv_cache *cache, const int64_t *slots, int64_t n_tokens,
+                             void *k, void *v, int32_t dtype, int64_t token_stride,
+                             int64_t head_stride, void *cuda_stream);
+
+/* Attention of the newest tokens over the cache, causal.  Request i owns the
+ * query tokens starts[i] .. starts[i+1]-1 of q (n_tokens rows in all) and
+ * seq_lens[i] cached tokens, its own newest among them: its query token t sits
+ * at position p = seq_lens[i] - (starts[i+1] - starts[i]) + t and sees the keys
+ * j <= p, and j > p - window if window > 0.  Query head h reads key-value head
+ * h / (n_heads / n_kv_heads):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,  lse = log sum_j exp(scale * q . k_j).
+ * A query that sees no key gets zeros and lse = -inf.  Keys past table_width
+ * pages and keys on pages outside the cache are left out.  Query rows that no
+ * request owns are not written.
+ *   q, out      device, row t of head h at t * token_stride + h * head_stride
+ *               (elements), head_dim in a row; each of its own type.
+ *   lse         device, n_tokens x n_heads float32, or NULL.
+ *   starts      n_requests + 1 int32; seq_lens, block_table as above.
+ *   max_new     the largest number of query tokens of a request (sizes the work
+ *               split and the workspace; a larger one is still computed right).
+ *   workspace   device, 16-byte aligned, at least
+ *               seedq_kv_attend_workspace_bytes(cache, n_heads, max_new) bytes,
+ *               zeroed once before its first use; calls that may overlap need
+ *               one each.
+ * Sums, the softmax statistics and the products' accumulators are float32.
+ * Errors: INVALID_ARG, UNSUPPORTED (as above; n_heads not a multiple of
+ * n_kv_heads), CUDA. */
+typedef struct {
+  int32_t n_requests;
+  int32_t n_heads;
+  int64_t n_tokens;
+  const void *q;
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  void *out;
+  int64_t out_token_stride;
+  int64_t out_head_stride;
+  int32_t q_dtype;
+  int32_t out_dtype;
+  float *lse;
+  const int32_t *seq_lens;
+  const int32_t *starts;
+  const int32_t *block_table;
+  int64_t table_stride;
+  int32_t table_width;
+  int32_t max_new;
+  int32_t window;
+  float scale;
+  void *workspace;
+  uint64_t workspace_bytes;
+} seedq_attend_args;
+
+/* 0 for arguments that seedq_kv_attend would refuse.  Host function (asks the
+ * current device for its number of SMs). */
+uint64_t seedq_kv_attend_workspace_bytes(const seedq_kv_cache *cache, int32_t n_heads,
+                                         int32_t max_new);
+seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_args *args,
+                             void *cuda_stream);
+
+/* What n_rows rows of logits say about one token each.  With z = scale * x over
+ * the vocab logits x of a row, lse = log sum exp z, p = exp(z - lse):
+ *   logprob[r]   z[target] - lse; 0 for target -1 (no target), NaN for any
+ *                other target outside the vocabulary
+ *   entropy[r]   -sum p log p
+ *   rank[r]      how many tokens come before the target, larger logits first and
+ *                lower index first among equals; -1 without a target
+ *   top_logprob, top_index[r][0..top_k-1]  the first top_k tokens in that order;
+ *                past the vocabulary -inf and -1.
+ * Logits of -inf count as excluded (p = 0); a row of nothing else has logprob
+ * and top_logprob -inf and entropy 0.  A row with a NaN or +inf has NaN for
+ * logprob, entropy and top_logprob (NaN counts as the largest for top_index;
+ * the rank of a row with a NaN is -1).
+ *   logits     device, row r at r * row_stride elements of type dtype.
+ *   targets    device int64, n_rows, or NULL (then logprob and rank are not
+ *              written and may be NULL).  entropy may be NULL.  top_k 0..32.
+ *   workspace  device, 16-byte aligned, seedq_token_logprobs_workspace_bytes
+ *              (n_rows, vocab) bytes, zeroed once before its first use; calls
+ *              that may overlap need one each.
+ * Errors: INVALID_ARG (NULL pointer, n_rows < 0, vocab outside 1..2^30,
+ * row_stride < vocab, scale not finite and positive, top_k out of range,
+ * workspace too small), CUDA.  n_rows = 0 is a no-op. */
+uint64_t seedq_token_logprobs_workspace_bytes(int64_t n_rows, int64_t vocab);
+seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab,
+                                  int64_t row_stride, float scale, const int64_t *targets,
+                                  float *logprob, float *entropy, int32_t *rank, int32_t top_k,
+                                  float *top_logprob, int32_t *top_index, void *workspace,
+                                  uint64_t workspace_bytes, void *cuda_stream);
+
 /* -------------------------------------------------------------- container
  * A file holding a compressed model: the global decoder table (Sec. 3.6, as
  * seedq_schedule) and, per tensor, what Alg. 2 reads besides it: shape,

@@ -83,6 +83,25 @@ class FactorDesc(C.Structure):
                 ("rho", C.POINTER(C.c_float))]
 
 
+class KvCacheDesc(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int64), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64)]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [("n_requests", C.c_int32), ("n_heads", C.c_int32), ("n_tokens", C.c_int64),
+                ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_token_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("q_dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("lse", C.c_void_p), ("seq_lens", C.c_void_p), ("starts", C.c_void_p),
+                ("block_table", C.c_void_p), ("table_stride", C.c_int64),
+                ("table_width", C.c_int32), ("max_new", C.c_int32), ("window", C.c_int32),
+                ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
 # Every symbol include/seedq.h declares, with its ctypes signature.
 SIGNATURES = {
     "seedq_layer_prepare": (C.c_int, [C.POINTER(LayerDesc), C.POINTER(Schedule), C.c_void_p,
@@ -136,6 +155,21 @@ SIGNATURES = {
                                  C.c_void_p, C.c_void_p, C.c_double, C.c_double, C.c_void_p,
                                  C.POINTER(C.c_int32), C.POINTER(C.c_double), C.c_void_p,
                                  C.c_void_p, C.c_void_p]),
+    "seedq_batch_plan": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                   C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p,
+                                   C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "seedq_kv_append": (C.c_int, [C.POINTER(KvCacheDesc), C.c_void_p, C.c_void_p, C.c_int32,
+                                  C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    "seedq_kv_gather": (C.c_int, [C.POINTER(KvCacheDesc), C.c_void_p, C.c_int64, C.c_void_p,
+                                  C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p]),
+    "seedq_kv_attend_workspace_bytes": (C.c_uint64, [C.POINTER(KvCacheDesc), C.c_int32, C.c_int32]),
+    "seedq_kv_attend": (C.c_int, [C.POINTER(KvCacheDesc), C.POINTER(AttendArgs), C.c_void_p]),
+    "seedq_token_logprobs_workspace_bytes": (C.c_uint64, [C.c_int64, C.c_int64]),
+    "seedq_token_logprobs": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64,
+                                       C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64,
+                                       C.c_void_p]),
     "seedq_status_string": (C.c_char_p, [C.c_int]),
     "seedq_last_cuda_error_string": (C.c_char_p, []),
 }
