@@ -360,8 +360,8 @@ seedq_status seedq_batch_plan(int32_t n_requests, const int32_t *seq_lens, const
 /* A paged key/value cache in 8 bits: n_pages pages of page_size tokens, and
  * per page and key-value head one float32 scale for the keys and one for the
  * values; a cached number is code * scale.  Codes are two's complement
- * (SEEDQ_KV_INT8) or OCP E4M3 (SEEDQ_KV_E4M3; its two NaN codes are never
- * written and read as +-480).  Token t of page p of head h begins at
+ * (SEEDQ_KV_INT8) or OCP E4M3 (SEEDQ_KV_E4M3; its NaN codes are never
+ * written).  Token t of page p of head h begins at
  * k + p * page_stride + h * head_stride + t * token_stride (bytes, multiples
  * of 16, each at least head_dim), head_dim codes in a row; the same for v.
  * k, v: device, 16-byte aligned.  k_scale, v_scale: device, n_pages x

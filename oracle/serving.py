@@ -72,11 +72,11 @@ LIMIT = {"int8": 127.0, "e4m3": 448.0}
 
 def e4m3_table():
     """The 256 numbers of the E4M3 codes (sign, 4 exponent bits of bias 7, 3
-    fraction bits); the two NaN codes as +-480, as the kernels read them."""
+    fraction bits; all of both set is NaN)."""
     v = np.zeros(256)
     for c in range(256):
         e, f = (c >> 3) & 15, c & 7
-        m = f / 8 * 2.0 ** -6 if e == 0 else (1 + f / 8) * 2.0 ** (e - 7)
+        m = np.nan if c & 127 == 127 else f / 8 * 2.0 ** -6 if e == 0 else (1 + f / 8) * 2.0 ** (e - 7)
         v[c] = -m if c >> 7 else m
     return v
 

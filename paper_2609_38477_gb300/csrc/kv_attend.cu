@@ -4,31 +4,33 @@
 // a head gives
 //   z_j = scale * s^k_j (q . c^k_j),  out = sum_j p_j s^v_j c^v_j / sum_j p_j,
 //   p_j = 2^(log2(e) z_j - m),  m a running maximum,
-// one pass over the keys.  Products run on the tensor cores as m16n8k16 binary16
-// products with float32 sums: codes are exact in binary16, and q and the weights
-// p_j s^v_j, which are not, are held as a high and a low half (22 bits).  A
-// decode step has few rows (query heads that share a key-value head, times new
-// tokens), so a tile carries 8 of them twice: the high halves in its rows 0-7,
-// the low halves in rows 8-15.  Both lands in the same thread, which adds them;
-// the second half costs no instruction.  Weights are taken relative to the
-// largest block scale so far and scaled by 2^14, so binary16's range never cuts
-// off more than 2^-39 of the largest.  Each step's products start from zero and
-// are added to float32 registers, so a long context is not accumulated inside
-// the tensor cores, which truncate.
+// one pass over the keys.  The products run on the tensor cores (m16n8k16,
+// binary16 with float32 sums) with the cache as the 16-row operand: a decode
+// step has few rows of its own (query heads that share a key-value head, times
+// new tokens) and they fit the 8 columns.  Codes are exact in binary16; q and
+// the weights p_j s^v_j, which are not, are held as a high and a low half (22
+// bits).  Up to 4 rows, the columns 0-3 carry the high and 4-7 the low halves of
+// the same rows and the second half costs nothing; from 5 rows on the low halves
+// are products of their own into the same sums.  q is scaled by a power of two
+// per row, weights are taken relative to the largest block scale so far and
+// scaled by 2^14, so binary16's range never cuts off more than 2^-38 of the
+// largest.  Each unit's products start from zero and are added to float32
+// registers, so a long context is not accumulated inside the tensor cores,
+// which truncate.
 //
 // What bounds it: the bytes of the cache, 2 head_dim per key and key-value
 // head.  At 8 rows a byte costs 16 operations, far below the balance, but every
-// code has to be widened (about 1.4 instructions) and multiplied.
+// code has to be widened (about 1.5 instructions) and multiplied.
 //
-// Layout.  For keys, a product's column is a token and its inner index the head
+// Layout.  For keys a product's row is a token and its inner index the head
 // dim; the order of the inner index is free as long as q uses the same, so each
-// lane takes 16 consecutive codes of one token (one 16-byte copy) and q's
+// lane takes 16 consecutive codes of a token (one 16-byte copy) and q's
 // fragments are laid out to match.  For values the inner index is the token and
-// a column a head dim, whose order is free again: lane (n, r) takes 16
-// consecutive codes of its four tokens.  So every lane copies (cp.async,
-// 16 bytes) exactly the codes it will multiply into a ring of its own in shared
-// memory: no barrier, no bank conflict, any strides, and what is past a
-// request's end is filled with zeros instead of being read.
+// a row a head dim, whose order is free again: lane (n, r) takes 16 consecutive
+// codes of its four tokens.  So every lane copies (cp.async, 16 bytes) exactly
+// the codes it will multiply into a ring of its own in shared memory: no
+// barrier, no bank conflict, any strides, and what is past a request's end is
+// filled with zeros instead of being read.
 //
 // Split.  The work list is every (request, key-value head, row tile) with its
 // keys in units of kUnit tokens; it is cut into equal ranges of units, one per
@@ -42,44 +44,55 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cp_async.cuh"
 #include "device_once.h"
+#include "f32x2.cuh"
 #include "serve.cuh"
 
 namespace seedq {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
 constexpr int kMaxCtas = 152;      // one per SM
 constexpr int kSmemMax = 227 * 1024;
+constexpr int kMaxChunks = 1024;   // entries of the table of units
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kWeight = 16384.f;  // weights are held times this
 
-template <int DP, int RT>
+// DP: head dim rounded up to 64, 128 or 256.  MODE: rows of a tile: 0: 4 (high
+// and low halves share the 8 columns), 1: 8, 2: 16.
+template <int DP, int MODE>
 struct Shape {
+  static constexpr int kRows = 4 << MODE;
+  static constexpr int kSets = MODE == 2 ? 2 : 1;    // sets of 8 columns
+  static constexpr int kHalves = MODE == 0 ? 1 : 2;  // operands per set
   static constexpr int kUnit = DP <= 128 ? 32 : 16;  // tokens of a unit
   static constexpr int kGroups = kUnit / 16;
-  static constexpr int kRows = 8 * RT;
   static constexpr int kChunks = DP / 64;            // 64 head dims: 16 codes of 4 lanes
   static constexpr int kVB = DP >= 128 ? 16 : 8;     // bytes of a lane's value piece
   static constexpr int kVParts = DP / (8 * kVB);
-  static constexpr int kTilesN = DP / 8;
+  static constexpr int kTiles = DP / 16;             // output tiles of 16 head dims
   static constexpr int kKeyPieces = kGroups * 2 * kChunks;
   static constexpr int kValPieces = kGroups * 4 * kVParts;
   static constexpr int kValAt = kKeyPieces * 512;
   static constexpr int kMetaAt = kValAt + kValPieces * 32 * kVB;
   static constexpr int kStage = kMetaAt + 16 * kGroups;  // meta: per group both scales and a flag
-  static constexpr int kSlot = kRows * (DP + 2);         // floats of a partial result: m, l, o
+  static constexpr int kWarps = (MODE == 2 || DP == 256) ? 8 : 12;
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kStages = DP == 64 ? 4 : kWarps == 12 ? 2 : 3;  // units in a warp's ring
+  static constexpr int kStats = 2 * 8 * kSets;                 // m and l of every column
+  static constexpr int kSlot = kStats + kSets * kTiles * 128;  // floats of a part: stats, then lanes' products
+  static_assert(kSlot * 4 <= kStages * kStage, "a part fits its warp's ring");
 };
 
 struct Args {
   seedq_kv_cache c;
   seedq_attend_args a;
-  int32_t group;       // query heads per key-value head
-  int32_t ctas, stages;
+  int32_t group;           // query heads per key-value head
+  int32_t ctas;
+  int32_t chunk;           // requests per entry of the table of units
   int32_t q_vec, out_vec;  // q / out rows allow 16-byte accesses
 };
 
@@ -89,21 +102,17 @@ __device__ __forceinline__ void cp_async16z(uint32_t dst, const void *src, bool 
 __device__ __forceinline__ void cp_async8z(uint32_t dst, const void *src, bool in) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(in ? 8 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async_wait_n(int n) {  // at most n groups pending
-  switch (n) {
-    case 0: cp_async_wait<0>(); break;
-    case 1: cp_async_wait<1>(); break;
-    case 2: cp_async_wait<2>(); break;
-    case 3: cp_async_wait<3>(); break;
-    default: cp_async_wait<4>(); break;
-  }
-}
-
-__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b)[2]) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
+}
+// Transpose of an 8 x 8 matrix of binary16 over the warp.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -120,26 +129,22 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t 
   lo = half2_bits(__floats2half2_rn(x - f.x, y - f.y));
 }
 
-// Widen the codes in bytes (0, 1) and (2, 3) of w.  int8: byte + 128 placed
-// under the exponent of 1024 is 1152 + code, exact.  E4M3: as code_value, less
-// its factor 2^8 (see code_unit).
-template <int KIND>
-__device__ __forceinline__ uint32_t widen(uint32_t w, uint32_t sel) {
-  if (KIND == SEEDQ_KV_INT8) {
-    const uint32_t x = __byte_perm(w, 0x64646464u, sel);
-    return half2_bits(__hsub2(*reinterpret_cast<const __half2 *>(&x), __float2half2_rn(1152.f)));
-  }
-  const uint32_t x = __byte_perm(w, 0u, sel);  // bytes to the top of each half
-  return ((x >> 1) & 0x3f803f80u) | (x & 0x80008000u);
-}
-template <int KIND>
-__device__ __forceinline__ uint32_t widen_lo(uint32_t w) { return widen<KIND>(w, KIND == SEEDQ_KV_INT8 ? 0x4140u : 0x1404u); }
-template <int KIND>
-__device__ __forceinline__ uint32_t widen_hi(uint32_t w) { return widen<KIND>(w, KIND == SEEDQ_KV_INT8 ? 0x4342u : 0x3424u); }
+// Widen the codes in bytes (0, 1) and (2, 3) of w to binary16, exactly.  int8:
+// byte + 128 placed under the exponent of 1024 is 1152 + code.
 template <int KIND>
 __device__ __forceinline__ uint32_t code_bias(uint32_t w) { return KIND == SEEDQ_KV_INT8 ? w ^ 0x80808080u : w; }
 template <int KIND>
-__device__ __forceinline__ constexpr float code_unit() { return KIND == SEEDQ_KV_INT8 ? 1.f : 256.f; }
+__device__ __forceinline__ uint32_t widen_lo(uint32_t w) {
+  if (KIND == SEEDQ_KV_E4M3) return e4m3x2_to_half2(w);
+  const uint32_t x = __byte_perm(w, 0x64646464u, 0x4140u);
+  return half2_bits(__hsub2(*reinterpret_cast<const __half2 *>(&x), __float2half2_rn(1152.f)));
+}
+template <int KIND>
+__device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
+  if (KIND == SEEDQ_KV_E4M3) return e4m3x2_to_half2(w >> 16);
+  const uint32_t x = __byte_perm(w, 0x64646464u, 0x4342u);
+  return half2_bits(__hsub2(*reinterpret_cast<const __half2 *>(&x), __float2half2_rn(1152.f)));
+}
 
 // A request's share of the work list.
 struct Req {
@@ -156,115 +161,177 @@ __device__ __forceinline__ Req request(const Args &p, int b) {
   r.first = min(max(p.a.starts[b], 0), n);
   r.fresh = max(min(max(p.a.starts[b + 1], 0), n) - r.first, 0);
   r.len = p.a.seq_lens[b];
-  const int64_t cap = (int64_t)p.a.table_width * p.c.page_size;
-  r.hi = (int)min((int64_t)max(r.len, 0), cap);
+  const int64_t cap = (int64_t)p.a.table_width * p.c.page_size;  // below 2^29
+  r.hi = min(max(r.len, 0), (int)cap);
   const int64_t lo = p.a.window > 0 ? (int64_t)r.len - r.fresh + 1 - p.a.window : 0;
   r.lo = (int)min(max(lo, (int64_t)0), (int64_t)r.hi);
   r.tiles = (int)(((int64_t)r.fresh * p.group + S::kRows - 1) / S::kRows);
   r.u0 = r.lo / S::kUnit;
-  r.units = max((int)((r.hi + (int64_t)S::kUnit - 1) / S::kUnit) - r.u0, 1);
+  r.units = max((r.hi + S::kUnit - 1) / S::kUnit - r.u0, 1);
   return r;
+}
+__device__ __forceinline__ int64_t units_of(const Args &p, const Req &r) {
+  return r.fresh ? (int64_t)r.units * r.tiles * p.c.n_kv_heads : 0;
 }
 
 // One entry of the work list: (request, key-value head, row tile).
 struct Entry {
   Req r;
   int b, h, tile;
-  int64_t begin, end;  // its units in the work list
+  int64_t begin;  // its first unit in the work list
 };
 template <typename S>
 __device__ __forceinline__ Entry entry_at(const Args &p, const int64_t *pre, int64_t u) {
   Entry e;
-  int lo = 0, hi = p.a.n_requests;
+  int lo = 0, hi = (p.a.n_requests + p.chunk - 1) / p.chunk;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (pre[mid] <= u) lo = mid;
     else hi = mid;
   }
-  e.b = lo;
-  e.r = request<S>(p, lo);
-  const int64_t k = (u - pre[lo]) / e.r.units;
-  e.h = (int)(k / e.r.tiles);
-  e.tile = (int)(k - (int64_t)e.h * e.r.tiles);
-  e.begin = pre[lo] + k * e.r.units;
-  e.end = e.begin + e.r.units;
+  int64_t base = pre[lo];
+  e.b = lo * p.chunk;
+  e.r = request<S>(p, e.b);
+  for (int i = 1; i < p.chunk; ++i) {
+    const int64_t n = units_of(p, e.r);
+    if (u < base + n) break;
+    base += n;
+    e.r = request<S>(p, ++e.b);
+  }
+  const int64_t x = u - base;
+  const int k = x >> 32 ? (int)(x / e.r.units) : (int)((uint32_t)x / (uint32_t)e.r.units);
+  e.h = k / e.r.tiles;
+  e.tile = k - e.h * e.r.tiles;
+  e.begin = base + (int64_t)k * e.r.units;
   return e;
 }
-
-// Where row `row` of an entry's tile goes; false if it holds no query.
 template <typename S>
-__device__ __forceinline__ bool row_of(const Args &p, const Entry &e, int row, int64_t &token, int &head, int &pos) {
-  const int r = e.tile * S::kRows + row, t = r / p.group;
-  token = e.r.first + t;
-  head = e.h * p.group + (r - t * p.group);
-  pos = e.r.len - e.r.fresh + t;
-  return t < e.r.fresh;
+__device__ __forceinline__ void next_entry(const Args &p, Entry &e) {  // only where one follows
+  e.begin += e.r.units;
+  if (++e.tile < e.r.tiles) return;
+  e.tile = 0;
+  if (++e.h < p.c.n_kv_heads) return;
+  e.h = 0;
+  do e.r = request<S>(p, ++e.b);
+  while (e.r.fresh == 0);
 }
 
-// Joins n partial results (each m, l per row in units of log2, then the rows'
-// averages o) into `to`, or, if to is null, writes the entry's output.  Weights
-// are l 2^m; averages, not sums, are kept, so nothing can overflow on the way.
-// The parts are from[0..n-1], or, without `from`, the second slot of the CTA
-// whose slots begin at from0 and the first slots of the n - 1 CTAs behind it.
-template <typename S, int DP, bool GLOBAL>
-__device__ void join(const Args &p, const Entry &e, int n, const float *const *from, const float *from0, int64_t step,
-                     float *to, float *wts) {
-  const int tid = threadIdx.x;
-  auto part = [&](int i) -> const float * { return from ? from[i] : i == 0 ? from0 + S::kSlot : from0 + i * step; };
-  auto get = [&](const float *x) { return GLOBAL ? __ldcg(x) : *x; };
-  float *ms = wts + n * S::kRows, *ls = ms + S::kRows;
-  if (tid < S::kRows) {
-    float m = -CUDART_INF_F, l = 0.f;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, get(part(i) + tid));
-    const float mu = m == -CUDART_INF_F ? 0.f : m;
-    for (int i = 0; i < n; ++i) {
-      const float w = get(part(i) + S::kRows + tid) * exp2_fast(get(part(i) + tid) - mu);
-      wts[i * S::kRows + tid] = w;
-      l += w;
+// What the products and the joins need to know of an entry.
+struct Desc {
+  int first, fresh, len, hi;
+  int h, tile;
+  int token0;  // the first token of a warp's first unit of it
+  int units;   // units of it that the warp holds
+  int64_t begin, end;
+};
+
+// Where a row of an entry's tile goes; false if it holds no query.
+template <typename S>
+__device__ __forceinline__ bool row_of(const Args &p, const Desc &e, int row, int64_t &token, int &head, int &pos) {
+  const int r = e.tile * S::kRows + row, t = r / p.group;
+  token = e.first + t;
+  head = e.h * p.group + (r - t * p.group);
+  pos = e.len - e.fresh + t;
+  return t < e.fresh;
+}
+
+template <int N>  // N = 2 or 4 elements in a row from i on
+__device__ __forceinline__ void store_row(void *out, int dt, int64_t i, const float (&x)[N], bool vec) {
+  if (!vec) {
+#pragma unroll
+    for (int y = 0; y < N; ++y) store_elem(out, dt, i + y, x[y]);
+  } else if (dt == SEEDQ_F32) {
+    if constexpr (N == 4) *(float4 *)((float *)out + i) = make_float4(x[0], x[1], x[2], x[3]);
+    else *(float2 *)((float *)out + i) = make_float2(x[0], x[1]);
+  } else {
+    uint32_t v[N / 2];
+#pragma unroll
+    for (int y = 0; y < N / 2; ++y) {
+      if (dt == SEEDQ_BF16) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * y], x[2 * y + 1]);
+        v[y] = *(const uint32_t *)&b;
+      } else {
+        v[y] = half2_bits(__floats2half2_rn(x[2 * y], x[2 * y + 1]));
+      }
     }
-    ms[tid] = m;
-    ls[tid] = l;
+    if constexpr (N == 4) *(uint2 *)((uint16_t *)out + i) = make_uint2(v[0], v[1]);
+    else *(uint32_t *)((uint16_t *)out + i) = v[0];
   }
-  __syncthreads();
-  for (int x = tid; x < S::kRows * DP; x += kThreads) {
-    const int row = x / DP, d = x - row * DP;
-    if (d >= p.c.head_dim) continue;
-    float o = 0.f;
+}
+
+// Joins n parts of an entry into `to`, or, if to is null, writes the entry's
+// output.  A part holds m (in units of log2) and l of every column and the
+// columns' averages o = sum / l as the products' accumulators lie in the lanes;
+// it weighs l 2^m.  Averages, not sums, are kept, so nothing overflows on the
+// way.  part(i) is the address of part i.  Every warp takes tiles of its own; a
+// lane reads the statistics of its two columns itself, so no barrier is needed.
+template <typename S, int MODE, bool GLOBAL, typename F>
+__device__ __forceinline__ void join(const Args &p, const Desc &e, int n, F part, float *to) {
+  const int lane = threadIdx.x & 31, nn = lane >> 2, q4 = lane & 3;
+  for (int tt = threadIdx.x >> 5; tt < S::kSets * S::kTiles; tt += S::kWarps) {
+    const int set = tt / S::kTiles, tile = tt - set * S::kTiles, col = set * 8 + 2 * q4;
+    auto stat = [&](int i, int at) -> float2 {
+      const float2 *x = (const float2 *)(part(i) + at);
+      return GLOBAL ? __ldcg(x) : *x;
+    };
+    float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F;
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
-      const float w = wts[i * S::kRows + row], v = get(part(i) + 2 * S::kRows + x);
-      o += w == 0.f ? 0.f : w * v;
+      const float2 m = stat(i, col);
+      m0 = fmaxf(m0, m.x);
+      m1 = fmaxf(m1, m.y);
     }
-    const float l = ls[row];
-    o = l == 0.f ? 0.f : o / l;
+    const float u0 = m0 == -CUDART_INF_F ? 0.f : m0, u1 = m1 == -CUDART_INF_F ? 0.f : m1;
+    float l0 = 0.f, l1 = 0.f, c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float2 m = stat(i, col), l = stat(i, S::kStats / 2 + col);
+      const float4 *src = (const float4 *)(part(i) + S::kStats) + tt * 32 + lane;
+      const float4 o = GLOBAL ? __ldcg(src) : *src;
+      const float w0 = l.x * exp2_fast(m.x - u0), w1 = l.y * exp2_fast(m.y - u1);
+      l0 += w0;
+      l1 += w1;
+      if (w0 != 0.f) c[0] = fmaf(w0, o.x, c[0]), c[2] = fmaf(w0, o.z, c[2]);
+      if (w1 != 0.f) c[1] = fmaf(w1, o.y, c[1]), c[3] = fmaf(w1, o.w, c[3]);
+    }
+    const float i0 = l0 == 0.f ? 0.f : __fdiv_rn(1.f, l0), i1 = l1 == 0.f ? 0.f : __fdiv_rn(1.f, l1);
+    c[0] *= i0;
+    c[1] *= i1;
+    c[2] *= i0;
+    c[3] *= i1;
     if (to) {
-      to[2 * S::kRows + x] = o;
-    } else {
+      if (tile == 0 && nn == 0) {
+        *(float2 *)(to + col) = make_float2(m0, m1);
+        *(float2 *)(to + S::kStats / 2 + col) = make_float2(l0, l1);
+      }
+      ((float4 *)(to + S::kStats))[tt * 32 + lane] = make_float4(c[0], c[1], c[2], c[3]);
+      continue;
+    }
+    if (MODE == 0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[k] += __shfl_xor_sync(~0u, c[k], 2);
+      if (q4 >= 2) continue;
+    }
+    const int d = (2 * tile / S::kVB) * 128 + nn * S::kVB + 2 * tile % S::kVB;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
       int64_t token;
       int head, pos;
-      if (row_of<S>(p, e, row, token, head, pos))
-        store_elem(p.a.out, p.a.out_dtype, token * p.a.out_token_stride + head * p.a.out_head_stride + d, o);
-    }
-  }
-  if (tid < S::kRows) {
-    if (to) {
-      to[tid] = ms[tid];
-      to[S::kRows + tid] = ls[tid];
-    } else if (p.a.lse) {
-      int64_t token;
-      int head, pos;
-      if (row_of<S>(p, e, tid, token, head, pos)) {
-        const float l = ls[tid];
-        p.a.lse[token * p.a.n_heads + head] = l == 0.f ? -CUDART_INF_F : (ms[tid] + log2f(l)) * kLn2;
+      if (!row_of<S>(p, e, col + k, token, head, pos)) continue;
+      const float x[2] = {c[k], c[2 + k]};
+      if (d < p.c.head_dim)
+        store_row<2>(p.a.out, p.a.out_dtype, token * p.a.out_token_stride + head * p.a.out_head_stride + d, x, p.out_vec);
+      if (p.a.lse && tile == 0 && nn == 0) {
+        const float l = k ? l1 : l0, m = k ? m1 : m0;
+        p.a.lse[token * p.a.n_heads + head] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
       }
     }
   }
-  __syncthreads();
 }
 
-template <int KIND, int DP, int RT>
-__global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ Args p) {
-  using S = Shape<DP, RT>;
+template <int KIND, int DP, int MODE>
+__global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const __grid_constant__ Args p) {
+  using S = Shape<DP, MODE>;
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int nn = lane >> 2, q4 = lane & 3;
@@ -272,108 +339,136 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ 
 
   // ---- the work list: exclusive sums of the requests' units
   int64_t *pre = (int64_t *)smem;
-  __shared__ int64_t s_sums[kWarps];
-  {
-    int64_t base = 0;
-    for (int b0 = 0; b0 < B; b0 += kThreads) {
-      const int b = b0 + tid;
-      int64_t u = 0;
-      if (b < B) {
-        const Req r = request<S>(p, b);
-        u = r.fresh ? (int64_t)r.units * r.tiles * p.c.n_kv_heads : 0;
-      }
-      int64_t x = u;
+  const int nc = (B + p.chunk - 1) / p.chunk;
+  __shared__ int64_t s_sums[S::kWarps];
+  int64_t total = 0;
+  for (int i0 = 0; i0 < nc; i0 += S::kThreads) {
+    const int i = i0 + tid;
+    int64_t u = 0;
+    for (int b = i * p.chunk; b < min((i + 1) * p.chunk, B); ++b) u += units_of(p, request<S>(p, b));
+    int64_t x = u;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(~0u, x, o);
-        if (lane >= o) x += y;
-      }
-      if (lane == 31) s_sums[w] = x;
-      __syncthreads();
-      int64_t before = base;
-      for (int i = 0; i < kWarps; ++i) {
-        if (i < w) before += s_sums[i];
-        base += s_sums[i];
-      }
-      if (b < B) pre[b] = before + x - u;
-      __syncthreads();
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(~0u, x, o);
+      if (lane >= o) x += y;
     }
-    if (tid == 0) pre[B] = base;
+    if (lane == 31) s_sums[w] = x;
+    __syncthreads();
+    int64_t before = total;
+    for (int k = 0; k < S::kWarps; ++k) {
+      if (k < w) before += s_sums[k];
+      total += s_sums[k];
+    }
+    if (i < nc) pre[i] = before + x - u;
+    __syncthreads();
   }
-  __syncthreads();
-  const int64_t total = pre[B];
   // Units per CTA: even shares, but at least one unit per warp, so that a short
   // context is joined within few CTAs.
-  const int64_t share = max((total + p.ctas - 1) / p.ctas, (int64_t)kWarps);
+  const int64_t share = max((total + p.ctas - 1) / p.ctas, (int64_t)S::kWarps);
   const int64_t c0 = min(share * blockIdx.x, total), c1 = min(c0 + share, total);
   if (c0 >= c1) return;
-  const int64_t w0 = c0 + (c1 - c0) * w / kWarps, w1 = c0 + (c1 - c0) * (w + 1) / kWarps;
+  const int64_t w0 = c0 + (c1 - c0) * w / S::kWarps, w1 = c0 + (c1 - c0) * (w + 1) / S::kWarps;
+  const int units = (int)(w1 - w0);
 
-  const int ring_at = ((B + 1) * 8 + 15) & ~15;
-  uint8_t *ring = smem + ring_at + (size_t)w * p.stages * S::kStage;
+  const int ring_at = ((nc + 1) * 8 + 15) & ~15;
+  uint8_t *ring = smem + ring_at + (size_t)w * S::kStages * S::kStage;
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
 
   float *ws = (float *)((uint8_t *)p.a.workspace + kMaxCtas * 4);
   float *cta_slots = ws + (size_t)blockIdx.x * 2 * S::kSlot;
-  float *head_slot = ws + (size_t)kMaxCtas * 2 * S::kSlot + ((size_t)blockIdx.x * kWarps + w) * S::kSlot;
+  // Entries on their way from the copies to the products.
+  __shared__ Desc s_desc[S::kWarps][S::kStages + 1];
   // Parts of cut entries, in the order of their keys: [2 w] a warp's first
   // entry if more follow, [2 w + 1] its last.
-  __shared__ const float *s_part[2 * kWarps];
-  __shared__ int64_t s_begin[2 * kWarps];
-  if (lane == 0) s_begin[2 * w] = s_begin[2 * w + 1] = -1;
+  __shared__ Desc s_cut[2 * S::kWarps];
+  if (lane < 2) s_cut[2 * w + lane].units = 0;
 
   // ---- copies
   const int gpp = p.c.page_size >> 4;  // groups of 16 tokens per page
-  Entry pe;                            // the entry being copied
-  int64_t pu = w0;                     // next unit to copy
-  int pgb = 0, ids = -1, ids_next = -1, pstage = 0, stage = 0;
+  const int64_t ts = p.c.token_stride, ts8 = 8 * ts;
+  const uint8_t *klane = (const uint8_t *)p.c.k + nn * ts + q4 * 16;
+  const uint8_t *vlane = (const uint8_t *)p.c.v + 2 * q4 * ts + nn * S::kVB;
+  Entry pe{};  // the entry being copied
   const int32_t *prow = nullptr;
-  pe.end = w0;
-  auto load_ids = [&](int g) -> int {  // page of group g + lane of the entry being copied
+  int pleft = 0;               // its units still to copy by this warp
+  int pg = 0, pgb = 0;         // the next group of 16 tokens; the group of lane 0's page
+  int poff = 0;                // the next group's place in its page
+  int ids = -1, ids_next = -1; // pages of the groups pgb + lane and pgb + 32 + lane
+  int pstage = 0, pdesc = 0, cdesc = 0, stage = 0, to_copy = units;
+  auto load_ids = [&](int g) -> int {
     const int64_t gl = (int64_t)g + lane;
-    return gl * 16 < pe.r.hi ? __ldg(prow + gl / gpp) : -1;
+    return gl * 16 < pe.r.hi ? __ldg(prow + (int)gl / gpp) : -1;
   };
-  auto issue = [&]() {
-    if (pu < w1) {
-      if (pu >= pe.end) {
-        pe = entry_at<S>(p, pre, pu);
+
+  // ---- products
+  uint32_t qf[S::kSets][S::kHalves][S::kChunks * 4][2];  // q as the second operand
+  float zf[S::kSets][2];      // z in units of log2 per unit of product, but for the key scale
+  int pos[S::kSets][2];       // positions of the lane's columns
+  float m[S::kSets][2], l[S::kSets][2], vmax = 0.f;
+  uint64_t o[S::kSets][S::kTiles][2];  // sums of the columns (2 q4, 2 q4 + 1) for two head dims
+  int cleft = 0, tok = 0, hi = 0, pos_first = 0, pos_last = 0;
+
+#pragma unroll 1
+  for (int it = 1 - S::kStages; it < units; ++it) {
+    __syncwarp();  // all lanes are done with the stage that is filled next
+    if (to_copy > 0) {
+      if (pleft == 0) {
+        if (to_copy == units) pe = entry_at<S>(p, pre, w0);
+        else next_entry<S>(p, pe);
+        const int64_t from = max(pe.begin, w0);
+        pleft = (int)(min(pe.begin + pe.r.units, w1) - from);
         prow = p.a.block_table + (int64_t)pe.b * p.a.table_stride;
-        pgb = (pe.r.u0 + (int)(pu - pe.begin)) * S::kGroups;
+        pg = pgb = (pe.r.u0 + (int)(from - pe.begin)) * S::kGroups;
+        poff = pg % gpp;
         ids = load_ids(pgb);
         ids_next = load_ids(pgb + 32);
+        if (lane == 0) {
+          Desc &x = s_desc[w][pdesc];
+          x.first = pe.r.first, x.fresh = pe.r.fresh, x.len = pe.r.len, x.hi = pe.r.hi;
+          x.h = pe.h, x.tile = pe.tile, x.token0 = pg * 16, x.units = pleft;
+          x.begin = pe.begin, x.end = pe.begin + pe.r.units;
+        }
+        pdesc = pdesc == S::kStages ? 0 : pdesc + 1;
       }
+      --pleft;
+      --to_copy;
       const uint32_t dst = ring_s + pstage * S::kStage;
-      pstage = pstage + 1 == p.stages ? 0 : pstage + 1;
-      const int g0 = (pe.r.u0 + (int)(pu - pe.begin)) * S::kGroups;
-      if (g0 - pgb >= 32) {
+      pstage = pstage + 1 == S::kStages ? 0 : pstage + 1;
+      if (pg - pgb >= 32) {
         pgb += 32;
         ids = ids_next;
         ids_next = load_ids(pgb + 32);
       }
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g) {
-        const int gi = g0 + g, page = __shfl_sync(~0u, ids, gi - pgb);
-        const int t0 = gi * 16;
+        const int page = __shfl_sync(~0u, ids, pg - pgb);
+        const int t0 = pg * 16;
         const bool in = page >= 0 && page < p.c.n_pages && t0 + 16 > pe.r.lo;  // ids is -1 past hi
         const int left = in ? pe.r.hi - t0 : 0;                                // tokens of the group that exist
-        const int64_t at = in ? page * p.c.page_stride + pe.h * p.c.head_stride + (int64_t)(gi % gpp) * 16 * p.c.token_stride : 0;
-        const uint8_t *kp = (const uint8_t *)p.c.k + at, *vp = (const uint8_t *)p.c.v + at;
+        const int64_t at = in ? page * p.c.page_stride + pe.h * p.c.head_stride + poff * 16 * ts : 0;
+        ++pg;
+        poff = poff + 1 == gpp ? 0 : poff + 1;
+        const uint8_t *kp = klane + at, *vp = vlane + at;
+        const uint32_t kd = dst + g * (2 * S::kChunks * 512) + lane * 16;
+        const uint32_t vd = dst + S::kValAt + g * (4 * S::kVParts * 32 * S::kVB) + lane * S::kVB;
+        const bool full = left >= 16 && D == DP;  // every copy is wanted
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int c = 0; c < S::kChunks; ++c) {
-            const int j = t * 8 + nn, d = c * 64 + q4 * 16;
-            const bool ok = j < left && d < D;
-            cp_async16z(dst + ((g * 2 + t) * S::kChunks + c) * 512 + lane * 16, ok ? kp + j * p.c.token_stride + d : (const uint8_t *)p.c.k, ok);
+            const bool ok = full || (t * 8 + nn < left && c * 64 + q4 * 16 < D);
+            const uint8_t *src = kp + t * ts8 + c * 64;
+            cp_async16z(kd + (t * S::kChunks + c) * 512, ok ? src : (const uint8_t *)p.c.k, ok);
           }
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int c = 0; c < S::kVParts; ++c) {
-            const int j = (t >> 1) * 8 + q4 * 2 + (t & 1), d = c * 128 + nn * S::kVB;
-            const bool ok = j < left && d < D;
-            const uint32_t to = dst + S::kValAt + ((g * 4 + t) * S::kVParts + c) * (32 * S::kVB) + lane * S::kVB;
-            const uint8_t *src = ok ? vp + j * p.c.token_stride + d : (const uint8_t *)p.c.v;
+            const int j = (t >> 1) * 8 + q4 * 2 + (t & 1);
+            const bool ok = full || (j < left && c * 128 + nn * S::kVB < D);
+            const uint32_t to = vd + (t * S::kVParts + c) * (32 * S::kVB);
+            const uint8_t *src = vp + (t >> 1) * ts8 + (t & 1) * ts + c * 128;
+            if (!ok) src = (const uint8_t *)p.c.v;
             if (S::kVB == 16) cp_async16z(to, src, ok);
             else cp_async8z(to, src, ok);
           }
@@ -389,95 +484,97 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ 
           asm volatile("st.shared.s32 [%0], %1;" ::"r"(meta + 8), "r"(in ? 1 : 0) : "memory");
         }
       }
-      ++pu;
     }
     cp_async_commit();
-  };
-  for (int i = 0; i < p.stages - 1; ++i) issue();
+    if (it < 0) continue;
 
-  // ---- products
-  uint32_t qf[RT][S::kChunks * 4][4];  // q as the products' first operand: high and low halves
-  float zf[RT];                        // z in units of log2 per unit of product, but for the key scale
-  int pos[RT];                         // the rows' positions
-  float o[RT][S::kTilesN][2];
-  float m[RT], l[RT], vmax = 0.f;
-  Entry e;
-  e.end = w0;
-  int pos_first = 0, pos_last = 0;
-
-  for (int64_t u = w0; u < w1; ++u) {
-    if (u >= e.end) {  // a new entry: its queries
-      e = entry_at<S>(p, pre, u);
+    if (cleft == 0) {  // a new entry: its queries
+      const Desc e = s_desc[w][cdesc];
+      cleft = e.units;
+      tok = e.token0;
+      hi = e.hi;
       vmax = 0.f;
-      pos_first = e.r.len - e.r.fresh + (e.tile * S::kRows) / p.group;
-      pos_last = min(e.r.len - e.r.fresh + (e.tile * S::kRows + S::kRows - 1) / p.group, e.r.len - 1);
+      pos_first = e.len - e.fresh + (e.tile * S::kRows) / p.group;
+      pos_last = min(e.len - e.fresh + (e.tile * S::kRows + S::kRows - 1) / p.group, e.len - 1);
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        m[i] = -CUDART_INF_F;
-        l[i] = 0.f;
+      for (int s = 0; s < S::kSets; ++s) {
 #pragma unroll
-        for (int j = 0; j < S::kTilesN; ++j) o[i][j][0] = o[i][j][1] = 0.f;
+        for (int j = 0; j < S::kTiles; ++j) o[s][j][0] = o[s][j][1] = 0;
         int64_t token;
-        int head;
-        const bool real = row_of<S>(p, e, i * 8 + nn, token, head, pos[i]);
+        int head, ps;
+        const bool real = row_of<S>(p, e, MODE == 0 ? nn & 3 : s * 8 + nn, token, head, ps);
         const int64_t at = real ? token * p.a.q_token_stride + head * p.a.q_head_stride : 0;
         float x[S::kChunks * 16], amax = 0.f;
 #pragma unroll
-        for (int c = 0; c < S::kChunks; ++c) {
-          const int d = c * 64 + q4 * 16;
-          if (!real || d >= D) {
+        for (int k = 0; k < S::kChunks * 16; ++k) x[k] = 0.f;
+        if (p.q_vec && p.a.q_dtype == SEEDQ_F32) {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) x[c * 16 + k] = 0.f;
-          } else if (p.q_vec && p.a.q_dtype == SEEDQ_F32) {
-            const float4 *src = (const float4 *)((const float *)p.a.q + at + d);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float4 f = __ldg(src + k);
-              x[c * 16 + k * 4] = f.x, x[c * 16 + k * 4 + 1] = f.y, x[c * 16 + k * 4 + 2] = f.z, x[c * 16 + k * 4 + 3] = f.w;
+          for (int k = 0; k < S::kChunks * 4; ++k) {
+            const int d = (k >> 2) * 64 + q4 * 16 + (k & 3) * 4;
+            if (real && d < D) {
+              const float4 f = __ldg((const float4 *)((const float *)p.a.q + at + d));
+              x[k * 4] = f.x, x[k * 4 + 1] = f.y, x[k * 4 + 2] = f.z, x[k * 4 + 3] = f.w;
             }
-          } else if (p.q_vec) {
-            const uint4 *src = (const uint4 *)((const uint16_t *)p.a.q + at + d);
+          }
+        } else if (p.q_vec) {
+          const bool bf = p.a.q_dtype == SEEDQ_BF16;
+          uint4 v[S::kChunks * 2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const uint4 f = __ldg(src + k);
-              const uint32_t v[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-              for (int y = 0; y < 4; ++y) {
-                float2 g;
-                if (p.a.q_dtype == SEEDQ_BF16) g = make_float2(__uint_as_float(v[y] << 16), __uint_as_float(v[y] & 0xffff0000u));
-                else g = __half22float2(*reinterpret_cast<const __half2 *>(&v[y]));
-                x[c * 16 + k * 8 + y * 2] = g.x;
-                x[c * 16 + k * 8 + y * 2 + 1] = g.y;
-              }
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) x[c * 16 + k] = load_elem(p.a.q, p.a.q_dtype, at + d + k);
+          for (int k = 0; k < S::kChunks * 2; ++k) {
+            const int d = (k >> 1) * 64 + q4 * 16 + (k & 1) * 8;
+            v[k] = real && d < D ? __ldg((const uint4 *)((const uint16_t *)p.a.q + at + d)) : make_uint4(0, 0, 0, 0);
           }
 #pragma unroll
-          for (int k = 0; k < 16; ++k) amax = fmaxf(amax, fabsf(x[c * 16 + k]));
+          for (int k = 0; k < S::kChunks * 8; ++k) {
+            const uint32_t y = (&v[k >> 2].x)[k & 3];
+            const float2 g = bf ? make_float2(__uint_as_float(y << 16), __uint_as_float(y & 0xffff0000u))
+                                : __half22float2(*reinterpret_cast<const __half2 *>(&y));
+            x[2 * k] = g.x, x[2 * k + 1] = g.y;
+          }
+        } else if (real) {
+#pragma unroll
+          for (int k = 0; k < S::kChunks * 16; ++k) {
+            const int d = (k >> 4) * 64 + q4 * 16 + (k & 15);
+            if (d < D) x[k] = load_elem(p.a.q, p.a.q_dtype, at + d);
+          }
         }
+#pragma unroll
+        for (int k = 0; k < S::kChunks * 16; ++k) amax = fmaxf(amax, fabsf(x[k]));
         amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
         // The row times a power of two, its largest number in [2^13, 2^14).
         int ex = amax > 0.f && amax < CUDART_INF_F ? 13 + 127 - (int)(__float_as_uint(amax) >> 23) : 0;
         ex = min(max(ex, -126), 126);
         const float up = __uint_as_float((uint32_t)(127 + ex) << 23);
-        zf[i] = p.a.scale * kLog2e * code_unit<KIND>() * __uint_as_float((uint32_t)(127 - ex) << 23);
+        const float f = p.a.scale * kLog2e * __uint_as_float((uint32_t)(127 - ex) << 23);
 #pragma unroll
-        for (int k = 0; k < S::kChunks * 4; ++k) {
-          split2(x[k * 4] * up, x[k * 4 + 1] * up, qf[i][k][0], qf[i][k][1]);
-          split2(x[k * 4 + 2] * up, x[k * 4 + 3] * up, qf[i][k][2], qf[i][k][3]);
+        for (int k = 0; k < S::kChunks * 4; ++k)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            uint32_t a, b;
+            split2(x[k * 4 + 2 * y] * up, x[k * 4 + 2 * y + 1] * up, a, b);
+            if (MODE == 0) {
+              qf[s][0][k][y] = nn < 4 ? a : b;
+            } else {
+              qf[s][0][k][y] = a;
+              qf[s][S::kHalves - 1][k][y] = b;
+            }
+          }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int col = 2 * q4 + k;
+          zf[s][k] = __shfl_sync(~0u, f, col * 4);
+          row_of<S>(p, e, MODE == 0 ? col & 3 : s * 8 + col, token, head, pos[s][k]);
+          m[s][k] = -CUDART_INF_F;
+          l[s][k] = 0.f;
         }
       }
     }
 
-    __syncwarp();  // all lanes are done with the stage that is filled next
-    issue();
-    cp_async_wait_n(p.stages - 1);
+    cp_async_wait<S::kStages - 1>();
     __syncwarp();
     const uint8_t *st = ring + stage * S::kStage;
-    stage = stage + 1 == p.stages ? 0 : stage + 1;
+    stage = stage + 1 == S::kStages ? 0 : stage + 1;
     float ks[S::kGroups], vs[S::kGroups];
     bool all_in = true;
 #pragma unroll
@@ -488,45 +585,49 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ 
       all_in = all_in && ((const int *)meta)[2];
     }
 
-    // scores: a tile of 8 tokens per column block
-    float z[RT][S::kGroups * 2][2];
+    // scores: 16 tokens by 8 columns per set
+    float z[S::kSets][S::kGroups][4];  // tokens n, n, n + 8, n + 8 of the columns 2 q4, 2 q4 + 1
 #pragma unroll
-    for (int t = 0; t < S::kGroups * 2; ++t) {
-      float acc[RT][4];
+    for (int g = 0; g < S::kGroups; ++g) {
+      float acc[S::kSets][4];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+      for (int s = 0; s < S::kSets; ++s) acc[s][0] = acc[s][1] = acc[s][2] = acc[s][3] = 0.f;
 #pragma unroll
       for (int c = 0; c < S::kChunks; ++c) {
-        const uint4 kw = *(const uint4 *)(st + (t * S::kChunks + c) * 512 + lane * 16);
-        const uint32_t v[4] = {kw.x, kw.y, kw.z, kw.w};
+        const uint4 x = *(const uint4 *)(st + ((g * 2 + 0) * S::kChunks + c) * 512 + lane * 16);
+        const uint4 y = *(const uint4 *)(st + ((g * 2 + 1) * S::kChunks + c) * 512 + lane * 16);
+        const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const uint32_t cw = code_bias<KIND>(v[y]);
-          const uint32_t b0 = widen_lo<KIND>(cw), b1 = widen_hi<KIND>(cw);
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t a = code_bias<KIND>(xw[k]), b = code_bias<KIND>(yw[k]);
+          const uint32_t a0 = widen_lo<KIND>(a), a1 = widen_lo<KIND>(b), a2 = widen_hi<KIND>(a), a3 = widen_hi<KIND>(b);
 #pragma unroll
-          for (int i = 0; i < RT; ++i) mma(acc[i], qf[i][c * 4 + y], b0, b1);
+          for (int s = 0; s < S::kSets; ++s)
+#pragma unroll
+            for (int hf = 0; hf < S::kHalves; ++hf) mma(acc[s], a0, a1, a2, a3, qf[s][hf][c * 4 + k]);
         }
       }
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const float f = zf[i] * ks[t >> 1];
-        z[i][t][0] = (acc[i][0] + acc[i][2]) * f;
-        z[i][t][1] = (acc[i][1] + acc[i][3]) * f;
-      }
+      for (int s = 0; s < S::kSets; ++s)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float v = acc[s][k];
+          if (MODE == 0) v += __shfl_xor_sync(~0u, v, 2);
+          z[s][g][k] = v * (zf[s][k & 1] * ks[g]);
+        }
     }
 
-    const int j0 = (e.r.u0 + (int)(u - e.begin)) * S::kUnit;
-    const bool masked = !all_in || j0 + S::kUnit - 1 > min(pos_first, e.r.hi - 1) || (p.a.window > 0 && j0 <= pos_last - p.a.window);
+    const bool masked = !all_in || tok + S::kUnit - 1 > min(pos_first, hi - 1) || (p.a.window > 0 && tok <= pos_last - p.a.window);
     if (masked) {
 #pragma unroll
-      for (int t = 0; t < S::kGroups * 2; ++t) {
-        const bool in = ((const int *)(st + S::kMetaAt + (t >> 1) * 16))[2];
+      for (int g = 0; g < S::kGroups; ++g) {
+        const bool in = ((const int *)(st + S::kMetaAt + g * 16))[2];
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+        for (int s = 0; s < S::kSets; ++s)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int j = j0 + t * 8 + q4 * 2 + k;
-            if (!in || j > pos[i] || j >= e.r.hi || (p.a.window > 0 && j <= pos[i] - p.a.window)) z[i][t][k] = -CUDART_INF_F;
+          for (int k = 0; k < 4; ++k) {
+            const int j = tok + g * 16 + nn + (k >> 1) * 8, ps = pos[s][k & 1];
+            if (!in || j > ps || j >= hi || (p.a.window > 0 && j <= ps - p.a.window)) z[s][g][k] = -CUDART_INF_F;
           }
       }
     }
@@ -541,34 +642,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ 
     if (vnew != vmax) vcorr = __fdiv_rn(vmax, vnew);
     vmax = vnew;
 
-    uint32_t pf[RT][S::kGroups][4];
-    float corr[RT];
+    uint32_t pf[S::kSets][S::kHalves][S::kGroups][2];
+    uint64_t corr[S::kSets];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      float mx = m[i];
+    for (int s = 0; s < S::kSets; ++s) {
+      float cr[2], mu[2];
 #pragma unroll
-      for (int t = 0; t < S::kGroups * 2; ++t) mx = fmaxf(mx, fmaxf(z[i][t][0], z[i][t][1]));
-      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
-      const float mu = mx == -CUDART_INF_F ? 0.f : mx;
-      const float cr = exp2_fast(m[i] - mu);
-      m[i] = mx;
-      float sum = 0.f;
+      for (int k = 0; k < 2; ++k) {
+        float mx = m[s][k];
 #pragma unroll
-      for (int g = 0; g < S::kGroups; ++g) {
-        float wt[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float pr = exp2_fast(z[i][g * 2 + (k >> 1)][k & 1] - mu);
-          sum += pr;
-          wt[k] = pr * vr[g];
-          if (masked && z[i][g * 2 + (k >> 1)][k & 1] == -CUDART_INF_F) wt[k] = 0.f;  // 0, whatever the scale is
-        }
-        split2(wt[0], wt[1], pf[i][g][0], pf[i][g][1]);
-        split2(wt[2], wt[3], pf[i][g][2], pf[i][g][3]);
+        for (int g = 0; g < S::kGroups; ++g) mx = fmaxf(mx, fmaxf(z[s][g][k], z[s][g][2 + k]));
+        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
+        mu[k] = mx == -CUDART_INF_F ? 0.f : mx;
+        cr[k] = exp2_fast(m[s][k] - mu[k]);
+        m[s][k] = mx;
+        l[s][k] *= cr[k];
       }
-      l[i] = l[i] * cr + sum;
-      corr[i] = cr * vcorr;
+      corr[s] = f2_pack(cr[0] * vcorr, cr[1] * vcorr);
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float wt[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float zz = z[s][g][2 * t + k], pr = exp2_fast(zz - mu[k]);
+            l[s][k] += pr;
+            wt[k] = pr * vr[g];
+            if (masked && zz == -CUDART_INF_F) wt[k] = 0.f;  // 0, whatever the scale is
+          }
+          uint32_t a, b;
+          split2(wt[0], wt[1], a, b);
+          if (MODE == 0) {
+            pf[s][0][g][t] = transpose8(q4 < 2 ? a : b);
+          } else {
+            pf[s][0][g][t] = transpose8(a);
+            pf[s][S::kHalves - 1][g][t] = transpose8(b);
+          }
+        }
     }
 
 #pragma unroll
@@ -579,9 +692,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ 
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const uint8_t *src = st + S::kValAt + ((g * 4 + t) * S::kVParts + part) * (32 * S::kVB) + lane * S::kVB;
-          if (S::kVB == 16) {
+          if constexpr (S::kVB == 16) {
             const uint4 x = *(const uint4 *)src;
-            vw[g][t][0] = x.x, vw[g][t][1] = x.y, vw[g][t][2 % (S::kVB / 4)] = x.z, vw[g][t][3 % (S::kVB / 4)] = x.w;
+            vw[g][t][0] = x.x, vw[g][t][1] = x.y, vw[g][t][2] = x.z, vw[g][t][3] = x.w;
           } else {
             const uint2 x = *(const uint2 *)src;
             vw[g][t][0] = x.x, vw[g][t][1] = x.y;
@@ -589,78 +702,104 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ 
         }
 #pragma unroll
       for (int y = 0; y < S::kVB / 4; ++y) {
-        uint32_t b[S::kGroups][4][2];
+        uint32_t a[S::kGroups][2][4];  // the bytes (0, 1) and (2, 3) of the words: two tiles
 #pragma unroll
         for (int g = 0; g < S::kGroups; ++g)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {  // the pairs (2r, 2r + 1) and (2r + 8, 2r + 9) of tokens
+          for (int k = 0; k < 2; ++k) {  // the tokens (2r, 2r + 1) and (2r + 8, 2r + 9)
             const uint32_t x = code_bias<KIND>(vw[g][2 * k][y]), xx = code_bias<KIND>(vw[g][2 * k + 1][y]);
-            const uint32_t lo = __byte_perm(x, xx, 0x5140), hi = __byte_perm(x, xx, 0x7362);
-            b[g][0][k] = widen_lo<KIND>(lo);
-            b[g][1][k] = widen_hi<KIND>(lo);
-            b[g][2][k] = widen_lo<KIND>(hi);
-            b[g][3][k] = widen_hi<KIND>(hi);
+            const uint32_t lo = __byte_perm(x, xx, 0x5140), up = __byte_perm(x, xx, 0x7362);
+            a[g][0][2 * k] = widen_lo<KIND>(lo);
+            a[g][0][2 * k + 1] = widen_hi<KIND>(lo);
+            a[g][1][2 * k] = widen_lo<KIND>(up);
+            a[g][1][2 * k + 1] = widen_hi<KIND>(up);
           }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int j = part * S::kVB + y * 4 + k;
+        for (int k = 0; k < 2; ++k) {
+          const int j = part * (S::kVB / 2) + y * 2 + k;
 #pragma unroll
-          for (int i = 0; i < RT; ++i) {
+          for (int s = 0; s < S::kSets; ++s) {
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int g = 0; g < S::kGroups; ++g) mma(acc, pf[i][g], b[g][k][0], b[g][k][1]);
-            o[i][j][0] = fmaf(o[i][j][0], corr[i], acc[0] + acc[2]);
-            o[i][j][1] = fmaf(o[i][j][1], corr[i], acc[1] + acc[3]);
+            for (int g = 0; g < S::kGroups; ++g)
+#pragma unroll
+              for (int hf = 0; hf < S::kHalves; ++hf) mma(acc, a[g][k][0], a[g][k][1], a[g][k][2], a[g][k][3], pf[s][hf][g]);
+            o[s][j][0] = f2_fma(o[s][j][0], corr[s], f2_pack(acc[0], acc[1]));
+            o[s][j][1] = f2_fma(o[s][j][1], corr[s], f2_pack(acc[2], acc[3]));
           }
         }
       }
     }
+    tok += S::kUnit;
+    if (--cleft) continue;
 
     // ---- the end of this warp's part of an entry
-    if (u + 1 == e.end || u + 1 == w1) {
-      const bool whole = e.begin >= w0 && e.end <= w1;
-      const bool last = u + 1 == w1;
-      float *part = last ? (float *)ring : head_slot;
-      if (!whole) {
-        if (last) cp_async_wait<0>();  // nothing of this warp is still on its way into the ring
-        __syncwarp();
-        if (lane == 0) {
-          s_part[2 * w + (last ? 1 : 0)] = part;
-          s_begin[2 * w + (last ? 1 : 0)] = e.begin;
+    const Desc e = s_desc[w][cdesc];
+    cdesc = cdesc == S::kStages ? 0 : cdesc + 1;
+    const bool whole = e.begin >= w0 && e.end <= w1, last = it + 1 == units;
+    float inv[S::kSets][2];
+#pragma unroll
+    for (int s = 0; s < S::kSets; ++s)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float sum = l[s][k];
+        sum += __shfl_xor_sync(~0u, sum, 4);
+        sum += __shfl_xor_sync(~0u, sum, 8);
+        sum += __shfl_xor_sync(~0u, sum, 16);
+        l[s][k] = sum;
+        // o / l first: the average code is small, the block scale may not be
+        inv[s][k] = sum == 0.f ? 0.f : __fdiv_rn(1.f / kWeight, sum);
+      }
+    if (!whole) {
+      // Its place: the ring if the warp is done, else a slot in the workspace.
+      float *part = last ? (float *)ring : ws + (size_t)(kMaxCtas * 2 + blockIdx.x * S::kWarps + w) * S::kSlot;
+      if (last) cp_async_wait<0>();
+      __syncwarp();
+      if (lane == 0) s_cut[2 * w + last] = e;
+#pragma unroll
+      for (int s = 0; s < S::kSets; ++s) {
+        if (nn == 0) {
+          *(float2 *)(part + s * 8 + 2 * q4) = make_float2(m[s][0], m[s][1]);
+          *(float2 *)(part + S::kStats / 2 + s * 8 + 2 * q4) = make_float2(l[s][0], l[s][1]);
+        }
+#pragma unroll
+        for (int j = 0; j < S::kTiles; ++j) {
+          const float2 x = f2_unpack(o[s][j][0]), y = f2_unpack(o[s][j][1]);
+          ((float4 *)(part + S::kStats))[(s * S::kTiles + j) * 32 + lane] =
+              make_float4(x.x * inv[s][0] * vmax, x.y * inv[s][1] * vmax, y.x * inv[s][0] * vmax, y.y * inv[s][1] * vmax);
         }
       }
+      continue;
+    }
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        float sum = l[i];
-        sum += __shfl_xor_sync(~0u, sum, 1);
-        sum += __shfl_xor_sync(~0u, sum, 2);
-        // o / l first: the average code is small, the block scale may not be
-        const float inv = sum == 0.f ? 0.f : __fdiv_rn(code_unit<KIND>() / kWeight, sum);
-        const int row = i * 8 + nn;
-        if (!whole) {
-          if (q4 == 0) part[row] = m[i], part[S::kRows + row] = sum;
-          float *dst = part + 2 * S::kRows + row * DP;
+    for (int s = 0; s < S::kSets; ++s) {
+      float x[S::kTiles][4];
 #pragma unroll
-          for (int j = 0; j < S::kTilesN; ++j) {
-            const int base = (j / S::kVB) * 128 + j % S::kVB;
-            dst[base + (2 * q4) * S::kVB] = o[i][j][0] * inv * vmax;
-            dst[base + (2 * q4 + 1) * S::kVB] = o[i][j][1] * inv * vmax;
-          }
-        } else {
-          int64_t token;
-          int head, ps;
-          if (row_of<S>(p, e, row, token, head, ps)) {
-            const int64_t at = token * p.a.out_token_stride + head * p.a.out_head_stride;
+      for (int j = 0; j < S::kTiles; ++j) {
+        const float2 a = f2_unpack(o[s][j][0]), b = f2_unpack(o[s][j][1]);
+        x[j][0] = a.x * inv[s][0] * vmax, x[j][1] = a.y * inv[s][1] * vmax;
+        x[j][2] = b.x * inv[s][0] * vmax, x[j][3] = b.y * inv[s][1] * vmax;
+        if (MODE == 0)
 #pragma unroll
-            for (int j = 0; j < S::kTilesN; ++j) {
-              const int d = (j / S::kVB) * 128 + (2 * q4) * S::kVB + j % S::kVB;
-              if (d < D) store_elem(p.a.out, p.a.out_dtype, at + d, o[i][j][0] * inv * vmax);
-              if (d + S::kVB < D) store_elem(p.a.out, p.a.out_dtype, at + d + S::kVB, o[i][j][1] * inv * vmax);
-            }
-            if (p.a.lse && q4 == 0)
-              p.a.lse[token * p.a.n_heads + head] = sum == 0.f ? -CUDART_INF_F : (m[i] + log2f(sum)) * kLn2;
-          }
+          for (int k = 0; k < 4; ++k) x[j][k] += __shfl_xor_sync(~0u, x[j][k], 2);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int row = MODE == 0 ? (2 * q4 + k) & 3 : s * 8 + 2 * q4 + k;
+        int64_t token;
+        int head, ps;
+        if (!row_of<S>(p, e, row, token, head, ps)) continue;
+        const int64_t at = token * p.a.out_token_stride + head * p.a.out_head_stride;
+#pragma unroll
+        for (int j = 0; j < S::kTiles; j += 2) {
+          // with 4 rows the lanes of the high and the low halves hold the same sums and take turns
+          if (MODE == 0 && (j >> 1 & 1) != (q4 >> 1)) continue;
+          const int d = (2 * j / S::kVB) * 128 + nn * S::kVB + 2 * j % S::kVB;
+          const float y[4] = {x[j][k], x[j][2 + k], x[j + 1][k], x[j + 1][2 + k]};
+          if (d < D) store_row<4>(p.a.out, p.a.out_dtype, at + d, y, p.out_vec);
         }
+        if (p.a.lse && nn == 0 && (MODE != 0 || q4 < 2))
+          p.a.lse[token * p.a.n_heads + head] = l[s][k] == 0.f ? -CUDART_INF_F : (m[s][k] + log2f(l[s][k])) * kLn2;
       }
     }
   }
@@ -668,28 +807,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ 
   __syncthreads();
 
   // ---- entries cut between warps of this CTA
-  __shared__ const float *s_from[2 * kWarps];
-  float *wts = (float *)(smem + ring_at + (size_t)kWarps * p.stages * S::kStage);
-  int64_t cross[2] = {-1, -1};  // entries cut between CTAs: the one that came from before, the one that goes on
-  for (int i = 0; i < 2 * kWarps;) {
-    const int64_t begin = s_begin[i];
-    if (begin < 0) {
+  int cross[2] = {-1, -1};  // cut between CTAs: the entry that came from before, the one that goes on
+  for (int i = 0; i < 2 * S::kWarps;) {
+    if (s_cut[i].units == 0) {
       ++i;
       continue;
     }
+    const Desc e = s_cut[i];
+    __shared__ const float *s_from[S::kWarps + 1];
     int n = 0;
-    __syncthreads();
-    for (; i < 2 * kWarps && (s_begin[i] == begin || s_begin[i] < 0); ++i)
-      if (s_begin[i] >= 0) {
-        if (tid == 0) s_from[n] = s_part[i];
-        ++n;
+    const int i0 = i;
+    for (; i < 2 * S::kWarps && (s_cut[i].units == 0 || s_cut[i].begin == e.begin); ++i) n += s_cut[i].units != 0;
+    if (n > 0) {
+      __syncthreads();  // the list of the join before is not read any more
+      if (tid < i - i0 && s_cut[i0 + tid].units) {
+        const int x = i0 + tid, pw = x >> 1;
+        int at = 0;
+        for (int k = i0; k < x; ++k) at += s_cut[k].units != 0;
+        s_from[at] = x & 1 ? (const float *)(smem + ring_at + (size_t)pw * S::kStages * S::kStage)
+                           : ws + (size_t)(kMaxCtas * 2 + blockIdx.x * S::kWarps + pw) * S::kSlot;
       }
-    __syncthreads();
-    e = entry_at<S>(p, pre, begin);
+      __syncthreads();
+    }
     const bool whole = e.begin >= c0 && e.end <= c1;
     const int side = e.begin < c0 ? 0 : 1;
-    join<S, DP, false>(p, e, n, s_from, nullptr, 0, whole ? nullptr : cta_slots + side * S::kSlot, wts);
-    if (!whole) cross[side] = begin;
+    join<S, MODE, false>(p, e, n, [&](int k) { return s_from[k]; }, whole ? nullptr : cta_slots + side * S::kSlot);
+    if (!whole) cross[side] = i0;
   }
 
   // ---- entries cut between CTAs: the last to arrive joins
@@ -697,61 +840,75 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend(const __grid_constant__ 
   __shared__ int s_last;
   for (int side = 0; side < 2; ++side) {
     if (cross[side] < 0) continue;
-    e = entry_at<S>(p, pre, cross[side]);
+    const Desc e = s_cut[cross[side]];
     const int first = (int)(e.begin / share), last = (int)((e.end - 1) / share);
     __threadfence();
     __syncthreads();
     if (tid == 0) {
-      const int seen = atomicAdd(counters + first, 1);
-      s_last = seen == last - first;
+      s_last = atomicAdd(counters + first, 1) == last - first;
       if (s_last) counters[first] = 0;
     }
     __syncthreads();
     if (!s_last) continue;
     __threadfence();
-    const int n = last - first + 1;
     // the first CTA's part is its second slot, the others' their first
-    const float *from0 = ws + (size_t)first * 2 * S::kSlot;
-    join<S, DP, true>(p, e, n, nullptr, from0, 2 * S::kSlot, nullptr, wts);
+    const float *from = ws + (size_t)first * 2 * S::kSlot;
+    join<S, MODE, true>(p, e, last - first + 1, [&](int k) { return from + (k ? k * 2 : 1) * S::kSlot; }, nullptr);
   }
 }
 
 struct Plan {
-  int dp, rt, rows;
+  int dp, mode, rows;
 };
+// Tiles of 4 rows where they hold all rows that share a head's keys (a decode
+// step of up to 4 query heads per key-value head: half the products of 8 rows),
+// else of 8, and of 16 where more than 8 rows would read the keys again; 256
+// head dims leave no registers for 16.
 Plan shape_for(const seedq_kv_cache *c, int32_t n_heads, int32_t max_new) {
   Plan s;
   s.dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
   const int64_t rows = (int64_t)(n_heads / c->n_kv_heads) * max_new;
-  s.rt = rows > 8 && s.dp < 256 ? 2 : 1;
-  s.rows = 8 * s.rt;
+  s.mode = rows <= 4 ? 0 : rows <= 8 || s.dp == 256 ? 1 : 2;
+  s.rows = 4 << s.mode;
   return s;
 }
+template <int DP, int MODE>
+constexpr uint64_t workspace_bytes() {
+  using S = Shape<DP, MODE>;
+  // arrival counters; per CTA two parts of entries cut between CTAs, per warp one of an entry cut between warps
+  return kMaxCtas * 4 + (uint64_t)kMaxCtas * (2 + S::kWarps) * S::kSlot * 4;
+}
 
-template <int KIND, int DP, int RT>
-seedq_status launch(Args &p, DeviceOnce &once, int dev, cudaStream_t st) {
-  using S = Shape<DP, RT>;
-  const size_t pre = (((size_t)p.a.n_requests + 1) * 8 + 15) & ~(size_t)15;
-  const size_t wts = (size_t)(kMaxCtas + 2) * S::kRows * 4;  // weights of a join of every CTA's part
-  const size_t room = kSmemMax - 1024 - pre - wts;
-  p.stages = (int)std::min<size_t>(5, room / ((size_t)kWarps * S::kStage));
-  if (p.stages < 2) return SEEDQ_ERR_UNSUPPORTED;
-  const size_t smem = pre + wts + (size_t)kWarps * p.stages * S::kStage;
+template <int KIND, int DP, int MODE>
+seedq_status launch(Args &p, int dev, cudaStream_t st) {
+  using S = Shape<DP, MODE>;
+  static DeviceOnce once;
+  p.chunk = (p.a.n_requests + kMaxChunks - 1) / kMaxChunks;
+  constexpr size_t smem = (((kMaxChunks + 1) * 8 + 15) & ~15) + (size_t)S::kWarps * S::kStages * S::kStage;
+  static_assert(smem + 6144 <= kSmemMax, "");
   const int rc = once.run(dev, [] {
-    return (int)cudaFuncSetAttribute(k_attend<KIND, DP, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax - 1024);
+    return (int)cudaFuncSetAttribute(k_attend<KIND, DP, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   });
   if (rc) return cuda_fail((cudaError_t)rc);
-  k_attend<KIND, DP, RT><<<p.ctas, kThreads, smem, st>>>(p);
+  k_attend<KIND, DP, MODE><<<p.ctas, S::kThreads, smem, st>>>(p);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
 }
-template <int KIND>
-seedq_status launch_kind(Args &p, const Plan &s, DeviceOnce *once, int dev, cudaStream_t st) {
-  if (s.dp == 64) return s.rt == 1 ? launch<KIND, 64, 1>(p, once[0], dev, st) : launch<KIND, 64, 2>(p, once[1], dev, st);
-  if (s.dp == 128) return s.rt == 1 ? launch<KIND, 128, 1>(p, once[2], dev, st) : launch<KIND, 128, 2>(p, once[3], dev, st);
-  return launch<KIND, 256, 1>(p, once[4], dev, st);
+// f(DP, MODE) for a plan, the two as types.
+template <typename F>
+auto with_shape(const Plan &s, F f) {
+  using std::integral_constant;
+  if (s.dp == 64)
+    return s.mode == 0   ? f(integral_constant<int, 64>(), integral_constant<int, 0>())
+           : s.mode == 1 ? f(integral_constant<int, 64>(), integral_constant<int, 1>())
+                         : f(integral_constant<int, 64>(), integral_constant<int, 2>());
+  if (s.dp == 128)
+    return s.mode == 0   ? f(integral_constant<int, 128>(), integral_constant<int, 0>())
+           : s.mode == 1 ? f(integral_constant<int, 128>(), integral_constant<int, 1>())
+                         : f(integral_constant<int, 128>(), integral_constant<int, 2>());
+  return s.mode == 0 ? f(integral_constant<int, 256>(), integral_constant<int, 0>())
+                     : f(integral_constant<int, 256>(), integral_constant<int, 1>());
 }
-DeviceOnce g_once[2][5];
 
 bool aligned(const void *base, int32_t dtype, int64_t ts, int64_t hs) {
   const int64_t per = 16 / dtype_bytes(dtype);
@@ -774,9 +931,7 @@ extern "C" {
 
 uint64_t seedq_kv_attend_workspace_bytes(const seedq_kv_cache *cache, int32_t n_heads, int32_t max_new) {
   if (check(cache, n_heads, max_new) != SEEDQ_OK) return 0;
-  const Plan s = shape_for(cache, n_heads, max_new);
-  // arrival counters; per CTA two parts of entries cut between CTAs, per warp one of an entry cut between warps
-  return kMaxCtas * 4 + (uint64_t)kMaxCtas * (2 + kWarps) * s.rows * (s.dp + 2) * 4;
+  return with_shape(shape_for(cache, n_heads, max_new), [](auto dp, auto mode) { return workspace_bytes<dp.value, mode.value>(); });
 }
 
 seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_args *args, void *cuda_stream) {
@@ -803,10 +958,11 @@ seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_arg
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return cuda_fail(e);
   p.ctas = std::min(sms, kMaxCtas);
-  const Plan s = shape_for(cache, a.n_heads, a.max_new);
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if (cache->kind == SEEDQ_KV_INT8) return launch_kind<SEEDQ_KV_INT8>(p, s, g_once[0], dev, stream);
-  return launch_kind<SEEDQ_KV_E4M3>(p, s, g_once[1], dev, stream);
+  return with_shape(shape_for(cache, a.n_heads, a.max_new), [&](auto dp, auto mode) {
+    return cache->kind == SEEDQ_KV_INT8 ? launch<SEEDQ_KV_INT8, dp.value, mode.value>(p, dev, stream)
+                                        : launch<SEEDQ_KV_E4M3, dp.value, mode.value>(p, dev, stream);
+  });
 }
 
 }  // extern "C"

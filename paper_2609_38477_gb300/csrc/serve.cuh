@@ -29,15 +29,17 @@ __device__ __forceinline__ void store_elem(void *p, int dt, int64_t i, float x) 
   else ((__half *)p)[i] = __float2half_rn(x);
 }
 
-// The number an 8-bit code stands for.  E4M3's seven magnitude bits, moved to
-// the exponent and fraction fields of a binary16 and multiplied by 2^8 (the
-// difference of the biases), are that number, subnormals included; the NaN
-// code reads as 480, so no garbage byte can become a NaN.
+// Two E4M3 codes as binary16 numbers (exact).
+__device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
+  return h;
+}
+// The number an 8-bit code stands for.
 template <int KIND>
 __device__ __forceinline__ float code_value(uint32_t b) {
   if (KIND == SEEDQ_KV_INT8) return (float)(int8_t)b;
-  const uint32_t h = ((b & 0x80u) << 8) | ((b & 0x7fu) << 7);
-  return __half2float(__ushort_as_half((unsigned short)h)) * 256.0f;
+  return __half2float(__ushort_as_half((unsigned short)e4m3x2_to_half2(b & 0xffu)));
 }
 // The code of x / s, |x / s| at most 127 or 448 by the choice of s; nearest even.
 template <int KIND>
