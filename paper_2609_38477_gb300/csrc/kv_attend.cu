@@ -24,13 +24,15 @@
 //
 // Layout.  For keys a product's row is a token and its inner index the head
 // dim; the order of the inner index is free as long as q uses the same, so each
-// lane takes 16 consecutive codes of a token (one 16-byte copy) and q's
-// fragments are laid out to match.  For values the inner index is the token and
-// a row a head dim, whose order is free again: lane (n, r) takes 16 consecutive
-// codes of its four tokens.  So every lane copies (cp.async, 16 bytes) exactly
-// the codes it will multiply into a ring of its own in shared memory: no
-// barrier, no bank conflict, any strides, and what is past a request's end is
-// filled with zeros instead of being read.
+// lane takes 16 consecutive codes of a token and q's fragments are laid out to
+// match.  For values the inner index is the token and a row a head dim, whose
+// order is free again: lane (n, r) takes 16 consecutive codes of its four
+// tokens.  A warp copies whole rows (cp.async, 16 bytes a lane: partial lines
+// are fetched from L2 in 64-byte steps, and lane-private pieces of 32 bytes cost
+// 1.75 times the traffic) into a ring of its own in shared memory, 16-byte pieces
+// permuted so that neither the copies nor the lanes' reads meet in a bank.  Only
+// the warp's own barrier is needed, strides are free, and what is past a
+// request's end is filled with zeros instead of being read.
 //
 // Split.  The work list is every (request, key-value head, row tile) with its
 // keys in units of kUnit tokens; it is cut into equal ranges of units, one per
@@ -56,7 +58,6 @@ namespace {
 
 constexpr int kMaxCtas = 152;      // one per SM
 constexpr int kSmemMax = 227 * 1024;
-constexpr int kMaxChunks = 1024;   // entries of the table of units
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kWeight = 16384.f;  // weights are held times this
@@ -71,17 +72,19 @@ struct Shape {
   static constexpr int kUnit = DP <= 128 ? 32 : 16;  // tokens of a unit
   static constexpr int kGroups = kUnit / 16;
   static constexpr int kChunks = DP / 64;            // 64 head dims: 16 codes of 4 lanes
-  static constexpr int kVB = DP >= 128 ? 16 : 8;     // bytes of a lane's value piece
+  static constexpr int kVB = DP >= 128 ? 16 : 8;     // codes of a lane's value piece
+  static constexpr int kLanes = DP / 16;             // lanes that copy a row
+  static constexpr int kStep = 32 / kLanes;          // rows of a copy
   static constexpr int kVParts = DP / (8 * kVB);
   static constexpr int kTiles = DP / 16;             // output tiles of 16 head dims
-  static constexpr int kKeyPieces = kGroups * 2 * kChunks;
-  static constexpr int kValPieces = kGroups * 4 * kVParts;
-  static constexpr int kValAt = kKeyPieces * 512;
-  static constexpr int kMetaAt = kValAt + kValPieces * 32 * kVB;
+  static constexpr int kValAt = kUnit * DP;
+  static constexpr int kMetaAt = 2 * kUnit * DP;
   static constexpr int kStage = kMetaAt + 16 * kGroups;  // meta: per group both scales and a flag
   static constexpr int kWarps = (MODE == 2 || DP == 256) ? 8 : 12;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kStages = DP == 64 ? 4 : kWarps == 12 ? 2 : 3;  // units in a warp's ring
+  static constexpr int kWhole = 8 * kWarps, kWholeWarp = 2;    // see the split of the work list
+  static constexpr int kRequests = kThreads;                   // that the shared table holds
   static constexpr int kStats = 2 * 8 * kSets;                 // m and l of every column
   static constexpr int kSlot = kStats + kSets * kTiles * 128;  // floats of a part: stats, then lanes' products
   static_assert(kSlot * 4 <= kStages * kStage, "a part fits its warp's ring");
@@ -91,16 +94,18 @@ struct Args {
   seedq_kv_cache c;
   seedq_attend_args a;
   int32_t group;           // query heads per key-value head
+  int32_t group_shift, gpp_shift;  // log2 of it, and of a page's groups of 16 tokens; -1 if there is none
   int32_t ctas;
   int32_t chunk;           // requests per entry of the table of units
+  uint64_t ctas_inv;       // 2^64 / ctas, rounded up
+  int32_t q_bytes;         // of an element of q
   int32_t q_vec, out_vec;  // q / out rows allow 16-byte accesses
 };
 
+__device__ __forceinline__ int divide(int x, int by, int shift) { return shift >= 0 ? x >> shift : x / by; }
+
 __device__ __forceinline__ void cp_async16z(uint32_t dst, const void *src, bool in) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async8z(uint32_t dst, const void *src, bool in) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(in ? 8 : 0) : "memory");
 }
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b)[2]) {
   asm volatile(
@@ -147,7 +152,7 @@ __device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
 }
 
 // A request's share of the work list.
-struct Req {
+struct __align__(16) Req {
   int first, fresh;  // its query tokens
   int len;           // cached tokens, the newest included
   int lo, hi;        // keys that any of its queries may see
@@ -180,18 +185,29 @@ struct Entry {
   int b, h, tile;
   int64_t begin;  // its first unit in the work list
 };
+// The table of requests in shared memory: units before every chunk of
+// requests, and, where a chunk is one request, the requests themselves.
 template <typename S>
-__device__ __forceinline__ Entry entry_at(const Args &p, const int64_t *pre, int64_t u) {
+struct Table {
+  int64_t before[S::kRequests];
+  Req req[S::kRequests];
+};
+template <typename S>
+__device__ __forceinline__ Req request(const Args &p, const Table<S> &t, int b) {
+  return p.chunk == 1 ? t.req[b] : request<S>(p, b);
+}
+template <typename S>
+__device__ __forceinline__ Entry entry_at(const Args &p, const Table<S> &t, int64_t u) {
   Entry e;
   int lo = 0, hi = (p.a.n_requests + p.chunk - 1) / p.chunk;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (pre[mid] <= u) lo = mid;
+    if (t.before[mid] <= u) lo = mid;
     else hi = mid;
   }
-  int64_t base = pre[lo];
+  int64_t base = t.before[lo];
   e.b = lo * p.chunk;
-  e.r = request<S>(p, e.b);
+  e.r = request<S>(p, t, e.b);
   for (int i = 1; i < p.chunk; ++i) {
     const int64_t n = units_of(p, e.r);
     if (u < base + n) break;
@@ -200,19 +216,19 @@ __device__ __forceinline__ Entry entry_at(const Args &p, const int64_t *pre, int
   }
   const int64_t x = u - base;
   const int k = x >> 32 ? (int)(x / e.r.units) : (int)((uint32_t)x / (uint32_t)e.r.units);
-  e.h = k / e.r.tiles;
+  e.h = e.r.tiles == 1 ? k : k / e.r.tiles;
   e.tile = k - e.h * e.r.tiles;
   e.begin = base + (int64_t)k * e.r.units;
   return e;
 }
 template <typename S>
-__device__ __forceinline__ void next_entry(const Args &p, Entry &e) {  // only where one follows
+__device__ __forceinline__ void next_entry(const Args &p, const Table<S> &t, Entry &e) {  // only where one follows
   e.begin += e.r.units;
   if (++e.tile < e.r.tiles) return;
   e.tile = 0;
   if (++e.h < p.c.n_kv_heads) return;
   e.h = 0;
-  do e.r = request<S>(p, ++e.b);
+  do e.r = request<S>(p, t, ++e.b);
   while (e.r.fresh == 0);
 }
 
@@ -228,7 +244,7 @@ struct Desc {
 // Where a row of an entry's tile goes; false if it holds no query.
 template <typename S>
 __device__ __forceinline__ bool row_of(const Args &p, const Desc &e, int row, int64_t &token, int &head, int &pos) {
-  const int r = e.tile * S::kRows + row, t = r / p.group;
+  const int r = e.tile * S::kRows + row, t = divide(r, p.group, p.group_shift);
   token = e.first + t;
   head = e.h * p.group + (r - t * p.group);
   pos = e.len - e.fresh + t;
@@ -259,25 +275,31 @@ __device__ __forceinline__ void store_row(void *out, int dt, int64_t i, const fl
   }
 }
 
+// A load that sees what other SMs wrote (generic address, past the L1 cache).
+template <typename T>
+__device__ __forceinline__ T load_fresh(const float *x) {
+  T v;
+  if constexpr (sizeof(T) == 8) asm volatile("ld.volatile.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(x) : "memory");
+  else asm volatile("ld.volatile.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(x) : "memory");
+  return v;
+}
+
 // Joins n parts of an entry into `to`, or, if to is null, writes the entry's
 // output.  A part holds m (in units of log2) and l of every column and the
 // columns' averages o = sum / l as the products' accumulators lie in the lanes;
 // it weighs l 2^m.  Averages, not sums, are kept, so nothing overflows on the
-// way.  part(i) is the address of part i.  Every warp takes tiles of its own; a
-// lane reads the statistics of its two columns itself, so no barrier is needed.
-template <typename S, int MODE, bool GLOBAL, typename F>
-__device__ __forceinline__ void join(const Args &p, const Desc &e, int n, F part, float *to) {
+// way.  Every warp takes tiles of its own; a lane reads the statistics of its
+// two columns itself, so no barrier is needed.
+template <typename S, int MODE>
+__device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const float *const *from, float *to) {
   const int lane = threadIdx.x & 31, nn = lane >> 2, q4 = lane & 3;
+#pragma unroll 1
   for (int tt = threadIdx.x >> 5; tt < S::kSets * S::kTiles; tt += S::kWarps) {
     const int set = tt / S::kTiles, tile = tt - set * S::kTiles, col = set * 8 + 2 * q4;
-    auto stat = [&](int i, int at) -> float2 {
-      const float2 *x = (const float2 *)(part(i) + at);
-      return GLOBAL ? __ldcg(x) : *x;
-    };
     float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F;
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
-      const float2 m = stat(i, col);
+      const float2 m = load_fresh<float2>(from[i] + col);
       m0 = fmaxf(m0, m.x);
       m1 = fmaxf(m1, m.y);
     }
@@ -285,16 +307,16 @@ __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, F part
     float l0 = 0.f, l1 = 0.f, c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
-      const float2 m = stat(i, col), l = stat(i, S::kStats / 2 + col);
-      const float4 *src = (const float4 *)(part(i) + S::kStats) + tt * 32 + lane;
-      const float4 o = GLOBAL ? __ldcg(src) : *src;
+      const float *x = from[i];
+      const float2 m = load_fresh<float2>(x + col), l = load_fresh<float2>(x + S::kStats / 2 + col);
+      const float4 o = load_fresh<float4>(x + S::kStats + (tt * 32 + lane) * 4);
       const float w0 = l.x * exp2_fast(m.x - u0), w1 = l.y * exp2_fast(m.y - u1);
       l0 += w0;
       l1 += w1;
       if (w0 != 0.f) c[0] = fmaf(w0, o.x, c[0]), c[2] = fmaf(w0, o.z, c[2]);
       if (w1 != 0.f) c[1] = fmaf(w1, o.y, c[1]), c[3] = fmaf(w1, o.w, c[3]);
     }
-    const float i0 = l0 == 0.f ? 0.f : __fdiv_rn(1.f, l0), i1 = l1 == 0.f ? 0.f : __fdiv_rn(1.f, l1);
+    const float i0 = l0 == 0.f ? 0.f : 1.f / l0, i1 = l1 == 0.f ? 0.f : 1.f / l1;
     c[0] *= i0;
     c[1] *= i1;
     c[2] *= i0;
@@ -313,12 +335,12 @@ __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, F part
       if (q4 >= 2) continue;
     }
     const int d = (2 * tile / S::kVB) * 128 + nn * S::kVB + 2 * tile % S::kVB;
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < 2; ++k) {
       int64_t token;
       int head, pos;
       if (!row_of<S>(p, e, col + k, token, head, pos)) continue;
-      const float x[2] = {c[k], c[2 + k]};
+      const float x[2] = {k ? c[1] : c[0], k ? c[3] : c[2]};
       if (d < p.c.head_dim)
         store_row<2>(p.a.out, p.a.out_dtype, token * p.a.out_token_stride + head * p.a.out_head_stride + d, x, p.out_vec);
       if (p.a.lse && tile == 0 && nn == 0) {
@@ -327,6 +349,15 @@ __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, F part
       }
     }
   }
+}
+
+// Rows of DP bytes in shared memory have their 16-byte pieces permuted, piece x
+// of row r at x ^ swizzle(r): the rows (2a, 2a + 1) that the lanes of a key
+// read share, and the rows 0, 2, 4, 6 of a value read, then lie in different
+// banks.
+template <int DP>
+__host__ __device__ constexpr int swizzle(int r) {
+  return DP >= 128 ? (r & 6) ^ ((r & 1) << 2) : (r >> 1) & 3;
 }
 
 template <int KIND, int DP, int MODE>
@@ -338,39 +369,68 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   const int B = p.a.n_requests, D = p.c.head_dim;
 
   // ---- the work list: exclusive sums of the requests' units
-  int64_t *pre = (int64_t *)smem;
-  const int nc = (B + p.chunk - 1) / p.chunk;
+  Table<S> &table = *(Table<S> *)smem;
   __shared__ int64_t s_sums[S::kWarps];
-  int64_t total = 0;
-  for (int i0 = 0; i0 < nc; i0 += S::kThreads) {
-    const int i = i0 + tid;
-    int64_t u = 0;
-    for (int b = i * p.chunk; b < min((i + 1) * p.chunk, B); ++b) u += units_of(p, request<S>(p, b));
+  __shared__ int s_most[S::kWarps];
+  int64_t total = 0, u = 0;
+  int most = 0;  // units of the longest entry
+  for (int b = tid * p.chunk; b < min((tid + 1) * p.chunk, B); ++b) {
+    const Req r = request<S>(p, b);
+    if (p.chunk == 1) table.req[b] = r;
+    u += units_of(p, r);
+    if (r.fresh) most = max(most, r.units);
+  }
+  {
     int64_t x = u;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t y = __shfl_up_sync(~0u, x, o);
       if (lane >= o) x += y;
     }
-    if (lane == 31) s_sums[w] = x;
+    most = __reduce_max_sync(~0u, most);
+    if (lane == 31) s_sums[w] = x, s_most[w] = most;
     __syncthreads();
-    int64_t before = total;
+    int64_t before = x - u;
+#pragma unroll
     for (int k = 0; k < S::kWarps; ++k) {
       if (k < w) before += s_sums[k];
       total += s_sums[k];
+      most = max(most, s_most[k]);
     }
-    if (i < nc) pre[i] = before + x - u;
+    table.before[tid] = before;
     __syncthreads();
   }
   // Units per CTA: even shares, but at least one unit per warp, so that a short
-  // context is joined within few CTAs.
-  const int64_t share = max((total + p.ctas - 1) / p.ctas, (int64_t)S::kWarps);
-  const int64_t c0 = min(share * blockIdx.x, total), c1 = min(c0 + share, total);
-  if (c0 >= c1) return;
-  const int64_t w0 = c0 + (c1 - c0) * w / S::kWarps, w1 = c0 + (c1 - c0) * (w + 1) / S::kWarps;
+  // context is joined within few CTAs.  Where no entry is longer than kWhole
+  // units the ends move to the nearest entry's: a join between CTAs costs about
+  // as much as 8 units of a warp, more than the uneven shares do; likewise
+  // between warps where no entry is longer than kWholeWarp units.
+  const int64_t share = max((int64_t)__umul64hi((uint64_t)total, p.ctas_inv) + 1, (int64_t)S::kWarps);
+  auto nearest = [&](int64_t u) -> int64_t {  // entry end nearest to u
+    if (u >= total) return total;
+    const Entry e = entry_at<S>(p, table, u);
+    return u - e.begin <= e.begin + e.r.units - u ? e.begin : e.begin + e.r.units;
+  };
+  int64_t c0 = min(share * blockIdx.x, total), c1 = min(c0 + share, total);
+  if (c0 >= total) return;
+  if (most <= S::kWhole) {
+    const int64_t c = nearest(lane ? c1 : c0);
+    c0 = __shfl_sync(~0u, c, 0);
+    c1 = __shfl_sync(~0u, c, 1);
+    if (c0 >= c1) return;
+  }
+  const uint32_t mine = (uint32_t)(c1 - c0);  // split in even shares without passing 32 bits
+  const uint32_t each = mine / S::kWarps, rest = mine - each * S::kWarps;
+  int64_t w0 = c0 + each * (uint32_t)w + min((uint32_t)w, rest);
+  int64_t w1 = w0 + each + (w < (int)rest);
+  if (most <= S::kWholeWarp) {
+    const int64_t c = nearest(lane ? w1 : w0);
+    w0 = __shfl_sync(~0u, c, 0);
+    w1 = __shfl_sync(~0u, c, 1);
+  }
   const int units = (int)(w1 - w0);
 
-  const int ring_at = ((nc + 1) * 8 + 15) & ~15;
+  constexpr int ring_at = sizeof(Table<S>);
   uint8_t *ring = smem + ring_at + (size_t)w * S::kStages * S::kStage;
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
 
@@ -385,9 +445,11 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
 
   // ---- copies
   const int gpp = p.c.page_size >> 4;  // groups of 16 tokens per page
-  const int64_t ts = p.c.token_stride, ts8 = 8 * ts;
-  const uint8_t *klane = (const uint8_t *)p.c.k + nn * ts + q4 * 16;
-  const uint8_t *vlane = (const uint8_t *)p.c.v + 2 * q4 * ts + nn * S::kVB;
+  const int64_t ts = p.c.token_stride, tstep = S::kStep * ts;
+  const int crow = lane / S::kLanes, cat = lane % S::kLanes * 16;  // the lane's row and first code of a copy
+  const int64_t clane = crow * ts + cat;
+  // The place of 16-byte piece x of row r: x ^ swizzle(r).
+  const uint32_t cdst = crow * DP + ((lane % S::kLanes) ^ swizzle<DP>(crow)) * 16;
   Entry pe{};  // the entry being copied
   const int32_t *prow = nullptr;
   int pleft = 0;               // its units still to copy by this warp
@@ -397,7 +459,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   int pstage = 0, pdesc = 0, cdesc = 0, stage = 0, to_copy = units;
   auto load_ids = [&](int g) -> int {
     const int64_t gl = (int64_t)g + lane;
-    return gl * 16 < pe.r.hi ? __ldg(prow + (int)gl / gpp) : -1;
+    return gl * 16 < pe.r.hi ? __ldg(prow + divide((int)gl, gpp, p.gpp_shift)) : -1;
   };
 
   // ---- products
@@ -407,19 +469,22 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   float m[S::kSets][2], l[S::kSets][2], vmax = 0.f;
   uint64_t o[S::kSets][S::kTiles][2];  // sums of the columns (2 q4, 2 q4 + 1) for two head dims
   int cleft = 0, tok = 0, hi = 0, pos_first = 0, pos_last = 0;
+  // and of a value tile: piece n (DP 64: half of piece n / 2) of row 2 q4
+  const uint32_t vat = 2 * q4 * DP + (S::kVB == 16 ? (nn ^ swizzle<DP>(2 * q4)) * 16 : ((nn >> 1) ^ swizzle<DP>(2 * q4)) * 16 + (nn & 1) * 8);
+  const uint32_t kat = nn * DP + (q4 ^ swizzle<DP>(nn)) * 16;  // the lane's first codes of a key tile
 
 #pragma unroll 1
   for (int it = 1 - S::kStages; it < units; ++it) {
     __syncwarp();  // all lanes are done with the stage that is filled next
     if (to_copy > 0) {
       if (pleft == 0) {
-        if (to_copy == units) pe = entry_at<S>(p, pre, w0);
-        else next_entry<S>(p, pe);
+        if (to_copy == units) pe = entry_at<S>(p, table, w0);
+        else next_entry<S>(p, table, pe);
         const int64_t from = max(pe.begin, w0);
         pleft = (int)(min(pe.begin + pe.r.units, w1) - from);
         prow = p.a.block_table + (int64_t)pe.b * p.a.table_stride;
         pg = pgb = (pe.r.u0 + (int)(from - pe.begin)) * S::kGroups;
-        poff = pg % gpp;
+        poff = pg - divide(pg, gpp, p.gpp_shift) * gpp;
         ids = load_ids(pgb);
         ids_next = load_ids(pgb + 32);
         if (lane == 0) {
@@ -429,6 +494,13 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
           x.begin = pe.begin, x.end = pe.begin + pe.r.units;
         }
         pdesc = pdesc == S::kStages ? 0 : pdesc + 1;
+        // its queries' first touch, while the page numbers are on their way
+        const int r = pe.tile * S::kRows + lane, t = divide(r, p.group, p.group_shift);
+        if (lane < S::kRows && t < pe.r.fresh) {
+          const char *row = (const char *)p.a.q + ((int64_t)(pe.r.first + t) * p.a.q_token_stride +
+                                                   (pe.h * p.group + r - t * p.group) * p.a.q_head_stride) * p.q_bytes;
+          for (int x = 0; x < D * p.q_bytes; x += 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(row + x));
+        }
       }
       --pleft;
       --to_copy;
@@ -448,30 +520,19 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
         const int64_t at = in ? page * p.c.page_stride + pe.h * p.c.head_stride + poff * 16 * ts : 0;
         ++pg;
         poff = poff + 1 == gpp ? 0 : poff + 1;
-        const uint8_t *kp = klane + at, *vp = vlane + at;
-        const uint32_t kd = dst + g * (2 * S::kChunks * 512) + lane * 16;
-        const uint32_t vd = dst + S::kValAt + g * (4 * S::kVParts * 32 * S::kVB) + lane * S::kVB;
+        const uint8_t *kp = (const uint8_t *)p.c.k + at + clane, *vp = (const uint8_t *)p.c.v + at + clane;
+        const uint32_t to = dst + g * (16 * DP);
         const bool full = left >= 16 && D == DP;  // every copy is wanted
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int c = 0; c < S::kChunks; ++c) {
-            const bool ok = full || (t * 8 + nn < left && c * 64 + q4 * 16 < D);
-            const uint8_t *src = kp + t * ts8 + c * 64;
-            cp_async16z(kd + (t * S::kChunks + c) * 512, ok ? src : (const uint8_t *)p.c.k, ok);
-          }
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int c = 0; c < S::kVParts; ++c) {
-            const int j = (t >> 1) * 8 + q4 * 2 + (t & 1);
-            const bool ok = full || (j < left && c * 128 + nn * S::kVB < D);
-            const uint32_t to = vd + (t * S::kVParts + c) * (32 * S::kVB);
-            const uint8_t *src = vp + (t >> 1) * ts8 + (t & 1) * ts + c * 128;
-            if (!ok) src = (const uint8_t *)p.c.v;
-            if (S::kVB == 16) cp_async16z(to, src, ok);
-            else cp_async8z(to, src, ok);
-          }
+        for (int t = 0; t < 16 / S::kStep; ++t) {
+          const int row = t * S::kStep;  // the lanes' rows begin here
+          const uint32_t x = to + ((row * DP + cdst) ^ (swizzle<DP>(row) * 16));
+          const bool ok = full || (row + crow < left && cat < D);
+          cp_async16z(x, ok ? kp : (const uint8_t *)p.c.k, ok);
+          cp_async16z(x + S::kValAt, ok ? vp : (const uint8_t *)p.c.v, ok);
+          kp += tstep;
+          vp += tstep;
+        }
         const uint32_t meta = dst + S::kMetaAt + g * 16;
         if (lane < 2) {
           if (in) {
@@ -486,7 +547,9 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       }
     }
     cp_async_commit();
-    if (it < 0) continue;
+    int ahead = it;
+    asm volatile("" : "+r"(ahead));  // keeps the compiler from splitting the loop here and writing the copies out twice
+    if (ahead < 0) continue;
 
     if (cleft == 0) {  // a new entry: its queries
       const Desc e = s_desc[w][cdesc];
@@ -494,8 +557,8 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       tok = e.token0;
       hi = e.hi;
       vmax = 0.f;
-      pos_first = e.len - e.fresh + (e.tile * S::kRows) / p.group;
-      pos_last = min(e.len - e.fresh + (e.tile * S::kRows + S::kRows - 1) / p.group, e.len - 1);
+      pos_first = e.len - e.fresh + divide(e.tile * S::kRows, p.group, p.group_shift);
+      pos_last = min(e.len - e.fresh + divide(e.tile * S::kRows + S::kRows - 1, p.group, p.group_shift), e.len - 1);
 #pragma unroll
       for (int s = 0; s < S::kSets; ++s) {
 #pragma unroll
@@ -532,11 +595,14 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
             x[2 * k] = g.x, x[2 * k + 1] = g.y;
           }
         } else if (real) {
-#pragma unroll
+          float slow[S::kChunks * 16];  // in local memory: rows that do not allow wide loads
+#pragma unroll 1
           for (int k = 0; k < S::kChunks * 16; ++k) {
             const int d = (k >> 4) * 64 + q4 * 16 + (k & 15);
-            if (d < D) x[k] = load_elem(p.a.q, p.a.q_dtype, at + d);
+            slow[k] = d < D ? load_elem(p.a.q, p.a.q_dtype, at + d) : 0.f;
           }
+#pragma unroll
+          for (int k = 0; k < S::kChunks * 16; ++k) x[k] = slow[k];
         }
 #pragma unroll
         for (int k = 0; k < S::kChunks * 16; ++k) amax = fmaxf(amax, fabsf(x[k]));
@@ -594,8 +660,8 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       for (int s = 0; s < S::kSets; ++s) acc[s][0] = acc[s][1] = acc[s][2] = acc[s][3] = 0.f;
 #pragma unroll
       for (int c = 0; c < S::kChunks; ++c) {
-        const uint4 x = *(const uint4 *)(st + ((g * 2 + 0) * S::kChunks + c) * 512 + lane * 16);
-        const uint4 y = *(const uint4 *)(st + ((g * 2 + 1) * S::kChunks + c) * 512 + lane * 16);
+        const uint32_t at = g * (16 * DP) + (kat ^ (c * 64));
+        const uint4 x = *(const uint4 *)(st + at), y = *(const uint4 *)(st + at + 8 * DP);  // the tokens n and n + 8
         const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -633,14 +699,23 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
     }
 
     // the block scales of the values, relative to the largest so far
-    float vnew = vmax, vr[S::kGroups], vcorr = 1.f;
+    float vr[S::kGroups], vcorr = 1.f;
+    bool same = vmax > 0.f;
 #pragma unroll
-    for (int g = 0; g < S::kGroups; ++g)
-      if (fabsf(vs[g]) < CUDART_INF_F) vnew = fmaxf(vnew, fabsf(vs[g]));
+    for (int g = 0; g < S::kGroups; ++g) same = same && vs[g] == vmax;
+    if (same) {
 #pragma unroll
-    for (int g = 0; g < S::kGroups; ++g) vr[g] = vs[g] == vnew ? (vnew > 0.f ? kWeight : 0.f) : __fdiv_rn(vs[g], vnew) * kWeight;
-    if (vnew != vmax) vcorr = __fdiv_rn(vmax, vnew);
-    vmax = vnew;
+      for (int g = 0; g < S::kGroups; ++g) vr[g] = kWeight;
+    } else {
+      float vnew = vmax;
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g)
+        if (fabsf(vs[g]) < CUDART_INF_F) vnew = fmaxf(vnew, fabsf(vs[g]));
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g) vr[g] = vs[g] == 0.f ? 0.f : vs[g] / vnew * kWeight;
+      if (vnew != vmax) vcorr = vmax / vnew;
+      vmax = vnew;
+    }
 
     uint32_t pf[S::kSets][S::kHalves][S::kGroups][2];
     uint64_t corr[S::kSets];
@@ -685,51 +760,49 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
     }
 
 #pragma unroll
-    for (int part = 0; part < S::kVParts; ++part) {
-      uint32_t vw[S::kGroups][4][S::kVB / 4];
+    for (int part = 0; part < S::kVParts; ++part)
 #pragma unroll
-      for (int g = 0; g < S::kGroups; ++g)
+      for (int g = 0; g < S::kGroups; ++g) {
+        uint32_t vw[4][S::kVB / 4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const uint8_t *src = st + S::kValAt + ((g * 4 + t) * S::kVParts + part) * (32 * S::kVB) + lane * S::kVB;
+          const int row = (t >> 1) * 8 + (t & 1);  // and 2 q4 rows on
+          const uint8_t *src = st + S::kValAt + g * (16 * DP) + row * DP + part * 128;
           if constexpr (S::kVB == 16) {
-            const uint4 x = *(const uint4 *)src;
-            vw[g][t][0] = x.x, vw[g][t][1] = x.y, vw[g][t][2] = x.z, vw[g][t][3] = x.w;
+            const uint4 x = *(const uint4 *)(src + (vat ^ (t & 1) * 64));
+            vw[t][0] = x.x, vw[t][1] = x.y, vw[t][2] = x.z, vw[t][3] = x.w;
           } else {
-            const uint2 x = *(const uint2 *)src;
-            vw[g][t][0] = x.x, vw[g][t][1] = x.y;
+            const uint2 x = *(const uint2 *)(src + vat);
+            vw[t][0] = x.x, vw[t][1] = x.y;
           }
         }
 #pragma unroll
-      for (int y = 0; y < S::kVB / 4; ++y) {
-        uint32_t a[S::kGroups][2][4];  // the bytes (0, 1) and (2, 3) of the words: two tiles
-#pragma unroll
-        for (int g = 0; g < S::kGroups; ++g)
+        for (int y = 0; y < S::kVB / 4; ++y) {
+          uint32_t a[2][4];  // the bytes (0, 1) and (2, 3) of the words: two tiles
 #pragma unroll
           for (int k = 0; k < 2; ++k) {  // the tokens (2r, 2r + 1) and (2r + 8, 2r + 9)
-            const uint32_t x = code_bias<KIND>(vw[g][2 * k][y]), xx = code_bias<KIND>(vw[g][2 * k + 1][y]);
+            const uint32_t x = code_bias<KIND>(vw[2 * k][y]), xx = code_bias<KIND>(vw[2 * k + 1][y]);
             const uint32_t lo = __byte_perm(x, xx, 0x5140), up = __byte_perm(x, xx, 0x7362);
-            a[g][0][2 * k] = widen_lo<KIND>(lo);
-            a[g][0][2 * k + 1] = widen_hi<KIND>(lo);
-            a[g][1][2 * k] = widen_lo<KIND>(up);
-            a[g][1][2 * k + 1] = widen_hi<KIND>(up);
+            a[0][2 * k] = widen_lo<KIND>(lo);
+            a[0][2 * k + 1] = widen_hi<KIND>(lo);
+            a[1][2 * k] = widen_lo<KIND>(up);
+            a[1][2 * k + 1] = widen_hi<KIND>(up);
           }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int j = part * (S::kVB / 2) + y * 2 + k;
+          for (int k = 0; k < 2; ++k) {
+            const int j = part * (S::kVB / 2) + y * 2 + k;
 #pragma unroll
-          for (int s = 0; s < S::kSets; ++s) {
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int s = 0; s < S::kSets; ++s) {
+              float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int g = 0; g < S::kGroups; ++g)
-#pragma unroll
-              for (int hf = 0; hf < S::kHalves; ++hf) mma(acc, a[g][k][0], a[g][k][1], a[g][k][2], a[g][k][3], pf[s][hf][g]);
-            o[s][j][0] = f2_fma(o[s][j][0], corr[s], f2_pack(acc[0], acc[1]));
-            o[s][j][1] = f2_fma(o[s][j][1], corr[s], f2_pack(acc[2], acc[3]));
+              for (int hf = 0; hf < S::kHalves; ++hf) mma(acc, a[k][0], a[k][1], a[k][2], a[k][3], pf[s][hf][g]);
+              const uint64_t a01 = f2_pack(acc[0], acc[1]), a23 = f2_pack(acc[2], acc[3]);
+              o[s][j][0] = g == 0 ? f2_fma(o[s][j][0], corr[s], a01) : f2_add(o[s][j][0], a01);
+              o[s][j][1] = g == 0 ? f2_fma(o[s][j][1], corr[s], a23) : f2_add(o[s][j][1], a23);
+            }
           }
         }
       }
-    }
     tok += S::kUnit;
     if (--cleft) continue;
 
@@ -771,89 +844,103 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       }
       continue;
     }
+    float4 x[S::kSets * S::kTiles];  // in local memory, so that what follows is a loop and not a page of code
+    float2 ml[S::kSets][2];
 #pragma unroll
     for (int s = 0; s < S::kSets; ++s) {
-      float x[S::kTiles][4];
 #pragma unroll
       for (int j = 0; j < S::kTiles; ++j) {
         const float2 a = f2_unpack(o[s][j][0]), b = f2_unpack(o[s][j][1]);
-        x[j][0] = a.x * inv[s][0] * vmax, x[j][1] = a.y * inv[s][1] * vmax;
-        x[j][2] = b.x * inv[s][0] * vmax, x[j][3] = b.y * inv[s][1] * vmax;
-        if (MODE == 0)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) x[j][k] += __shfl_xor_sync(~0u, x[j][k], 2);
+        x[s * S::kTiles + j] = make_float4(a.x * inv[s][0] * vmax, a.y * inv[s][1] * vmax, b.x * inv[s][0] * vmax, b.y * inv[s][1] * vmax);
       }
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int row = MODE == 0 ? (2 * q4 + k) & 3 : s * 8 + 2 * q4 + k;
-        int64_t token;
-        int head, ps;
-        if (!row_of<S>(p, e, row, token, head, ps)) continue;
-        const int64_t at = token * p.a.out_token_stride + head * p.a.out_head_stride;
+      for (int k = 0; k < 2; ++k) ml[s][k] = make_float2(m[s][k], l[s][k]);
+    }
+#pragma unroll 1
+    for (int k = 0; k < 2 * S::kSets; ++k) {
+      const int s = k >> 1, row = MODE == 0 ? (2 * q4 + k) & 3 : s * 8 + 2 * q4 + (k & 1);
+      int64_t token;
+      int head, ps;
+      const bool real = row_of<S>(p, e, row, token, head, ps);
+      const int64_t at = token * p.a.out_token_stride + head * p.a.out_head_stride;
+#pragma unroll 1
+      for (int j = 0; j < S::kTiles; j += 2) {
+        const float4 a = x[s * S::kTiles + j], b = x[s * S::kTiles + j + 1];
+        float y[4] = {k & 1 ? a.y : a.x, k & 1 ? a.w : a.z, k & 1 ? b.y : b.x, k & 1 ? b.w : b.z};
+        if (MODE == 0) {
+          // the lanes of the high and the low halves then hold the same sums and take turns
 #pragma unroll
-        for (int j = 0; j < S::kTiles; j += 2) {
-          // with 4 rows the lanes of the high and the low halves hold the same sums and take turns
-          if (MODE == 0 && (j >> 1 & 1) != (q4 >> 1)) continue;
-          const int d = (2 * j / S::kVB) * 128 + nn * S::kVB + 2 * j % S::kVB;
-          const float y[4] = {x[j][k], x[j][2 + k], x[j + 1][k], x[j + 1][2 + k]};
-          if (d < D) store_row<4>(p.a.out, p.a.out_dtype, at + d, y, p.out_vec);
+          for (int t = 0; t < 4; ++t) y[t] += __shfl_xor_sync(~0u, y[t], 2);
+          if ((j >> 1 & 1) != (q4 >> 1)) continue;
         }
-        if (p.a.lse && nn == 0 && (MODE != 0 || q4 < 2))
-          p.a.lse[token * p.a.n_heads + head] = l[s][k] == 0.f ? -CUDART_INF_F : (m[s][k] + log2f(l[s][k])) * kLn2;
+        const int d = (2 * j / S::kVB) * 128 + nn * S::kVB + 2 * j % S::kVB;
+        if (real && d < D) store_row<4>(p.a.out, p.a.out_dtype, at + d, y, p.out_vec);
+      }
+      if (real && p.a.lse && nn == 0 && (MODE != 0 || q4 < 2)) {
+        const float2 v = ml[s][k & 1];
+        p.a.lse[token * p.a.n_heads + head] = v.y == 0.f ? -CUDART_INF_F : (v.x + log2f(v.y)) * kLn2;
       }
     }
   }
   cp_async_wait<0>();
   __syncthreads();
 
-  // ---- entries cut between warps of this CTA
-  int cross[2] = {-1, -1};  // cut between CTAs: the entry that came from before, the one that goes on
-  for (int i = 0; i < 2 * S::kWarps;) {
-    if (s_cut[i].units == 0) {
-      ++i;
-      continue;
-    }
-    const Desc e = s_cut[i];
-    __shared__ const float *s_from[S::kWarps + 1];
-    int n = 0;
-    const int i0 = i;
-    for (; i < 2 * S::kWarps && (s_cut[i].units == 0 || s_cut[i].begin == e.begin); ++i) n += s_cut[i].units != 0;
-    if (n > 0) {
-      __syncthreads();  // the list of the join before is not read any more
-      if (tid < i - i0 && s_cut[i0 + tid].units) {
-        const int x = i0 + tid, pw = x >> 1;
-        int at = 0;
-        for (int k = i0; k < x; ++k) at += s_cut[k].units != 0;
-        s_from[at] = x & 1 ? (const float *)(smem + ring_at + (size_t)pw * S::kStages * S::kStage)
-                           : ws + (size_t)(kMaxCtas * 2 + blockIdx.x * S::kWarps + pw) * S::kSlot;
-      }
-      __syncthreads();
-    }
-    const bool whole = e.begin >= c0 && e.end <= c1;
-    const int side = e.begin < c0 ? 0 : 1;
-    join<S, MODE, false>(p, e, n, [&](int k) { return s_from[k]; }, whole ? nullptr : cta_slots + side * S::kSlot);
-    if (!whole) cross[side] = i0;
-  }
-
-  // ---- entries cut between CTAs: the last to arrive joins
-  int *counters = (int *)p.a.workspace;
+  // ---- joins: first the entries cut between warps of this CTA, then, if this
+  // CTA is the last to arrive, those cut between CTAs
+  __shared__ const float *s_from[kMaxCtas];
   __shared__ int s_last;
-  for (int side = 0; side < 2; ++side) {
-    if (cross[side] < 0) continue;
-    const Desc e = s_cut[cross[side]];
-    const int first = (int)(e.begin / share), last = (int)((e.end - 1) / share);
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) {
-      s_last = atomicAdd(counters + first, 1) == last - first;
-      if (s_last) counters[first] = 0;
+  int *counters = (int *)p.a.workspace;
+  int cross[2] = {-1, -1};  // cut between CTAs: the entry that came from before, the one that goes on
+#pragma unroll 1
+  for (int i = 0, side = 0;;) {
+    int i0 = i, n = 0;
+    float *to = nullptr;
+    Desc e;
+    if (i < 2 * S::kWarps) {
+      const int64_t begin = lane < 2 * S::kWarps && s_cut[lane].units ? s_cut[lane].begin : -1;
+      const uint32_t left = __ballot_sync(~0u, begin >= 0) & (~0u << i);
+      if (left == 0) {
+        i = 2 * S::kWarps;
+        continue;
+      }
+      i0 = __ffs(left) - 1;
+      e = s_cut[i0];
+      const uint32_t same = __ballot_sync(~0u, begin == e.begin);  // its parts are neighbours
+      n = __popc(same);
+      i = 32 - __clz(same);
+      __syncthreads();  // the list of the join before is not read any more
+      if (w == 0 && same >> lane & 1) {
+        const int pw = lane >> 1;
+        s_from[__popc(same & ((1u << lane) - 1))] =
+            lane & 1 ? (const float *)(smem + ring_at + (size_t)pw * S::kStages * S::kStage)
+                     : ws + (size_t)(kMaxCtas * 2 + blockIdx.x * S::kWarps + pw) * S::kSlot;
+      }
+      if (e.begin < c0 || e.end > c1) {
+        const int k = e.begin < c0 ? 0 : 1;
+        cross[k] = i0;
+        to = cta_slots + k * S::kSlot;
+      }
+    } else {
+      if (side == 2) break;
+      const int k = cross[side++];
+      if (k < 0) continue;
+      e = s_cut[k];
+      const int first = (int)(e.begin / share);
+      n = (int)((e.end - 1) / share) - first + 1;
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        s_last = atomicAdd(counters + first, 1) == n - 1;
+        if (s_last) counters[first] = 0;
+      }
+      // the first CTA's part is its second slot, the others' their first
+      for (int x = tid; x < n; x += S::kThreads) s_from[x] = ws + ((size_t)(first + x) * 2 + (x == 0)) * S::kSlot;
+      __syncthreads();
+      if (!s_last) continue;
+      __threadfence();
     }
     __syncthreads();
-    if (!s_last) continue;
-    __threadfence();
-    // the first CTA's part is its second slot, the others' their first
-    const float *from = ws + (size_t)first * 2 * S::kSlot;
-    join<S, MODE, true>(p, e, last - first + 1, [&](int k) { return from + (k ? k * 2 : 1) * S::kSlot; }, nullptr);
+    join<S, MODE>(p, e, n, s_from, to);
   }
 }
 
@@ -883,8 +970,8 @@ template <int KIND, int DP, int MODE>
 seedq_status launch(Args &p, int dev, cudaStream_t st) {
   using S = Shape<DP, MODE>;
   static DeviceOnce once;
-  p.chunk = (p.a.n_requests + kMaxChunks - 1) / kMaxChunks;
-  constexpr size_t smem = (((kMaxChunks + 1) * 8 + 15) & ~15) + (size_t)S::kWarps * S::kStages * S::kStage;
+  p.chunk = (p.a.n_requests + S::kRequests - 1) / S::kRequests;
+  constexpr size_t smem = sizeof(Table<S>) + (size_t)S::kWarps * S::kStages * S::kStage;
   static_assert(smem + 6144 <= kSmemMax, "");
   const int rc = once.run(dev, [] {
     return (int)cudaFuncSetAttribute(k_attend<KIND, DP, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -913,6 +1000,13 @@ auto with_shape(const Plan &s, F f) {
 bool aligned(const void *base, int32_t dtype, int64_t ts, int64_t hs) {
   const int64_t per = 16 / dtype_bytes(dtype);
   return (uintptr_t)base % 16 == 0 && ts % per == 0 && hs % per == 0;
+}
+
+int log2_of(int x) {  // -1 if x is no power of two
+  if (x & (x - 1)) return -1;
+  int n = 0;
+  while (x >>= 1) ++n;
+  return n;
 }
 
 seedq_status check(const seedq_kv_cache *c, int32_t n_heads, int32_t max_new) {
@@ -951,6 +1045,9 @@ seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_arg
   p.c = *cache;
   p.a = a;
   p.group = a.n_heads / cache->n_kv_heads;
+  p.group_shift = log2_of(p.group);
+  p.gpp_shift = log2_of(cache->page_size / 16);
+  p.q_bytes = dtype_bytes(a.q_dtype);
   p.q_vec = aligned(a.q, a.q_dtype, a.q_token_stride, a.q_head_stride);
   p.out_vec = aligned(a.out, a.out_dtype, a.out_token_stride, a.out_head_stride);
   int dev = 0, sms = 0;
@@ -958,6 +1055,7 @@ seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_arg
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return cuda_fail(e);
   p.ctas = std::min(sms, kMaxCtas);
+  p.ctas_inv = ~0ull / (uint64_t)p.ctas + 1;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   return with_shape(shape_for(cache, a.n_heads, a.max_new), [&](auto dp, auto mode) {
     return cache->kind == SEEDQ_KV_INT8 ? launch<SEEDQ_KV_INT8, dp.value, mode.value>(p, dev, stream)
