@@ -489,7 +489,7 @@ seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_arg
  *              (n_rows, vocab) bytes, zeroed once before its first use; calls
  *              that may overlap need one each.
  * Errors: INVALID_ARG (NULL pointer, n_rows < 0, vocab outside 1..2^30,
- * row_stride < vocab, scale not finite and positive, top_k out of range,
+ * row_stride < vocab, scale not positive and below 2^127, top_k out of range,
  * workspace too small), CUDA.  n_rows = 0 is a no-op. */
 uint64_t seedq_token_logprobs_workspace_bytes(int64_t n_rows, int64_t vocab);
 seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab,

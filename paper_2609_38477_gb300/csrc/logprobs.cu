@@ -1,31 +1,75 @@
 // Log probability, rank, entropy and top alternatives of a token under a row of
 // logits (seedq_token_logprobs).
+//
+// Mathematics, one pass over the logits x with c = scale * log2(e):
+//   m = max x,  d = c (x - m),  s1 = sum 2^d,  s2 = sum d 2^d,
+//   logprob = ln2 (c (x_t - m) - log2 s1),  entropy = ln2 (log2 s1 - s2 / s1);
+// when the running maximum rises by e / c, s1 and s2 become s1 2^-e and
+// (s2 - e s1) 2^-e.  Differences come first: nothing overflows, and a large
+// common part of the logits does not cost precision.  The rank counts logits
+// above the target's; equal ones count where their index is lower.
+//
+// The first top_k tokens are kept as a sorted list, one 64-bit key per lane of a
+// warp (the logit as an ordered integer, then the inverted index: equal logits
+// go by the lower index).  A tile of logits is looked at only if its maximum
+// reaches the list's last entry, which happens about top_k * ln(vocab) times
+// per list; a list starts from the top_k-th largest of the lanes' own maxima of
+// its first tile instead of from nothing.
+//
+// What bounds it: many rows, the bytes of the logits (about 9 instructions and
+// one 2^x per logit leave the SMs at half their rate for float32); few rows, the
+// latency of the joins.
+//
+// Split.  All rows' tiles form one sequence, cut into equal ranges, one per warp
+// (at least one tile each).  A warp that holds a whole row writes its results;
+// parts of rows cut between warps are joined by the CTA, those cut between CTAs
+// by the last CTA to arrive (a counter per CTA, reset by that CTA), in the order
+// of the tokens.
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <cmath>
 
+#include "cp_async.cuh"
+#include "device_once.h"
+#include "f32x2.cuh"
 #include "serve.cuh"
 
 namespace seedq {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kWarps = 16;
+constexpr int kThreads = kWarps * 32;
+constexpr int kMaxCtas = 152;
 constexpr int kMaxTop = 32;
+constexpr int kStages = 4;       // tiles in a warp's ring
+constexpr int kTileBytes = 2048; // 64 bytes per lane
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 struct ScoreArgs {
   const void *x;
-  int dtype;
-  int64_t stride;
-  int32_t vocab;
-  float scale;
+  int64_t stride, rows;
+  int32_t vocab, tiles;  // tiles of a row
+  float c;               // scale * log2(e)
   const int64_t *targets;
   float *logprob, *entropy;
   int32_t *rank;
-  int top_k;
+  int32_t top_k;
   float *top_logprob;
   int32_t *top_index;
+  void *workspace;
+  int32_t ctas;
+  int64_t share;  // tiles per CTA
+};
+
+// What a range of a row's logits comes to.
+struct Part {
+  float m, s1, s2;  // as above
+  int32_t count;    // logits before the target
+  uint64_t key[kMaxTop];
 };
 
 // A logit's place in the order as a whole number: larger logits first, NaN
@@ -39,83 +83,422 @@ __device__ __forceinline__ float key_value(uint64_t key) {
   const uint32_t u = (uint32_t)(key >> 32);
   return u == 0xffffffffu ? CUDART_NAN_F : __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u);
 }
+__device__ __forceinline__ int key_index(uint64_t key) { return (int)~(uint32_t)key; }
 
-__device__ float cta_sum(float v, float *sm) {
-  sm[threadIdx.x] = v;
-  __syncthreads();
-  for (int s = kThreads / 2; s; s >>= 1) {
-    if (threadIdx.x < s) sm[threadIdx.x] += sm[threadIdx.x + s];
-    __syncthreads();
-  }
-  v = sm[0];
-  __syncthreads();
-  return v;
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
 }
-__device__ uint64_t cta_max(uint64_t v, uint64_t *sm) {
-  sm[threadIdx.x] = v;
-  __syncthreads();
-  for (int s = kThreads / 2; s; s >>= 1) {
-    if (threadIdx.x < s) sm[threadIdx.x] = max(sm[threadIdx.x], sm[threadIdx.x + s]);
-    __syncthreads();
-  }
-  v = sm[0];
-  __syncthreads();
-  return v;
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-// One CTA per row, one pass for the maximum, one for the sums, one per
-// alternative.
-__global__ void __launch_bounds__(kThreads) k_score(ScoreArgs a) {
-  __shared__ float smf[kThreads];
-  __shared__ uint64_t smk[kThreads];
-  __shared__ int s_rank;
-  const int64_t row = blockIdx.x, base = row * a.stride;
-  uint64_t best = 0;
-  for (int i = threadIdx.x; i < a.vocab; i += kThreads) best = max(best, order_key(load_elem(a.x, a.dtype, base + i), i));
-  best = cta_max(best, smk);
-  const float m = key_value(best) * a.scale;
-  const bool empty = m == -CUDART_INF_F, bad = isnan(m) || m == CUDART_INF_F;
-  const int64_t t = a.targets ? a.targets[row] : -1;
-  const bool has = t >= 0 && t < a.vocab;
-  const float xt = has ? load_elem(a.x, a.dtype, base + t) : 0.f;
-  const uint64_t kt = has ? order_key(xt, (int)t) : ~0ull;
-  float s1 = 0.f, s2 = 0.f;
-  int before = 0;
-  for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-    const float x = load_elem(a.x, a.dtype, base + i), d = x * a.scale - m;
-    before += order_key(x, i) > kt;
-    const float e = expf(d);
-    if (e > 0.f) s1 += e, s2 += e * d;
+// A load past the L1 cache: sees what other SMs wrote.
+template <typename T>
+__device__ __forceinline__ T fresh_load(const T *x) { return *(const volatile T *)x; }
+
+// The sums relative to a maximum `to` that is no smaller.
+__device__ __forceinline__ void rebase(float &m, float &s1, float &s2, float to, float c) {
+  const float d = m == -CUDART_INF_F ? 0.f : max_nan((m - to) * c, -1e4f), e = exp2_fast(d);
+  s2 = (s2 + d * s1) * e;
+  s1 *= e;
+  m = to;
+}
+
+// Both lists' first 32 keys in order: of two descending lists, the larger of a's
+// i-th and b's (31 - i)-th are the 32 largest, a bitonic sequence.
+__device__ __forceinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane) {
+  b = __shfl_sync(~0u, b, 31 - lane);
+  uint64_t x = a > b ? a : b;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const uint64_t y = __shfl_xor_sync(~0u, x, o);
+    x = (lane & o) == 0 ? (x > y ? x : y) : (x < y ? x : y);
   }
-  s1 = cta_sum(s1, smf);
-  s2 = cta_sum(s2, smf);
-  if (threadIdx.x == 0) s_rank = 0;
-  __syncthreads();
-  atomicAdd(&s_rank, before);
-  __syncthreads();
-  const int rank = s_rank;
-  const float ln = logf(s1);
-  if (threadIdx.x == 0) {
-    if (a.entropy) a.entropy[row] = bad ? CUDART_NAN_F : empty ? 0.f : ln - s2 / s1;
+  return x;
+}
+
+// Writes a row's results: key is the lane's entry of the list, the rest is the
+// same in all lanes.
+__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, float m, float s1, float s2, int count, uint64_t key,
+                                          int64_t t, float xt) {
+  const int lane = threadIdx.x & 31;
+  const bool bad = isnan(m) || m == CUDART_INF_F, empty = m == -CUDART_INF_F;
+  const float lg = log2f(s1);
+  if (lane == 0) {
+    if (a.entropy) a.entropy[row] = bad ? CUDART_NAN_F : empty ? 0.f : kLn2 * (lg - s2 / s1);
     if (a.targets) {
-      a.logprob[row] = t == -1 ? 0.f : !has || bad ? CUDART_NAN_F : empty ? -CUDART_INF_F : xt * a.scale - m - ln;
-      a.rank[row] = has && !isnan(m) ? rank : -1;
+      const bool has = t >= 0 && t < a.vocab;
+      a.logprob[row] = t == -1          ? 0.f
+                       : !has || bad    ? CUDART_NAN_F
+                       : empty          ? -CUDART_INF_F
+                                        : kLn2 * ((xt - m) * a.c - lg);
+      a.rank[row] = has && !isnan(m) ? count : -1;
     }
   }
-  uint64_t last = ~0ull;
-  for (int k = 0; k < a.top_k; ++k) {
-    uint64_t b = 0;
-    for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-      const uint64_t key = order_key(load_elem(a.x, a.dtype, base + i), i);
-      if (key < last) b = max(b, key);
-    }
-    last = cta_max(b, smk);
-    if (threadIdx.x == 0) {
-      a.top_index[row * a.top_k + k] = last ? (int)~(uint32_t)last : -1;
-      a.top_logprob[row * a.top_k + k] = !last || empty ? -CUDART_INF_F : bad ? CUDART_NAN_F
-                                                        : key_value(last) * a.scale - m - ln;
-    }
+  if (lane < a.top_k) {
+    const float x = key_value(key);
+    a.top_index[row * a.top_k + lane] = key ? key_index(key) : -1;
+    a.top_logprob[row * a.top_k + lane] = !key || empty ? -CUDART_INF_F : bad ? CUDART_NAN_F : kLn2 * ((x - m) * a.c - lg);
   }
+}
+
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ ScoreArgs a) {
+  constexpr int kPer = DT == SEEDQ_F32 ? 16 : 32;  // logits of a lane and tile
+  constexpr int kVec = DT == SEEDQ_F32 ? 4 : 8;    // in one 16-byte load
+  constexpr int kTile = 32 * kPer;
+  constexpr int kSize = DT == SEEDQ_F32 ? 4 : 2;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ Part s_part[2 * kWarps];
+  __shared__ int64_t s_row[2 * kWarps];  // its row, or -1
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  if (lane < 2) s_row[2 * w + lane] = -1;
+
+  const int64_t total = a.rows * a.tiles;
+  const int64_t c0 = a.share * blockIdx.x, c1 = min(c0 + a.share, total);
+  const uint32_t mine = (uint32_t)(c1 - c0), each = mine / kWarps, rest = mine - each * kWarps;
+  const int64_t w0 = c0 + each * (uint32_t)w + min((uint32_t)w, rest);
+  const int64_t w1 = w0 + each + (w < (int)rest);
+
+  uint8_t *ring = smem + w * (kStages * kTileBytes) + lane * 16;
+  const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+
+  int64_t row = w0 / a.tiles, prow = row;
+  int tile = (int)(w0 - row * a.tiles), ptile = tile;
+  int64_t left = w1 - w0;
+  int pstage = 0, stage = 0;
+  int64_t pleft = left;
+  auto issue = [&]() {
+    if (VEC && pleft > 0) {
+      const char *src = (const char *)a.x + (prow * a.stride + (int64_t)ptile * kTile + lane * kVec) * kSize;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        // the pieces of a row's last tile that lie past its end are not read
+        const int i = ptile * kTile + v * (32 * kVec) + lane * kVec;
+        const int bytes = min(max(a.vocab - i, 0) * kSize, 16);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ring_s + pstage * kTileBytes + v * 512),
+                     "l"(bytes ? src + v * 512 : (const char *)a.x), "r"(bytes)
+                     : "memory");
+      }
+      --pleft;
+      pstage = pstage + 1 == kStages ? 0 : pstage + 1;
+      if (++ptile == a.tiles) ptile = 0, ++prow;
+    }
+    cp_async_commit();
+  };
+  if (left > 0)
+    for (int i = 0; i < kStages - 1; ++i) issue();
+
+  // The targets of this row and the next two, and the logits of the first two,
+  // are on their way before they are needed.
+  auto target = [&](int64_t r) -> int64_t { return a.targets && r < a.rows ? a.targets[r] : -1; };
+  auto logit = [&](int64_t r, int64_t t) -> float {
+    return t >= 0 && t < a.vocab ? load_elem(a.x, DT, r * a.stride + t) : 0.f;
+  };
+  int64_t t = target(row), t1 = target(row + 1);
+  float xt = logit(row, t), xt1 = logit(row + 1, t1);
+  float above = 0.f, from = 0.f;  // logits greater than these come before the target: past it and ahead of it
+
+  float m = 0.f, s1 = 0.f, s2 = 0.f, tau = 0.f;
+  int count = 0;
+  uint64_t key = 0, last = 0;  // the lane's entry of the list; the list's last
+  bool fresh = true;           // the row begins for this warp
+  const int64_t row0 = row;
+
+  for (; left > 0; --left) {
+    if (fresh) {
+      if (row != row0) {
+        t = t1, xt = xt1;
+        t1 = target(row + 1);
+        xt1 = logit(row + 1, t1);
+      }
+      m = -CUDART_INF_F;
+      s1 = s2 = 0.f;
+      count = 0;
+      key = last = 0;
+      above = xt;
+      // x >= xt as x > the number before xt; for -inf every x: no x is <= NaN
+      from = xt == -CUDART_INF_F ? CUDART_NAN_F
+             : xt == 0.f         ? __uint_as_float(0x80000001u)
+                                 : __uint_as_float(__float_as_uint(xt) + (xt > 0.f ? -1 : 1));
+    }
+    issue();
+    float x[kPer];
+    const int base = tile * kTile;
+    if (VEC) {
+      cp_async_wait<kStages - 1>();
+      const uint8_t *src = ring + stage * kTileBytes;
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const uint4 y = *(const uint4 *)(src + v * 512);
+        const uint32_t z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (DT == SEEDQ_F32) {
+            x[v * 4 + k] = __uint_as_float(z[k]);
+          } else if (DT == SEEDQ_BF16) {
+            x[v * 8 + 2 * k] = __uint_as_float(z[k] << 16);
+            x[v * 8 + 2 * k + 1] = __uint_as_float(z[k] & 0xffff0000u);
+          } else {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&z[k]));
+            x[v * 8 + 2 * k] = f.x, x[v * 8 + 2 * k + 1] = f.y;
+          }
+        }
+      }
+    }
+    const uint8_t *held = ring + (stage == 0 ? kStages - 1 : stage - 1) * kTileBytes;
+    // index of element e: rows that allow wide loads give a lane 16 bytes in a row, others single logits
+    auto index = [&](int e) -> int {
+      return base + (VEC ? (e / kVec) * (32 * kVec) + lane * kVec + e % kVec : e * 32 + lane);
+    };
+    // element e again, for the rare loops that are not unrolled
+    auto fetch = [&](int e) -> float {
+      if (index(e) >= a.vocab) return -CUDART_INF_F;
+      return VEC ? load_elem(held + (e / kVec) * 512, DT, e % kVec) : load_elem(a.x, DT, row * a.stride + index(e));
+    };
+    const bool partial = base + kTile > a.vocab;
+    if (!VEC) {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) x[e] = index(e) < a.vocab ? load_elem(a.x, DT, row * a.stride + index(e)) : -CUDART_INF_F;
+    } else if (partial) {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e)
+        if (index(e) >= a.vocab) x[e] = -CUDART_INF_F;
+    }
+
+    // the rank
+    if (a.targets) {
+      if (partial || (t >= base && t < base + kTile)) {
+#pragma unroll 1
+        for (int e = 0; e < kPer; ++e) count += index(e) < a.vocab && !(fetch(e) <= (index(e) < t ? from : above));
+      } else {
+        const float thr = base < t ? from : above;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) count += !(x[e] <= thr);
+      }
+    }
+
+    // the sums
+    float mv[4], mx;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      mv[v] = x[v * (kPer / 4)];
+#pragma unroll
+      for (int e = 1; e < kPer / 4; ++e) mv[v] = max_nan(mv[v], x[v * (kPer / 4) + e]);
+    }
+    mx = max_nan(max_nan(mv[0], mv[1]), max_nan(mv[2], mv[3]));
+    const float to = max_nan(m, mx);
+    rebase(m, s1, s2, to, a.c);
+    const float off = to == -CUDART_INF_F ? 0.f : -to;
+    const uint64_t off2 = f2_pack(off, off), c2 = f2_pack(a.c, a.c);
+    uint64_t p1 = 0, p2 = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2) {
+      const float2 d = f2_unpack(f2_mul(f2_add(f2_pack(x[e], x[e + 1]), off2), c2));
+      const float d0 = max_nan(d.x, -1e4f), d1 = max_nan(d.y, -1e4f);  // 2^-10000 is 0, and so is its product with d
+      const uint64_t y = f2_pack(exp2_fast(d0), exp2_fast(d1));
+      p1 = f2_add(p1, y);
+      p2 = f2_fma(y, f2_pack(d0, d1), p2);
+    }
+    const float2 q1 = f2_unpack(p1), q2 = f2_unpack(p2);
+    s1 += q1.x + q1.y;
+    s2 += q2.x + q2.y;
+
+    // the list
+    if (a.top_k) {
+      if (fresh) {  // the top_k-th largest of the lanes' maxima: at least top_k logits reach it
+        int before = 0;
+#pragma unroll
+        for (int o = 0; o < 32; ++o) {
+          const float y = __shfl_sync(~0u, mx, o);
+          before += !(y <= mx) || (y == mx && o < lane);
+        }
+        tau = __shfl_sync(~0u, mx, __ffs(__ballot_sync(~0u, before == a.top_k - 1) | 0x80000000u) - 1);
+        if (!__any_sync(~0u, before == a.top_k - 1)) tau = -CUDART_INF_F;  // NaN among them
+      }
+      if (__any_sync(~0u, !(mx < tau))) {
+#pragma unroll 1
+        for (int v = 0; v < 4; ++v) {
+          const float most = v == 0 ? mv[0] : v == 1 ? mv[1] : v == 2 ? mv[2] : mv[3];
+          if (!__any_sync(~0u, !(most < tau))) continue;
+#pragma unroll 1
+          for (int e = v * (kPer / 4); e < (v + 1) * (kPer / 4); ++e) {
+            const float y = fetch(e);
+            const uint64_t own = order_key(y, index(e));
+            uint32_t todo = __ballot_sync(~0u, !(y < tau) && own > last && index(e) < a.vocab);
+            if (todo == 0) continue;
+            while (todo) {
+              const uint64_t cand = __shfl_sync(~0u, own, __ffs(todo) - 1);
+              todo &= todo - 1;
+              const uint64_t up = __shfl_up_sync(~0u, key, 1);
+              if (key < cand) key = lane > 0 && up < cand ? up : cand;
+            }
+            last = __shfl_sync(~0u, key, a.top_k - 1);
+            if (last) tau = key_value(last);
+          }
+        }
+      }
+    }
+    fresh = false;
+
+    if (++tile < a.tiles && left > 1) continue;
+
+    // ---- the end of this warp's part of a row
+    const int64_t begin = row * a.tiles;
+    const bool whole = begin >= w0 && begin + a.tiles <= w1;
+    float M = m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) M = max_nan(M, __shfl_xor_sync(~0u, M, o));
+    rebase(m, s1, s2, M, a.c);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      s1 += __shfl_xor_sync(~0u, s1, o);
+      s2 += __shfl_xor_sync(~0u, s2, o);
+    }
+    count = __reduce_add_sync(~0u, count);
+    if (whole) {
+      write_row(a, row, m, s1, s2, count, key, t, xt);
+    } else {
+      const int at = 2 * w + (left == 1);
+      s_part[at].key[lane] = key;
+      if (lane == 0) {
+        s_part[at].m = m, s_part[at].s1 = s1, s_part[at].s2 = s2, s_part[at].count = count;
+        s_row[at] = row;
+      }
+    }
+    tile = 0;
+    ++row;
+    fresh = true;
+  }
+  cp_async_wait<0>();
+  __syncthreads();
+
+  // ---- joins: rows cut between the warps of this CTA, then, if it is the last
+  // to arrive, rows cut between CTAs
+  Part *slots = (Part *)((uint8_t *)a.workspace + kMaxCtas * 8);  // two per CTA
+  int *counters = (int *)a.workspace;
+  __shared__ Part s_sum[kWarps];
+  __shared__ int s_last, s_index[32];
+  int64_t cross[2] = {-1, -1};
+#pragma unroll 1
+  for (int i = 0, side = 0;;) {
+    int64_t r;
+    int n;
+    const Part *parts;  // n in a row, or, between CTAs, one in two but for the first
+    Part *to = nullptr;
+    bool mem = false;
+    if (i < 2 * kWarps) {
+      const int64_t mine_row = s_row[lane];
+      const uint32_t todo = __ballot_sync(~0u, mine_row >= 0) & (~0u << i);
+      if (todo == 0) {
+        i = 2 * kWarps;
+        continue;
+      }
+      r = s_row[__ffs(todo) - 1];
+      const uint32_t same = __ballot_sync(~0u, mine_row == r);
+      n = __popc(same);
+      i = 32 - __clz(same);
+      parts = s_part;
+      if (w == 0 && same >> lane & 1) s_index[__popc(same & ((1u << lane) - 1))] = lane;
+      __syncthreads();
+      const int64_t begin = r * a.tiles;
+      if (begin < c0 || begin + a.tiles > c1) {
+        const int k = begin < c0 ? 0 : 1;
+        cross[k] = r;
+        to = slots + 2 * blockIdx.x + k;
+      }
+    } else {
+      if (side == 2) break;
+      r = cross[side++];
+      if (r < 0) continue;
+      const int first = (int)(r * a.tiles / a.share);
+      n = (int)(((r + 1) * a.tiles - 1) / a.share) - first + 1;
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        s_last = atomicAdd(counters + first, 1) == n - 1;
+        if (s_last) counters[first] = 0;
+      }
+      __syncthreads();
+      if (!s_last) continue;
+      __threadfence();
+      parts = slots + 2 * first;
+      mem = true;
+    }
+    // part j of n
+    auto part = [&](int j) -> const Part * {
+      return parts + (mem ? (j ? 2 * j : 1) : s_index[j]);
+    };
+    // every warp joins its share in order, then pairs of neighbours are joined
+    const int lo = n * w / kWarps, hi = n * (w + 1) / kWarps;
+    float fm = -CUDART_INF_F, f1 = 0.f, f2 = 0.f;
+    int fc = 0;
+    uint64_t fk = 0;
+    for (int j = lo; j < hi; ++j) {
+      const Part *q = part(j);
+      float m2 = fresh_load(&q->m), b1 = fresh_load(&q->s1), b2 = fresh_load(&q->s2);
+      fc += fresh_load(&q->count);
+      const uint64_t k2 = a.top_k ? fresh_load(&q->key[lane]) : 0;
+      const float M = max_nan(fm, m2);
+      rebase(fm, f1, f2, M, a.c);
+      rebase(m2, b1, b2, M, a.c);
+      f1 += b1, f2 += b2;
+      if (a.top_k) fk = merge_lists(fk, k2, lane);
+    }
+    for (int o = 1; o < kWarps; o <<= 1) {
+      __syncthreads();
+      if (w & o) {
+        s_sum[w].key[lane] = fk;
+        if (lane == 0) s_sum[w].m = fm, s_sum[w].s1 = f1, s_sum[w].s2 = f2, s_sum[w].count = fc;
+      }
+      __syncthreads();
+      if ((w & (2 * o - 1)) == 0) {
+        const Part &q = s_sum[w + o];
+        float m2 = q.m, b1 = q.s1, b2 = q.s2;
+        fc += q.count;
+        const float M = max_nan(fm, m2);
+        rebase(fm, f1, f2, M, a.c);
+        rebase(m2, b1, b2, M, a.c);
+        f1 += b1, f2 += b2;
+        if (a.top_k) fk = merge_lists(fk, q.key[lane], lane);
+      }
+    }
+    if (w == 0) {
+      if (to) {
+        to->key[lane] = fk;
+        if (lane == 0) to->m = fm, to->s1 = f1, to->s2 = f2, to->count = fc;
+      } else {
+        const int64_t tt = target(r);
+        write_row(a, r, fm, f1, f2, fc, fk, tt, logit(r, tt));
+      }
+    }
+    __syncthreads();
+  }
+}
+
+DeviceOnce g_once[6];
+
+template <int DT, bool VEC>
+seedq_status launch(ScoreArgs &a, int sms, int dev, cudaStream_t st) {
+  constexpr int kTile = 32 * (DT == SEEDQ_F32 ? 16 : 32);
+  a.tiles = (a.vocab + kTile - 1) / kTile;
+  const int64_t total = a.rows * a.tiles;
+  const int ctas = std::min(sms, kMaxCtas);
+  a.share = std::max<int64_t>((total + ctas - 1) / ctas, kWarps);
+  a.ctas = (int)((total + a.share - 1) / a.share);
+  constexpr size_t smem = (size_t)kWarps * kStages * kTileBytes;
+  const int rc = g_once[DT * 2 + VEC].run(dev, [] {
+    return (int)cudaFuncSetAttribute(k_score<DT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  });
+  if (rc) return cuda_fail((cudaError_t)rc);
+  k_score<DT, VEC><<<a.ctas, kThreads, smem, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
 }
 
 }  // namespace
@@ -126,8 +509,8 @@ using namespace seedq;
 extern "C" {
 
 uint64_t seedq_token_logprobs_workspace_bytes(int64_t n_rows, int64_t vocab) {
-  (void)vocab;
-  return n_rows < 0 ? 0 : 16;
+  if (n_rows < 0 || vocab < 1) return 0;
+  return kMaxCtas * 8 + (uint64_t)kMaxCtas * 2 * sizeof(Part);  // arrival counters; two parts of rows per CTA
 }
 
 seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
@@ -135,17 +518,27 @@ seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_r
                                   int32_t top_k, float *top_logprob, int32_t *top_index, void *workspace,
                                   uint64_t workspace_bytes, void *cuda_stream) {
   if (!dtype_ok(dtype) || n_rows < 0 || n_rows > INT32_MAX || vocab < 1 || vocab > (1 << 30) || row_stride < vocab ||
-      !std::isfinite(scale) || scale <= 0.f || top_k < 0 || top_k > kMaxTop)
+      !std::isfinite(scale * kLog2e) || scale <= 0.f || top_k < 0 || top_k > kMaxTop)
     return SEEDQ_ERR_INVALID_ARG;
   if (n_rows == 0) return SEEDQ_OK;
   if (!logits || (targets && (!logprob || !rank)) || (top_k && (!top_logprob || !top_index)) || !workspace ||
       (uintptr_t)workspace % 16 || workspace_bytes < seedq_token_logprobs_workspace_bytes(n_rows, vocab))
     return SEEDQ_ERR_INVALID_ARG;
-  const ScoreArgs a{logits, dtype, row_stride, (int32_t)vocab, scale, targets, logprob, entropy, rank, top_k, top_logprob,
-                    top_index};
-  k_score<<<(unsigned)n_rows, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
-  const cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
+  ScoreArgs a{};
+  a.x = logits, a.stride = row_stride, a.rows = n_rows, a.vocab = (int32_t)vocab, a.c = scale * kLog2e;
+  a.targets = targets, a.logprob = logprob, a.entropy = entropy, a.rank = rank;
+  a.top_k = top_k, a.top_logprob = top_logprob, a.top_index = top_index, a.workspace = workspace;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return cuda_fail(e);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const bool vec = (uintptr_t)logits % 16 == 0 && (n_rows == 1 || row_stride * dtype_bytes(dtype) % 16 == 0);
+  switch (dtype) {
+    case SEEDQ_F32: return vec ? launch<SEEDQ_F32, true>(a, sms, dev, st) : launch<SEEDQ_F32, false>(a, sms, dev, st);
+    case SEEDQ_BF16: return vec ? launch<SEEDQ_BF16, true>(a, sms, dev, st) : launch<SEEDQ_BF16, false>(a, sms, dev, st);
+    default: return vec ? launch<SEEDQ_F16, true>(a, sms, dev, st) : launch<SEEDQ_F16, false>(a, sms, dev, st);
+  }
 }
 
 }  // extern "C"
