@@ -1002,13 +1002,6 @@ bool aligned(const void *base, int32_t dtype, int64_t ts, int64_t hs) {
   return (uintptr_t)base % 16 == 0 && ts % per == 0 && hs % per == 0;
 }
 
-int log2_of(int x) {  // -1 if x is no power of two
-  if (x & (x - 1)) return -1;
-  int n = 0;
-  while (x >>= 1) ++n;
-  return n;
-}
-
 seedq_status check(const seedq_kv_cache *c, int32_t n_heads, int32_t max_new) {
   const seedq_status st = kv_check(c);
   if (st != SEEDQ_OK) return st;

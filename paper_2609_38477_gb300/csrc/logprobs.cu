@@ -14,7 +14,10 @@
 // go by the lower index).  A tile of logits is looked at only if its maximum
 // reaches the list's last entry, which happens about top_k * ln(vocab) times
 // per list; a list starts from the top_k-th largest of the lanes' own maxima of
-// its first tile instead of from nothing.
+// its first tile instead of from nothing.  Where few lanes hold logits that
+// reach it, the whole warp looks at one lane's logits at a time and inserts what
+// passes (about 75 cycles a key); else they are packed in shared memory, sorted
+// 32 at a time and merged (about 600 cycles).
 //
 // What bounds it: many rows, the bytes of the logits (about 9 instructions and
 // one 2^x per logit leave the SMs at half their rate for float32); few rows, the
@@ -40,11 +43,12 @@
 namespace seedq {
 namespace {
 
-constexpr int kWarps = 16;
+constexpr int kWarps = 12;
 constexpr int kThreads = kWarps * 32;
-constexpr int kMaxCtas = 152;
+constexpr int kCtasPerSm = 2;
+constexpr int kMaxCtas = 152 * kCtasPerSm;
 constexpr int kMaxTop = 32;
-constexpr int kStages = 4;       // tiles in a warp's ring
+constexpr int kStages = 3;       // tiles in a warp's ring
 constexpr int kTileBytes = 2048; // 64 bytes per lane
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -90,6 +94,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either i
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -110,7 +119,7 @@ __device__ __forceinline__ void rebase(float &m, float &s1, float &s2, float to,
 
 // Both lists' first 32 keys in order: of two descending lists, the larger of a's
 // i-th and b's (31 - i)-th are the 32 largest, a bitonic sequence.
-__device__ __forceinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane) {
+__device__ __noinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane) {
   b = __shfl_sync(~0u, b, 31 - lane);
   uint64_t x = a > b ? a : b;
 #pragma unroll
@@ -121,9 +130,22 @@ __device__ __forceinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane
   return x;
 }
 
+// A warp's keys in descending order (bitonic).
+__device__ __noinline__ uint64_t sort_keys(uint64_t x, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+    for (int o = size >> 1; o; o >>= 1) {
+      const uint64_t y = __shfl_xor_sync(~0u, x, o);
+      const bool larger = ((lane & o) == 0) == ((lane & size) == 0);
+      x = (x > y) == larger ? x : y;
+    }
+  return x;
+}
+
 // Writes a row's results: key is the lane's entry of the list, the rest is the
 // same in all lanes.
-__device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, float m, float s1, float s2, int count, uint64_t key,
+__device__ __noinline__ void write_row(const ScoreArgs &a, int64_t row, float m, float s1, float s2, int count, uint64_t key,
                                           int64_t t, float xt) {
   const int lane = threadIdx.x & 31;
   const bool bad = isnan(m) || m == CUDART_INF_F, empty = m == -CUDART_INF_F;
@@ -147,7 +169,7 @@ __device__ __forceinline__ void write_row(const ScoreArgs &a, int64_t row, float
 }
 
 template <int DT, bool VEC>
-__global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ ScoreArgs a) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_score(const __grid_constant__ ScoreArgs a) {
   constexpr int kPer = DT == SEEDQ_F32 ? 16 : 32;  // logits of a lane and tile
   constexpr int kVec = DT == SEEDQ_F32 ? 4 : 8;    // in one 16-byte load
   constexpr int kTile = 32 * kPer;
@@ -155,6 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ Part s_part[2 * kWarps];
   __shared__ int64_t s_row[2 * kWarps];  // its row, or -1
+  __shared__ uint64_t s_buffer[kWarps][64];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   if (lane < 2) s_row[2 * w + lane] = -1;
 
@@ -164,6 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
   const int64_t w0 = c0 + each * (uint32_t)w + min((uint32_t)w, rest);
   const int64_t w1 = w0 + each + (w < (int)rest);
 
+  uint64_t *buffer = s_buffer[w];
   uint8_t *ring = smem + w * (kStages * kTileBytes) + lane * 16;
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
 
@@ -172,21 +196,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
   int64_t left = w1 - w0;
   int pstage = 0, stage = 0;
   int64_t pleft = left;
+  const char *psrc = (const char *)a.x + (prow * a.stride + (int64_t)ptile * kTile + lane * kVec) * kSize;
   auto issue = [&]() {
     if (VEC && pleft > 0) {
-      const char *src = (const char *)a.x + (prow * a.stride + (int64_t)ptile * kTile + lane * kVec) * kSize;
+      const uint32_t dst = ring_s + pstage * kTileBytes;
+      if ((ptile + 1) * kTile <= a.vocab) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        // the pieces of a row's last tile that lie past its end are not read
-        const int i = ptile * kTile + v * (32 * kVec) + lane * kVec;
-        const int bytes = min(max(a.vocab - i, 0) * kSize, 16);
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ring_s + pstage * kTileBytes + v * 512),
-                     "l"(bytes ? src + v * 512 : (const char *)a.x), "r"(bytes)
-                     : "memory");
+        for (int v = 0; v < 4; ++v)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + v * 512), "l"(psrc + v * 512) : "memory");
+      } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          // what lies past the row's end is not read
+          const int i = ptile * kTile + v * (32 * kVec) + lane * kVec;
+          const int bytes = min(max(a.vocab - i, 0) * kSize, 16);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + v * 512),
+                       "l"(bytes ? psrc + v * 512 : (const char *)a.x), "r"(bytes)
+                       : "memory");
+        }
       }
       --pleft;
       pstage = pstage + 1 == kStages ? 0 : pstage + 1;
-      if (++ptile == a.tiles) ptile = 0, ++prow;
+      psrc += kTile * kSize;
+      if (++ptile == a.tiles) {
+        ptile = 0;
+        ++prow;
+        psrc = (const char *)a.x + (prow * a.stride + lane * kVec) * kSize;
+      }
     }
     cp_async_commit();
   };
@@ -201,9 +237,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
   };
   int64_t t = target(row), t1 = target(row + 1);
   float xt = logit(row, t), xt1 = logit(row + 1, t1);
-  float above = 0.f, from = 0.f;  // logits greater than these come before the target: past it and ahead of it
 
   float m = 0.f, s1 = 0.f, s2 = 0.f, tau = 0.f;
+  float above = 0.f, from = 0.f;  // logits greater than these come before the target: past it and ahead of it
   int count = 0;
   uint64_t key = 0, last = 0;  // the lane's entry of the list; the list's last
   bool fresh = true;           // the row begins for this warp
@@ -220,11 +256,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
       s1 = s2 = 0.f;
       count = 0;
       key = last = 0;
-      above = xt;
-      // x >= xt as x > the number before xt; for -inf every x: no x is <= NaN
-      from = xt == -CUDART_INF_F ? CUDART_NAN_F
-             : xt == 0.f         ? __uint_as_float(0x80000001u)
-                                 : __uint_as_float(__float_as_uint(xt) + (xt > 0.f ? -1 : 1));
     }
     issue();
     float x[kPer];
@@ -271,27 +302,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
         if (index(e) >= a.vocab) x[e] = -CUDART_INF_F;
     }
 
-    // the rank
-    if (a.targets) {
-      if (partial || (t >= base && t < base + kTile)) {
-#pragma unroll 1
-        for (int e = 0; e < kPer; ++e) count += index(e) < a.vocab && !(fetch(e) <= (index(e) < t ? from : above));
-      } else {
-        const float thr = base < t ? from : above;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) count += !(x[e] <= thr);
-      }
-    }
-
     // the sums
-    float mv[4], mx;
+    float mx = max_nan(x[0], x[1]), mo = max_nan(x[2], x[3]);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      mv[v] = x[v * (kPer / 4)];
-#pragma unroll
-      for (int e = 1; e < kPer / 4; ++e) mv[v] = max_nan(mv[v], x[v * (kPer / 4) + e]);
+    for (int e = 4; e < kPer; e += 4) {
+      mx = max_nan(mx, x[e], x[e + 1]);
+      mo = max_nan(mo, x[e + 2], x[e + 3]);
     }
-    mx = max_nan(max_nan(mv[0], mv[1]), max_nan(mv[2], mv[3]));
+    mx = max_nan(mx, mo);
     const float to = max_nan(m, mx);
     rebase(m, s1, s2, to, a.c);
     const float off = to == -CUDART_INF_F ? 0.f : -to;
@@ -313,7 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
     if (a.top_k) {
       if (fresh) {  // the top_k-th largest of the lanes' maxima: at least top_k logits reach it
         int before = 0;
-#pragma unroll
+#pragma unroll 4
         for (int o = 0; o < 32; ++o) {
           const float y = __shfl_sync(~0u, mx, o);
           before += !(y <= mx) || (y == mx && o < lane);
@@ -321,27 +339,76 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
         tau = __shfl_sync(~0u, mx, __ffs(__ballot_sync(~0u, before == a.top_k - 1) | 0x80000000u) - 1);
         if (!__any_sync(~0u, before == a.top_k - 1)) tau = -CUDART_INF_F;  // NaN among them
       }
-      if (__any_sync(~0u, !(mx < tau))) {
-#pragma unroll 1
-        for (int v = 0; v < 4; ++v) {
-          const float most = v == 0 ? mv[0] : v == 1 ? mv[1] : v == 2 ? mv[2] : mv[3];
-          if (!__any_sync(~0u, !(most < tau))) continue;
-#pragma unroll 1
-          for (int e = v * (kPer / 4); e < (v + 1) * (kPer / 4); ++e) {
-            const float y = fetch(e);
-            const uint64_t own = order_key(y, index(e));
-            uint32_t todo = __ballot_sync(~0u, !(y < tau) && own > last && index(e) < a.vocab);
+      uint32_t lanes = __ballot_sync(~0u, !(mx < tau));  // whose logits reach the list
+      if (lanes) {
+        __syncwarp();
+        if (__popc(lanes) <= 8) {
+          // a lane's logits are looked at by the whole warp
+          do {
+            const int from_lane = __ffs(lanes) - 1;
+            const int i = base + (VEC ? (lane / kVec) * (32 * kVec) + from_lane * kVec + lane % kVec : lane * 32 + from_lane);
+            const bool there = lane < kPer && i < a.vocab;
+            float y = -CUDART_INF_F;
+            if (there)
+              y = VEC ? load_elem(held + (from_lane - lane) * 16 + (lane / kVec) * 512, DT, lane % kVec)
+                      : load_elem(a.x, DT, row * a.stride + i);
+            const uint64_t own = order_key(y, i);
+            uint32_t todo = __ballot_sync(~0u, there && !(y < tau) && own > last);
+            lanes &= lanes - 1;
             if (todo == 0) continue;
-            while (todo) {
-              const uint64_t cand = __shfl_sync(~0u, own, __ffs(todo) - 1);
-              todo &= todo - 1;
-              const uint64_t up = __shfl_up_sync(~0u, key, 1);
+            do {
+              const uint64_t cand = __shfl_sync(~0u, own, __ffs(todo) - 1), up = __shfl_up_sync(~0u, key, 1);
               if (key < cand) key = lane > 0 && up < cand ? up : cand;
-            }
+              todo &= todo - 1;
+            } while (todo);
             last = __shfl_sync(~0u, key, a.top_k - 1);
             if (last) tau = key_value(last);
+            lanes &= __ballot_sync(~0u, !(mx < tau));
+          } while (lanes);
+        } else {
+          int packed = 0;
+          auto flush = [&]() {
+            __syncwarp();
+            for (int at = 0; at < packed; at += 32)
+              key = merge_lists(key, sort_keys(at + lane < packed ? buffer[at + lane] : 0, lane), lane);
+            packed = 0;
+            last = __shfl_sync(~0u, key, a.top_k - 1);
+            if (last) tau = key_value(last);
+            __syncwarp();
+          };
+#pragma unroll 1
+          for (int e = 0; e < kPer; ++e) {
+            const float y = fetch(e);
+            const uint64_t own = order_key(y, index(e));
+            const bool in = !(y < tau) && own > last && index(e) < a.vocab;
+            const uint32_t todo = __ballot_sync(~0u, in);
+            if (todo == 0) continue;
+            if (in) buffer[packed + __popc(todo & ((1u << lane) - 1))] = own;
+            packed += __popc(todo);
+            if (packed > 32) flush();
           }
+          if (packed) flush();
         }
+        __syncwarp();
+      }
+    }
+
+    // the rank
+    if (a.targets) {
+      if (fresh) {
+        above = xt;
+        // x >= xt as x > the number before xt; for -inf every x: no x is <= NaN
+        from = xt == -CUDART_INF_F ? CUDART_NAN_F
+               : xt == 0.f         ? __uint_as_float(0x80000001u)
+                                   : __uint_as_float(__float_as_uint(xt) + (xt > 0.f ? -1 : 1));
+      }
+      const float thr = base < t ? from : above;
+      if (partial || (t >= base && t < base + kTile)) {
+#pragma unroll 1
+        for (int e = 0; e < kPer; ++e) count += index(e) < a.vocab && !(fetch(e) <= (index(e) < t ? from : above));
+      } else if (__any_sync(~0u, !(mx <= thr))) {  // else no logit of the tile comes before the target
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) count += !(x[e] <= thr);
       }
     }
     fresh = false;
@@ -378,106 +445,102 @@ __global__ void __launch_bounds__(kThreads, 1) k_score(const __grid_constant__ S
   cp_async_wait<0>();
   __syncthreads();
 
-  // ---- joins: rows cut between the warps of this CTA, then, if it is the last
-  // to arrive, rows cut between CTAs
+  // ---- joins.  Parts are taken in order; a join of few is one warp's work, so
+  // that many rows are joined at a time, one of many the whole CTA's.
   Part *slots = (Part *)((uint8_t *)a.workspace + kMaxCtas * 8);  // two per CTA
   int *counters = (int *)a.workspace;
   __shared__ Part s_sum[kWarps];
-  __shared__ int s_last, s_index[32];
-  int64_t cross[2] = {-1, -1};
-#pragma unroll 1
-  for (int i = 0, side = 0;;) {
-    int64_t r;
-    int n;
-    const Part *parts;  // n in a row, or, between CTAs, one in two but for the first
-    Part *to = nullptr;
-    bool mem = false;
-    if (i < 2 * kWarps) {
-      const int64_t mine_row = s_row[lane];
-      const uint32_t todo = __ballot_sync(~0u, mine_row >= 0) & (~0u << i);
-      if (todo == 0) {
-        i = 2 * kWarps;
-        continue;
-      }
-      r = s_row[__ffs(todo) - 1];
-      const uint32_t same = __ballot_sync(~0u, mine_row == r);
-      n = __popc(same);
-      i = 32 - __clz(same);
-      parts = s_part;
-      if (w == 0 && same >> lane & 1) s_index[__popc(same & ((1u << lane) - 1))] = lane;
-      __syncthreads();
-      const int64_t begin = r * a.tiles;
-      if (begin < c0 || begin + a.tiles > c1) {
-        const int k = begin < c0 ? 0 : 1;
-        cross[k] = r;
-        to = slots + 2 * blockIdx.x + k;
-      }
-    } else {
-      if (side == 2) break;
-      r = cross[side++];
-      if (r < 0) continue;
-      const int first = (int)(r * a.tiles / a.share);
-      n = (int)(((r + 1) * a.tiles - 1) / a.share) - first + 1;
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        s_last = atomicAdd(counters + first, 1) == n - 1;
-        if (s_last) counters[first] = 0;
-      }
-      __syncthreads();
-      if (!s_last) continue;
-      __threadfence();
-      parts = slots + 2 * first;
-      mem = true;
-    }
-    // part j of n
-    auto part = [&](int j) -> const Part * {
-      return parts + (mem ? (j ? 2 * j : 1) : s_index[j]);
-    };
-    // every warp joins its share in order, then pairs of neighbours are joined
-    const int lo = n * w / kWarps, hi = n * (w + 1) / kWarps;
-    float fm = -CUDART_INF_F, f1 = 0.f, f2 = 0.f;
-    int fc = 0;
-    uint64_t fk = 0;
-    for (int j = lo; j < hi; ++j) {
-      const Part *q = part(j);
-      float m2 = fresh_load(&q->m), b1 = fresh_load(&q->s1), b2 = fresh_load(&q->s2);
-      fc += fresh_load(&q->count);
-      const uint64_t k2 = a.top_k ? fresh_load(&q->key[lane]) : 0;
-      const float M = max_nan(fm, m2);
-      rebase(fm, f1, f2, M, a.c);
-      rebase(m2, b1, b2, M, a.c);
-      f1 += b1, f2 += b2;
-      if (a.top_k) fk = merge_lists(fk, k2, lane);
-    }
+  __shared__ int s_last[2];
+  float fm, f1, f2;
+  int fc;
+  uint64_t fk;
+  auto clear = [&]() { fm = -CUDART_INF_F, f1 = f2 = 0.f, fc = 0, fk = 0; };
+  auto add = [&](const Part *q) {
+    float qm = fresh_load(&q->m), q1 = fresh_load(&q->s1), q2 = fresh_load(&q->s2);
+    const uint64_t qk = a.top_k ? fresh_load(&q->key[lane]) : 0;
+    fc += fresh_load(&q->count);
+    const float to = max_nan(fm, qm);
+    rebase(fm, f1, f2, to, a.c);
+    rebase(qm, q1, q2, to, a.c);
+    f1 += q1, f2 += q2;
+    if (a.top_k) fk = merge_lists(fk, qk, lane);
+  };
+  auto put = [&](Part *q) {
+    q->key[lane] = fk;
+    if (lane == 0) q->m = fm, q->s1 = f1, q->s2 = f2, q->count = fc;
+  };
+  auto finish = [&](int64_t r, Part *to) {
+    if (to) return put(to);
+    const int64_t tr = target(r);
+    write_row(a, r, fm, f1, f2, fc, fk, tr, logit(r, tr));
+  };
+  auto tree = [&]() {  // the warps' sums into warp 0's
     for (int o = 1; o < kWarps; o <<= 1) {
       __syncthreads();
-      if (w & o) {
-        s_sum[w].key[lane] = fk;
-        if (lane == 0) s_sum[w].m = fm, s_sum[w].s1 = f1, s_sum[w].s2 = f2, s_sum[w].count = fc;
-      }
+      if (w & o) put(&s_sum[w]);
       __syncthreads();
-      if ((w & (2 * o - 1)) == 0) {
-        const Part &q = s_sum[w + o];
-        float m2 = q.m, b1 = q.s1, b2 = q.s2;
-        fc += q.count;
-        const float M = max_nan(fm, m2);
-        rebase(fm, f1, f2, M, a.c);
-        rebase(m2, b1, b2, M, a.c);
-        f1 += b1, f2 += b2;
-        if (a.top_k) fk = merge_lists(fk, q.key[lane], lane);
-      }
+      if ((w & (2 * o - 1)) == 0 && w + o < kWarps) add(&s_sum[w + o]);
     }
-    if (w == 0) {
-      if (to) {
-        to->key[lane] = fk;
-        if (lane == 0) to->m = fm, to->s1 = f1, to->s2 = f2, to->count = fc;
-      } else {
-        const int64_t tt = target(r);
-        write_row(a, r, fm, f1, f2, fc, fk, tt, logit(r, tt));
-      }
+  };
+
+  // rows cut between the warps of this CTA
+  const int64_t part_row = lane < 2 * kWarps ? s_row[lane] : -1;
+  const uint32_t valid = __ballot_sync(~0u, part_row >= 0);
+  if (valid == 0) return;
+  const uint32_t below = valid & ((1u << lane) - 1);
+  const int64_t row_before = __shfl_sync(~0u, part_row, below ? 31 - __clz(below) : 0);
+  const uint32_t heads = __ballot_sync(~0u, part_row >= 0 && (below == 0 || row_before != part_row));
+  int64_t cross[2];  // rows cut between CTAs: the one that came from before, the one that goes on
+  cross[0] = __shfl_sync(~0u, part_row, __ffs(valid) - 1);
+  cross[1] = __shfl_sync(~0u, part_row, 31 - __clz(valid));
+  if (cross[1] * a.tiles < c0 || (cross[1] + 1) * a.tiles <= c1) cross[1] = -1;
+  if (cross[0] * a.tiles >= c0) cross[0] = -1;
+  auto slot_of = [&](int64_t r) -> Part * {
+    return r == cross[0] ? slots + 2 * blockIdx.x : r == cross[1] ? slots + 2 * blockIdx.x + 1 : nullptr;
+  };
+  const bool alone = __popc(heads) > 2;  // joins by single warps
+  uint32_t todo = heads;
+  for (int g = 0; todo; ++g, todo &= todo - 1) {
+    if (alone && g % kWarps != w) continue;
+    const int64_t r = __shfl_sync(~0u, part_row, __ffs(todo) - 1);
+    uint32_t same = __ballot_sync(~0u, part_row == r);
+    clear();
+    const int n = __popc(same);
+    const int lo = alone ? 0 : n * w / kWarps, hi = alone ? n : n * (w + 1) / kWarps;
+    for (int j = 0; same; ++j, same &= same - 1)
+      if (j >= lo && j < hi) add(&s_part[__ffs(same) - 1]);
+    if (!alone) tree();
+    if (alone || w == 0) finish(r, slot_of(r));
+  }
+  if (cross[0] < 0 && cross[1] < 0) return;
+
+  // rows cut between CTAs: the last to arrive joins
+  __threadfence();
+  __syncthreads();
+  if (lane == 0 && w < 2) {
+    const int64_t r = w ? cross[1] : cross[0];
+    int last_one = 0;
+    if (r >= 0) {
+      const int first = (int)(r * a.tiles / a.share), n = (int)(((r + 1) * a.tiles - 1) / a.share) - first + 1;
+      last_one = atomicAdd(counters + first, 1) == n - 1 ? n : 0;
+      if (last_one) counters[first] = 0;
     }
-    __syncthreads();
+    s_last[w] = last_one;
+  }
+  __syncthreads();
+  __threadfence();
+  for (int side = 0; side < 2; ++side) {
+    const int n = s_last[side];
+    const bool single = n <= 8;
+    if (n == 0 || (single && w != side)) continue;
+    const int64_t r = cross[side];
+    // the first CTA's part is its second slot, the others' their first
+    const Part *from_slot = slots + 2 * (int)(r * a.tiles / a.share);
+    const int lo = single ? 0 : n * w / kWarps, hi = single ? n : n * (w + 1) / kWarps;
+    clear();
+    for (int j = lo; j < hi; ++j) add(from_slot + (j ? 2 * j : 1));
+    if (!single) tree();
+    if (single || w == 0) finish(r, nullptr);
   }
 }
 
@@ -488,7 +551,7 @@ seedq_status launch(ScoreArgs &a, int sms, int dev, cudaStream_t st) {
   constexpr int kTile = 32 * (DT == SEEDQ_F32 ? 16 : 32);
   a.tiles = (a.vocab + kTile - 1) / kTile;
   const int64_t total = a.rows * a.tiles;
-  const int ctas = std::min(sms, kMaxCtas);
+  const int ctas = std::min(sms * kCtasPerSm, kMaxCtas);
   a.share = std::max<int64_t>((total + ctas - 1) / ctas, kWarps);
   a.ctas = (int)((total + a.share - 1) / a.share);
   constexpr size_t smem = (size_t)kWarps * kStages * kTileBytes;

@@ -63,6 +63,13 @@ __device__ __forceinline__ float block_scale(uint32_t abits) {
   return __uint_as_float((uint32_t)e << 23);
 }
 
+inline int log2_of(int x) {  // -1 if x is no power of two
+  if (x & (x - 1)) return -1;
+  int n = 0;
+  while (x >>= 1) ++n;
+  return n;
+}
+
 // What the cache calls refuse.
 inline seedq_status kv_check(const seedq_kv_cache *c) {
   if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return SEEDQ_ERR_INVALID_ARG;
