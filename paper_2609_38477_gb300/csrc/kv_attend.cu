@@ -655,11 +655,12 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
     float z[S::kSets][S::kGroups][4];  // tokens n, n, n + 8, n + 8 of the columns 2 q4, 2 q4 + 1
 #pragma unroll
     for (int g = 0; g < S::kGroups; ++g) {
-      float acc[S::kSets][4];
-#pragma unroll
-      for (int s = 0; s < S::kSets; ++s) acc[s][0] = acc[s][1] = acc[s][2] = acc[s][3] = 0.f;
+      // Sums of at most 4 products within the tensor cores, which truncate where
+      // they add: one for 64 head dims and half.
+      uint64_t sum[S::kSets][2];
 #pragma unroll
       for (int c = 0; c < S::kChunks; ++c) {
+        float acc[S::kSets][S::kHalves][4] = {};
         const uint32_t at = g * (16 * DP) + (kat ^ (c * 64));
         const uint4 x = *(const uint4 *)(st + at), y = *(const uint4 *)(st + at + 8 * DP);  // the tokens n and n + 8
         const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
@@ -670,14 +671,24 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
 #pragma unroll
           for (int s = 0; s < S::kSets; ++s)
 #pragma unroll
-            for (int hf = 0; hf < S::kHalves; ++hf) mma(acc[s], a0, a1, a2, a3, qf[s][hf][c * 4 + k]);
+            for (int hf = 0; hf < S::kHalves; ++hf) mma(acc[s][hf], a0, a1, a2, a3, qf[s][hf][c * 4 + k]);
         }
+#pragma unroll
+        for (int s = 0; s < S::kSets; ++s)
+#pragma unroll
+          for (int hf = 0; hf < S::kHalves; ++hf)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint64_t x = f2_pack(acc[s][hf][2 * k], acc[s][hf][2 * k + 1]);
+              sum[s][k] = c + hf == 0 ? x : f2_add(sum[s][k], x);
+            }
       }
 #pragma unroll
       for (int s = 0; s < S::kSets; ++s)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          float v = acc[s][k];
+          const float2 pair = f2_unpack(sum[s][k >> 1]);
+          float v = k & 1 ? pair.y : pair.x;
           if (MODE == 0) v += __shfl_xor_sync(~0u, v, 2);
           z[s][g][k] = v * (zf[s][k & 1] * ks[g]);
         }
