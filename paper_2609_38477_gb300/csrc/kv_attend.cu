@@ -83,7 +83,7 @@ struct Shape {
   static constexpr int kWarps = (MODE == 2 || DP == 256) ? 8 : 12;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kStages = DP == 64 ? 4 : kWarps == 12 ? 2 : 3;  // units in a warp's ring
-  static constexpr int kWhole = 8 * kWarps, kWholeWarp = 2;    // see the split of the work list
+  static constexpr int kWhole = 4 * kWarps, kWholeLittle = 8, kWholeWarp = 2;  // units, see the split of the work list
   static constexpr int kRequests = kThreads;                   // that the shared table holds
   static constexpr int kStats = 2 * 8 * kSets;                 // m and l of every column
   static constexpr int kSlot = kStats + kSets * kTiles * 128;  // floats of a part: stats, then lanes' products
@@ -102,7 +102,13 @@ struct Args {
   int32_t q_vec, out_vec;  // q / out rows allow 16-byte accesses
 };
 
-__device__ __forceinline__ int divide(int x, int by, int shift) { return shift >= 0 ? x >> shift : x / by; }
+// x / by for x >= 0, by > 0.  Below 2^20, (x + 1/2) / by is further from a whole
+// number than the approximate quotient errs.
+__device__ __forceinline__ int quotient(int64_t x, int by) {
+  if (x < (1 << 20)) return (int)__fdividef((float)(int)x + 0.5f, (float)by);
+  return x >> 31 ? (int)(x / by) : (int)((uint32_t)x / (uint32_t)by);
+}
+__device__ __forceinline__ int divide(int x, int by, int shift) { return shift >= 0 ? x >> shift : quotient(x, by); }
 
 __device__ __forceinline__ void cp_async16z(uint32_t dst, const void *src, bool in) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
@@ -214,9 +220,8 @@ __device__ __forceinline__ Entry entry_at(const Args &p, const Table<S> &t, int6
     base += n;
     e.r = request<S>(p, ++e.b);
   }
-  const int64_t x = u - base;
-  const int k = x >> 32 ? (int)(x / e.r.units) : (int)((uint32_t)x / (uint32_t)e.r.units);
-  e.h = e.r.tiles == 1 ? k : k / e.r.tiles;
+  const int k = quotient(u - base, e.r.units);
+  e.h = e.r.tiles == 1 ? k : quotient(k, e.r.tiles);
   e.tile = k - e.h * e.r.tiles;
   e.begin = base + (int64_t)k * e.r.units;
   return e;
@@ -288,33 +293,47 @@ __device__ __forceinline__ T load_fresh(const float *x) {
 // output.  A part holds m (in units of log2) and l of every column and the
 // columns' averages o = sum / l as the products' accumulators lie in the lanes;
 // it weighs l 2^m.  Averages, not sums, are kept, so nothing overflows on the
-// way.  Every warp takes tiles of its own; a lane reads the statistics of its
-// two columns itself, so no barrier is needed.
+// way.  The warp takes the tiles first, first + step, ...; a lane reads the
+// statistics of its two columns itself, so no barrier is needed.
 template <typename S, int MODE>
-__device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const float *const *from, float *to) {
+__device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const float *const *from, float *to, int first,
+                                     int step) {
   const int lane = threadIdx.x & 31, nn = lane >> 2, q4 = lane & 3;
 #pragma unroll 1
-  for (int tt = threadIdx.x >> 5; tt < S::kSets * S::kTiles; tt += S::kWarps) {
+  for (int tt = first; tt < S::kSets * S::kTiles; tt += step) {
     const int set = tt / S::kTiles, tile = tt - set * S::kTiles, col = set * 8 + 2 * q4;
-    float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F;
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const float2 m = load_fresh<float2>(from[i] + col);
-      m0 = fmaxf(m0, m.x);
-      m1 = fmaxf(m1, m.y);
-    }
-    const float u0 = m0 == -CUDART_INF_F ? 0.f : m0, u1 = m1 == -CUDART_INF_F ? 0.f : m1;
-    float l0 = 0.f, l1 = 0.f, c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const float *x = from[i];
-      const float2 m = load_fresh<float2>(x + col), l = load_fresh<float2>(x + S::kStats / 2 + col);
-      const float4 o = load_fresh<float4>(x + S::kStats + (tt * 32 + lane) * 4);
-      const float w0 = l.x * exp2_fast(m.x - u0), w1 = l.y * exp2_fast(m.y - u1);
-      l0 += w0;
-      l1 += w1;
-      if (w0 != 0.f) c[0] = fmaf(w0, o.x, c[0]), c[2] = fmaf(w0, o.z, c[2]);
-      if (w1 != 0.f) c[1] = fmaf(w1, o.y, c[1]), c[3] = fmaf(w1, o.w, c[3]);
+    float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F, l0 = 0.f, l1 = 0.f, c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int i = 0; i < n; i += 4) {  // four parts at a time: one latency
+      float2 m[4], l[4];
+      float4 o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float *x = from[min(i + k, n - 1)];
+        m[k] = load_fresh<float2>(x + col);
+        l[k] = load_fresh<float2>(x + S::kStats / 2 + col);
+        o[k] = load_fresh<float4>(x + S::kStats + (tt * 32 + lane) * 4);
+      }
+      const float was0 = m0, was1 = m1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i + k >= n) l[k] = make_float2(0.f, 0.f);
+        m0 = fmaxf(m0, m[k].x);
+        m1 = fmaxf(m1, m[k].y);
+      }
+      const float u0 = m0 == -CUDART_INF_F ? 0.f : m0, u1 = m1 == -CUDART_INF_F ? 0.f : m1;
+      const float s0 = exp2_fast(was0 - u0), s1 = exp2_fast(was1 - u1);
+      l0 *= s0, c[0] *= s0, c[2] *= s0;
+      l1 *= s1, c[1] *= s1, c[3] *= s1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float w0 = l[k].x == 0.f ? 0.f : l[k].x * exp2_fast(m[k].x - u0);
+        const float w1 = l[k].y == 0.f ? 0.f : l[k].y * exp2_fast(m[k].y - u1);
+        l0 += w0;
+        l1 += w1;
+        if (w0 != 0.f) c[0] = fmaf(w0, o[k].x, c[0]), c[2] = fmaf(w0, o[k].z, c[2]);
+        if (w1 != 0.f) c[1] = fmaf(w1, o[k].y, c[1]), c[3] = fmaf(w1, o[k].w, c[3]);
+      }
     }
     const float i0 = l0 == 0.f ? 0.f : 1.f / l0, i1 = l1 == 0.f ? 0.f : 1.f / l1;
     c[0] *= i0;
@@ -374,7 +393,11 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   __shared__ int s_most[S::kWarps];
   int64_t total = 0, u = 0;
   int most = 0;  // units of the longest entry
-  for (int b = tid * p.chunk; b < min((tid + 1) * p.chunk, B); ++b) {
+  // With up to 32 requests every warp makes the sums, and all write the same
+  // table; no barrier.
+  const bool few = B <= 32;
+  const int slot = few ? lane : tid;
+  for (int b = slot * p.chunk; b < min((slot + 1) * p.chunk, B); ++b) {
     const Req r = request<S>(p, b);
     if (p.chunk == 1) table.req[b] = r;
     u += units_of(p, r);
@@ -388,24 +411,32 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       if (lane >= o) x += y;
     }
     most = __reduce_max_sync(~0u, most);
-    if (lane == 31) s_sums[w] = x, s_most[w] = most;
-    __syncthreads();
     int64_t before = x - u;
+    if (few) {
+      total = __shfl_sync(~0u, x, 31);
+      table.before[lane] = before;
+      __syncwarp();
+    } else {
+      if (lane == 31) s_sums[w] = x, s_most[w] = most;
+      __syncthreads();
 #pragma unroll
-    for (int k = 0; k < S::kWarps; ++k) {
-      if (k < w) before += s_sums[k];
-      total += s_sums[k];
-      most = max(most, s_most[k]);
+      for (int k = 0; k < S::kWarps; ++k) {
+        if (k < w) before += s_sums[k];
+        total += s_sums[k];
+        most = max(most, s_most[k]);
+      }
+      table.before[tid] = before;
+      __syncthreads();
     }
-    table.before[tid] = before;
-    __syncthreads();
   }
-  // Units per CTA: even shares, but at least one unit per warp, so that a short
-  // context is joined within few CTAs.  Where no entry is longer than kWhole
-  // units the ends move to the nearest entry's: a join between CTAs costs about
-  // as much as 8 units of a warp, more than the uneven shares do; likewise
-  // between warps where no entry is longer than kWholeWarp units.
-  const int64_t share = max((int64_t)__umul64hi((uint64_t)total, p.ctas_inv) + 1, (int64_t)S::kWarps);
+  // Even shares of units for the CTAs' warps, at least one unit each.  Little work
+  // goes to 4 warps per CTA, one per scheduler, and so to more SMs.  Where no
+  // entry is longer than a few units per warp the shares' ends move to the
+  // nearest entry's: a join between CTAs costs about as much as the uneven
+  // shares; likewise between warps where no entry is longer than kWholeWarp.
+  const bool little = total <= (int64_t)p.ctas * 8;
+  const int warps = little ? 4 : S::kWarps;
+  const int64_t share = max((int64_t)__umul64hi((uint64_t)total, p.ctas_inv) + 1, (int64_t)warps);
   auto nearest = [&](int64_t u) -> int64_t {  // entry end nearest to u
     if (u >= total) return total;
     const Entry e = entry_at<S>(p, table, u);
@@ -413,16 +444,16 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   };
   int64_t c0 = min(share * blockIdx.x, total), c1 = min(c0 + share, total);
   if (c0 >= total) return;
-  if (most <= S::kWhole) {
+  if (most <= (little ? S::kWholeLittle : S::kWhole)) {
     const int64_t c = nearest(lane ? c1 : c0);
     c0 = __shfl_sync(~0u, c, 0);
     c1 = __shfl_sync(~0u, c, 1);
     if (c0 >= c1) return;
   }
   const uint32_t mine = (uint32_t)(c1 - c0);  // split in even shares without passing 32 bits
-  const uint32_t each = mine / S::kWarps, rest = mine - each * S::kWarps;
-  int64_t w0 = c0 + each * (uint32_t)w + min((uint32_t)w, rest);
-  int64_t w1 = w0 + each + (w < (int)rest);
+  const uint32_t each = little ? mine / 4 : mine / S::kWarps, rest = mine - each * warps;
+  int64_t w0 = c0 + each * (uint32_t)min(w, warps) + min((uint32_t)w, rest);
+  int64_t w1 = w < warps ? w0 + each + (w < (int)rest) : w0;
   if (most <= S::kWholeWarp) {
     const int64_t c = nearest(lane ? w1 : w0);
     w0 = __shfl_sync(~0u, c, 0);
@@ -899,59 +930,72 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   // ---- joins: first the entries cut between warps of this CTA, then, if this
   // CTA is the last to arrive, those cut between CTAs
   __shared__ const float *s_from[kMaxCtas];
-  __shared__ int s_last;
+  __shared__ int s_last[2];
   int *counters = (int *)p.a.workspace;
-  int cross[2] = {-1, -1};  // cut between CTAs: the entry that came from before, the one that goes on
+  const int64_t begin = lane < 2 * S::kWarps && s_cut[lane].units ? s_cut[lane].begin : -1;
+  const uint32_t parts = __ballot_sync(~0u, begin >= 0);
+  if (parts == 0) return;
+  // the entries' first parts; an entry's parts are neighbours
+  const uint32_t below = parts & ((1u << lane) - 1);
+  const int64_t begin_before = __shfl_sync(~0u, begin, below ? 31 - __clz(below) : 0);
+  const uint32_t heads = __ballot_sync(~0u, begin >= 0 && (below == 0 || begin_before != begin));
+  if (w == 0 && begin >= 0) {
+    const int pw = lane >> 1;
+    s_from[__popc(below)] = lane & 1 ? (const float *)(smem + ring_at + (size_t)pw * S::kStages * S::kStage)
+                                     : ws + (size_t)(kMaxCtas * 2 + blockIdx.x * S::kWarps + pw) * S::kSlot;
+  }
+  // cut between CTAs: the entry that came from before, the one that goes on
+  int cross[2] = {__ffs(parts) - 1, 31 - __clz(parts)};
+  if (s_cut[cross[1]].begin < c0 || s_cut[cross[1]].end <= c1) cross[1] = -1;
+  if (s_cut[cross[0]].begin >= c0) cross[0] = -1;
+  // One or two entries are joined by all warps, tile by tile, more by a warp each.
+  const bool shared = __popc(heads) <= 2;
+  __syncthreads();
+  int turn = 0, side = -1;
+  uint32_t todo = heads;
 #pragma unroll 1
-  for (int i = 0, side = 0;;) {
-    int i0 = i, n = 0;
+  while (true) {
+    int n, first = w, step = S::kWarps;
+    const float *const *list = s_from;
     float *to = nullptr;
     Desc e;
-    if (i < 2 * S::kWarps) {
-      const int64_t begin = lane < 2 * S::kWarps && s_cut[lane].units ? s_cut[lane].begin : -1;
-      const uint32_t left = __ballot_sync(~0u, begin >= 0) & (~0u << i);
-      if (left == 0) {
-        i = 2 * S::kWarps;
-        continue;
+    if (todo) {
+      const int i = __ffs(todo) - 1;
+      todo &= todo - 1;
+      if (!shared) {
+        if (turn++ % S::kWarps != w) continue;
+        first = 0, step = 1;
       }
-      i0 = __ffs(left) - 1;
-      e = s_cut[i0];
-      const uint32_t same = __ballot_sync(~0u, begin == e.begin);  // its parts are neighbours
-      n = __popc(same);
-      i = 32 - __clz(same);
-      __syncthreads();  // the list of the join before is not read any more
-      if (w == 0 && same >> lane & 1) {
-        const int pw = lane >> 1;
-        s_from[__popc(same & ((1u << lane) - 1))] =
-            lane & 1 ? (const float *)(smem + ring_at + (size_t)pw * S::kStages * S::kStage)
-                     : ws + (size_t)(kMaxCtas * 2 + blockIdx.x * S::kWarps + pw) * S::kSlot;
-      }
-      if (e.begin < c0 || e.end > c1) {
-        const int k = e.begin < c0 ? 0 : 1;
-        cross[k] = i0;
-        to = cta_slots + k * S::kSlot;
-      }
+      e = s_cut[i];
+      n = __popc(__ballot_sync(~0u, begin == e.begin));
+      list += __popc(parts & ((1u << i) - 1));
+      if (e.begin < c0) to = cta_slots;
+      else if (e.end > c1) to = cta_slots + S::kSlot;
     } else {
-      if (side == 2) break;
-      const int k = cross[side++];
-      if (k < 0) continue;
-      e = s_cut[k];
-      const int first = (int)(e.begin / share);
-      n = (int)((e.end - 1) / share) - first + 1;
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        s_last = atomicAdd(counters + first, 1) == n - 1;
-        if (s_last) counters[first] = 0;
+      if (side < 0) {  // the parts are written: the last CTA to arrive joins them
+        if (cross[0] < 0 && cross[1] < 0) break;
+        __threadfence();
+        __syncthreads();
+        if (lane == 0 && w < 2 && cross[w] >= 0) {
+          const Desc &x = s_cut[cross[w]];
+          const int a = (int)(x.begin / share), all = (int)((x.end - 1) / share) - a + 1;
+          s_last[w] = atomicAdd(counters + a, 1) == all - 1 ? all : 0;
+          if (s_last[w]) counters[a] = 0;
+        }
+        __syncthreads();
+        __threadfence();
       }
+      if (++side == 2) break;
+      if (cross[side] < 0 || s_last[side] == 0) continue;
+      e = s_cut[cross[side]];
+      n = s_last[side];
       // the first CTA's part is its second slot, the others' their first
-      for (int x = tid; x < n; x += S::kThreads) s_from[x] = ws + ((size_t)(first + x) * 2 + (x == 0)) * S::kSlot;
+      const int a = (int)(e.begin / share);
+      __syncthreads();  // the list of the joins before is not read any more
+      for (int x = tid; x < n; x += S::kThreads) s_from[x] = ws + ((size_t)(a + x) * 2 + (x == 0)) * S::kSlot;
       __syncthreads();
-      if (!s_last) continue;
-      __threadfence();
     }
-    __syncthreads();
-    join<S, MODE>(p, e, n, s_from, to);
+    join<S, MODE>(p, e, n, list, to, first, step);
   }
 }
 
