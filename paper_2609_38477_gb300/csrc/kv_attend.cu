@@ -79,7 +79,7 @@ struct Shape {
   static constexpr int kTiles = DP / 16;             // output tiles of 16 head dims
   static constexpr int kValAt = kUnit * DP;
   static constexpr int kMetaAt = 2 * kUnit * DP;
-  static constexpr int kStage = kMetaAt + 16 * kGroups;  // meta: per group both scales and a flag
+  static constexpr int kStage = kMetaAt + 128;       // meta: per group both scales and a flag
   static constexpr int kWarps = (MODE == 2 || DP == 256) ? 8 : 12;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kStages = DP == 64 ? 4 : kWarps == 12 ? 2 : 3;  // units in a warp's ring
@@ -181,16 +181,18 @@ __device__ __forceinline__ Req request(const Args &p, int b) {
   r.units = max((r.hi + S::kUnit - 1) / S::kUnit - r.u0, 1);
   return r;
 }
-__device__ __forceinline__ int64_t units_of(const Args &p, const Req &r) {
-  return r.fresh ? (int64_t)r.units * r.tiles * p.c.n_kv_heads : 0;
+// Steps of the work list: an entry's units and kStart more, the cost of its start
+// (queries) and end, so that many short contexts weigh what they take.
+constexpr int kStart = 1;
+__device__ __forceinline__ int64_t steps_of(const Args &p, const Req &r) {
+  return r.fresh ? (int64_t)(r.units + kStart) * r.tiles * p.c.n_kv_heads : 0;
 }
 
 // One entry of the work list: (request, key-value head, row tile).
 struct Entry {
   Req r;
   int b, h, tile;
-  int64_t begin;  // its first unit in the work list
-};
+};  // its units are the steps after its first kStart
 // The table of requests in shared memory: units before every chunk of
 // requests, and, where a chunk is one request, the requests themselves.
 template <typename S>
@@ -203,7 +205,7 @@ __device__ __forceinline__ Req request(const Args &p, const Table<S> &t, int b) 
   return p.chunk == 1 ? t.req[b] : request<S>(p, b);
 }
 template <typename S>
-__device__ __forceinline__ Entry entry_at(const Args &p, const Table<S> &t, int64_t u) {
+__device__ __forceinline__ Entry entry_at(const Args &p, const Table<S> &t, int64_t u, int64_t &begin) {
   Entry e;
   int lo = 0, hi = (p.a.n_requests + p.chunk - 1) / p.chunk;
   while (hi - lo > 1) {
@@ -215,20 +217,19 @@ __device__ __forceinline__ Entry entry_at(const Args &p, const Table<S> &t, int6
   e.b = lo * p.chunk;
   e.r = request<S>(p, t, e.b);
   for (int i = 1; i < p.chunk; ++i) {
-    const int64_t n = units_of(p, e.r);
+    const int64_t n = steps_of(p, e.r);
     if (u < base + n) break;
     base += n;
     e.r = request<S>(p, ++e.b);
   }
-  const int k = quotient(u - base, e.r.units);
+  const int k = quotient(u - base, e.r.units + kStart);
   e.h = e.r.tiles == 1 ? k : quotient(k, e.r.tiles);
   e.tile = k - e.h * e.r.tiles;
-  e.begin = base + (int64_t)k * e.r.units;
+  begin = base + (int64_t)k * (e.r.units + kStart);
   return e;
 }
 template <typename S>
 __device__ __forceinline__ void next_entry(const Args &p, const Table<S> &t, Entry &e) {  // only where one follows
-  e.begin += e.r.units;
   if (++e.tile < e.r.tiles) return;
   e.tile = 0;
   if (++e.h < p.c.n_kv_heads) return;
@@ -243,7 +244,8 @@ struct Desc {
   int h, tile;
   int token0;  // the first token of a warp's first unit of it
   int units;   // units of it that the warp holds
-  int64_t begin, end;
+  int whole;   // whether these are all
+  int64_t begin, end;  // the steps of its units
 };
 
 // Where a row of an entry's tile goes; false if it holds no query.
@@ -298,17 +300,18 @@ __device__ __forceinline__ T load_fresh(const float *x) {
 template <typename S, int MODE>
 __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const float *const *from, float *to, int first,
                                      int step) {
+  constexpr int kAtATime = 8;
   const int lane = threadIdx.x & 31, nn = lane >> 2, q4 = lane & 3;
 #pragma unroll 1
   for (int tt = first; tt < S::kSets * S::kTiles; tt += step) {
     const int set = tt / S::kTiles, tile = tt - set * S::kTiles, col = set * 8 + 2 * q4;
     float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F, l0 = 0.f, l1 = 0.f, c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-    for (int i = 0; i < n; i += 4) {  // four parts at a time: one latency
-      float2 m[4], l[4];
-      float4 o[4];
+    for (int i = 0; i < n; i += kAtATime) {  // one latency
+      float2 m[kAtATime], l[kAtATime];
+      float4 o[kAtATime];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kAtATime; ++k) {
         const float *x = from[min(i + k, n - 1)];
         m[k] = load_fresh<float2>(x + col);
         l[k] = load_fresh<float2>(x + S::kStats / 2 + col);
@@ -316,7 +319,7 @@ __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const 
       }
       const float was0 = m0, was1 = m1;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kAtATime; ++k) {
         if (i + k >= n) l[k] = make_float2(0.f, 0.f);
         m0 = fmaxf(m0, m[k].x);
         m1 = fmaxf(m1, m[k].y);
@@ -326,7 +329,7 @@ __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const 
       l0 *= s0, c[0] *= s0, c[2] *= s0;
       l1 *= s1, c[1] *= s1, c[3] *= s1;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kAtATime; ++k) {
         const float w0 = l[k].x == 0.f ? 0.f : l[k].x * exp2_fast(m[k].x - u0);
         const float w1 = l[k].y == 0.f ? 0.f : l[k].y * exp2_fast(m[k].y - u1);
         l0 += w0;
@@ -382,7 +385,8 @@ __host__ __device__ constexpr int swizzle(int r) {
 template <int KIND, int DP, int MODE>
 __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const __grid_constant__ Args p) {
   using S = Shape<DP, MODE>;
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  uint8_t *smem = smem_raw + (128 - ((uint32_t)__cvta_generic_to_shared(smem_raw) & 127)) % 128;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int nn = lane >> 2, q4 = lane & 3;
   const int B = p.a.n_requests, D = p.c.head_dim;
@@ -390,9 +394,9 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   // ---- the work list: exclusive sums of the requests' units
   Table<S> &table = *(Table<S> *)smem;
   __shared__ int64_t s_sums[S::kWarps];
-  __shared__ int s_most[S::kWarps];
+  __shared__ int s_most[S::kWarps], s_least[S::kWarps];
   int64_t total = 0, u = 0;
-  int most = 0;  // units of the longest entry
+  int most = 0, least = INT32_MAX;  // units of the longest and of the shortest entry
   // With up to 32 requests every warp makes the sums, and all write the same
   // table; no barrier.
   const bool few = B <= 32;
@@ -400,8 +404,8 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   for (int b = slot * p.chunk; b < min((slot + 1) * p.chunk, B); ++b) {
     const Req r = request<S>(p, b);
     if (p.chunk == 1) table.req[b] = r;
-    u += units_of(p, r);
-    if (r.fresh) most = max(most, r.units);
+    u += steps_of(p, r);
+    if (r.fresh) most = max(most, r.units), least = min(least, r.units);
   }
   {
     int64_t x = u;
@@ -411,62 +415,89 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       if (lane >= o) x += y;
     }
     most = __reduce_max_sync(~0u, most);
+    least = __reduce_min_sync(~0u, least);
     int64_t before = x - u;
     if (few) {
       total = __shfl_sync(~0u, x, 31);
       table.before[lane] = before;
       __syncwarp();
     } else {
-      if (lane == 31) s_sums[w] = x, s_most[w] = most;
+      if (lane == 31) s_sums[w] = x, s_most[w] = most, s_least[w] = least;
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < S::kWarps; ++k) {
         if (k < w) before += s_sums[k];
         total += s_sums[k];
         most = max(most, s_most[k]);
+        least = min(least, s_least[k]);
       }
       table.before[tid] = before;
       __syncthreads();
     }
   }
-  // Even shares of units for the CTAs' warps, at least one unit each.  Little work
-  // goes to 4 warps per CTA, one per scheduler, and so to more SMs.  Where no
-  // entry is longer than a few units per warp the shares' ends move to the
-  // nearest entry's: a join between CTAs costs about as much as the uneven
-  // shares; likewise between warps where no entry is longer than kWholeWarp.
+  // Even shares of steps for the CTAs' warps, at least one each.  Little work goes
+  // to 4 warps per CTA, one per scheduler, and so to more SMs.  Entries of one
+  // length (one request, or a batch in step) are each cut for the same number of
+  // CTAs, so that no CTA has parts of two.  Else, where no entry is longer than a
+  // few units per warp, the shares' ends move to the nearest entry's: a join
+  // between CTAs costs about as much as the uneven shares; likewise between warps
+  // where no entry is longer than kWholeWarp.
   const bool little = total <= (int64_t)p.ctas * 8;
   const int warps = little ? 4 : S::kWarps;
   const int64_t share = max((int64_t)__umul64hi((uint64_t)total, p.ctas_inv) + 1, (int64_t)warps);
+  int cuts = 0;  // CTAs per entry, where all have as many
+  if (most == least && total <= (int64_t)p.ctas * (most + kStart)) {
+    const int entries = quotient(total, most + kStart);
+    cuts = min(quotient(p.ctas, entries), (most + warps - 1) / warps);
+    if (!little && entries * cuts * 10 < p.ctas * 9) cuts = 0;
+  }
   auto nearest = [&](int64_t u) -> int64_t {  // entry end nearest to u
     if (u >= total) return total;
-    const Entry e = entry_at<S>(p, table, u);
-    return u - e.begin <= e.begin + e.r.units - u ? e.begin : e.begin + e.r.units;
+    int64_t begin;
+    const int length = entry_at<S>(p, table, u, begin).r.units + kStart;
+    return u - begin <= begin + length - u ? begin : begin + length;
   };
-  int64_t c0 = min(share * blockIdx.x, total), c1 = min(c0 + share, total);
-  if (c0 >= total) return;
-  if (most <= (little ? S::kWholeLittle : S::kWhole)) {
-    const int64_t c = nearest(lane ? c1 : c0);
-    c0 = __shfl_sync(~0u, c, 0);
-    c1 = __shfl_sync(~0u, c, 1);
-    if (c0 >= c1) return;
+  int64_t c0, c1;
+  if (cuts) {
+    const int entry = quotient(blockIdx.x, cuts), piece = blockIdx.x - entry * cuts;
+    const int64_t at = (int64_t)entry * (most + kStart) + kStart;
+    if (at >= total) return;
+    c0 = at + quotient((int64_t)most * piece, cuts);
+    c1 = at + quotient((int64_t)most * (piece + 1), cuts);
+  } else {
+    c0 = min(share * blockIdx.x, total), c1 = min(c0 + share, total);
+    if (c0 >= total) return;
+    if (most <= (little ? S::kWholeLittle : S::kWhole)) {
+      const int64_t c = nearest(lane ? c1 : c0);
+      c0 = __shfl_sync(~0u, c, 0);
+      c1 = __shfl_sync(~0u, c, 1);
+      if (c0 >= c1) return;
+    }
   }
   const uint32_t mine = (uint32_t)(c1 - c0);  // split in even shares without passing 32 bits
   const uint32_t each = little ? mine / 4 : mine / S::kWarps, rest = mine - each * warps;
   int64_t w0 = c0 + each * (uint32_t)min(w, warps) + min((uint32_t)w, rest);
   int64_t w1 = w < warps ? w0 + each + (w < (int)rest) : w0;
-  if (most <= S::kWholeWarp) {
+  if (most <= S::kWholeWarp && cuts <= 1) {
     const int64_t c = nearest(lane ? w1 : w0);
     w0 = __shfl_sync(~0u, c, 0);
     w1 = __shfl_sync(~0u, c, 1);
   }
-  const int units = (int)(w1 - w0);
 
-  constexpr int ring_at = sizeof(Table<S>);
+  // Rows begin at multiples of 128 bytes: a copy whose 32-byte sectors straddle
+  // those of shared memory is fetched twice from L2.
+  constexpr int ring_at = (sizeof(Table<S>) + 127) & ~127;
   uint8_t *ring = smem + ring_at + (size_t)w * S::kStages * S::kStage;
   const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
 
   float *ws = (float *)((uint8_t *)p.a.workspace + kMaxCtas * 4);
   float *cta_slots = ws + (size_t)blockIdx.x * 2 * S::kSlot;
+  // What the joins need again, so that it takes no registers until then.
+  __shared__ struct { int64_t share, c0, c1; int cuts, length; } s_split;
+  __shared__ int64_t s_first[S::kWarps];  // the warps' first steps
+  if (tid == 0) s_split = {share, c0, c1, cuts, most + kStart};
+  if (lane == 0) s_first[w] = w0;
+  const int steps = (int)(w1 - w0);
   // Entries on their way from the copies to the products.
   __shared__ Desc s_desc[S::kWarps][S::kStages + 1];
   // Parts of cut entries, in the order of their keys: [2 w] a warp's first
@@ -481,48 +512,72 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   const int64_t clane = crow * ts + cat;
   // The place of 16-byte piece x of row r: x ^ swizzle(r).
   const uint32_t cdst = crow * DP + ((lane % S::kLanes) ^ swizzle<DP>(crow)) * 16;
-  Entry pe{};  // the entry being copied
+  __shared__ Entry s_entry[S::kWarps];  // the entries being copied
+  int pb = -1, ph = 0, plo = 0, phi = 0;  // of this warp's: its request, head and keys
+  int plast = 0;                          // where it ends, in steps from the warp's first
   const int32_t *prow = nullptr;
   int pleft = 0;               // its units still to copy by this warp
+  int copied = 0;              // units copied so far
+  bool more = steps > 0;       // whether there are others
   int pg = 0, pgb = 0;         // the next group of 16 tokens; the group of lane 0's page
   int poff = 0;                // the next group's place in its page
   int ids = -1, ids_next = -1; // pages of the groups pgb + lane and pgb + 32 + lane
-  int pstage = 0, pdesc = 0, cdesc = 0, stage = 0, to_copy = units;
+  int pstage = 0, pdesc = 0, cdesc = 0, stage = 0;
   auto load_ids = [&](int g) -> int {
     const int64_t gl = (int64_t)g + lane;
-    return gl * 16 < pe.r.hi ? __ldg(prow + divide((int)gl, gpp, p.gpp_shift)) : -1;
+    return gl * 16 < phi ? __ldg(prow + divide((int)gl, gpp, p.gpp_shift)) : -1;
   };
 
   // ---- products
   uint32_t qf[S::kSets][S::kHalves][S::kChunks * 4][2];  // q as the second operand
   float zf[S::kSets][2];      // z in units of log2 per unit of product, but for the key scale
-  int pos[S::kSets][2];       // positions of the lane's columns
   float m[S::kSets][2], l[S::kSets][2], vmax = 0.f;
   uint64_t o[S::kSets][S::kTiles][2];  // sums of the columns (2 q4, 2 q4 + 1) for two head dims
-  int cleft = 0, tok = 0, hi = 0, pos_first = 0, pos_last = 0;
+  int cleft = 0, tok = 0, see_all = 0, see_from = 0;  // units of the tokens see_from < t <= see_all need no mask
   // and of a value tile: piece n (DP 64: half of piece n / 2) of row 2 q4
   const uint32_t vat = 2 * q4 * DP + (S::kVB == 16 ? (nn ^ swizzle<DP>(2 * q4)) * 16 : ((nn >> 1) ^ swizzle<DP>(2 * q4)) * 16 + (nn & 1) * 8);
   const uint32_t kat = nn * DP + (q4 ^ swizzle<DP>(nn)) * 16;  // the lane's first codes of a key tile
 
 #pragma unroll 1
-  for (int it = 1 - S::kStages; it < units; ++it) {
+  for (int it = 1 - S::kStages;; ++it) {
     __syncwarp();  // all lanes are done with the stage that is filled next
-    if (to_copy > 0) {
-      if (pleft == 0) {
-        if (to_copy == units) pe = entry_at<S>(p, table, w0);
-        else next_entry<S>(p, table, pe);
-        const int64_t from = max(pe.begin, w0);
-        pleft = (int)(min(pe.begin + pe.r.units, w1) - from);
+    if (more && pleft == 0) {
+      // The next entry with a unit in the warp's steps.
+      if (copied > 0 && plast >= steps) {
+        more = false;
+      } else {
+        Entry pe;
+        int begin = plast;
+        if (copied == 0) {
+          int64_t at;
+          pe = entry_at<S>(p, table, s_first[w], at);
+          begin = (int)(at - s_first[w]);
+        } else {
+          pe = s_entry[w];
+          next_entry<S>(p, table, pe);
+        }
+        __syncwarp();
+        if (lane == 0) s_entry[w] = pe;
+        plast = begin + kStart + pe.r.units;
+        const int from = max(begin + kStart, 0);
+        pleft = max(min(plast, steps) - from, 0);
+        more = pleft > 0;  // else its start alone
+        plo = pe.r.lo, phi = pe.r.hi, ph = pe.h;
         prow = p.a.block_table + (int64_t)pe.b * p.a.table_stride;
-        pg = pgb = (pe.r.u0 + (int)(from - pe.begin)) * S::kGroups;
+        pg = (pe.r.u0 + from - begin - kStart) * S::kGroups;
         poff = pg - divide(pg, gpp, p.gpp_shift) * gpp;
-        ids = load_ids(pgb);
-        ids_next = load_ids(pgb + 32);
+        if (pe.b != pb || pg != pgb) {  // the next head of a request reads the same pages
+          pgb = pg;
+          ids = load_ids(pgb);
+          ids_next = load_ids(pgb + 32);
+        }
+        pb = pe.b;
         if (lane == 0) {
           Desc &x = s_desc[w][pdesc];
           x.first = pe.r.first, x.fresh = pe.r.fresh, x.len = pe.r.len, x.hi = pe.r.hi;
           x.h = pe.h, x.tile = pe.tile, x.token0 = pg * 16, x.units = pleft;
-          x.begin = pe.begin, x.end = pe.begin + pe.r.units;
+          x.begin = s_first[w] + begin + kStart, x.end = x.begin + pe.r.units;
+          x.whole = pleft == pe.r.units;
         }
         pdesc = pdesc == S::kStages ? 0 : pdesc + 1;
         // its queries' first touch, while the page numbers are on their way
@@ -533,8 +588,12 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
           for (int x = 0; x < D * p.q_bytes; x += 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(row + x));
         }
       }
+    }
+    if (more) {
+      __syncwarp();
+      int my_page = -1;
       --pleft;
-      --to_copy;
+      ++copied;
       const uint32_t dst = ring_s + pstage * S::kStage;
       pstage = pstage + 1 == S::kStages ? 0 : pstage + 1;
       if (pg - pgb >= 32) {
@@ -546,9 +605,9 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       for (int g = 0; g < S::kGroups; ++g) {
         const int page = __shfl_sync(~0u, ids, pg - pgb);
         const int t0 = pg * 16;
-        const bool in = page >= 0 && page < p.c.n_pages && t0 + 16 > pe.r.lo;  // ids is -1 past hi
-        const int left = in ? pe.r.hi - t0 : 0;                                // tokens of the group that exist
-        const int64_t at = in ? page * p.c.page_stride + pe.h * p.c.head_stride + poff * 16 * ts : 0;
+        const bool in = page >= 0 && page < p.c.n_pages && t0 + 16 > plo;  // ids is -1 past hi
+        const int left = in ? phi - t0 : 0;                                // tokens of the group that exist
+        const int64_t at = in ? page * p.c.page_stride + ph * p.c.head_stride + poff * 16 * ts : 0;
         ++pg;
         poff = poff + 1 == gpp ? 0 : poff + 1;
         const uint8_t *kp = (const uint8_t *)p.c.k + at + clane, *vp = (const uint8_t *)p.c.v + at + clane;
@@ -564,32 +623,37 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
           kp += tstep;
           vp += tstep;
         }
-        const uint32_t meta = dst + S::kMetaAt + g * 16;
-        if (lane < 2) {
-          if (in) {
-            const float *sc = (lane ? p.c.v_scale : p.c.k_scale) + (int64_t)page * p.c.n_kv_heads + pe.h;
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(meta + lane * 4), "l"(sc) : "memory");
-          } else {
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(meta + lane * 4), "f"(0.f) : "memory");
-          }
-        } else if (lane == 2) {
-          asm volatile("st.shared.s32 [%0], %1;" ::"r"(meta + 8), "r"(in ? 1 : 0) : "memory");
+        if ((lane >> 1) == g) my_page = in ? page : -1;
+      }
+      // the groups' scales and flags, two lanes a group, after all copies: a warp
+      // that has split up fetches lines twice
+      if (lane < 2 * S::kGroups) {
+        const uint32_t meta = dst + S::kMetaAt + (lane >> 1) * 16;
+        if (my_page >= 0) {
+          const float *sc = (lane & 1 ? p.c.v_scale : p.c.k_scale) + (int64_t)my_page * p.c.n_kv_heads + ph;
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(meta + (lane & 1) * 4), "l"(sc) : "memory");
+        } else {
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(meta + (lane & 1) * 4), "f"(0.f) : "memory");
         }
+        if ((lane & 1) == 0) asm volatile("st.shared.s32 [%0], %1;" ::"r"(meta + 8), "r"(my_page >= 0 ? 1 : 0) : "memory");
       }
     }
     cp_async_commit();
     int ahead = it;
     asm volatile("" : "+r"(ahead));  // keeps the compiler from splitting the loop here and writing the copies out twice
     if (ahead < 0) continue;
+    if (ahead == copied) break;  // the copies run ahead, so there is no other unit
 
     if (cleft == 0) {  // a new entry: its queries
       const Desc e = s_desc[w][cdesc];
       cleft = e.units;
       tok = e.token0;
-      hi = e.hi;
       vmax = 0.f;
-      pos_first = e.len - e.fresh + divide(e.tile * S::kRows, p.group, p.group_shift);
-      pos_last = min(e.len - e.fresh + divide(e.tile * S::kRows + S::kRows - 1, p.group, p.group_shift), e.len - 1);
+      {
+        const int r0 = e.tile * S::kRows, t0 = divide(r0, p.group, p.group_shift), t1 = divide(r0 + S::kRows - 1, p.group, p.group_shift);
+        see_all = min(e.len - e.fresh + t0, e.hi - 1);
+        see_from = p.a.window > 0 ? min(e.len - e.fresh + t1, e.len - 1) - p.a.window : -1;
+      }
 #pragma unroll
       for (int s = 0; s < S::kSets; ++s) {
 #pragma unroll
@@ -661,7 +725,6 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
         for (int k = 0; k < 2; ++k) {
           const int col = 2 * q4 + k;
           zf[s][k] = __shfl_sync(~0u, f, col * 4);
-          row_of<S>(p, e, MODE == 0 ? col & 3 : s * 8 + col, token, head, pos[s][k]);
           m[s][k] = -CUDART_INF_F;
           l[s][k] = 0.f;
         }
@@ -725,19 +788,27 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
         }
     }
 
-    const bool masked = !all_in || tok + S::kUnit - 1 > min(pos_first, hi - 1) || (p.a.window > 0 && tok <= pos_last - p.a.window);
+    const bool masked = !all_in || tok + S::kUnit - 1 > see_all || tok <= see_from;
     if (masked) {
+      const Desc e = s_desc[w][cdesc];
 #pragma unroll
-      for (int g = 0; g < S::kGroups; ++g) {
-        const bool in = ((const int *)(st + S::kMetaAt + g * 16))[2];
+      for (int s = 0; s < S::kSets; ++s)
 #pragma unroll
-        for (int s = 0; s < S::kSets; ++s)
+        for (int c = 0; c < 2; ++c) {
+          int64_t token;
+          int head, pos;
+          row_of<S>(p, e, MODE == 0 ? (2 * q4 + c) & 3 : s * 8 + 2 * q4 + c, token, head, pos);
+          const int to = min(pos, e.hi - 1), from = p.a.window > 0 ? pos - p.a.window : -1;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int j = tok + g * 16 + nn + (k >> 1) * 8, ps = pos[s][k & 1];
-            if (!in || j > ps || j >= hi || (p.a.window > 0 && j <= ps - p.a.window)) z[s][g][k] = -CUDART_INF_F;
+          for (int g = 0; g < S::kGroups; ++g) {
+            const bool in = ((const int *)(st + S::kMetaAt + g * 16))[2];
+#pragma unroll
+            for (int k = c; k < 4; k += 2) {
+              const int j = tok + g * 16 + nn + (k >> 1) * 8;
+              if (!in || j > to || j <= from) z[s][g][k] = -CUDART_INF_F;
+            }
           }
-      }
+        }
     }
 
     // the block scales of the values, relative to the largest so far
@@ -849,9 +920,10 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
     if (--cleft) continue;
 
     // ---- the end of this warp's part of an entry
-    const Desc e = s_desc[w][cdesc];
+    const int edesc = cdesc;
+    const Desc e = s_desc[w][edesc];
     cdesc = cdesc == S::kStages ? 0 : cdesc + 1;
-    const bool whole = e.begin >= w0 && e.end <= w1, last = it + 1 == units;
+    const bool whole = e.whole, last = !more && it + 1 == copied;
     float inv[S::kSets][2];
 #pragma unroll
     for (int s = 0; s < S::kSets; ++s)
@@ -870,7 +942,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       float *part = last ? (float *)ring : ws + (size_t)(kMaxCtas * 2 + blockIdx.x * S::kWarps + w) * S::kSlot;
       if (last) cp_async_wait<0>();
       __syncwarp();
-      if (lane == 0) s_cut[2 * w + last] = e;
+      if (lane < (int)sizeof(Desc) / 4) ((int *)&s_cut[2 * w + last])[lane] = ((const int *)&s_desc[w][edesc])[lane];
 #pragma unroll
       for (int s = 0; s < S::kSets; ++s) {
         if (nn == 0) {
@@ -932,6 +1004,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   __shared__ const float *s_from[kMaxCtas];
   __shared__ int s_last[2];
   int *counters = (int *)p.a.workspace;
+  c0 = s_split.c0, c1 = s_split.c1;
   const int64_t begin = lane < 2 * S::kWarps && s_cut[lane].units ? s_cut[lane].begin : -1;
   const uint32_t parts = __ballot_sync(~0u, begin >= 0);
   if (parts == 0) return;
@@ -951,6 +1024,14 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   // One or two entries are joined by all warps, tile by tile, more by a warp each.
   const bool shared = __popc(heads) <= 2;
   __syncthreads();
+  // the CTAs that hold a cut entry
+  auto first_cta = [&](const Desc &x) -> int {
+    const int n = s_split.cuts;
+    return n ? quotient(x.begin, s_split.length) * n : (int)(x.begin / s_split.share);
+  };
+  auto cta_count = [&](const Desc &x) -> int {
+    return s_split.cuts ? s_split.cuts : (int)((x.end - 1) / s_split.share) - first_cta(x) + 1;
+  };
   int turn = 0, side = -1;
   uint32_t todo = heads;
 #pragma unroll 1
@@ -974,23 +1055,23 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
     } else {
       if (side < 0) {  // the parts are written: the last CTA to arrive joins them
         if (cross[0] < 0 && cross[1] < 0) break;
-        __threadfence();
         __syncthreads();
         if (lane == 0 && w < 2 && cross[w] >= 0) {
+          __threadfence();  // the CTA's parts, seen through the barrier, before the arrival
           const Desc &x = s_cut[cross[w]];
-          const int a = (int)(x.begin / share), all = (int)((x.end - 1) / share) - a + 1;
+          const int a = first_cta(x), all = cta_count(x);
           s_last[w] = atomicAdd(counters + a, 1) == all - 1 ? all : 0;
           if (s_last[w]) counters[a] = 0;
+          __threadfence();
         }
         __syncthreads();
-        __threadfence();
       }
       if (++side == 2) break;
       if (cross[side] < 0 || s_last[side] == 0) continue;
       e = s_cut[cross[side]];
       n = s_last[side];
       // the first CTA's part is its second slot, the others' their first
-      const int a = (int)(e.begin / share);
+      const int a = first_cta(e);
       __syncthreads();  // the list of the joins before is not read any more
       for (int x = tid; x < n; x += S::kThreads) s_from[x] = ws + ((size_t)(a + x) * 2 + (x == 0)) * S::kSlot;
       __syncthreads();
@@ -1026,7 +1107,7 @@ seedq_status launch(Args &p, int dev, cudaStream_t st) {
   using S = Shape<DP, MODE>;
   static DeviceOnce once;
   p.chunk = (p.a.n_requests + S::kRequests - 1) / S::kRequests;
-  constexpr size_t smem = sizeof(Table<S>) + (size_t)S::kWarps * S::kStages * S::kStage;
+  constexpr size_t smem = ((sizeof(Table<S>) + 127) & ~127) + 128 + (size_t)S::kWarps * S::kStages * S::kStage;
   static_assert(smem + 6144 <= kSmemMax, "");
   const int rc = once.run(dev, [] {
     return (int)cudaFuncSetAttribute(k_attend<KIND, DP, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);

@@ -174,7 +174,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_score(const __grid_con
   constexpr int kVec = DT == SEEDQ_F32 ? 4 : 8;    // in one 16-byte load
   constexpr int kTile = 32 * kPer;
   constexpr int kSize = DT == SEEDQ_F32 ? 4 : 2;
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  // at a multiple of 128 bytes: a copy whose 32-byte sectors straddle those of
+  // shared memory is fetched twice from L2
+  uint8_t *smem = smem_raw + (128 - ((uint32_t)__cvta_generic_to_shared(smem_raw) & 127)) % 128;
   __shared__ Part s_part[2 * kWarps];
   __shared__ int64_t s_row[2 * kWarps];  // its row, or -1
   __shared__ uint64_t s_buffer[kWarps][64];
@@ -554,7 +557,7 @@ seedq_status launch(ScoreArgs &a, int sms, int dev, cudaStream_t st) {
   const int ctas = std::min(sms * kCtasPerSm, kMaxCtas);
   a.share = std::max<int64_t>((total + ctas - 1) / ctas, kWarps);
   a.ctas = (int)((total + a.share - 1) / a.share);
-  constexpr size_t smem = (size_t)kWarps * kStages * kTileBytes;
+  constexpr size_t smem = (size_t)kWarps * kStages * kTileBytes + 128;
   const int rc = g_once[DT * 2 + VEC].run(dev, [] {
     return (int)cudaFuncSetAttribute(k_score<DT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   });
