@@ -48,6 +48,11 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kCtasPerSm = 2;
 constexpr int kMaxCtas = 152 * kCtasPerSm;
 constexpr int kMaxTop = 32;
+// k_score_few: threads, the most CTAs of a call, candidates that a CTA sorts
+constexpr int kFewThreads = 256;
+constexpr int kFewWarps = kFewThreads / 32;
+constexpr int kFewMax = 16 * 152;
+constexpr int kFewKeys = 512;
 constexpr int kStages = 3;       // tiles in a warp's ring
 constexpr int kTileBytes = 2048; // 64 bytes per lane
 constexpr float kLog2e = 1.4426950408889634f;
@@ -78,11 +83,11 @@ struct Part {
 
 // A logit's place in the order as a whole number: larger logits first, NaN
 // before all, -0 equal to +0, the lower index first among equals.  Never 0.
-__device__ __forceinline__ uint64_t order_key(float x, int i) {
+__device__ __forceinline__ uint32_t order_word(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
-  const uint32_t u = isnan(x) ? 0xffffffffu : (b >> 31) ? ~b : (b | 0x80000000u);
-  return ((uint64_t)u << 32) | (uint32_t)~i;
+  return isnan(x) ? 0xffffffffu : (b >> 31) ? ~b : (b | 0x80000000u);
 }
+__device__ __forceinline__ uint64_t order_key(float x, int i) { return ((uint64_t)order_word(x) << 32) | (uint32_t)~i; }
 __device__ __forceinline__ float key_value(uint64_t key) {
   const uint32_t u = (uint32_t)(key >> 32);
   return u == 0xffffffffu ? CUDART_NAN_F : __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u);
@@ -98,6 +103,11 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
   float y;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
+}
+// x >= xt as x > the number before xt; for -inf every x: no x is <= NaN.
+__device__ __forceinline__ float number_before(float xt) {
+  if (xt == -CUDART_INF_F) return CUDART_NAN_F;
+  return xt == 0.f ? __uint_as_float(0x80000001u) : __uint_as_float(__float_as_uint(xt) + (xt > 0.f ? -1 : 1));
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -400,10 +410,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_score(const __grid_con
     if (a.targets) {
       if (fresh) {
         above = xt;
-        // x >= xt as x > the number before xt; for -inf every x: no x is <= NaN
-        from = xt == -CUDART_INF_F ? CUDART_NAN_F
-               : xt == 0.f         ? __uint_as_float(0x80000001u)
-                                   : __uint_as_float(__float_as_uint(xt) + (xt > 0.f ? -1 : 1));
+        from = number_before(xt);
       }
       const float thr = base < t ? from : above;
       if (partial || (t >= base && t < base + kTile)) {
@@ -450,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_score(const __grid_con
 
   // ---- joins.  Parts are taken in order; a join of few is one warp's work, so
   // that many rows are joined at a time, one of many the whole CTA's.
-  Part *slots = (Part *)((uint8_t *)a.workspace + kMaxCtas * 8);  // two per CTA
+  Part *slots = (Part *)((uint8_t *)a.workspace + kFewMax * 4);  // two per CTA
   int *counters = (int *)a.workspace;
   __shared__ Part s_sum[kWarps];
   __shared__ int s_last[2];
@@ -547,11 +554,280 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_score(const __grid_con
   }
 }
 
+// ---------------------------------------------------------------- few rows
+//
+// A row's chunk per CTA, held in registers.  With few rows latency is all: the
+// lists of k_score would each be built from one or two tiles.  Here every warp
+// finds the ceil(top_k / 8)-th largest of its lanes' maxima; at least top_k
+// logits of the CTA reach the smallest of these, and few more do, so these few
+// are packed and put in order by counting, for each, how many come before it.
+// The last CTA of a row to arrive does the same with the chunks' lists.
+
+// Puts the first 32 of n <= kFewKeys distinct keys in order into list (zeroed).
+__device__ __forceinline__ void order_keys(const uint64_t *keys, int n, uint64_t *list) {
+  for (int i = threadIdx.x; i < n; i += kFewThreads) {
+    const uint64_t own = keys[i];
+    int before = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) before += keys[j] > own;
+    if (before < kMaxTop) list[before] = own;
+  }
+}
+
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kFewThreads, 4) k_score_few(const __grid_constant__ ScoreArgs a) {
+  constexpr int kPer = DT == SEEDQ_F32 ? 16 : 32, kVec = DT == SEEDQ_F32 ? 4 : 8;
+  __shared__ uint64_t s_keys[kFewKeys], s_list[kMaxTop], s_best[kFewWarps];
+  __shared__ float s_1[kFewWarps], s_2[kFewWarps];
+  __shared__ uint32_t s_most[kFewWarps], s_reach[kFewWarps];
+  __shared__ int s_count[kFewWarps], s_n, s_last;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  const int64_t row = blockIdx.x / a.tiles;
+  const int chunk = blockIdx.x - (int)row * a.tiles;
+  const int base = chunk * (kFewThreads * kPer);
+
+  auto index = [&](int e) -> int {
+    return base + (VEC ? (e / kVec) * (kFewThreads * kVec) + tid * kVec + e % kVec : e * kFewThreads + tid);
+  };
+  float x[kPer];
+  if (VEC) {
+    const char *src = (const char *)a.x + (row * a.stride + base + tid * kVec) * (16 / kVec);
+    uint4 y[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+      y[v] = index(v * kVec) + kVec <= a.vocab ? __ldg((const uint4 *)(src + v * (kFewThreads * 16))) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const uint32_t z[4] = {y[v].x, y[v].y, y[v].z, y[v].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (DT == SEEDQ_F32) {
+          x[v * 4 + k] = __uint_as_float(z[k]);
+        } else if (DT == SEEDQ_BF16) {
+          x[(v * 8 + 2 * k) % kPer] = __uint_as_float(z[k] << 16);
+          x[(v * 8 + 2 * k + 1) % kPer] = __uint_as_float(z[k] & 0xffff0000u);
+        } else {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&z[k]));
+          x[(v * 8 + 2 * k) % kPer] = f.x, x[(v * 8 + 2 * k + 1) % kPer] = f.y;
+        }
+      }
+    }
+  }
+  if (!VEC || base + kFewThreads * kPer > a.vocab) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int i = index(e);
+      // of a piece that the row's end cuts, what is there is read alone
+      if (i >= a.vocab) x[e] = -CUDART_INF_F;
+      else if (!VEC || i - e % kVec + kVec > a.vocab) x[e] = load_elem(a.x, DT, row * a.stride + i);
+    }
+  }
+  const int64_t t = a.targets ? a.targets[row] : -1;
+  const float xt = t >= 0 && t < a.vocab ? load_elem(a.x, DT, row * a.stride + t) : 0.f;
+
+  if (tid < kMaxTop) s_list[tid] = 0;
+  if (tid == 0) s_n = 0;
+  float mx = max_nan(x[0], x[1]);
+#pragma unroll
+  for (int e = 2; e < kPer; e += 2) mx = max_nan(mx, x[e], x[e + 1]);
+  const uint32_t um = index(0) < a.vocab ? order_word(mx) : 0;
+  uint32_t reach = 0, rest = um;
+  const uint32_t most = __reduce_max_sync(~0u, um);
+  for (int j = 0; j < (a.top_k + kFewWarps - 1) / kFewWarps; ++j) {
+    reach = __reduce_max_sync(~0u, rest);
+    if (lane == __ffs(__ballot_sync(~0u, rest == reach)) - 1) rest = 0;
+  }
+  if (lane == 0) s_most[w] = most, s_reach[w] = reach;
+  __syncthreads();
+  uint32_t top = 0;
+  reach = ~0u;
+#pragma unroll
+  for (int k = 0; k < kFewWarps; ++k) top = max(top, s_most[k]), reach = min(reach, s_reach[k]);
+  const float m = key_value((uint64_t)top << 32);
+
+  if (a.top_k && um && um >= reach) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const uint64_t key = order_key(x[e], index(e));
+      if ((uint32_t)(key >> 32) >= reach && index(e) < a.vocab) {
+        const int at = atomicAdd(&s_n, 1);
+        if (at < kFewKeys) s_keys[at] = key;
+      }
+    }
+  }
+  const float off = m == -CUDART_INF_F ? 0.f : -m;
+  const uint64_t off2 = f2_pack(off, off), c2 = f2_pack(a.c, a.c);
+  uint64_t p1 = 0, p2 = 0;
+#pragma unroll
+  for (int e = 0; e < kPer; e += 2) {
+    const float2 d = f2_unpack(f2_mul(f2_add(f2_pack(x[e], x[e + 1]), off2), c2));
+    const float d0 = max_nan(d.x, -1e4f), d1 = max_nan(d.y, -1e4f);
+    const uint64_t y = f2_pack(exp2_fast(d0), exp2_fast(d1));
+    p1 = f2_add(p1, y);
+    p2 = f2_fma(y, f2_pack(d0, d1), p2);
+  }
+  float s1 = f2_unpack(p1).x + f2_unpack(p1).y, s2 = f2_unpack(p2).x + f2_unpack(p2).y;
+  int count = 0;
+  if (a.targets) {
+    const float from = number_before(xt);
+    if (base + kFewThreads * kPer > a.vocab || (t >= base && t < base + kFewThreads * kPer)) {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) count += index(e) < a.vocab && !(x[e] <= (index(e) < t ? from : xt));
+    } else {
+      const float thr = base < t ? from : xt;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) count += !(x[e] <= thr);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    s1 += __shfl_xor_sync(~0u, s1, o);
+    s2 += __shfl_xor_sync(~0u, s2, o);
+  }
+  count = __reduce_add_sync(~0u, count);
+  if (lane == 0) s_1[w] = s1, s_2[w] = s2, s_count[w] = count;
+  __syncthreads();
+  if (s_n <= kFewKeys) {
+    order_keys(s_keys, s_n, s_list);
+  } else {
+    // more than fit reach it (equal logits): one key after another
+    uint64_t last = ~0ull;
+    for (int k = 0; k < a.top_k; ++k) {
+      uint64_t best = 0;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const uint64_t key = order_key(x[e], index(e));
+        if (key < last && key > best && index(e) < a.vocab) best = key;
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) best = max(best, __shfl_xor_sync(~0u, best, o));
+      if (lane == 0) s_best[w] = best;
+      __syncthreads();
+      last = 0;
+      for (int j = 0; j < kFewWarps; ++j) last = max(last, s_best[j]);
+      if (tid == 0) s_list[k] = last;
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+
+  Part *parts = (Part *)((uint8_t *)a.workspace + kFewMax * 4) + row * a.tiles;
+  int *counter = (int *)a.workspace + row;
+  if (w == 0) {
+    s1 = s2 = 0.f;
+    count = 0;
+    for (int k = 0; k < kFewWarps; ++k) s1 += s_1[k], s2 += s_2[k], count += s_count[k];
+    if (a.tiles == 1) {
+      write_row(a, row, m, s1, s2, count, s_list[lane], t, xt);
+    } else {
+      Part &q = parts[chunk];
+      q.key[lane] = s_list[lane];
+      if (lane == 0) q.m = m, q.s1 = s1, q.s2 = s2, q.count = count;
+      __syncwarp();
+      if (lane == 0) {
+        __threadfence();
+        s_last = atomicAdd(counter, 1) == a.tiles - 1;
+        if (s_last) *counter = 0;
+        __threadfence();
+        s_n = 0;
+      }
+    }
+  }
+  if (a.tiles == 1) return;
+  __syncthreads();
+  if (!s_last) return;
+
+  // the row's chunks
+  const int n = a.tiles;
+  if (tid < kMaxTop) s_list[tid] = 0;
+  // At least top_k keys reach the smallest of the chunks' ceil(top_k / n)-th, and
+  // the largest of their top_k-th.
+  uint64_t low = ~0ull, high = 0;
+  if (a.top_k) {
+    const int j = (a.top_k + n - 1) / n - 1;
+    // the first keys are on their way meanwhile
+    constexpr int kAhead = 4;
+    uint64_t ahead[kAhead];
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      const int i = tid + r * kFewThreads, q = i / a.top_k;
+      ahead[r] = i < n * a.top_k ? fresh_load(&parts[q].key[i - q * a.top_k]) : 0;
+    }
+    for (int i = tid; i < n; i += kFewThreads) {
+      low = min(low, fresh_load(&parts[i].key[j]));
+      high = max(high, fresh_load(&parts[i].key[a.top_k - 1]));
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      low = min(low, __shfl_xor_sync(~0u, low, o));
+      high = max(high, __shfl_xor_sync(~0u, high, o));
+    }
+    if (lane == 0) s_best[w] = low, s_keys[w] = high;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kFewWarps; ++k) low = min(low, s_best[k]), high = max(high, s_keys[k]);
+    low = max(max(low, high), (uint64_t)1);
+    __syncthreads();
+    auto push = [&](uint64_t key) {
+      if (key < low) return;
+      const int at = atomicAdd(&s_n, 1);
+      if (at < kFewKeys) s_keys[at] = key;
+    };
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) push(ahead[r]);
+    for (int i = tid + kAhead * kFewThreads; i < n * a.top_k; i += kFewThreads) {
+      const int q = i / a.top_k;
+      push(fresh_load(&parts[q].key[i - q * a.top_k]));
+    }
+    __syncthreads();
+    if (s_n <= kFewKeys) {
+      order_keys(s_keys, s_n, s_list);
+    } else if (w == 0) {
+      uint64_t key = 0;
+      for (int i = 0; i < n; ++i) key = merge_lists(key, fresh_load(&parts[i].key[lane]), lane);
+      s_list[lane] = key;
+    }
+    __syncthreads();
+  }
+  if (w == 0) {
+    float fm = -CUDART_INF_F, f1 = 0.f, f2 = 0.f;
+    int fc = 0;
+    for (int i = lane; i < n; i += 32) {
+      float qm = fresh_load(&parts[i].m), q1 = fresh_load(&parts[i].s1), q2 = fresh_load(&parts[i].s2);
+      fc += fresh_load(&parts[i].count);
+      const float to = max_nan(fm, qm);
+      rebase(fm, f1, f2, to, a.c);
+      rebase(qm, q1, q2, to, a.c);
+      f1 += q1, f2 += q2;
+    }
+    float to = fm;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) to = max_nan(to, __shfl_xor_sync(~0u, to, o));
+    rebase(fm, f1, f2, to, a.c);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      f1 += __shfl_xor_sync(~0u, f1, o);
+      f2 += __shfl_xor_sync(~0u, f2, o);
+    }
+    fc = __reduce_add_sync(~0u, fc);
+    write_row(a, row, fm, f1, f2, fc, s_list[lane], t, xt);
+  }
+}
+
 DeviceOnce g_once[6];
 
 template <int DT, bool VEC>
 seedq_status launch(ScoreArgs &a, int sms, int dev, cudaStream_t st) {
-  constexpr int kTile = 32 * (DT == SEEDQ_F32 ? 16 : 32);
+  constexpr int kPer = DT == SEEDQ_F32 ? 16 : 32, kTile = 32 * kPer, kChunk = kFewThreads * kPer;
+  a.tiles = (a.vocab + kChunk - 1) / kChunk;
+  // Few rows: 16 of 128256 with 20 alternatives take 14 us there and 27 below, 64
+  // take 29 and 41, 256 with 5 take 76 and 47; rows of a tile or two are one
+  // warp's work below (2000 of 1000: 20 and 15 us).
+  if (a.vocab > 2 * kTile && a.rows * a.tiles <= kFewMax) {
+    k_score_few<DT, VEC><<<(unsigned)(a.rows * a.tiles), kFewThreads, 0, st>>>(a);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
+  }
   a.tiles = (a.vocab + kTile - 1) / kTile;
   const int64_t total = a.rows * a.tiles;
   const int ctas = std::min(sms * kCtasPerSm, kMaxCtas);
@@ -576,7 +852,8 @@ extern "C" {
 
 uint64_t seedq_token_logprobs_workspace_bytes(int64_t n_rows, int64_t vocab) {
   if (n_rows < 0 || vocab < 1) return 0;
-  return kMaxCtas * 8 + (uint64_t)kMaxCtas * 2 * sizeof(Part);  // arrival counters; two parts of rows per CTA
+  static_assert(kMaxCtas * 2 <= kFewMax, "");
+  return kFewMax * 4 + (uint64_t)kFewMax * sizeof(Part);  // arrival counters and parts of rows
 }
 
 seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
