@@ -1,0 +1,125 @@
+"""The decode loop over compressed layers against a plain recomputation in fp64.
+
+The reference multiplies the decoded weights, rounds to bfloat16 where the loop
+does, and attends over the numbers that the loop's caches hold (read back by
+gather), so what remains are float32 sums and bfloat16 roundings that fall the
+other way: each of those moves a product's input by 2^-8 of a number, a few per
+row of hundreds, and two layers of them stay well below 1% of the largest logit.
+A wrong page, slot, position, head or mask moves logits by their own size.
+"""
+import os
+import sys
+
+import numpy as np
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+sys.path.insert(0, ROOT)
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def G():
+    from paper_2609_38477_gb300 import build
+
+    build.build()
+    from paper_2609_38477_gb300 import generate
+
+    return generate
+
+
+def dense(layer):
+    w = torch.empty((layer.rows, layer.cols), device="cuda")
+    layer.decode_weights(w)
+    return w.double()
+
+
+def bf(x):
+    return x.float().bfloat16().double()
+
+
+def norm(x, gain):
+    return bf(x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-5) * gain.double())
+
+
+def rope(x, pos, freqs):
+    a = pos[:, None].double() * freqs.double()
+    c, s = torch.cos(a)[:, None], torch.sin(a)[:, None]
+    u, v = x.chunk(2, 2)
+    return torch.cat([u * c - v * s, v * c + u * s], 2)
+
+
+def reference(d, weights, history, r, count):
+    """Logits of the last `count` tokens of request r, whose tokens are history."""
+    s = d.spec
+    n = len(history)
+    slots = d.table[r, torch.arange(n, device="cuda") // d.page_size].long() * d.page_size + torch.arange(n, device="cuda") % d.page_size
+    pos = torch.arange(n - count, n, device="cuda")
+    x = d.embedding[torch.tensor(history[n - count:], device="cuda")].double()
+    for block, cache, w in zip(d.blocks, d.caches, weights):
+        h = norm(x, block["attn_norm"])
+        q = rope((h @ w["q"].T).view(count, s.n_heads, s.head_dim), pos, d.freqs)
+        k, v = (torch.empty((n, s.n_kv_heads, s.head_dim), device="cuda") for _ in range(2))
+        cache.gather(slots, k, v)
+        own = rope((h @ w["k"].T).view(count, s.n_kv_heads, s.head_dim), pos, d.freqs)
+        # A page's power-of-two scale is at most its largest number / 63.5, and older tokens on the page count.
+        step = max(float(own.abs().max()), float(k.abs().max())) / 63
+        assert float((k[n - count:].double() - own).abs().max()) <= (step if cache.kind == "int8" else 4 * step)
+        g = s.n_heads // s.n_kv_heads
+        z = torch.einsum("thd,jhd->thj", q, k.double().repeat_interleave(g, 1)) * s.head_dim ** -0.5
+        z = z.masked_fill((torch.arange(n, device="cuda") > pos[:, None])[:, None], -np.inf)
+        o = torch.einsum("thj,jhd->thd", z.softmax(2), v.double().repeat_interleave(g, 1))
+        x = x + bf(o).reshape(count, -1) @ w["o"].T
+        h = norm(x, block["mlp_norm"])
+        x = x + bf(torch.nn.functional.silu(h @ w["gate"].T) * (h @ w["up"].T)) @ w["down"].T
+    return norm(x, d.final_norm) @ weights[-1]["head"].T
+
+
+@pytest.mark.parametrize("name,kind,page", [("tiny", "int8", 16), ("tiny", "e4m3", 32), ("tiny_odd", "int8", 16)])
+def test_decode_loop(G, name, kind, page):
+    d = G.synthetic_decoder(name, max_requests=3, n_pages=7, page_size=page, kind=kind)
+    weights = [{k: dense(b[k]) for k in ("q", "k", "v", "o", "gate", "up", "down")} for b in d.blocks] + [{"head": dense(d.head)}]
+    rng = np.random.RandomState(3)
+    vocab = d.spec.vocab
+    history = [[], [], []]
+    # prompts in pieces, single tokens, a pause, an end whose pages another request takes
+    for new in ([5, 1, 9], [7, 9, 0], [1, 1, 1], [1, 0, 1], [16, 0, 0], [-1, 1, 1], [4, 0, 12], [1, 1, 1]):
+        tokens = []
+        for r, n in enumerate(new):
+            if n < 0:
+                history[r] = []
+            fresh = [int(t) for t in rng.randint(0, vocab, max(n, 0))]
+            history[r] += fresh
+            tokens += fresh
+        logits = d.step(torch.tensor(tokens, device="cuda"), torch.tensor(new, dtype=torch.int32, device="cuda"))
+        assert d.plan.status.tolist() == [0, 0, 0]
+        assert d.seq_lens.tolist() == [len(h) for h in history]
+        at = 0
+        for r, n in enumerate(new):
+            if n <= 0:
+                continue
+            want = reference(d, weights, history[r], r, n)
+            got = logits[at:at + n].double()
+            assert float((got - want).abs().max()) <= 0.01 * float(want.abs().max())
+            at += n
+        targets = torch.tensor([int(t) for t in rng.randint(0, vocab, at)], device="cuda")
+        logp, entropy, rank, top, best = d.score(logits, targets, top_k=4, temperature=0.8)
+        ref = torch.log_softmax(logits.double() / 0.8, 1)
+        assert torch.allclose(logp.double(), ref.gather(1, targets[:, None])[:, 0], atol=1e-5)
+        assert torch.allclose(entropy.double(), -(ref.exp() * ref).sum(1), atol=1e-5)
+        assert torch.equal(best[:, 0].long(), logits.argmax(1)) and torch.allclose(top.double(), ref.topk(4).values, atol=1e-5)
+    assert int(d.free_count) + int((-(-d.seq_lens // page)).sum()) == 7
+    with_room = d.table.clone()
+    # a request that the pages cannot hold is told so, and its neighbours go on
+    d.step(torch.tensor([1] * 16, device="cuda"), torch.tensor([0, 16, 0], dtype=torch.int32, device="cuda"))
+    while int(d.plan.status[1]) == 0:
+        d.step(torch.tensor([1] * 16, device="cuda"), torch.tensor([0, 16, 0], dtype=torch.int32, device="cuda"))
+    assert d.plan.status.tolist() == [0, 1, 0] and bool((d.plan.slots == -1).all())
+    assert torch.equal(d.table[0], with_room[0]) and torch.equal(d.table[2], with_room[2])
+
+
+def test_example_runs(G, capsys):
+    G.main()
+    assert capsys.readouterr().out.count("step") == 6

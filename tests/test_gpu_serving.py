@@ -550,6 +550,43 @@ def test_score_workspace_of_a_larger_batch(V):
         check_score(V, x, [v // 2] * n, 1.0, 6, ws)
 
 
+def test_score_lists_that_overflow(V):
+    """Few rows, cut into chunks: one of equal logits, small whole numbers with
+    ties at every edge, and chunks of which all but one reach the list with almost
+    all of their alternatives."""
+    v = 40 * 4096 + 77
+    g = torch.Generator("cuda").manual_seed(1)
+    rows = [torch.zeros(v, device="cuda"), torch.randint(0, 9, (v,), generator=g, device="cuda").float(),
+            torch.full((v,), -5.0, device="cuda")]
+    for c in range(41):
+        if c != 7:
+            at = c * 4096 + torch.randperm(77, generator=g, device="cuda")[:31]
+            rows[2][at] = 5 + torch.rand(31, generator=g, device="cuda")
+    x = torch.stack(rows)
+    check_score(V, x, [v - 1, 4000, 8], 1.0, 32)
+    check_score(V, x.bfloat16(), [0, 4000, 8], 1.0, 32)
+    check_score(V, x[1:2, 1:], [17], 2.0, 9)
+
+
+def test_score_row_counts_around_the_split(V):
+    """Row counts and lengths on both sides of every choice between the kernels."""
+    for n, v in ((1, 1024), (1, 1025), (3, 2049), (2432, 1500), (2433, 1500), (76, 128256), (77, 128256), (608, 16384), (609, 16384)):
+        x = torch.randn((n, v), device="cuda") * 3
+        lp, en = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+        rk, t = torch.empty(n, dtype=torch.int32, device="cuda"), torch.randint(0, v, (n,), device="cuda")
+        tl, ti = torch.empty(n, 6, device="cuda"), torch.empty(n, 6, dtype=torch.int32, device="cuda")
+        V.token_logprobs(x, t, lp, en, rk, tl, ti, V.score_workspace(n, v))
+        ref = torch.log_softmax(x.double(), 1)
+        tol = (v / 128 + 72) * 2.0 ** -24 + 8 * 2.0 ** -24 * float(x.abs().max()) + 2.0 ** -22
+        assert float((lp - ref.gather(1, t[:, None])[:, 0]).abs().max()) <= tol
+        assert float((en + (ref.exp() * ref).sum(1)).abs().max()) <= 40 * tol
+        best = torch.sort(x.double(), dim=1, descending=True, stable=True).indices[:, :6]
+        assert torch.equal(ti.long(), best)
+        assert float((tl - ref.gather(1, best)).abs().max()) <= tol
+        xt = x.gather(1, t[:, None])
+        assert torch.equal(rk.long(), ((x > xt) | ((x == xt) & (torch.arange(v, device="cuda") < t[:, None]))).sum(1))
+
+
 # ---------------------------------------------------------------- together
 
 def test_side_stream_and_graph(V):
