@@ -295,11 +295,13 @@ __device__ __forceinline__ T load_fresh(const float *x) {
 // output.  A part holds m (in units of log2) and l of every column and the
 // columns' averages o = sum / l as the products' accumulators lie in the lanes;
 // it weighs l 2^m.  Averages, not sums, are kept, so nothing overflows on the
-// way.  The warp takes the tiles first, first + step, ...; a lane reads the
-// statistics of its two columns itself, so no barrier is needed.
+// way.  The parts are from[0..n-1], or, without `from`, the second of the two
+// slots of the CTA at `slots` and the first ones of the n - 1 CTAs behind it.
+// The warp takes the tiles first, first + step, ...; a lane reads the statistics
+// of its two columns itself, so no barrier is needed.
 template <typename S, int MODE>
-__device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const float *const *from, float *to, int first,
-                                     int step) {
+__device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const float *const *from, const float *slots,
+                                     float *to, int first, int step) {
   constexpr int kAtATime = 8;
   const int lane = threadIdx.x & 31, nn = lane >> 2, q4 = lane & 3;
 #pragma unroll 1
@@ -312,7 +314,8 @@ __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const 
       float4 o[kAtATime];
 #pragma unroll
       for (int k = 0; k < kAtATime; ++k) {
-        const float *x = from[min(i + k, n - 1)];
+        const int j = min(i + k, n - 1);
+        const float *x = from ? from[j] : slots + (j ? 2 * j : 1) * S::kSlot;
         m[k] = load_fresh<float2>(x + col);
         l[k] = load_fresh<float2>(x + S::kStats / 2 + col);
         o[k] = load_fresh<float4>(x + S::kStats + (tt * 32 + lane) * 4);
@@ -448,7 +451,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   int cuts = 0;  // CTAs per entry, where all have as many
   if (most == least && total <= (int64_t)p.ctas * (most + kStart)) {
     const int entries = quotient(total, most + kStart);
-    cuts = min(quotient(p.ctas, entries), (most + warps - 1) / warps);
+    cuts = min(quotient(p.ctas, entries), little ? (most + 3) >> 2 : (most + S::kWarps - 1) / S::kWarps);
     if (!little && entries * cuts * 10 < p.ctas * 9) cuts = 0;
   }
   auto nearest = [&](int64_t u) -> int64_t {  // entry end nearest to u
@@ -1001,7 +1004,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
 
   // ---- joins: first the entries cut between warps of this CTA, then, if this
   // CTA is the last to arrive, those cut between CTAs
-  __shared__ const float *s_from[kMaxCtas];
+  __shared__ const float *s_from[2 * S::kWarps];
   __shared__ int s_last[2];
   int *counters = (int *)p.a.workspace;
   c0 = s_split.c0, c1 = s_split.c1;
@@ -1038,6 +1041,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   while (true) {
     int n, first = w, step = S::kWarps;
     const float *const *list = s_from;
+    const float *slots = nullptr;
     float *to = nullptr;
     Desc e;
     if (todo) {
@@ -1057,12 +1061,13 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
         if (cross[0] < 0 && cross[1] < 0) break;
         __syncthreads();
         if (lane == 0 && w < 2 && cross[w] >= 0) {
-          __threadfence();  // the CTA's parts, seen through the barrier, before the arrival
           const Desc &x = s_cut[cross[w]];
           const int a = first_cta(x), all = cta_count(x);
-          s_last[w] = atomicAdd(counters + a, 1) == all - 1 ? all : 0;
+          // the CTA's parts, seen through the barrier, before the arrival, and the others' after it
+          int seen;
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(seen) : "l"(counters + a) : "memory");
+          s_last[w] = seen == all - 1 ? all : 0;
           if (s_last[w]) counters[a] = 0;
-          __threadfence();
         }
         __syncthreads();
       }
@@ -1071,12 +1076,10 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       e = s_cut[cross[side]];
       n = s_last[side];
       // the first CTA's part is its second slot, the others' their first
-      const int a = first_cta(e);
-      __syncthreads();  // the list of the joins before is not read any more
-      for (int x = tid; x < n; x += S::kThreads) s_from[x] = ws + ((size_t)(a + x) * 2 + (x == 0)) * S::kSlot;
-      __syncthreads();
+      list = nullptr;
+      slots = ws + (size_t)first_cta(e) * 2 * S::kSlot;
     }
-    join<S, MODE>(p, e, n, list, to, first, step);
+    join<S, MODE>(p, e, n, list, slots, to, first, step);
   }
 }
 
