@@ -9,14 +9,14 @@
 // step has few rows of its own (query heads that share a key-value head, times
 // new tokens) and they fit the 8 columns.  Codes are exact in binary16; q and
 // the weights p_j s^v_j, which are not, are held as a high and a low half (22
-// bits).  Up to 4 rows, the columns 0-3 carry the high and 4-7 the low halves of
-// the same rows and the second half costs nothing; from 5 rows on the low halves
-// are products of their own into the same sums.  q is scaled by a power of two
-// per row, weights are taken relative to the largest block scale so far and
-// scaled by 2^14, so binary16's range never cuts off more than 2^-38 of the
-// largest.  Each unit's products start from zero and are added to float32
-// registers, so a long context is not accumulated inside the tensor cores,
-// which truncate.
+// bits; of q in a 16-bit type, scaled, the high half is all).  Up to 4 rows, the
+// columns 0-3 carry the high and 4-7 the low halves of the same rows and the
+// second half costs nothing; from 5 rows on the low halves are products of their
+// own into the same sums.  q is scaled by a power of two per row, weights are
+// taken relative to the largest block scale so far and scaled by 2^14, so
+// binary16's range never cuts off more than 2^-38 of the largest.  Each unit's
+// products start from zero and are added to float32 registers, so a long
+// context is not accumulated inside the tensor cores, which truncate.
 //
 // What bounds it: the bytes of the cache, 2 head_dim per key and key-value
 // head.  At 8 rows a byte costs 16 operations, far below the balance, but every
@@ -63,12 +63,14 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kWeight = 16384.f;  // weights are held times this
 
 // DP: head dim rounded up to 64, 128 or 256.  MODE: rows of a tile: 0: 4 (high
-// and low halves share the 8 columns), 1: 8, 2: 16.
-template <int DP, int MODE>
+// and low halves share the 8 columns), 1: 8, 2: 16.  HALVES: of q, 1 where its
+// type has no more than binary16's 11 bits.
+template <int DP, int MODE, int HALVES>
 struct Shape {
   static constexpr int kRows = 4 << MODE;
   static constexpr int kSets = MODE == 2 ? 2 : 1;    // sets of 8 columns
-  static constexpr int kHalves = MODE == 0 ? 1 : 2;  // operands per set
+  static constexpr int kHalves = MODE == 0 ? 1 : 2;  // of the weights: operands per set
+  static constexpr int kQHalves = MODE == 0 ? 1 : HALVES;  // of q
   static constexpr int kUnit = DP <= 128 ? 32 : 16;  // tokens of a unit
   static constexpr int kGroups = kUnit / 16;
   static constexpr int kChunks = DP / 64;            // 64 head dims: 16 codes of 4 lanes
@@ -385,9 +387,9 @@ __host__ __device__ constexpr int swizzle(int r) {
   return DP >= 128 ? (r & 6) ^ ((r & 1) << 2) : (r >> 1) & 3;
 }
 
-template <int KIND, int DP, int MODE>
-__global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const __grid_constant__ Args p) {
-  using S = Shape<DP, MODE>;
+template <int KIND, int DP, int MODE, int HALVES>
+__global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend(const __grid_constant__ Args p) {
+  using S = Shape<DP, MODE, HALVES>;
   extern __shared__ __align__(128) uint8_t smem_raw[];
   uint8_t *smem = smem_raw + (128 - ((uint32_t)__cvta_generic_to_shared(smem_raw) & 127)) % 128;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
@@ -532,7 +534,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
   };
 
   // ---- products
-  uint32_t qf[S::kSets][S::kHalves][S::kChunks * 4][2];  // q as the second operand
+  uint32_t qf[S::kSets][S::kQHalves][S::kChunks * 4][2];  // q as the second operand
   float zf[S::kSets][2];      // z in units of log2 per unit of product, but for the key scale
   float m[S::kSets][2], l[S::kSets][2], vmax = 0.f;
   uint64_t o[S::kSets][S::kTiles][2];  // sums of the columns (2 q4, 2 q4 + 1) for two head dims
@@ -721,7 +723,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
               qf[s][0][k][y] = nn < 4 ? a : b;
             } else {
               qf[s][0][k][y] = a;
-              qf[s][S::kHalves - 1][k][y] = b;
+              if (S::kQHalves == 2) qf[s][S::kQHalves - 1][k][y] = b;
             }
           }
 #pragma unroll
@@ -757,7 +759,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
       uint64_t sum[S::kSets][2];
 #pragma unroll
       for (int c = 0; c < S::kChunks; ++c) {
-        float acc[S::kSets][S::kHalves][4] = {};
+        float acc[S::kSets][S::kQHalves][4] = {};
         const uint32_t at = g * (16 * DP) + (kat ^ (c * 64));
         const uint4 x = *(const uint4 *)(st + at), y = *(const uint4 *)(st + at + 8 * DP);  // the tokens n and n + 8
         const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
@@ -768,12 +770,12 @@ __global__ void __launch_bounds__(Shape<DP, MODE>::kThreads, 1) k_attend(const _
 #pragma unroll
           for (int s = 0; s < S::kSets; ++s)
 #pragma unroll
-            for (int hf = 0; hf < S::kHalves; ++hf) mma(acc[s][hf], a0, a1, a2, a3, qf[s][hf][c * 4 + k]);
+            for (int hf = 0; hf < S::kQHalves; ++hf) mma(acc[s][hf], a0, a1, a2, a3, qf[s][hf][c * 4 + k]);
         }
 #pragma unroll
         for (int s = 0; s < S::kSets; ++s)
 #pragma unroll
-          for (int hf = 0; hf < S::kHalves; ++hf)
+          for (int hf = 0; hf < S::kQHalves; ++hf)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               const uint64_t x = f2_pack(acc[s][hf][2 * k], acc[s][hf][2 * k + 1]);
@@ -1100,23 +1102,23 @@ Plan shape_for(const seedq_kv_cache *c, int32_t n_heads, int32_t max_new) {
 }
 template <int DP, int MODE>
 constexpr uint64_t workspace_bytes() {
-  using S = Shape<DP, MODE>;
+  using S = Shape<DP, MODE, 2>;
   // arrival counters; per CTA two parts of entries cut between CTAs, per warp one of an entry cut between warps
   return kMaxCtas * 4 + (uint64_t)kMaxCtas * (2 + S::kWarps) * S::kSlot * 4;
 }
 
-template <int KIND, int DP, int MODE>
+template <int KIND, int DP, int MODE, int HALVES>
 seedq_status launch(Args &p, int dev, cudaStream_t st) {
-  using S = Shape<DP, MODE>;
+  using S = Shape<DP, MODE, HALVES>;
   static DeviceOnce once;
   p.chunk = (p.a.n_requests + S::kRequests - 1) / S::kRequests;
   constexpr size_t smem = ((sizeof(Table<S>) + 127) & ~127) + 128 + (size_t)S::kWarps * S::kStages * S::kStage;
   static_assert(smem + 6144 <= kSmemMax, "");
   const int rc = once.run(dev, [] {
-    return (int)cudaFuncSetAttribute(k_attend<KIND, DP, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return (int)cudaFuncSetAttribute(k_attend<KIND, DP, MODE, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   });
   if (rc) return cuda_fail((cudaError_t)rc);
-  k_attend<KIND, DP, MODE><<<p.ctas, S::kThreads, smem, st>>>(p);
+  k_attend<KIND, DP, MODE, HALVES><<<p.ctas, S::kThreads, smem, st>>>(p);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
 }
@@ -1190,8 +1192,12 @@ seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_arg
   p.ctas_inv = ~0ull / (uint64_t)p.ctas + 1;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   return with_shape(shape_for(cache, a.n_heads, a.max_new), [&](auto dp, auto mode) {
-    return cache->kind == SEEDQ_KV_INT8 ? launch<SEEDQ_KV_INT8, dp.value, mode.value>(p, dev, stream)
-                                        : launch<SEEDQ_KV_E4M3, dp.value, mode.value>(p, dev, stream);
+    constexpr int kShort = mode.value == 0 ? 2 : 1;  // rows of 4 carry both halves anyway
+    if (a.q_dtype == SEEDQ_F32)
+      return cache->kind == SEEDQ_KV_INT8 ? launch<SEEDQ_KV_INT8, dp.value, mode.value, 2>(p, dev, stream)
+                                          : launch<SEEDQ_KV_E4M3, dp.value, mode.value, 2>(p, dev, stream);
+    return cache->kind == SEEDQ_KV_INT8 ? launch<SEEDQ_KV_INT8, dp.value, mode.value, kShort>(p, dev, stream)
+                                        : launch<SEEDQ_KV_E4M3, dp.value, mode.value, kShort>(p, dev, stream);
   });
 }
 
