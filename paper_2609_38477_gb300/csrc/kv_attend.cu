@@ -85,7 +85,8 @@ struct Shape {
   static constexpr int kWarps = (MODE == 2 || DP == 256) ? 8 : 12;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kStages = DP == 64 ? 4 : kWarps == 12 ? 2 : 3;  // units in a warp's ring
-  static constexpr int kWhole = 4 * kWarps, kWholeLittle = 8, kWholeWarp = 2;  // units, see the split of the work list
+  // units, see the split of the work list
+  static constexpr int kWhole = 8 * kWarps, kWholeLittle = 8, kWholeWarp = 6, kWholeWarpLittle = 2;
   static constexpr int kRequests = kThreads;                   // that the shared table holds
   static constexpr int kStats = 2 * 8 * kSets;                 // m and l of every column
   static constexpr int kSlot = kStats + kSets * kTiles * 128;  // floats of a part: stats, then lanes' products
@@ -184,8 +185,10 @@ __device__ __forceinline__ Req request(const Args &p, int b) {
   return r;
 }
 // Steps of the work list: an entry's units and kStart more, the cost of its start
-// (queries) and end, so that many short contexts weigh what they take.
-constexpr int kStart = 1;
+// (queries) and end, so that many short contexts weigh what they take (8 ragged
+// contexts up to 4096: 20 us without and with 1, 18, 17 and 15 with 2 to 4; 64 up
+// to 300: 23 without, 18, 18, 19 and 20 with 1 to 4).
+constexpr int kStart = 3;
 __device__ __forceinline__ int64_t steps_of(const Args &p, const Req &r) {
   return r.fresh ? (int64_t)(r.units + kStart) * r.tiles * p.c.n_kv_heads : 0;
 }
@@ -441,12 +444,15 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
     }
   }
   // Even shares of steps for the CTAs' warps, at least one each.  Little work goes
-  // to 4 warps per CTA, one per scheduler, and so to more SMs.  Entries of one
-  // length (one request, or a batch in step) are each cut for the same number of
-  // CTAs, so that no CTA has parts of two.  Else, where no entry is longer than a
+  // to 4 warps per CTA, one per scheduler, and so to more SMs (one request of 1000:
+  // 12 us, with 12 warps 15).  Entries of one length (one request, or a batch in
+  // step) are each cut for the same number of CTAs, so that no CTA has parts of two
+  // (one request of 4096: 15 us, else 17).  Else, where no entry is longer than a
   // few units per warp, the shares' ends move to the nearest entry's: a join
-  // between CTAs costs about as much as the uneven shares; likewise between warps
-  // where no entry is longer than kWholeWarp.
+  // between CTAs costs about as much as the uneven shares (16 requests of 2048, 64
+  // heads on 8: 28 us, without 30; with entries of up to 16 units per warp 8 of
+  // 4096 take 34 us instead of 18); likewise between warps where no entry is longer
+  // than kWholeWarp (200 requests of 100: 23 us, else 31).
   const bool little = total <= (int64_t)p.ctas * 8;
   const int warps = little ? 4 : S::kWarps;
   const int64_t share = max((int64_t)__umul64hi((uint64_t)total, p.ctas_inv) + 1, (int64_t)warps);
@@ -483,10 +489,15 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
   const uint32_t each = little ? mine / 4 : mine / S::kWarps, rest = mine - each * warps;
   int64_t w0 = c0 + each * (uint32_t)min(w, warps) + min((uint32_t)w, rest);
   int64_t w1 = w < warps ? w0 + each + (w < (int)rest) : w0;
-  if (most <= S::kWholeWarp && cuts <= 1) {
-    const int64_t c = nearest(lane ? w1 : w0);
-    w0 = __shfl_sync(~0u, c, 0);
-    w1 = __shfl_sync(~0u, c, 1);
+  if (most <= (little ? S::kWholeWarpLittle : S::kWholeWarp)) {
+    if (cuts == 1) {  // the CTA's only entry
+      w0 = c0;
+      w1 = w == 0 ? c1 : c0;
+    } else if (cuts == 0) {
+      const int64_t c = nearest(lane ? w1 : w0);
+      w0 = __shfl_sync(~0u, c, 0);
+      w1 = __shfl_sync(~0u, c, 1);
+    }
   }
 
   // Rows begin at multiples of 128 bytes: a copy whose 32-byte sectors straddle
