@@ -3,7 +3,7 @@
 //
 // Mathematics, one pass over the logits x with c = scale * log2(e):
 //   m = max x,  d = c (x - m),  s1 = sum 2^d,  s2 = sum d 2^d,
-//   logprob = ln2 (c (x_t - m) - log2 s1),  entropy = ln2 (log2 s1 - s2 / s1);
+//   logprob = scale (x_t - m) - ln s1,  entropy = ln2 (log2 s1 - s2 / s1);
 // when the running maximum rises by e / c, s1 and s2 become s1 2^-e and
 // (s2 - e s1) 2^-e.  Differences come first: nothing overflows, and a large
 // common part of the logits does not cost precision.  The rank counts logits
@@ -62,7 +62,7 @@ struct ScoreArgs {
   const void *x;
   int64_t stride, rows;
   int32_t vocab, tiles;  // tiles of a row
-  float c;               // scale * log2(e)
+  float scale, c;        // c = scale * log2(e)
   const int64_t *targets;
   float *logprob, *entropy;
   int32_t *rank;
@@ -119,6 +119,23 @@ __device__ __forceinline__ float exp2_fast(float x) {
 template <typename T>
 __device__ __forceinline__ T fresh_load(const T *x) { return *(const volatile T *)x; }
 
+// How many of x are above thr, all of them if thr is NaN: the signs of thr - x,
+// shifted into a word (a compare and an add per number cost twice as much).
+template <int N>
+__device__ __forceinline__ int count_above(const float (&x)[N], float thr) {
+  static_assert(N <= 32, "");
+  if (isnan(thr)) return N;
+  const uint64_t thr2 = f2_pack(thr, thr), minus = f2_pack(-1.f, -1.f);
+  uint32_t signs = 0;
+#pragma unroll
+  for (int e = 0; e < N; e += 2) {
+    const float2 d = f2_unpack(f2_fma(f2_pack(x[e], x[e + 1]), minus, thr2));
+    signs = __funnelshift_l(__float_as_uint(d.x), signs, 1);
+    signs = __funnelshift_l(__float_as_uint(d.y), signs, 1);
+  }
+  return __popc(signs);
+}
+
 // The sums relative to a maximum `to` that is no smaller.
 __device__ __forceinline__ void rebase(float &m, float &s1, float &s2, float to, float c) {
   const float d = m == -CUDART_INF_F ? 0.f : max_nan((m - to) * c, -1e4f), e = exp2_fast(d);
@@ -159,7 +176,7 @@ __device__ __noinline__ void write_row(const ScoreArgs &a, int64_t row, float m,
                                           int64_t t, float xt) {
   const int lane = threadIdx.x & 31;
   const bool bad = isnan(m) || m == CUDART_INF_F, empty = m == -CUDART_INF_F;
-  const float lg = log2f(s1);
+  const float lg = log2f(s1), ln_s1 = kLn2 * lg;  // differences by scale itself: c would carry a mask's value past the type
   if (lane == 0) {
     if (a.entropy) a.entropy[row] = bad ? CUDART_NAN_F : empty ? 0.f : kLn2 * (lg - s2 / s1);
     if (a.targets) {
@@ -167,14 +184,14 @@ __device__ __noinline__ void write_row(const ScoreArgs &a, int64_t row, float m,
       a.logprob[row] = t == -1          ? 0.f
                        : !has || bad    ? CUDART_NAN_F
                        : empty          ? -CUDART_INF_F
-                                        : kLn2 * ((xt - m) * a.c - lg);
+                                        : a.scale * (xt - m) - ln_s1;
       a.rank[row] = has && !isnan(m) ? count : -1;
     }
   }
   if (lane < a.top_k) {
     const float x = key_value(key);
     a.top_index[row * a.top_k + lane] = key ? key_index(key) : -1;
-    a.top_logprob[row * a.top_k + lane] = !key || empty ? -CUDART_INF_F : bad ? CUDART_NAN_F : kLn2 * ((x - m) * a.c - lg);
+    a.top_logprob[row * a.top_k + lane] = !key || empty ? -CUDART_INF_F : bad ? CUDART_NAN_F : a.scale * (x - m) - ln_s1;
   }
 }
 
@@ -413,12 +430,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_score(const __grid_con
         from = number_before(xt);
       }
       const float thr = base < t ? from : above;
-      if (partial || (t >= base && t < base + kTile)) {
+      if ((partial && isnan(thr)) || (t >= base && t < base + kTile)) {  // what is past the row's end is -inf
 #pragma unroll 1
         for (int e = 0; e < kPer; ++e) count += index(e) < a.vocab && !(fetch(e) <= (index(e) < t ? from : above));
       } else if (__any_sync(~0u, !(mx <= thr))) {  // else no logit of the tile comes before the target
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) count += !(x[e] <= thr);
+        count += count_above<kPer>(x, thr);
       }
     }
     fresh = false;
@@ -674,9 +690,7 @@ __global__ void __launch_bounds__(kFewThreads, 4) k_score_few(const __grid_const
 #pragma unroll
       for (int e = 0; e < kPer; ++e) count += index(e) < a.vocab && !(x[e] <= (index(e) < t ? from : xt));
     } else {
-      const float thr = base < t ? from : xt;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) count += !(x[e] <= thr);
+      count += count_above<kPer>(x, base < t ? from : xt);
     }
   }
 #pragma unroll
@@ -868,7 +882,7 @@ seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_r
       (uintptr_t)workspace % 16 || workspace_bytes < seedq_token_logprobs_workspace_bytes(n_rows, vocab))
     return SEEDQ_ERR_INVALID_ARG;
   ScoreArgs a{};
-  a.x = logits, a.stride = row_stride, a.rows = n_rows, a.vocab = (int32_t)vocab, a.c = scale * kLog2e;
+  a.x = logits, a.stride = row_stride, a.rows = n_rows, a.vocab = (int32_t)vocab, a.scale = scale, a.c = scale * kLog2e;
   a.targets = targets, a.logprob = logprob, a.entropy = entropy, a.rank = rank;
   a.top_k = top_k, a.top_logprob = top_logprob, a.top_index = top_index, a.workspace = workspace;
   int dev = 0, sms = 0;

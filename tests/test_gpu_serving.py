@@ -534,6 +534,45 @@ def test_score_orders_that_go_wrong(V):
     check_score(V, b, t, 0.5, 20)
 
 
+@pytest.mark.parametrize("v", [900, 3000])
+def test_score_orders_in_long_batches(V, v):
+    """The same kinds of rows where every row is a warp's work, and among thousands of others."""
+    inf, nan = float("inf"), float("nan")
+    g = torch.Generator("cuda").manual_seed(v)
+    x = torch.randn((13, v), generator=g, device="cuda")
+    x[0], x[1], x[2] = torch.arange(v, device="cuda") / 100, -torch.arange(v, device="cuda") / 100, 0
+    x[3] = -inf
+    x[4] = -inf
+    x[4, [7, v // 2, v - 1]] = torch.tensor([1.0, 2.0, 1.0], device="cuda")
+    x[5, ::3] = -inf
+    x[6, 123] = nan
+    x[7] = torch.arange(v, device="cuda") % 7
+    x[8, 77] = inf
+    x[9] *= 1e4
+    x[10] = -3.4e38
+    x[11, v - 5], x[11, 5] = nan, inf
+    x[12] = torch.finfo(torch.float32).min
+    x[12, 300:310] = 1.0
+    t = np.array([v - 1, 0, v // 3, 3, v - 1, 3, 9, v // 2 + 1, 77, 5, v - 2, 1, 305])
+    for dtype in DT.values():
+        y = x.to(dtype)
+        check_score(V, y, t, 1.0, 20)  # 13 rows
+        n = 13 * 260
+        many, tt = y.repeat(260, 1), dev(np.tile(t, 260), torch.int64)
+        f = lambda *s, d=torch.float32: torch.full(s, 5, dtype=d, device="cuda")  # noqa: E731
+        out = [[f(k), f(k), f(k, d=torch.int32), f(k, 20), f(k, 20, d=torch.int32)] for k in (13, n)]
+        V.token_logprobs(y, tt[:13], *out[0], V.score_workspace(13, v))
+        V.token_logprobs(many, tt, *out[1], V.score_workspace(n, v))
+        for a, b, name in zip(out[0], out[1], ("logprob", "entropy", "rank", "top", "index")):
+            a = a.repeat((260,) + (1,) * (a.dim() - 1))
+            if a.dtype is torch.int32:
+                assert torch.equal(a, b), name
+            else:
+                assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.isinf(), b.isinf()), name
+                ok = a.isfinite()
+                assert torch.allclose(a[ok], b[ok], rtol=2e-5, atol=2e-5), name
+
+
 def test_score_strided_unaligned_rows(V):
     for dt in DT.values():
         flat = torch.randn(6 * 1003 + 5, device="cuda").to(dt)
