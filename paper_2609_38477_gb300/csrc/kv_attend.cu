@@ -82,7 +82,11 @@ struct Shape {
   static constexpr int kValAt = kUnit * DP;
   static constexpr int kMetaAt = 2 * kUnit * DP;
   static constexpr int kStage = kMetaAt + 128;       // meta: per group both scales and a flag
-  static constexpr int kWarps = (MODE == 2 || DP == 256) ? 8 : 12;
+  // 12 warps with a ring of 2 units or 8 with 3: tiles of 4 rows, few registers, take
+  // 12 (64 requests of 2048, 32 heads on 8: 66 us, 8 warps 73); the work of 8 rows
+  // is as fast either way (64 on 8 heads: 78 us) and leaves fewer parts to join (16
+  // ragged requests up to 8192: 19 us, 12 warps 22).
+  static constexpr int kWarps = MODE == 0 && DP <= 128 ? 12 : 8;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kStages = DP == 64 ? 4 : kWarps == 12 ? 2 : 3;  // units in a warp's ring
   // units, see the split of the work list
@@ -185,10 +189,11 @@ __device__ __forceinline__ Req request(const Args &p, int b) {
   return r;
 }
 // Steps of the work list: an entry's units and kStart more, the cost of its start
-// (queries) and end, so that many short contexts weigh what they take (8 ragged
-// contexts up to 4096: 20 us without and with 1, 18, 17 and 15 with 2 to 4; 64 up
-// to 300: 23 without, 18, 18, 19 and 20 with 1 to 4).
+// (queries) and end, so that many short contexts weigh what they take (16 ragged
+// contexts up to 8192: 26 us without, 20, 19 and 20 with 2 to 4; 64 up to 300: 23
+// without, 18 with 2 to 4).
 constexpr int kStart = 3;
+constexpr int kOver = 24;
 __device__ __forceinline__ int64_t steps_of(const Args &p, const Req &r) {
   return r.fresh ? (int64_t)(r.units + kStart) * r.tiles * p.c.n_kv_heads : 0;
 }
@@ -445,14 +450,15 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
   }
   // Even shares of steps for the CTAs' warps, at least one each.  Little work goes
   // to 4 warps per CTA, one per scheduler, and so to more SMs (one request of 1000:
-  // 12 us, with 12 warps 15).  Entries of one length (one request, or a batch in
+  // 12 us, with all warps 15).  Entries of one length (one request, or a batch in
   // step) are each cut for the same number of CTAs, so that no CTA has parts of two
-  // (one request of 4096: 15 us, else 17).  Else, where no entry is longer than a
-  // few units per warp, the shares' ends move to the nearest entry's: a join
-  // between CTAs costs about as much as the uneven shares (16 requests of 2048, 64
-  // heads on 8: 28 us, without 30; with entries of up to 16 units per warp 8 of
-  // 4096 take 34 us instead of 18); likewise between warps where no entry is longer
-  // than kWholeWarp (200 requests of 100: 23 us, else 31).
+  // (one request of 4096: 14 us, else 16).  Else, where no entry is longer than a
+  // few units per warp and than a share by kOver, the shares' ends move to the
+  // nearest entry's: a join between CTAs costs 3 to 4 us (40 ragged requests up to
+  // 1000, 32 heads on 8: 19 us, without 22; 100: 26 and 30; but 16 up to 2048, whose
+  // longest entry is twice a share, 22 with and 18 without; 256 up to 4096, 82 and
+  // 78).  Likewise between warps where no entry is longer than kWholeWarp (200
+  // requests up to 100: 19 us, else 25).
   const bool little = total <= (int64_t)p.ctas * 8;
   const int warps = little ? 4 : S::kWarps;
   const int64_t share = max((int64_t)__umul64hi((uint64_t)total, p.ctas_inv) + 1, (int64_t)warps);
@@ -478,7 +484,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
   } else {
     c0 = min(share * blockIdx.x, total), c1 = min(c0 + share, total);
     if (c0 >= total) return;
-    if (most <= (little ? S::kWholeLittle : S::kWhole)) {
+    if (little ? most <= S::kWholeLittle : most <= S::kWhole && most + kStart <= share + kOver) {
       const int64_t c = nearest(lane ? c1 : c0);
       c0 = __shfl_sync(~0u, c, 0);
       c1 = __shfl_sync(~0u, c, 1);
@@ -1100,8 +1106,10 @@ struct Plan {
   int dp, mode, rows;
 };
 // Tiles of 4 rows where they hold all rows that share a head's keys (a decode
-// step of up to 4 query heads per key-value head: half the products of 8 rows),
-// else of 8, and of 16 where more than 8 rows would read the keys again; 256
+// step of up to 4 query heads per key-value head, half the products of 8 rows:
+// 66 us for 64 requests of 2048, 32 heads on 8, else 78), else of 8 (5 to 8 rows in
+// tiles of 16: 113 us instead of 78), and of 16 where more than 8 rows would read
+// the keys again (16 tokens of 32 heads on 8 over 32768 keys: 90 us, else 109); 256
 // head dims leave no registers for 16.
 Plan shape_for(const seedq_kv_cache *c, int32_t n_heads, int32_t max_new) {
   Plan s;
