@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "cp_async.cuh"
+#include "f32x2.cuh"
 #include "serve.cuh"
 
 namespace seedq {
@@ -13,7 +15,7 @@ struct CacheArgs {
   void *x[2];          // the tokens' keys and values
   int64_t ts, hs, n;   // their strides (elements) and number
   const int64_t *slots;
-  int32_t vec;         // rows of x allow 16-byte accesses
+  int32_t vec;         // 2 or 1 where rows of x allow accesses of 32 or 16 bytes, else 0
   int32_t group_shift; // append: log2 of the tokens of a CTA
   int32_t page_shift;  // log2 of the page size, -1 if it is no power of two
 };
@@ -51,36 +53,58 @@ struct Eight {
     if (DT == SEEDQ_BF16) return __uint_as_float(h << 16);
     return __half2float(__ushort_as_half((unsigned short)h));
   }
-  __device__ __forceinline__ void store(void *p, int64_t i, const float (&v)[8], bool vec) const {
-    uint32_t y[kWords];
+  __device__ __forceinline__ uint64_t pair(int k) const {  // elements 2k and 2k + 1
+    if (DT == SEEDQ_F16) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[k % kWords]));
+      return f2_pack(f.x, f.y);
+    }
+    return f2_pack(get(2 * k), get(2 * k + 1));
+  }
+  // Largest magnitudes so far, in the type itself; a NaN stays.
+  __device__ __forceinline__ void largest(uint32_t &m) const {
 #pragma unroll
     for (int k = 0; k < kWords; ++k) {
-      if (DT == SEEDQ_F32) {
-        y[k] = __float_as_uint(v[k]);
-      } else if (DT == SEEDQ_BF16) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k % 8], v[(2 * k + 1) % 8]);
-        y[k] = *(const uint32_t *)&h;
-      } else {
-        const __half2 h = __floats2half2_rn(v[2 * k % 8], v[(2 * k + 1) % 8]);
-        y[k] = *(const uint32_t *)&h;
-      }
-    }
-    if (vec) {
-      uint4 *dst = (uint4 *)((char *)p + i * (DT == SEEDQ_F32 ? 4 : 2));
-#pragma unroll
-      for (int k = 0; k < kWords / 4; ++k) dst[k] = make_uint4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
-    } else if (DT == SEEDQ_F32) {
-#pragma unroll
-      for (int k = 0; k < kWords; ++k) ((uint32_t *)p)[i + k] = y[k];
-    } else {
-#pragma unroll
-      for (int k = 0; k < kWords; ++k) {
-        ((uint16_t *)p)[i + 2 * k] = (uint16_t)y[k];
-        ((uint16_t *)p)[i + 2 * k + 1] = (uint16_t)(y[k] >> 16);
-      }
+      if (DT == SEEDQ_F32) m = max(m, w[k] & 0x7fffffffu);
+      else m = __vmaxu2(m, w[k] & 0x7fff7fffu);
     }
   }
+  static __device__ __forceinline__ uint32_t largest_bits(uint32_t m) {  // as the bits of a float
+    if (DT == SEEDQ_F32) return m;
+    const uint32_t x = max(m & 0xffffu, m >> 16);
+    return DT == SEEDQ_BF16 ? x << 16 : __float_as_uint(__half2float(__ushort_as_half((unsigned short)x)));
+  }
 };
+
+// Four codes of x times a power of two, where no product is past the largest code.
+// int8: 1.5 * 2^23 has unit 1, so adding it rounds to an integer in the low bits.
+template <int KIND>
+__device__ __forceinline__ uint32_t four_codes(uint64_t x01, uint64_t x23, uint64_t by2) {
+  if (KIND == SEEDQ_KV_INT8) {
+    const uint64_t one = f2_pack(12582912.f, 12582912.f);
+    const float2 a = f2_unpack(f2_fma(x01, by2, one)), b = f2_unpack(f2_fma(x23, by2, one));
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
+                       __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+  }
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(f2_unpack(f2_mul(x01, by2)), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(f2_unpack(f2_mul(x23, by2)), __NV_SATFINITE, __NV_E4M3);
+  return lo | hi << 16;
+}
+// The numbers of four codes, in pairs.  int8: byte + 128 in the low bits of 2^23.
+template <int KIND>
+__device__ __forceinline__ void four_values(uint32_t w, uint64_t &x01, uint64_t &x23) {
+  if (KIND == SEEDQ_KV_INT8) {
+    const uint32_t y = w ^ 0x80808080u;
+    const uint64_t off = f2_pack(-8388736.f, -8388736.f);
+    auto wide = [&](int sel) { return __uint_as_float(__byte_perm(y, 0x4b000000u, sel)); };
+    x01 = f2_add(f2_pack(wide(0x7440), wide(0x7441)), off);
+    x23 = f2_add(f2_pack(wide(0x7442), wide(0x7443)), off);
+  } else {
+    const uint32_t lo = e4m3x2_to_half2(w), hi = e4m3x2_to_half2(w >> 16);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&lo));
+    const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
+    x01 = f2_pack(a.x, a.y), x23 = f2_pack(b.x, b.y);
+  }
+}
 
 // ---------------------------------------------------------------- append
 //
@@ -94,13 +118,16 @@ struct Eight {
 // again, from cache.
 constexpr int kAppendWarps = 4;
 constexpr int kAppendBlocks = 7;  // per SM: 28 warps of up to 73 registers
+constexpr int kKeptPieces = 14;   // of a lane in shared memory: 7 KB per warp
 
 template <int KIND, int DT>
 __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(const __grid_constant__ CacheArgs a) {
-  constexpr int kHeld = DT == SEEDQ_F32 ? 4 : 8;
-  const int lane = threadIdx.x & 31;
+  constexpr int kHeld = DT == SEEDQ_F32 ? 1 : 2, kPieces = DT == SEEDQ_F32 ? 2 : 1;  // 16-byte pieces of a lane and step
+  constexpr int kKept = kKeptPieces / kPieces;
+  __shared__ uint4 s_kept[kAppendWarps][kKeptPieces][32];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int P = a.c.page_size, D = a.c.head_dim, per = D / 8;  // pieces of a token
-  int64_t id = (int64_t)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
+  int64_t id = (int64_t)blockIdx.x * kAppendWarps + w;
   const int pair = (int)(id % (2 * a.c.n_kv_heads)), h = pair >> 1, which = pair & 1;
   const int64_t g0 = id / (2 * a.c.n_kv_heads) << a.group_shift;
   const int64_t g1 = min(g0 + (1 << a.group_shift), a.n);
@@ -141,22 +168,42 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(
       const int mine = idle ? 0 : m;
       Eight<DT> held[kHeld];
       uint32_t amax = 0;
+      const int kept = a.vec ? kKept : 0;
+      if (kHeld * step < m)
+        for (int k = 0; k < kept; ++k) {
+          const int t = t_first + (kHeld + k) * step;
+          if (t < mine)
+#pragma unroll
+            for (int y = 0; y < kPieces; ++y)
+              cp_async16(&s_kept[w][k * kPieces + y][lane],
+                         (const char *)x + (at + t * a.ts) * (kPieces * 2) + 16 * y);
+        }
+      auto from_kept = [&](int k) {
+        Eight<DT> e;
+#pragma unroll
+        for (int y = 0; y < kPieces; ++y) {
+          const uint4 v = s_kept[w][k * kPieces + y][lane];
+          e.w[4 * y] = v.x, e.w[4 * y + 1] = v.y, e.w[4 * y + 2] = v.z, e.w[4 * y + 3] = v.w;
+        }
+        return e;
+      };
 #pragma unroll
       for (int k = 0; k < kHeld; ++k)
         if (t_first + k * step < mine) held[k].load(x, at + (t_first + k * step) * a.ts, a.vec);
 #pragma unroll
       for (int k = 0; k < kHeld; ++k)
-        if (t_first + k * step < mine)
-#pragma unroll
-          for (int y = 0; y < 8; ++y) amax = max(amax, __float_as_uint(held[k].get(y)) & 0x7fffffffu);
+        if (t_first + k * step < mine) held[k].largest(amax);
 #pragma unroll 4
-      for (int t = t_first + kHeld * step; t < mine; t += step) {
+      for (int t = t_first + (kHeld + kept) * step; t < mine; t += step) {
         Eight<DT> e;
         e.load(x, at + t * a.ts, a.vec);
-#pragma unroll
-        for (int y = 0; y < 8; ++y) amax = max(amax, __float_as_uint(e.get(y)) & 0x7fffffffu);
+        e.largest(amax);
       }
-      const float want = block_scale<KIND>(__reduce_max_sync(~0u, amax));
+      cp_async_commit();
+      cp_async_wait<0>();
+#pragma unroll 2
+      for (int k = 0; k < kept && t_first + (kHeld + k) * step < mine; ++k) from_kept(k).largest(amax);
+      const float want = block_scale<KIND>(__reduce_max_sync(~0u, Eight<DT>::largest_bits(amax)));
       float now = want;
       if (off > 0 && !(want > old) && !isnan(want)) now = old;  // a NaN scale stays
       if (off > 0 && now > old) {
@@ -177,11 +224,12 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(
       const uint32_t nb = __float_as_uint(now);
       const bool exact = (nb & 0x7fffffu) == 0 && nb < 0x7f000000u && nb != 0;
       const float inv = exact ? __uint_as_float(0x7f000000u - nb) : 0.f;
+      const uint64_t inv2 = f2_pack(inv, inv);
       auto write = [&](const Eight<DT> &e, int t) {
         uint32_t z[2] = {0, 0};
         if (exact) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) z[k / 4] |= value_code<KIND>(e.get(k) * inv) << 8 * (k & 3);
+          z[0] = four_codes<KIND>(e.pair(0), e.pair(1), inv2);
+          z[1] = four_codes<KIND>(e.pair(2), e.pair(3), inv2);
         } else if (now > 0.f) {
 #pragma unroll 1
           for (int k = 0; k < 8; ++k) {
@@ -196,7 +244,9 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(
       for (int k = 0; k < kHeld; ++k)
         if (t_first + k * step < mine) write(held[k], t_first + k * step);
 #pragma unroll 2
-      for (int t = t_first + kHeld * step; t < mine; t += step) {
+      for (int k = 0; k < kept && t_first + (kHeld + k) * step < mine; ++k) write(from_kept(k), t_first + (kHeld + k) * step);
+#pragma unroll 4
+      for (int t = t_first + (kHeld + kept) * step; t < mine; t += step) {
         Eight<DT> e;
         e.load(x, at + t * a.ts, a.vec);
         write(e, t);
@@ -212,43 +262,86 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(
 
 // ---------------------------------------------------------------- gather
 //
-// A thread takes 16 codes of a key and of a value; bytes bound it.
-template <int KIND, int DT>
+// A thread takes as many codes of a key and of a value as make BYTES bytes of the
+// output; bytes bound it.
+constexpr int64_t kGatherSmall = 152 * 2048;
+
+template <int KIND, int DT, int BYTES>
 __global__ void __launch_bounds__(256) k_kv_gather(const __grid_constant__ CacheArgs a) {
-  const int P = a.c.page_size, per = a.c.head_dim / 16;
+  constexpr int kWidth = DT == SEEDQ_F32 ? 4 : 2, kCodes = BYTES / kWidth, kWords = BYTES / 4;
+  const int P = a.c.page_size, per = a.c.head_dim / kCodes;
   const int row = a.c.n_kv_heads * per;  // threads of a token
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int64_t t = i >> 32 ? i / row : (int64_t)((uint32_t)i / (uint32_t)row);
   if (t >= a.n) return;
-  const int r = (int)(i - t * row), h = r / per, d = (r - h * per) * 16;
+  const int r = (int)(i - t * row), h = r / per, d = (r - h * per) * kCodes;
   const int64_t slot = a.slots[t];
   const int64_t page = page_of(a, slot);
-  uint4 code[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  uint32_t code[2][kCodes / 4] = {};
   float scale[2] = {0.f, 0.f};
   if (page >= 0 && page < a.c.n_pages) {
     const int64_t at = page * a.c.page_stride + h * a.c.head_stride + (slot - page * P) * a.c.token_stride + d;
     const int64_t s = page * a.c.n_kv_heads + h;
-    code[0] = *(const uint4 *)((const uint8_t *)a.c.k + at);
-    code[1] = *(const uint4 *)((const uint8_t *)a.c.v + at);
-    scale[0] = a.c.k_scale[s];
-    scale[1] = a.c.v_scale[s];
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const uint8_t *src = (const uint8_t *)(which ? a.c.v : a.c.k) + at;
+      if constexpr (kCodes == 16) {
+        const uint4 v = *(const uint4 *)src;
+        code[which][0] = v.x, code[which][1] = v.y, code[which][2] = v.z, code[which][3] = v.w;
+      } else if constexpr (kCodes == 8) {
+        const uint2 v = *(const uint2 *)src;
+        code[which][0] = v.x, code[which][1] = v.y;
+      } else {
+        code[which][0] = *(const uint32_t *)src;
+      }
+      scale[which] = (which ? a.c.v_scale : a.c.k_scale)[s];
+    }
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
-    const uint32_t w[4] = {code[which].x, code[which].y, code[which].z, code[which].w};
+    const uint64_t by = f2_pack(scale[which], scale[which]);
+    uint32_t y[kWords];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      float v[8];
+    for (int k = 0; k < kCodes / 2; ++k) {
+      uint64_t x[2];
+      four_values<KIND>(code[which][k / 2], x[0], x[1]);
+      const float2 f = f2_unpack(f2_mul(x[k & 1], by));
+      if (DT == SEEDQ_F32) {
+        y[2 * k % kWords] = __float_as_uint(f.x), y[(2 * k + 1) % kWords] = __float_as_uint(f.y);
+      } else if (DT == SEEDQ_BF16) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+        y[k] = *(const uint32_t *)&b;
+      } else {
+        const __half2 b = __floats2half2_rn(f.x, f.y);
+        y[k] = *(const uint32_t *)&b;
+      }
+    }
+    char *to = (char *)a.x[which] + (t * a.ts + h * a.hs + d) * kWidth;
+    if (BYTES == 32 && a.vec == 2) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(y[0]), "r"(y[1]), "r"(y[2]),
+                   "r"(y[3]), "r"(y[4 % kWords]), "r"(y[5 % kWords]), "r"(y[6 % kWords]), "r"(y[7 % kWords])
+                   : "memory");
+    } else if (a.vec) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = code_value<KIND>(w[half * 2 + k / 4] >> 8 * (k & 3) & 0xffu) * scale[which];
-      Eight<DT>().store(a.x[which], t * a.ts + h * a.hs + d + half * 8, v, a.vec);
+      for (int k = 0; k < kWords; k += 4) *(uint4 *)(to + 4 * k) = make_uint4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) {
+        if (DT == SEEDQ_F32) {
+          ((uint32_t *)to)[k] = y[k];
+        } else {
+          ((uint16_t *)to)[2 * k] = (uint16_t)y[k];
+          ((uint16_t *)to)[2 * k + 1] = (uint16_t)(y[k] >> 16);
+        }
+      }
     }
   }
 }
 
-bool rows_aligned(const void *k, const void *v, int32_t dtype, int64_t ts, int64_t hs) {
-  const int64_t per = 16 / dtype_bytes(dtype);
-  return ((uintptr_t)k | (uintptr_t)v) % 16 == 0 && ts % per == 0 && hs % per == 0;
+// 2 or 1 where rows allow accesses of 32 or 16 bytes, else 0
+int32_t rows_aligned(const void *k, const void *v, int32_t dtype, int64_t ts, int64_t hs) {
+  const uint64_t all = (uint64_t)(uintptr_t)k | (uint64_t)(uintptr_t)v | (uint64_t)(ts * dtype_bytes(dtype)) | (uint64_t)(hs * dtype_bytes(dtype));
+  return all % 32 == 0 ? 2 : all % 16 == 0;
 }
 
 template <int KIND, int DT>
@@ -258,8 +351,9 @@ void launch_append(const CacheArgs &a, cudaStream_t st) {
 }
 template <int KIND, int DT>
 void launch_gather(const CacheArgs &a, cudaStream_t st) {
-  const int64_t threads = a.n * a.c.n_kv_heads * (a.c.head_dim / 16);
-  k_kv_gather<KIND, DT><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(a);
+  const int64_t pieces = a.n * a.c.n_kv_heads * a.c.head_dim / (DT == SEEDQ_F32 ? 4 : 8);
+  if (pieces <= kGatherSmall) k_kv_gather<KIND, DT, 16><<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(a);
+  else k_kv_gather<KIND, DT, 32><<<(unsigned)((pieces / 2 + 255) / 256), 256, 0, st>>>(a);
 }
 using Launch = void (*)(const CacheArgs &, cudaStream_t);
 constexpr Launch kAppend[2][3] = {
