@@ -75,13 +75,13 @@ struct Eight {
   }
 };
 
-// Four codes of x times a power of two, where no product is past the largest code.
+// Four codes of the products x times a number, where none is past the largest code.
 // int8: 1.5 * 2^23 has unit 1, so adding it rounds to an integer in the low bits.
 template <int KIND>
 __device__ __forceinline__ uint32_t four_codes(uint64_t x01, uint64_t x23, uint64_t by2) {
   if (KIND == SEEDQ_KV_INT8) {
     const uint64_t one = f2_pack(12582912.f, 12582912.f);
-    const float2 a = f2_unpack(f2_fma(x01, by2, one)), b = f2_unpack(f2_fma(x23, by2, one));
+    const float2 a = f2_unpack(f2_add(f2_mul(x01, by2), one)), b = f2_unpack(f2_add(f2_mul(x23, by2), one));
     return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
                        __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
   }
@@ -108,30 +108,43 @@ __device__ __forceinline__ void four_values(uint32_t w, uint64_t &x01, uint64_t 
 
 // ---------------------------------------------------------------- append
 //
-// A page's tokens are read, their largest magnitude is found over a warp, and
-// the codes are written.  Bytes bound it for prompts, latency for a decode step
-// (slots, then scale and tokens, then codes), so the work is cut for many warps
-// and no barrier: a warp owns one head and tensor of the stretches of tokens on
-// one page that begin among 2^group_shift tokens.  A lane takes 8 elements of a
-// token; the first kHeld steps of the warp stay in registers between the maximum
-// and the codes (16 tokens of 128 head dims, 8 in float32), longer runs are read
+// A page's tokens are read, their largest magnitude is found, and the codes are
+// written.  Bytes bound it for prompts, latency for a decode step (slots, then
+// scale and tokens, then codes), so the work is cut for many warps: a warp owns
+// one head and tensor of the stretches of tokens on one page that begin among
+// 2^group_shift tokens.  A lane takes 8 elements of a token; the first kHeld
+// steps of a run stay in its registers between the maximum and the codes, the
+// next ones in shared memory, where asynchronous copies put them (30 tokens of
+// 128 head dims, 16 in float32).  A run that is longer than that the CTA's warps,
+// which own pairs of the same tokens, take together, one pair after the other,
+// so that it too is read once (4 prompts of 1024, pages of 64, 32 heads: 24 us
+// instead of 28; pages of 128: 30 instead of 49); what is longer still is read
 // again, from cache.
+//
+// Measured, 128 head dims: 4 prompts of 1024 tokens, 32 heads, bfloat16, 24 us
+// (4.2 TB/s, 62% of the copy rate; float32 45 us, 3.7 TB/s); 16 single tokens of
+// 8 heads 3.4 us, launch and three dependent reads.  28 warps per SM: 24, with
+// more registers, take 28 and, for 256 single tokens of 32 heads, 12 us instead
+// of 10; 32 take 24 and 10.
 constexpr int kAppendWarps = 4;
 constexpr int kAppendBlocks = 7;  // per SM: 28 warps of up to 73 registers
 constexpr int kKeptPieces = 14;   // of a lane in shared memory: 7 KB per warp
 
 template <int KIND, int DT>
 __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(const __grid_constant__ CacheArgs a) {
-  constexpr int kHeld = DT == SEEDQ_F32 ? 1 : 2, kPieces = DT == SEEDQ_F32 ? 2 : 1;  // 16-byte pieces of a lane and step
+  constexpr int kHeld = 1, kPieces = DT == SEEDQ_F32 ? 2 : 1;  // 16-byte pieces of a lane and step
   constexpr int kKept = kKeptPieces / kPieces;
   __shared__ uint4 s_kept[kAppendWarps][kKeptPieces][32];
+  __shared__ uint32_t s_max[kAppendWarps][kAppendWarps];  // of a pair, by warp
+  __shared__ float s_old[kAppendWarps];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int P = a.c.page_size, D = a.c.head_dim, per = D / 8;  // pieces of a token
-  int64_t id = (int64_t)blockIdx.x * kAppendWarps + w;
-  const int pair = (int)(id % (2 * a.c.n_kv_heads)), h = pair >> 1, which = pair & 1;
-  const int64_t g0 = id / (2 * a.c.n_kv_heads) << a.group_shift;
+  const int pairs = 2 * a.c.n_kv_heads, ctas = (pairs + kAppendWarps - 1) / kAppendWarps;
+  const int64_t group = blockIdx.x / (uint32_t)ctas;
+  const int pair0 = (int)(blockIdx.x - (uint32_t)group * ctas) * kAppendWarps;  // the CTA's first
+  const bool owner = pair0 + w < pairs;
+  const int64_t g0 = group << a.group_shift;
   const int64_t g1 = min(g0 + (1 << a.group_shift), a.n);
-  if (g0 >= a.n) return;
   // Stretches begin where the page differs from the token's before: a lane per token.
   uint32_t starts;
   {
@@ -141,7 +154,6 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(
     if (lane == 0) before = g0 > 0 ? page_of(a, a.slots[g0 - 1]) : -1;
     starts = __ballot_sync(~0u, page >= 0 && page < a.c.n_pages && page != before);
   }
-  const void *x = a.x[which];
   const int step = 32 / per, t_first = lane / per, d = (lane - t_first * per) * 8;  // tokens of a step; the lane's piece
   const bool idle = t_first >= step;
   const int64_t ts = a.c.token_stride;
@@ -150,9 +162,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(
     int64_t t0 = g0 + __ffs(starts) - 1;
     int64_t slot = a.slots[t0];
     const int64_t page = page_of(a, slot);
-    float *scale = (which ? a.c.v_scale : a.c.k_scale) + page * a.c.n_kv_heads + h;
-    uint8_t *code = (uint8_t *)(which ? a.c.v : a.c.k) + page * a.c.page_stride + h * a.c.head_stride + d;
-    float old = *scale;
+    float *scale = ((pair0 + w) & 1 ? a.c.v_scale : a.c.k_scale) + page * a.c.n_kv_heads + (pair0 + w) / 2;
+    float old = owner ? *scale : 0.f;
     do {  // runs of consecutive slots on the page
       const int off = (int)(slot - page * P);
       // the run's length: up to the first of the next tokens whose slot does not follow, found 32 at a time
@@ -164,106 +175,126 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(
         m += stop ? __ffs(stop) - 1 : 32;
         if (stop) break;
       }
-      const int64_t at = t0 * a.ts + h * a.hs + d;
+      const bool together = m > (kHeld + kKept) * step;  // the same in all warps
+      const int nw = together ? kAppendWarps : 1;
+      const int first = t_first + (together ? w : 0) * step, stride = nw * step;  // the lane's tokens
       const int mine = idle ? 0 : m;
-      Eight<DT> held[kHeld];
-      uint32_t amax = 0;
-      const int kept = a.vec ? kKept : 0;
-      if (kHeld * step < m)
-        for (int k = 0; k < kept; ++k) {
-          const int t = t_first + (kHeld + k) * step;
-          if (t < mine)
+      for (int p = together ? 0 : w; p < (together ? kAppendWarps : w + 1) && pair0 + p < pairs; ++p) {
+        const int h = (pair0 + p) >> 1, which = p & 1;
+        const void *x = a.x[which];
+        uint8_t *code = (uint8_t *)(which ? a.c.v : a.c.k) + page * a.c.page_stride + h * a.c.head_stride + d;
+        const int64_t at = t0 * a.ts + h * a.hs + d;
+        Eight<DT> held[kHeld];
+        uint32_t amax = 0;
+        const int kept = a.vec ? kKept : 0;
+        if (kHeld * stride < m)
+          for (int k = 0; k < kept; ++k) {
+            const int t = first + (kHeld + k) * stride;
+            if (t < mine)
 #pragma unroll
-            for (int y = 0; y < kPieces; ++y)
-              cp_async16(&s_kept[w][k * kPieces + y][lane],
-                         (const char *)x + (at + t * a.ts) * (kPieces * 2) + 16 * y);
-        }
-      auto from_kept = [&](int k) {
-        Eight<DT> e;
+              for (int y = 0; y < kPieces; ++y)
+                cp_async16(&s_kept[w][k * kPieces + y][lane], (const char *)x + (at + t * a.ts) * (kPieces * 2) + 16 * y);
+          }
+        auto from_kept = [&](int k) {
+          Eight<DT> e;
 #pragma unroll
-        for (int y = 0; y < kPieces; ++y) {
-          const uint4 v = s_kept[w][k * kPieces + y][lane];
-          e.w[4 * y] = v.x, e.w[4 * y + 1] = v.y, e.w[4 * y + 2] = v.z, e.w[4 * y + 3] = v.w;
-        }
-        return e;
-      };
+          for (int y = 0; y < kPieces; ++y) {
+            const uint4 v = s_kept[w][k * kPieces + y][lane];
+            e.w[4 * y] = v.x, e.w[4 * y + 1] = v.y, e.w[4 * y + 2] = v.z, e.w[4 * y + 3] = v.w;
+          }
+          return e;
+        };
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k)
-        if (t_first + k * step < mine) held[k].load(x, at + (t_first + k * step) * a.ts, a.vec);
+        for (int k = 0; k < kHeld; ++k)
+          if (first + k * stride < mine) held[k].load(x, at + (first + k * stride) * a.ts, a.vec);
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k)
-        if (t_first + k * step < mine) held[k].largest(amax);
-#pragma unroll 4
-      for (int t = t_first + (kHeld + kept) * step; t < mine; t += step) {
-        Eight<DT> e;
-        e.load(x, at + t * a.ts, a.vec);
-        e.largest(amax);
-      }
-      cp_async_commit();
-      cp_async_wait<0>();
+        for (int k = 0; k < kHeld; ++k)
+          if (first + k * stride < mine) held[k].largest(amax);
 #pragma unroll 2
-      for (int k = 0; k < kept && t_first + (kHeld + k) * step < mine; ++k) from_kept(k).largest(amax);
-      const float want = block_scale<KIND>(__reduce_max_sync(~0u, Eight<DT>::largest_bits(amax)));
-      float now = want;
-      if (off > 0 && !(want > old) && !isnan(want)) now = old;  // a NaN scale stays
-      if (off > 0 && now > old) {
-        const float r = __fdiv_rn(old, now);
-#pragma unroll 4
-        for (int t = t_first; t < (idle ? 0 : off); t += step) {
-          uint2 *p = (uint2 *)(code + t * ts);
-          const uint2 v = *p;
-          const uint32_t y[2] = {v.x, v.y};
-          uint32_t z[2] = {0, 0};
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            z[k / 4] |= value_code<KIND>(code_value<KIND>(y[k / 4] >> 8 * (k & 3) & 0xffu) * r) << 8 * (k & 3);
-          *p = make_uint2(z[0], z[1]);
+        for (int t = first + (kHeld + kept) * stride; t < mine; t += stride) {
+          Eight<DT> e;
+          e.load(x, at + t * a.ts, a.vec);
+          e.largest(amax);
         }
-      }
-      // x / now; by the reciprocal where that is exact: now a power of two whose reciprocal is a normal number
-      const uint32_t nb = __float_as_uint(now);
-      const bool exact = (nb & 0x7fffffu) == 0 && nb < 0x7f000000u && nb != 0;
-      const float inv = exact ? __uint_as_float(0x7f000000u - nb) : 0.f;
-      const uint64_t inv2 = f2_pack(inv, inv);
-      auto write = [&](const Eight<DT> &e, int t) {
-        uint32_t z[2] = {0, 0};
-        if (exact) {
-          z[0] = four_codes<KIND>(e.pair(0), e.pair(1), inv2);
-          z[1] = four_codes<KIND>(e.pair(2), e.pair(3), inv2);
-        } else if (now > 0.f) {
-#pragma unroll 1
-          for (int k = 0; k < 8; ++k) {
-            const uint32_t c = value_code<KIND>(__fdiv_rn(load_elem(x, DT, at + t * a.ts + k), now)) << 8 * (k & 3);
-            if (k < 4) z[0] |= c;
-            else z[1] |= c;
+        cp_async_commit();
+        cp_async_wait<0>();
+#pragma unroll 2
+        for (int k = 0; k < kept && first + (kHeld + k) * stride < mine; ++k) from_kept(k).largest(amax);
+        amax = __reduce_max_sync(~0u, Eight<DT>::largest_bits(amax));
+        float was = old;
+        if (together) {  // what is written here was last read before another pair's barrier
+          if (lane == 0) s_max[p][w] = amax;
+          if (lane == 0 && p == w) s_old[w] = old;
+          __syncthreads();
+#pragma unroll
+          for (int k = 0; k < kAppendWarps; ++k) amax = max(amax, s_max[p][k]);
+          was = s_old[p];
+        }
+        const float want = block_scale<KIND>(amax);
+        float now = want;
+        if (off > 0 && !(want > was) && !isnan(want)) now = was;  // a NaN scale stays
+        if (off > 0 && now > was) {
+          const float r = __fdiv_rn(was, now);
+          const uint64_t r2 = f2_pack(r, r);
+#pragma unroll 2
+          for (int t = first; t < (idle ? 0 : off); t += stride) {
+            uint2 *q = (uint2 *)(code + t * ts);
+            const uint2 v = *q;
+            uint64_t x0, x1, x2, x3;
+            four_values<KIND>(v.x, x0, x1);
+            four_values<KIND>(v.y, x2, x3);
+            *q = make_uint2(four_codes<KIND>(x0, x1, r2), four_codes<KIND>(x2, x3, r2));
           }
         }
-        *(uint2 *)(code + (off + t) * ts) = make_uint2(z[0], z[1]);
-      };
+        // x / now; by the reciprocal where that is exact: now a power of two whose reciprocal is a normal number
+        const uint32_t nb = __float_as_uint(now);
+        const bool exact = (nb & 0x7fffffu) == 0 && nb < 0x7f000000u && nb != 0;
+        const float inv = exact ? __uint_as_float(0x7f000000u - nb) : 0.f;
+        const uint64_t inv2 = f2_pack(inv, inv);
+        auto write = [&](const Eight<DT> &e, int t) {
+          uint32_t z[2] = {0, 0};
+          if (exact) {
+            z[0] = four_codes<KIND>(e.pair(0), e.pair(1), inv2);
+            z[1] = four_codes<KIND>(e.pair(2), e.pair(3), inv2);
+          } else if (now > 0.f) {
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t c = value_code<KIND>(__fdiv_rn(load_elem(x, DT, at + t * a.ts + k), now)) << 8 * (k & 3);
+              if (k < 4) z[0] |= c;
+              else z[1] |= c;
+            }
+          }
+          *(uint2 *)(code + (off + t) * ts) = make_uint2(z[0], z[1]);
+        };
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k)
-        if (t_first + k * step < mine) write(held[k], t_first + k * step);
+        for (int k = 0; k < kHeld; ++k)
+          if (first + k * stride < mine) write(held[k], first + k * stride);
 #pragma unroll 2
-      for (int k = 0; k < kept && t_first + (kHeld + k) * step < mine; ++k) write(from_kept(k), t_first + (kHeld + k) * step);
-#pragma unroll 4
-      for (int t = t_first + (kHeld + kept) * step; t < mine; t += step) {
-        Eight<DT> e;
-        e.load(x, at + t * a.ts, a.vec);
-        write(e, t);
+        for (int k = 0; k < kept && first + (kHeld + k) * stride < mine; ++k) write(from_kept(k), first + (kHeld + k) * stride);
+#pragma unroll 2
+        for (int t = first + (kHeld + kept) * stride; t < mine; t += stride) {
+          Eight<DT> e;
+          e.load(x, at + t * a.ts, a.vec);
+          write(e, t);
+        }
+        if (p == w) old = now;
       }
-      old = now;
       t0 += m;
       slot = t0 < a.n ? a.slots[t0] : -1;
-      __syncwarp();
+      if (together) __syncthreads();  // the page's next run is perhaps a warp's alone
+      else __syncwarp();
     } while (page_of(a, slot) == page);
-    if (lane == 0) *scale = old;
+    if (owner && lane == 0) *scale = old;
   }
 }
 
 // ---------------------------------------------------------------- gather
 //
 // A thread takes as many codes of a key and of a value as make BYTES bytes of the
-// output; bytes bound it.
+// output; bytes bound it.  32 bytes are one store where rows begin at multiples of
+// 32 (4096 tokens of 32 heads, 128 head dims: 18 us, 5.5 TB/s, 81% of the copy
+// rate, float32 28 us; with stores of 16 bytes 20 and 35), 16 bytes make twice
+// the threads of a small call (217 tokens of 4 heads of 64: 2.3 us, else 2.5).
 constexpr int64_t kGatherSmall = 152 * 2048;
 
 template <int KIND, int DT, int BYTES>
@@ -346,8 +377,9 @@ int32_t rows_aligned(const void *k, const void *v, int32_t dtype, int64_t ts, in
 
 template <int KIND, int DT>
 void launch_append(const CacheArgs &a, cudaStream_t st) {
-  const int64_t warps = ((a.n + (1 << a.group_shift) - 1) >> a.group_shift) * a.c.n_kv_heads * 2;
-  k_kv_append<KIND, DT><<<(unsigned)((warps + kAppendWarps - 1) / kAppendWarps), kAppendWarps * 32, 0, st>>>(a);
+  const int64_t groups = (a.n + (1 << a.group_shift) - 1) >> a.group_shift;
+  const int ctas = (a.c.n_kv_heads * 2 + kAppendWarps - 1) / kAppendWarps;
+  k_kv_append<KIND, DT><<<(unsigned)(groups * ctas), kAppendWarps * 32, 0, st>>>(a);
 }
 template <int KIND, int DT>
 void launch_gather(const CacheArgs &a, cudaStream_t st) {
@@ -386,9 +418,10 @@ seedq_status seedq_kv_append(const seedq_kv_cache *cache, const void *k, const v
   const seedq_status st = prepare(cache, k, v, dtype, token_stride, head_stride, slots, n_tokens, a);
   if (st != SEEDQ_OK || n_tokens == 0) return st;
   // One token per warp until the warps fill the GPU twice over, then more.  Each may
-  // be a page of its own (32 heads, 256 single tokens: 13 us, 14 with one token per
-  // warp, 17 at half the threshold, 57 with 32 tokens), or all on a page (4 prompts
-  // of 1024, pages of 64: 39 us, with one token per warp 100).
+  // be a page of its own (32 heads, 256 single tokens: 10 us; measured before the
+  // shared memory, 13, and 14 with one token per warp, 17 at half the threshold, 57
+  // with 32), or all on a page (4 prompts of 1024, pages of 64: then 39 us, with one
+  // token per warp 100).
   a.group_shift = 0;
   while (a.group_shift < 5 && (n_tokens >> a.group_shift) * cache->n_kv_heads * 2 > 2 * 152 * 48) ++a.group_shift;
   kAppend[cache->kind][dtype](a, (cudaStream_t)cuda_stream);
