@@ -244,6 +244,39 @@ def test_append_strides_and_alignment(V):
         assert bool((o[:, 2 * h * d:] == 0).all()) and out[0] == 0
 
 
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("heads,page,dim", [(3, 256, 128), (5, 256, 16), (2, 144, 256), (1, 240, 96), (7, 128, 64)])
+def test_append_long_runs(V, kind, dtype, heads, page, dim):
+    """Runs longer than a warp keeps beside short ones of the same page, each step exact; odd offsets of the rows."""
+    rng = np.random.RandomState(heads * page + dim)
+    c = new_cache(V, 4, heads, page, dim, kind)
+    codes, scales = codes_of(c)
+    for step in range(5):
+        slots = []
+        for b in rng.permutation(4)[:3]:
+            cuts = np.sort(rng.permutation(page + 1)[:6])
+            for a, e in zip(cuts[::2], cuts[1::2]):  # three runs of the page, gaps between
+                slots += list(range(b * page + a, b * page + e))
+            if rng.rand() < 0.5:
+                slots.append(-1)
+        n = len(slots)
+        size = 2.0 ** rng.randint(-9, 9, (2, n, 1, 1))
+        x = torch.from_numpy((size * rng.randn(2, n, heads, dim)).astype(np.float32)).to(DT[dtype])
+        odd = step % 2
+        y = torch.zeros(2 * n * heads * dim + odd, dtype=DT[dtype], device="cuda")[odd:].view(2, n, heads, dim)
+        y.copy_(x)
+        c.append(y[0], y[1], dev(slots, torch.int64))
+        for i in range(2):
+            S.append(codes[i], scales[i], x[i].float().numpy(), slots, page, kind)
+        same_cache(c, codes, scales, step)
+        out = torch.full((2 * n * heads * dim + odd,), 9.0, dtype=DT[dtype], device="cuda")[odd:].view(2, n, heads, dim)
+        c.gather(dev(slots, torch.int64), out[0], out[1])
+        for i in range(2):
+            want = torch.from_numpy(S.gather(codes[i], scales[i], slots, page, kind)).to(DT[dtype])
+            assert torch.equal(out[i].cpu(), want)
+
+
 # ---------------------------------------------------------------- attention
 
 def fill_cache(c, seed, kind):
