@@ -24,14 +24,14 @@
 namespace seedq {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kSat = 0x7fffffff;
 
 struct PlanArgs {
   const int32_t *seq_lens, *n_new, *free_count;
   int32_t *table, *free_pages;
   int64_t table_stride;
-  int32_t n, page, width, capacity, max_tokens;
+  int32_t n, page, page_shift, width, capacity, max_tokens;  // page_shift: log2 of page, -1 if it is no power of two
   int64_t *slots;
   int32_t *positions, *requests, *seq_out, *starts, *status, *count_out;
 };
@@ -40,32 +40,41 @@ __device__ __forceinline__ int sat_add(int a, int b) {  // a, b >= 0
   return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)kSat);
 }
 
-// Exclusive sum of v over the CTA (saturating), and the total.
-__device__ __forceinline__ int cta_scan(int v, int *warp_sums, int &total) {
+// Exclusive sums of v over the CTA (saturating), N at once, and the totals.
+template <int N>
+__device__ __forceinline__ void cta_scan(int (&v)[N], int (*warp_sums)[N], int (&total)[N]) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  int x = v;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(~0u, x, o);
-    if (lane >= o) x = sat_add(x, y);
-  }
-  if (lane == 31) warp_sums[w] = x;
+  for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int y = __shfl_up_sync(~0u, v[k], o);
+      if (lane >= o) v[k] = sat_add(v[k], y);
+    }
+  if (lane == 31)
+#pragma unroll
+    for (int k = 0; k < N; ++k) warp_sums[w][k] = v[k];
   __syncthreads();
-  int before = 0, all = 0;
-  const int nw = blockDim.x >> 5;
-  for (int i = 0; i < nw; ++i) {
-    const int s = warp_sums[i];
-    if (i < w) before = sat_add(before, s);
-    all = sat_add(all, s);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    int x = lane < kWarps ? warp_sums[lane][k] : 0;  // every warp sums the warps' again: one latency
+#pragma unroll
+    for (int o = 1; o < kWarps; o <<= 1) {
+      const int y = __shfl_up_sync(~0u, x, o);
+      if (lane >= o) x = sat_add(x, y);
+    }
+    total[k] = __shfl_sync(~0u, x, kWarps - 1);
+    const int before = __shfl_sync(~0u, x, max(w - 1, 0)), excl = __shfl_up_sync(~0u, v[k], 1);
+    v[k] = sat_add(w ? before : 0, lane ? excl : 0);
   }
   __syncthreads();
-  total = all;
-  int excl = __shfl_up_sync(~0u, x, 1);
-  if (lane == 0) excl = 0;
-  return sat_add(before, excl);
 }
 
-__device__ __forceinline__ int pages_of(int64_t tokens, int page) { return (int)min((tokens + page - 1) / page, (int64_t)kSat); }
+// For tokens >= 0; the sum is below 2^32.
+__device__ __forceinline__ int pages_of(int tokens, const PlanArgs &a) {
+  const uint32_t x = (uint32_t)tokens + (uint32_t)a.page - 1;
+  return (int)(a.page_shift >= 0 ? x >> a.page_shift : x / (uint32_t)a.page);
+}
 
 // Last i in [0, n) with v[i] <= x (v ascending, v[0] <= x).
 __device__ __forceinline__ int find_last(const int *v, int n, int x) {
@@ -78,13 +87,13 @@ __device__ __forceinline__ int find_last(const int *v, int n, int x) {
   return lo;
 }
 
-__global__ void __launch_bounds__(kThreads) k_batch_plan(PlanArgs a) {
+__global__ void __launch_bounds__(kThreads) k_batch_plan(const __grid_constant__ PlanArgs a) {
   extern __shared__ int sm[];
   int *start = sm;              // n + 1: token offsets
   int *back = sm + a.n + 1;     // n + 1: stack places of returned pages
   int *need = back + a.n + 1;   // n + 1: stack entries popped before
   int *state = need + a.n + 1;  // n: status, or -1 for a finished request
-  __shared__ int warp_sums[32];
+  __shared__ int warp_sums[kWarps][2], warp_need[kWarps][1];
   const int page = a.page;
   const int count = min(max(*a.free_count, 0), a.capacity);
   const int room = a.capacity - count;
@@ -97,14 +106,14 @@ __global__ void __launch_bounds__(kThreads) k_batch_plan(PlanArgs a) {
       L = a.seq_lens[i];
       m = a.n_new[i];
       const int64_t len = (int64_t)L + max(m, 0);
-      if (m < -1 || L < 0 || len > kSat || pages_of(len, page) > a.width) st = SEEDQ_REQ_BAD;
-      else if (m == -1) st = -1, ret = pages_of(L, page);
+      if (m < -1 || L < 0 || len > kSat || pages_of((int)len, a) > a.width) st = SEEDQ_REQ_BAD;
+      else if (m == -1) st = -1, ret = pages_of(L, a);
     }
-    int total;
-    const int t = sat_add(tok0, cta_scan(max(m, 0), warp_sums, total));
-    tok0 = sat_add(tok0, total);
-    const int b = sat_add(back0, cta_scan(ret, warp_sums, total));
-    back0 = sat_add(back0, total);
+    int sums[2] = {max(m, 0), ret}, total[2];
+    cta_scan(sums, warp_sums, total);
+    const int t = sat_add(tok0, sums[0]), b = sat_add(back0, sums[1]);
+    tok0 = sat_add(tok0, total[0]);
+    back0 = sat_add(back0, total[1]);
     if (i < a.n) {
       if (st == SEEDQ_REQ_OK && sat_add(t, max(m, 0)) > a.max_tokens) st = SEEDQ_REQ_NO_ROOM;
       if (st == -1 && sat_add(b, ret) > room) st = SEEDQ_REQ_NO_ROOM;
@@ -122,7 +131,7 @@ __global__ void __launch_bounds__(kThreads) k_batch_plan(PlanArgs a) {
   __syncthreads();
   if (back0 > room)
     for (int i = threadIdx.x; i < a.n; i += blockDim.x)
-      if (state[i] == -1) atomicMax(&s_returned, back[i] + pages_of(a.seq_lens[i], page));
+      if (state[i] == -1) atomicMax(&s_returned, back[i] + pages_of(a.seq_lens[i], a));
   __syncthreads();
   const int avail = count + s_returned;
 
@@ -132,11 +141,12 @@ __global__ void __launch_bounds__(kThreads) k_batch_plan(PlanArgs a) {
     int want = 0;
     if (i < a.n && state[i] == SEEDQ_REQ_OK) {
       const int L = a.seq_lens[i];
-      want = pages_of((int64_t)L + a.n_new[i], page) - pages_of(L, page);
+      want = pages_of(L + a.n_new[i], a) - pages_of(L, a);
     }
-    int total;
-    const int t = sat_add(need0, cta_scan(want, warp_sums, total));
-    need0 = sat_add(need0, total);
+    int sums[1] = {want}, total[1];
+    cta_scan(sums, warp_need, total);
+    const int t = sat_add(need0, sums[0]);
+    need0 = sat_add(need0, total[0]);
     if (i < a.n) {
       need[i] = t;
       if (want > 0) {
@@ -171,11 +181,11 @@ __global__ void __launch_bounds__(kThreads) k_batch_plan(PlanArgs a) {
   for (int i = first >> 5; i < a.n; i += stride >> 5) {
     const int L = a.seq_lens[i], st = state[i];
     int32_t *row = a.table + (int64_t)i * a.table_stride;
-    const int held = pages_of(max(L, 0), page);
+    const int held = pages_of(max(L, 0), a);
     if (st == -1) {
       for (int c = lane; c < held; c += 32) a.free_pages[count + back[i] + c] = row[c];
     } else if (st == SEEDQ_REQ_OK) {
-      const int want = pages_of((int64_t)L + a.n_new[i], page) - held;
+      const int want = pages_of(L + a.n_new[i], a) - held;
       for (int c = lane; c < want; c += 32) row[held + c] = stack(avail - 1 - need[i] - c);
     }
   }
@@ -188,7 +198,7 @@ __global__ void __launch_bounds__(kThreads) k_batch_plan(PlanArgs a) {
       const int L = a.seq_lens[req], d = t - start[req];
       pos = (int)min((int64_t)L + d, (int64_t)kSat);
       if (state[req] == SEEDQ_REQ_OK) {
-        const int pg = pos / page, held = pages_of(L, page);
+        const int pg = a.page_shift >= 0 ? pos >> a.page_shift : pos / page, held = pages_of(L, a);
         const int id = pg < held ? a.table[(int64_t)req * a.table_stride + pg] : stack(avail - 1 - need[req] - (pg - held));
         slot = (int64_t)id * page + (pos - pg * page);
       }
@@ -223,7 +233,7 @@ extern "C" seedq_status seedq_batch_plan(int32_t n_requests, const int32_t *seq_
   // Other CTAs still read the inputs while the first ones write.
   for (const int32_t *o : {positions, requests, seq_lens_out, starts, status, free_count_out})
     if (o == seq_lens || o == n_new || o == free_count) return SEEDQ_ERR_INVALID_ARG;
-  PlanArgs a{seq_lens, n_new, free_count, block_table, free_pages, table_stride, n_requests, page_size, table_width,
+  PlanArgs a{seq_lens, n_new, free_count, block_table, free_pages, table_stride, n_requests, page_size, log2_of(page_size), table_width,
              free_capacity, max_tokens, slots, positions, requests, seq_lens_out, starts, status, free_count_out};
   const size_t smem = sizeof(int) * (4 * (size_t)n_requests + 3);
   int dev = 0;
