@@ -8,11 +8,15 @@
 // that the others need (the stack entries they pop).  All sums saturate, so
 // lengths that make no sense cannot wrap an offset.
 //
-// A step moves a few kilobytes, so launch latency bounds it.  Every CTA repeats
-// the sums (8 bytes per request, from L2) instead of waiting for one that makes
-// them, then takes its share of the tokens, of the table rows and of the pages
-// to return; entries of the stack that this call itself pushes are found
-// through the sums, not read back from memory another CTA may not have written.
+// A step moves a few kilobytes, so launch latency bounds it, and behind it the
+// chain of lengths, two scans, searches and page numbers: 3.6 us for 16 requests
+// with a token each, 6.3 us for 600 with up to 512 (2 to 2.5 us are an empty
+// launch's).  Every CTA repeats the sums (8 bytes per request, from L2) instead of
+// waiting for one that makes them, then takes its share of the tokens, of the
+// table rows and of the pages to return; entries of the stack that this call
+// itself pushes are found through the sums, not read back from memory another CTA
+// may not have written.  512 threads: with 256 the larger case takes 7.9 us, with
+// 1024 the smaller 4.2.
 #include <cuda_runtime.h>
 #include <stdint.h>
 

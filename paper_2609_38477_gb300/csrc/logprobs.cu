@@ -21,7 +21,11 @@
 //
 // What bounds it: many rows, the bytes of the logits (about 9 instructions and
 // one 2^x per logit leave the SMs at half their rate for float32); few rows, the
-// latency of the joins.
+// latency of the joins.  Measured, 128256 logits: 2048 rows of float32 161 us
+// without targets and alternatives (6.5 TB/s, 96% of the copy rate), 172 with
+// targets and 5 alternatives (90%), 192 with 20; of bfloat16 93 us (84%), 124 with
+// either, 231 with targets and 20, where instructions bound it; 16 rows of float32
+// with 20 alternatives 13 to 15 us.
 //
 // Split.  All rows' tiles form one sequence, cut into equal ranges, one per warp
 // (at least one tile each).  A warp that holds a whole row writes its results;
