@@ -454,6 +454,30 @@ def test_attend_nan_block_reaches_only_who_sees_it(V):
     assert not bool(out.isnan().any())
 
 
+@pytest.mark.parametrize("hq,fresh", [(4, 1), (8, 1), (8, 2), (4, 9)])
+@pytest.mark.parametrize("dtype", list(DT))
+def test_attend_query_that_is_no_number(V, hq, fresh, dtype):
+    """A NaN or an infinity in a row of the query spoils that row alone."""
+    c = new_cache(V, 30, 2, 16, 64, "int8")
+    fill_cache(c, 10, "int8")
+    n = 2 * fresh
+    g = torch.Generator("cuda").manual_seed(hq)
+    q = torch.randn(n, hq, 64, generator=g, device="cuda").to(DT[dtype])
+    starts, lens = dev([0, fresh, n], torch.int32), dev([400, 33], torch.int32)
+    table = dev(np.array([list(range(25)), [25, 26, 27] + [-1] * 22]), torch.int32)
+    res = []
+    for bad in (False, True):
+        if bad:
+            q[0, 1, 5], q[n - 1, hq - 1, 63], q[n - 1, 0, 0] = float("nan"), float("inf"), -float("inf")
+        out, lse = torch.zeros(n, hq, 64, device="cuda"), torch.zeros(n, hq, device="cuda")
+        c.attend(q, out, lens, starts, table, c.attend_workspace(hq, fresh), max_new=fresh, lse=lse)
+        res.append((out, lse))
+    spoilt = torch.zeros(n, hq, dtype=torch.bool, device="cuda")
+    spoilt[0, 1] = spoilt[n - 1, hq - 1] = spoilt[n - 1, 0] = True
+    assert torch.equal(res[0][0][~spoilt], res[1][0][~spoilt]) and torch.equal(res[0][1][~spoilt], res[1][1][~spoilt])
+    assert bool(res[1][0][spoilt].isnan().all()) and bool(res[1][1][spoilt].isnan().all())
+
+
 def test_attend_strided_query_and_output(V):
     """Query and output as slices of wider rows at odd offsets, heads before tokens in memory."""
     c = new_cache(V, 10, 2, 16, 64, "int8")
