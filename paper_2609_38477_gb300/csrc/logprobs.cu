@@ -21,11 +21,11 @@
 //
 // What bounds it: many rows, the bytes of the logits (about 9 instructions and
 // one 2^x per logit leave the SMs at half their rate for float32); few rows, the
-// latency of the joins.  Measured, 128256 logits: 2048 rows of float32 161 us
-// without targets and alternatives (6.5 TB/s, 96% of the copy rate), 172 with
-// targets and 5 alternatives (90%), 192 with 20; of bfloat16 93 us (84%), 124 with
-// either, 231 with targets and 20, where instructions bound it; 16 rows of float32
-// with 20 alternatives 13 to 15 us.
+// latency of the joins.  Measured, 128256 logits: 2048 rows of float32 153 us
+// without targets and alternatives (6.9 TB/s, 101% of the copy rate), 171 with
+// targets and 5 alternatives (91%), 212 with 20; of bfloat16 86 us (90%), 117 with
+// targets, 190 with 20 alternatives as well, where instructions bound it; 16 rows
+// of float32 with 20 alternatives 13 to 15 us.
 //
 // Split.  All rows' tiles form one sequence, cut into equal ranges, one per warp
 // (at least one tile each).  A warp that holds a whole row writes its results;
@@ -47,7 +47,11 @@
 namespace seedq {
 namespace {
 
-constexpr int kWarps = 12;
+// 16 warps per SM: 24 take 124 us instead of 117 for 2048 rows of bfloat16 with
+// targets (fewer registers), 12 as much and 194 instead of 171 in float32 with 5
+// alternatives (too few copies under way); one CTA of 16, 17 us instead of 11 for
+// 2000 rows of 600.
+constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kCtasPerSm = 2;
 constexpr int kMaxCtas = 152 * kCtasPerSm;
@@ -57,7 +61,7 @@ constexpr int kFewThreads = 256;
 constexpr int kFewWarps = kFewThreads / 32;
 constexpr int kFewMax = 16 * 152;
 constexpr int kFewKeys = 512;
-constexpr int kStages = 3;       // tiles in a warp's ring
+constexpr int kStages = 3;       // tiles in a warp's ring (5: 160 us instead of 153 without targets and alternatives)
 constexpr int kTileBytes = 2048; // 64 bytes per lane
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
