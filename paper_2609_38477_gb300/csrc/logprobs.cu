@@ -25,7 +25,7 @@
 // without targets and alternatives (6.9 TB/s, 101% of the copy rate), 171 with
 // targets and 5 alternatives (91%), 212 with 20; of bfloat16 86 us (90%), 117 with
 // targets, 190 with 20 alternatives as well, where instructions bound it; 16 rows
-// of float32 with 20 alternatives 13 to 15 us.
+// of float32 with 20 alternatives 12 us.
 //
 // Split.  All rows' tiles form one sequence, cut into equal ranges, one per warp
 // (at least one tile each).  A warp that holds a whole row writes its results;
@@ -58,7 +58,7 @@ constexpr int kMaxCtas = 152 * kCtasPerSm;
 constexpr int kMaxTop = 32;
 // k_score_few: threads, the most CTAs of a call, candidates that a CTA sorts
 constexpr int kFewThreads = 256;
-constexpr int kFewWarps = kFewThreads / 32;
+constexpr int kFewWarps = kFewThreads / 32, kFewEach = 32 / kFewWarps;
 constexpr int kFewMax = 16 * 152;
 constexpr int kFewKeys = 512;
 constexpr int kStages = 3;       // tiles in a warp's ring (5: 160 us instead of 153 without targets and alternatives)
@@ -582,10 +582,23 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_score(const __grid_con
 //
 // A row's chunk per CTA, held in registers.  With few rows latency is all: the
 // lists of k_score would each be built from one or two tiles.  Here every warp
-// finds the ceil(top_k / 8)-th largest of its lanes' maxima; at least top_k
-// logits of the CTA reach the smallest of these, and few more do, so these few
-// are packed and put in order by counting, for each, how many come before it.
-// The last CTA of a row to arrive does the same with the chunks' lists.
+// finds the four largest of its lanes' maxima; at least top_k logits of the CTA
+// reach the top_k-th of these 32, and few more do, so these few are packed and put
+// in order by counting, for each, how many come before it.  The last CTA of a row
+// to arrive does the same with the chunks' lists.
+
+// The n-th largest of the lanes' words (1 <= n <= 32), in all lanes.
+template <typename T>
+__device__ __forceinline__ T nth_of_warp(T x, int n) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const T y = __shfl_sync(~0u, x, j);
+    before += y > x || (y == x && j < lane);
+  }
+  return __shfl_sync(~0u, x, __ffs(__ballot_sync(~0u, before == n - 1)) - 1);
+}
 
 // Puts the first 32 of n <= kFewKeys distinct keys in order into list (zeroed).
 __device__ __forceinline__ void order_keys(const uint64_t *keys, int n, uint64_t *list) {
@@ -603,7 +616,7 @@ __global__ void __launch_bounds__(kFewThreads, 4) k_score_few(const __grid_const
   constexpr int kPer = DT == SEEDQ_F32 ? 16 : 32, kVec = DT == SEEDQ_F32 ? 4 : 8;
   __shared__ uint64_t s_keys[kFewKeys], s_list[kMaxTop], s_best[kFewWarps];
   __shared__ float s_1[kFewWarps], s_2[kFewWarps];
-  __shared__ uint32_t s_most[kFewWarps], s_reach[kFewWarps];
+  __shared__ uint32_t s_reach[32];
   __shared__ int s_count[kFewWarps], s_n, s_last;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int64_t row = blockIdx.x / a.tiles;
@@ -655,19 +668,18 @@ __global__ void __launch_bounds__(kFewThreads, 4) k_score_few(const __grid_const
 #pragma unroll
   for (int e = 2; e < kPer; e += 2) mx = max_nan(mx, x[e], x[e + 1]);
   const uint32_t um = index(0) < a.vocab ? order_word(mx) : 0;
-  uint32_t reach = 0, rest = um;
-  const uint32_t most = __reduce_max_sync(~0u, um);
-  for (int j = 0; j < (a.top_k + kFewWarps - 1) / kFewWarps; ++j) {
-    reach = __reduce_max_sync(~0u, rest);
-    if (lane == __ffs(__ballot_sync(~0u, rest == reach)) - 1) rest = 0;
+  uint32_t rest = um;
+  const int each = a.top_k ? kFewEach : 1;
+#pragma unroll 1
+  for (int j = 0; j < each; ++j) {
+    const uint32_t word = __reduce_max_sync(~0u, rest);
+    if (lane == __ffs(__ballot_sync(~0u, rest == word)) - 1) rest = 0;
+    if (lane == 0) s_reach[w * kFewEach + j] = word;
   }
-  if (lane == 0) s_most[w] = most, s_reach[w] = reach;
   __syncthreads();
-  uint32_t top = 0;
-  reach = ~0u;
-#pragma unroll
-  for (int k = 0; k < kFewWarps; ++k) top = max(top, s_most[k]), reach = min(reach, s_reach[k]);
-  const float m = key_value((uint64_t)top << 32);
+  const uint32_t word = lane % kFewEach < each ? s_reach[lane] : 0;
+  const float m = key_value((uint64_t)__reduce_max_sync(~0u, word) << 32);
+  const uint32_t reach = a.top_k ? nth_of_warp(word, a.top_k) : 0;
 
   if (a.top_k && um && um >= reach) {
 #pragma unroll
@@ -762,11 +774,7 @@ __global__ void __launch_bounds__(kFewThreads, 4) k_score_few(const __grid_const
   // the row's chunks
   const int n = a.tiles;
   if (tid < kMaxTop) s_list[tid] = 0;
-  // At least top_k keys reach the smallest of the chunks' ceil(top_k / n)-th, and
-  // the largest of their top_k-th.
-  uint64_t low = ~0ull, high = 0;
   if (a.top_k) {
-    const int j = (a.top_k + n - 1) / n - 1;
     // the first keys are on their way meanwhile
     constexpr int kAhead = 4;
     uint64_t ahead[kAhead];
@@ -775,21 +783,11 @@ __global__ void __launch_bounds__(kFewThreads, 4) k_score_few(const __grid_const
       const int i = tid + r * kFewThreads, q = i / a.top_k;
       ahead[r] = i < n * a.top_k ? fresh_load(&parts[q].key[i - q * a.top_k]) : 0;
     }
-    for (int i = tid; i < n; i += kFewThreads) {
-      low = min(low, fresh_load(&parts[i].key[j]));
-      high = max(high, fresh_load(&parts[i].key[a.top_k - 1]));
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      low = min(low, __shfl_xor_sync(~0u, low, o));
-      high = max(high, __shfl_xor_sync(~0u, high, o));
-    }
-    if (lane == 0) s_best[w] = low, s_keys[w] = high;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kFewWarps; ++k) low = min(low, s_best[k]), high = max(high, s_keys[k]);
-    low = max(max(low, high), (uint64_t)1);
-    __syncthreads();
+    // 32 keys of the row: the chunks' first, second, ..., or the largest of every 32nd chunk's first
+    uint64_t some = n < 32 ? fresh_load(&parts[lane % n].key[lane / n]) : 0;
+    if (n >= 32)
+      for (int i = lane; i < n; i += 32) some = max(some, fresh_load(&parts[i].key[0]));
+    const uint64_t low = max(nth_of_warp(some, a.top_k), (uint64_t)1);
     auto push = [&](uint64_t key) {
       if (key < low) return;
       const int at = atomicAdd(&s_n, 1);
@@ -842,9 +840,9 @@ template <int DT, bool VEC>
 seedq_status launch(ScoreArgs &a, int sms, int dev, cudaStream_t st) {
   constexpr int kPer = DT == SEEDQ_F32 ? 16 : 32, kTile = 32 * kPer, kChunk = kFewThreads * kPer;
   a.tiles = (a.vocab + kChunk - 1) / kChunk;
-  // Few rows: 16 of 128256 with 20 alternatives take 14 us there and 27 below, 64
-  // take 29 and 41, 256 with 5 take 76 and 47; rows of a tile or two are one
-  // warp's work below (2000 of 1000: 20 and 15 us).
+  // Few rows: 16 of 128256 with 20 alternatives take 12 us there and 23 below, 64
+  // take 27 and 36, 256 with 5 take 78 and 44; rows of a tile or two are one
+  // warp's work below (2000 of 1000: 21 and 13 us).
   if (a.vocab > 2 * kTile && a.rows * a.tiles <= kFewMax) {
     k_score_few<DT, VEC><<<(unsigned)(a.rows * a.tiles), kFewThreads, 0, st>>>(a);
     const cudaError_t e = cudaGetLastError();
