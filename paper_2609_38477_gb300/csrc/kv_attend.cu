@@ -21,8 +21,8 @@
 // What bounds it: the bytes of the cache, 2 head_dim per key and key-value
 // head.  At 8 rows a byte costs 16 operations, far below the balance, but every
 // code has to be widened (about 1.5 instructions) and multiplied.  Measured, 128
-// head dims: 4 contexts of about 121000, 32 query on 8 key-value heads, 160 us (6.2
-// TB/s, 91% of the copy rate); 64 of 2048 on 8 heads, 66 us with 32 query heads
+// head dims: 4 contexts of about 121000, 32 query on 8 key-value heads, 162 us (6.1
+// TB/s, 90% of the copy rate); 64 of 2048 on 8 heads, 66 us with 32 query heads
 // (4.0 TB/s) and 78 with 64, where the instructions bound it; 16 tokens of 32 heads
 // over 32768 keys 90 us (tiles of 16 rows read the keys four times, from L2); one
 // request of 1000 12 us, the latency of lengths, page numbers, keys and the joins.
