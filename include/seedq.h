@@ -306,8 +306,8 @@ seedq_status seedq_fp64_fma_probe(int64_t iters, int32_t blocks_per_sm, double *
  * says about a token (seedq_token_logprobs).  No paper counterpart: the paper
  * covers the weights only.
  *
- * All calls are hot calls: they validate on the host, enqueue one or two
- * launches, allocate nothing and do not synchronize; every length, slot and
+ * All calls are hot calls: they validate on the host, enqueue one launch,
+ * allocate nothing and do not synchronize; every length, slot and
  * page number stays on the device, so a step can be captured in a CUDA graph.
  * Kernels check what they read from device memory (pages, slots, offsets)
  * against the sizes given here and skip what is out of range. */
@@ -436,7 +436,7 @@ seedq_status seedq_kv_gather(const seedq_kv_cache *cache, const int64_t *slots, 
  *               one each.
  * Sums, the softmax statistics and the products' accumulators are float32.
  * Errors: INVALID_ARG, UNSUPPORTED (as above; n_heads not a multiple of
- * n_kv_heads), CUDA. */
+ * n_kv_heads; n_tokens x n_heads / n_kv_heads of 2^31 - 32 or more), CUDA. */
 typedef struct {
   int32_t n_requests;
   int32_t n_heads;
@@ -462,8 +462,7 @@ typedef struct {
   uint64_t workspace_bytes;
 } seedq_attend_args;
 
-/* 0 for arguments that seedq_kv_attend would refuse.  Host function (asks the
- * current device for its number of SMs). */
+/* 0 for arguments that seedq_kv_attend would refuse.  Host function. */
 uint64_t seedq_kv_attend_workspace_bytes(const seedq_kv_cache *cache, int32_t n_heads,
                                          int32_t max_new);
 seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_args *args,

@@ -1199,6 +1199,7 @@ seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_arg
   if (!a.q || !a.out || !a.seq_lens || !a.starts || !a.block_table || !a.workspace || (uintptr_t)a.workspace % 16 ||
       a.workspace_bytes < seedq_kv_attend_workspace_bytes(cache, a.n_heads, a.max_new))
     return SEEDQ_ERR_INVALID_ARG;
+  if (a.n_tokens * (a.n_heads / cache->n_kv_heads) >= INT32_MAX - 31) return SEEDQ_ERR_UNSUPPORTED;  // rows are numbered in 32 bits
   Args p;
   p.c = *cache;
   p.a = a;

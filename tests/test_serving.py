@@ -194,6 +194,12 @@ def test_attend_refuses(Q, kw, status):
     assert L.seedq_kv_attend(None, C.byref(_attend(Q)), None) == 1
 
 
+@pytest.mark.parametrize("n,heads", [(1 << 30, 4), ((1 << 31) - 1, 2), (((1 << 31) - 32) // 8, 16)])
+def test_attend_refuses_more_rows_than_it_numbers(Q, n, heads):
+    d = _desc(Q)
+    assert Q.lib().seedq_kv_attend(C.byref(d), C.byref(_attend(Q, n_tokens=n, n_heads=heads)), None) == 6
+
+
 @pytest.mark.parametrize("kw", [
     dict(x=None), dict(dt=3), dict(rows=-1), dict(vocab=0), dict(vocab=(1 << 30) + 1, stride=1 << 31), dict(stride=9),
     dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(lp=None), dict(rank=None), dict(k=-1), dict(k=33),
