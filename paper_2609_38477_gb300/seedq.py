@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -102,6 +103,11 @@ class AttendArgs(C.Structure):
                 ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
+# The same as packed bytes (a pointer that is NULL as 0), in a quarter of the time.
+ATTEND_ARGS = struct.Struct("@iiqPqqPqqiiPPPPqiiifPQ")
+assert ATTEND_ARGS.size == C.sizeof(AttendArgs)
+
+
 # Every symbol include/seedq.h declares, with its ctypes signature.
 SIGNATURES = {
     "seedq_layer_prepare": (C.c_int, [C.POINTER(LayerDesc), C.POINTER(Schedule), C.c_void_p,
@@ -164,7 +170,7 @@ SIGNATURES = {
     "seedq_kv_gather": (C.c_int, [C.POINTER(KvCacheDesc), C.c_void_p, C.c_int64, C.c_void_p,
                                   C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p]),
     "seedq_kv_attend_workspace_bytes": (C.c_uint64, [C.POINTER(KvCacheDesc), C.c_int32, C.c_int32]),
-    "seedq_kv_attend": (C.c_int, [C.POINTER(KvCacheDesc), C.POINTER(AttendArgs), C.c_void_p]),
+    "seedq_kv_attend": (C.c_int, [C.POINTER(KvCacheDesc), C.c_void_p, C.c_void_p]),
     "seedq_token_logprobs_workspace_bytes": (C.c_uint64, [C.c_int64, C.c_int64]),
     "seedq_token_logprobs": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64,
                                        C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,

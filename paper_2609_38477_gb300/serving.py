@@ -10,6 +10,7 @@ here and raises ValueError; what it refuses itself raises SeedQError.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
@@ -61,12 +62,12 @@ def _code_strides(t):
 
 
 def _rows(t, name: str, tokens, heads, dim, device):
-    """Checks a (tokens, heads, dim) tensor of any strides but the last, and returns its type's code."""
-    dt = DTYPES.get(t.dtype)
-    if dt is None or t.shape != (tokens, heads, dim) or t.device != device or t.stride(2) != 1:
+    """Checks a (tokens, heads, dim) tensor of any strides but the last, and returns its type's code and the strides."""
+    dt, st = DTYPES.get(t.dtype), t.stride()
+    if dt is None or t.shape != (tokens, heads, dim) or t.device != device or st[2] != 1:
         raise ValueError(f"{name}: ({tokens}, {heads}, {dim}) float32, bfloat16 or float16 with contiguous last dimension "
                          f"on {device} is wanted, got {tuple(t.shape)} {t.dtype}")
-    return dt
+    return dt, st
 
 
 class BatchPlan:
@@ -139,23 +140,23 @@ class KVCache:
 
     def append(self, k, v, slots, stream=None):
         """seedq_kv_append: k, v (n_tokens, n_kv_heads, head_dim) to slots (int64)."""
-        n, dt = self._pair(k, v, slots)
-        _check(Q.lib().seedq_kv_append(self._ref, k.data_ptr(), v.data_ptr(), dt, k.stride(0), k.stride(1),
+        n, dt, st = self._pair(k, v, slots)
+        _check(Q.lib().seedq_kv_append(self._ref, k.data_ptr(), v.data_ptr(), dt, st[0], st[1],
                                        slots.data_ptr(), n, _stream(stream, self.device)), "seedq_kv_append")
 
     def gather(self, slots, k, v, stream=None):
         """seedq_kv_gather: the cached numbers at slots into k, v."""
-        n, dt = self._pair(k, v, slots)
+        n, dt, st = self._pair(k, v, slots)
         _check(Q.lib().seedq_kv_gather(self._ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), dt,
-                                       k.stride(0), k.stride(1), _stream(stream, self.device)), "seedq_kv_gather")
+                                       st[0], st[1], _stream(stream, self.device)), "seedq_kv_gather")
 
     def _pair(self, k, v, slots):
         n, dev = k.shape[0], self.device
-        dt = _rows(k, "k", n, self.n_kv_heads, self.head_dim, dev)
-        if v.shape != k.shape or v.dtype is not k.dtype or v.device != dev or v.stride() != k.stride():
+        dt, st = _rows(k, "k", n, self.n_kv_heads, self.head_dim, dev)
+        if v.shape != k.shape or v.dtype is not k.dtype or v.device != dev or v.stride() != st:
             raise ValueError("v: the shape, type, strides and device of k are wanted")
         _ints(slots, n, torch.int64, dev, "slots")
-        return n, dt
+        return n, dt, st
 
     def attend_workspace(self, n_heads: int, max_new: int = 1):
         """A zeroed workspace for attend() with that many query heads and, per
@@ -170,8 +171,8 @@ class KVCache:
         (n_tokens, n_heads) float32 or None; scale defaults to head_dim^-1/2."""
         n, heads, _ = q.shape
         dev = self.device
-        qt = _rows(q, "q", n, heads, self.head_dim, dev)
-        ot = _rows(out, "out", n, heads, self.head_dim, dev)
+        qt, qs = _rows(q, "q", n, heads, self.head_dim, dev)
+        ot, os = _rows(out, "out", n, heads, self.head_dim, dev)
         b = starts.shape[0] - 1
         _ints(starts, 2, torch.int32, dev, "starts")
         _ints(seq_lens, b, torch.int32, dev, "seq_lens")
@@ -181,11 +182,14 @@ class KVCache:
         if lse is not None and not (lse.dtype is torch.float32 and lse.shape == (n, heads) and lse.is_contiguous()
                                     and lse.device == dev):
             raise ValueError(f"lse: contiguous float32 ({n}, {heads}) on {dev} is wanted")
-        a = Q.AttendArgs(b, heads, n, q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
-                         qt, ot, None if lse is None else lse.data_ptr(), seq_lens.data_ptr(), starts.data_ptr(),
-                         block_table.data_ptr(), _row_stride(block_table), block_table.shape[1], max_new, window,
-                         self.head_dim ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.nbytes)
-        _check(Q.lib().seedq_kv_attend(self._ref, C.byref(a), _stream(stream, dev)), "seedq_kv_attend")
+        try:
+            a = Q.ATTEND_ARGS.pack(b, heads, n, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1],
+                                   qt, ot, 0 if lse is None else lse.data_ptr(), seq_lens.data_ptr(), starts.data_ptr(),
+                                   block_table.data_ptr(), _row_stride(block_table), block_table.shape[1], max_new, window,
+                                   self.head_dim ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.nbytes)
+        except (struct.error, OverflowError) as e:
+            raise ValueError(f"max_new, window: 32-bit integers, scale: a float32 number are wanted ({e})") from None
+        _check(Q.lib().seedq_kv_attend(self._ref, a, _stream(stream, dev)), "seedq_kv_attend")
 
 
 def score_workspace(n_rows: int, vocab: int, device="cuda"):
