@@ -187,8 +187,8 @@ class KVCache:
                                    qt, ot, 0 if lse is None else lse.data_ptr(), seq_lens.data_ptr(), starts.data_ptr(),
                                    block_table.data_ptr(), _row_stride(block_table), block_table.shape[1], max_new, window,
                                    self.head_dim ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.nbytes)
-        except (struct.error, OverflowError) as e:
-            raise ValueError(f"max_new, window: 32-bit integers, scale: a float32 number are wanted ({e})") from None
+        except struct.error as e:
+            raise ValueError(f"max_new, window: 32-bit integers, scale: a number are wanted ({e})") from None
         _check(Q.lib().seedq_kv_attend(self._ref, a, _stream(stream, dev)), "seedq_kv_attend")
 
 
@@ -203,26 +203,37 @@ def token_logprobs(logits, targets, logprob, entropy, rank, top_logprob, top_ind
     logprob, entropy (n,) float32, rank (n,) int32, top_logprob (n, k) float32
     and top_index (n, k) int32 are written.  Each of them may be None (logprob
     and rank only without targets, the two top tensors only together)."""
-    _want(logits.dim() == 2 and logits.dtype in DTYPES and logits.stride(1) == 1 and logits.is_cuda,
-          "logits: (rows, vocab) float32, bfloat16 or float16 with contiguous rows on a CUDA device is wanted")
-    n, dev = logits.shape[0], logits.device
-    _want((targets is None or (logprob is not None and rank is not None)), "logprob and rank: wanted beside targets")
-    for t, dt, name in ((targets, torch.int64, "targets"), (logprob, torch.float32, "logprob"),
-                        (entropy, torch.float32, "entropy"), (rank, torch.int32, "rank")):
-        if t is not None:
-            _ints(t, n, dt, dev, name)
+    dt, st = DTYPES.get(logits.dtype), logits.stride()
+    if len(st) != 2 or dt is None or st[1] != 1 or not logits.is_cuda:
+        raise ValueError("logits: (rows, vocab) float32, bfloat16 or float16 with contiguous rows on a CUDA device is wanted")
+    (n, vocab), dev = logits.shape, logits.device
+    pt = pl = pe = pr = px = pi = None
+    if targets is not None:
+        if logprob is None or rank is None:
+            raise ValueError("logprob and rank: wanted beside targets")
+        _ints(targets, n, torch.int64, dev, "targets")
+        pt = targets.data_ptr()
+    if logprob is not None:
+        _ints(logprob, n, torch.float32, dev, "logprob")
+        pl = logprob.data_ptr()
+    if entropy is not None:
+        _ints(entropy, n, torch.float32, dev, "entropy")
+        pe = entropy.data_ptr()
+    if rank is not None:
+        _ints(rank, n, torch.int32, dev, "rank")
+        pr = rank.data_ptr()
     k = 0
     if top_index is not None or top_logprob is not None:
-        _want(top_index is not None and top_logprob is not None, "top_logprob and top_index: wanted together")
+        if top_index is None or top_logprob is None:
+            raise ValueError("top_logprob and top_index: wanted together")
         k = top_index.shape[-1]
-        for t, dt in ((top_logprob, torch.float32), (top_index, torch.int32)):
-            if not (t.dtype is dt and t.shape == (n, k) and t.is_contiguous() and t.device == dev):
-                raise ValueError(f"top_logprob, top_index: contiguous float32 and int32 ({n}, k) on {dev} are wanted")
-
-    def p(t):
-        return None if t is None else t.data_ptr()
-
+        if not (top_logprob.dtype is torch.float32 and top_index.dtype is torch.int32
+                and top_logprob.shape == top_index.shape == (n, k) and top_logprob.is_contiguous()
+                and top_index.is_contiguous() and top_logprob.device == dev and top_index.device == dev):
+            raise ValueError(f"top_logprob, top_index: contiguous float32 and int32 ({n}, k) on {dev} are wanted")
+        px, pi = top_logprob.data_ptr(), top_index.data_ptr()
+    if not workspace.is_contiguous() or workspace.device != dev:
+        raise ValueError("workspace: a tensor of score_workspace is wanted")
     _check(Q.lib().seedq_token_logprobs(
-        logits.data_ptr(), DTYPES[logits.dtype], n, logits.shape[1], _row_stride(logits),
-        scale, p(targets), p(logprob), p(entropy), p(rank), k, p(top_logprob), p(top_index), workspace.data_ptr(),
+        logits.data_ptr(), dt, n, vocab, st[0] if n > 1 else vocab, scale, pt, pl, pe, pr, k, px, pi, workspace.data_ptr(),
         workspace.nbytes, _stream(stream, dev)), "seedq_token_logprobs")

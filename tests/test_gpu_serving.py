@@ -646,6 +646,25 @@ def test_score_workspace_of_a_larger_batch(V):
         check_score(V, x, [v // 2] * n, 1.0, 6, ws)
 
 
+def test_workspaces_elsewhere_are_refused(V):
+    x = torch.zeros(2, 50, device="cuda")
+    e = torch.zeros(2, device="cuda")
+    for ws in (V.score_workspace(2, 50).cpu(), V.score_workspace(2, 50).view(-1, 2)[:, 0]):
+        with pytest.raises(ValueError, match="workspace"):
+            V.token_logprobs(x, None, None, e, None, None, None, ws)
+    c = new_cache(V, 4, 2, 16, 64, "int8")
+    q = torch.zeros(1, 2, 64, device="cuda")
+    z = dev([1, 0], torch.int32)
+    a = (q, q.clone(), z[:1], z, z[None])
+    with pytest.raises(ValueError, match="workspace"):
+        c.attend(*a, c.attend_workspace(2).cpu())
+    for kw in (dict(window=1 << 40), dict(max_new=1.5)):
+        with pytest.raises(ValueError):
+            c.attend(*a, c.attend_workspace(2), **kw)
+    with pytest.raises(V.Q.SeedQError):  # an infinity in float32
+        c.attend(*a, c.attend_workspace(2), scale=1e300)
+
+
 def test_score_lists_that_overflow(V):
     """Few rows, cut into chunks: one of equal logits, small whole numbers with
     ties at every edge, and chunks of which all but one reach the list with almost
