@@ -462,8 +462,9 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
   // nearest entry's: a join between CTAs costs 3 to 4 us (40 ragged requests up to
   // 1000, 32 heads on 8: 19 us, without 22; 100: 26 and 30; but 16 up to 2048, whose
   // longest entry is twice a share, 22 with and 18 without; 256 up to 4096, 82 and
-  // 78).  Likewise between warps where no entry is longer than kWholeWarp (200
-  // requests up to 100: 19 us, else 25).
+  // 78); with little work where none is longer than kWholeLittle (21 requests that
+  // see a window of 33: 11 us, else 13).  Likewise between warps where no entry is
+  // longer than kWholeWarp (200 requests up to 100: 19 us, else 25).
   const bool little = total <= (int64_t)p.ctas * 8;
   const int warps = little ? 4 : S::kWarps;
   const int64_t share = max((int64_t)__umul64hi((uint64_t)total, p.ctas_inv) + 1, (int64_t)warps);
