@@ -127,8 +127,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
 template <typename T>
 __device__ __forceinline__ T fresh_load(const T *x) { return *(const volatile T *)x; }
 
+// A target's logit, -0 as +0: count_above would take every +0 for larger than -0.
+__device__ __forceinline__ float target_logit(const void *p, int dt, int64_t i) { return load_elem(p, dt, i) + 0.f; }
+
 // How many of x are above thr, all of them if thr is NaN: the signs of thr - x,
-// shifted into a word (a compare and an add per number cost twice as much).
+// shifted into a word (a compare and an add per number cost twice as much).  thr
+// is not -0.
 template <int N>
 __device__ __forceinline__ int count_above(const float (&x)[N], float thr) {
   static_assert(N <= 32, "");
@@ -271,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_score(const __grid_con
   // are on their way before they are needed.
   auto target = [&](int64_t r) -> int64_t { return a.targets && r < a.rows ? a.targets[r] : -1; };
   auto logit = [&](int64_t r, int64_t t) -> float {
-    return t >= 0 && t < a.vocab ? load_elem(a.x, DT, r * a.stride + t) : 0.f;
+    return t >= 0 && t < a.vocab ? target_logit(a.x, DT, r * a.stride + t) : 0.f;
   };
   int64_t t = target(row), t1 = target(row + 1);
   float xt = logit(row, t), xt1 = logit(row + 1, t1);
@@ -660,7 +664,7 @@ __global__ void __launch_bounds__(kFewThreads, 4) k_score_few(const __grid_const
     }
   }
   const int64_t t = a.targets ? a.targets[row] : -1;
-  const float xt = t >= 0 && t < a.vocab ? load_elem(a.x, DT, row * a.stride + t) : 0.f;
+  const float xt = t >= 0 && t < a.vocab ? target_logit(a.x, DT, row * a.stride + t) : 0.f;
 
   if (tid < kMaxTop) s_list[tid] = 0;
   if (tid == 0) s_n = 0;

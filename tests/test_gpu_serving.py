@@ -630,6 +630,28 @@ def test_score_orders_in_long_batches(V, v):
                 assert torch.allclose(a[ok], b[ok], rtol=2e-5, atol=2e-5), name
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("n,v", [(1, 20000), (3, 20003), (2500, 1500), (2500, 2047), (2000, 9000)])
+def test_score_rank_of_a_negative_zero(V, dtype, n, v):
+    """-0 and +0 are equal logits, placed by their index: targets of either sign
+    at a row's start, middle and end, among larger and smaller logits, and zeros
+    behind them in every tile; few rows and many, wide loads and single ones."""
+    g = torch.Generator("cuda").manual_seed(n + v)
+    for odd in (0, 1):
+        flat = torch.randint(-1, 2, (n * v + odd,), generator=g, device="cuda").float()
+        flat[torch.rand(flat.shape, generator=g, device="cuda") < 0.5] *= -1  # zeros of both signs
+        x = flat.to(DT[dtype])[odd:].view(n, v)
+        f = lambda *s, d=torch.float32: torch.empty(s, dtype=d, device="cuda")  # noqa: E731
+        lp, en, rk, tl, ti, ws = f(n), f(n), f(n, d=torch.int32), f(n, 0), f(n, 0, d=torch.int32), V.score_workspace(n, v)
+        for at in (0, v // 2, v - 1):
+            for zero in (-0.0, 0.0):
+                x[:, at] = zero
+                t = torch.full((n,), at, device="cuda")
+                V.token_logprobs(x, t, lp, en, rk, tl, ti, ws)
+                want = (x > 0).sum(1) + (x[:, :at] == 0).sum(1)
+                assert torch.equal(rk.long(), want), (odd, at, zero)
+
+
 def test_score_strided_unaligned_rows(V):
     for dt in DT.values():
         flat = torch.randn(6 * 1003 + 5, device="cuda").to(dt)
