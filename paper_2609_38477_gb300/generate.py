@@ -81,7 +81,8 @@ class Decoder:
 
     def step(self, tokens, n_new):
         """The next tokens (int64, one request's after another's) of every
-        request, n_new of each (int32; -1 ends a request).  Returns the logits
+        request, n_new of each (int32; -1 ends a request); of fewer requests
+        than the decoder was made for, the others wait.  Returns the logits
         of every token; plan and seq_lens describe the step."""
         s, n = self.spec, tokens.shape[0]
         p = self.plan
@@ -100,7 +101,7 @@ class Decoder:
             gate, up = self._products(rms_norm(x, block["mlp_norm"]), ("gate", "up"), block)
             act = (torch.nn.functional.silu(gate) * up).bfloat16()
             x = x + self._products(act, ("down",), block)[0]
-        self.seq_lens.copy_(p.seq_lens)
+        self.seq_lens[:p.n_requests].copy_(p.seq_lens)
         self.free_count.copy_(p.free_count)
         return self._products(rms_norm(x, self.final_norm), ("head",), {"head": self.head})[0]
 

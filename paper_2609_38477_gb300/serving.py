@@ -74,17 +74,23 @@ class BatchPlan:
     """The outputs of seedq_batch_plan for up to max_requests requests and
     max_tokens new tokens a step: slots, positions, requests (per token),
     seq_lens, starts, status (per request), free_count.  They are allocated
-    once, so a captured graph keeps its addresses."""
+    once, so a captured graph keeps its addresses; seq_lens, starts and status
+    are as long as the last build had requests, starts one more."""
 
     def __init__(self, max_requests: int, max_tokens: int, device="cuda"):
         r, t = int(max_requests), int(max_tokens)
         self.max_requests, self.max_tokens = r, t
         self.slots = torch.full((t,), -1, dtype=torch.int64, device=device)
         ints = torch.zeros(2 * t + 3 * r + 2, dtype=torch.int32, device=device)
-        (self.positions, self.requests, self.seq_lens, self.starts, self.status,
-         self.free_count) = ints.split([t, t, r, r + 1, r, 1])
+        self.positions, self.requests, *self._per_request, self.free_count = ints.split([t, t, r, r + 1, r, 1])
         self._out = tuple(C.c_void_p(t.data_ptr()) for t in (
-            self.slots, self.positions, self.requests, self.seq_lens, self.starts, self.status, self.free_count))
+            self.slots, self.positions, self.requests, *self._per_request, self.free_count))
+        self._resize(r)
+
+    def _resize(self, n: int):
+        # What lies past n requests is an earlier step's.
+        lens, starts, status = self._per_request
+        self.n_requests, self.seq_lens, self.starts, self.status = n, lens[:n], starts[:n + 1], status[:n]
 
     def build(self, seq_lens, n_new, block_table, free_pages, free_count, page_size: int, stream=None):
         """seedq_batch_plan: lengths and new-token counts (int32 vectors) in,
@@ -101,6 +107,8 @@ class BatchPlan:
             n, seq_lens.data_ptr(), n_new.data_ptr(), page_size, block_table.data_ptr(), _row_stride(block_table),
             block_table.shape[1], free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(),
             self.max_tokens, *self._out, _stream(stream, dev)), "seedq_batch_plan")
+        if n != self.n_requests:
+            self._resize(n)
 
 
 class KVCache:

@@ -123,3 +123,16 @@ def test_decode_loop(G, name, kind, page):
 def test_example_runs(G, capsys):
     G.main()
     assert capsys.readouterr().out.count("step") == 6
+
+
+def test_step_of_fewer_requests(G):
+    """A step of the first requests alone: the others keep their lengths, and the logits are those of a smaller batch."""
+    t = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    d, e = (G.synthetic_decoder("tiny", max_requests=r, n_pages=6) for r in (3, 2))
+    tokens = torch.arange(16, device="cuda")
+    d.step(tokens, t(5, 4, 7))
+    e.step(tokens[:9], t(5, 4))
+    for new in ((3, 6), (1, 1), (0, 2)):
+        a, b = (x.step(tokens[:sum(new)], t(*new)) for x in (d, e))
+        assert float((a - b).abs().max()) <= 0.01 * float(b.abs().max())
+    assert d.seq_lens.tolist() == [9, 13, 7] and e.seq_lens.tolist() == [9, 13]

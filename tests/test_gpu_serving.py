@@ -726,6 +726,34 @@ def test_score_row_counts_around_the_split(V):
 
 # ---------------------------------------------------------------- together
 
+def test_batch_that_shrinks_on_one_plan(V):
+    """Fewer requests than the plan was made for, after a step of more: what the
+    plan then hands on has no request of the earlier step in it."""
+    H, HQ, D, P = 2, 4, 64, 16
+    plan = V.BatchPlan(4, 16)
+    c = V.KVCache.empty(20, H, D, P)
+    table = torch.full((4, 4), -1, dtype=torch.int32, device="cuda")
+    free, count = torch.arange(20, dtype=torch.int32, device="cuda"), dev([20], torch.int32)
+    seq = torch.zeros(4, dtype=torch.int32, device="cuda")
+    g = torch.Generator("cuda").manual_seed(0)
+    for new in ([9, 1, 3, 2], [1, 1, 1, 1], [3, 3], [1, 2, 1], [5], [2, 1, 4, 1]):
+        r, n = len(new), sum(new)
+        plan.build(seq, dev(new, torch.int32), table, free, count, P)
+        assert plan.starts.tolist() == [sum(new[:i]) for i in range(r + 1)] and plan.status.tolist() == [0] * r
+        kv, q = (torch.randn(s, generator=g, device="cuda") for s in ((2, n, H, D), (n, HQ, D)))
+        c.append(kv[0], kv[1], plan.slots)
+        out, alone = torch.zeros(n, HQ, D, device="cuda"), torch.zeros(n, HQ, D, device="cuda")
+        ws = c.attend_workspace(HQ, max(new))
+        c.attend(q, out, plan.seq_lens, plan.starts, table, ws, max_new=max(new))
+        for i in range(r):  # a request at a time
+            a, b = sum(new[:i]), sum(new[:i + 1])
+            c.attend(q[a:b], alone[a:b], plan.seq_lens[i:], dev([0, b - a], torch.int32), table[i:], ws, max_new=max(new))
+        assert torch.allclose(out, alone, atol=1e-5)
+        assert plan.seq_lens.tolist() == [x + y for x, y in zip(seq.tolist(), new)]
+        seq[:r] = plan.seq_lens
+        count.copy_(plan.free_count)
+
+
 def test_side_stream_and_graph(V):
     """plan, append, attend and score captured in a graph on a stream of their own, replayed for
     new lengths, against the calls one by one."""

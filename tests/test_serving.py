@@ -238,3 +238,21 @@ def test_binding_refuses_what_the_abi_cannot_see(Q):
         a.update(bad)
         with pytest.raises(ValueError):
             plan.build(**a)
+
+
+def test_plan_of_fewer_requests_hands_on_no_others(Q, monkeypatch):
+    """A build with fewer requests writes fewer offsets; what is handed on ends there, at the same addresses."""
+    from paper_2609_38477_gb300 import serving as V
+
+    class Library:
+        def seedq_batch_plan(self, n, *a):
+            return 0
+
+    plan = V.BatchPlan(4, 16, device="cpu")
+    base = [t.data_ptr() for t in (plan.seq_lens, plan.starts, plan.status)]
+    monkeypatch.setattr(Q, "lib", Library)
+    i = torch.zeros(4, dtype=torch.int32)
+    for n in (4, 2, 2, 3, 1, 4):
+        plan.build(i, i[:n], torch.zeros((4, 3), dtype=torch.int32), i, i[:1], 16, stream=0)
+        assert (plan.seq_lens.shape[0], plan.starts.shape[0], plan.status.shape[0]) == (n, n + 1, n)
+        assert [t.data_ptr() for t in (plan.seq_lens, plan.starts, plan.status)] == base
