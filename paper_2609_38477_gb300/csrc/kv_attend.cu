@@ -12,9 +12,10 @@
 // bits; of q in a 16-bit type, scaled, the high half is all).  Up to 4 rows, the
 // columns 0-3 carry the high and 4-7 the low halves of the same rows and the
 // second half costs nothing; from 5 rows on the low halves are products of their
-// own into the same sums.  q is scaled by a power of two per row, weights are
-// taken relative to the largest block scale so far and scaled by 2^14, so
-// binary16's range never cuts off more than 2^-38 of the largest.  Each unit's
+// own into the same sums.  q is scaled by a power of two per row, the weights
+// p_j s^v_j of a row by one that brings the largest so far of its own (keys that it
+// does not see count for nothing, whatever their scale) to 2^13, so binary16's
+// range never cuts off more than 2^-37 of it.  Each unit's
 // products start from zero and are added to float32 registers, so a long
 // context is not accumulated inside the tensor cores, which truncate.
 //
@@ -65,7 +66,7 @@ constexpr int kMaxCtas = 152;      // one per SM
 constexpr int kSmemMax = 227 * 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kWeight = 16384.f;  // weights are held times this
+constexpr int kWeight = 13;  // a row's largest weight is held near 2^kWeight
 
 // DP: head dim rounded up to 64, 128 or 256.  MODE: rows of a tile: 0: 4 (high
 // and low halves share the 8 columns), 1: 8, 2: 16.  HALVES: of q, 1 where its
@@ -142,6 +143,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The whole number next to x, -127 at least, held as 1.5 * 2^23 more: differences
+// are exact, and the low bits are the number.
+__device__ __forceinline__ float exponent(float x) { return fmaxf(x, -127.f) + 12582912.f; }
+__device__ __forceinline__ int exponent_bits(float x) { return (int)(__float_as_uint(x) - __float_as_uint(12582912.f)); }
 __device__ __forceinline__ uint32_t half2_bits(__half2 h) { return *reinterpret_cast<uint32_t *>(&h); }
 
 // x = hi + lo in binary16 (pairs).
@@ -559,7 +564,8 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
   // ---- products
   uint32_t qf[S::kSets][S::kQHalves][S::kChunks * 4][2];  // q as the second operand
   float zf[S::kSets][2];      // z in units of log2 per unit of product, but for the key scale
-  float m[S::kSets][2], l[S::kSets][2], vmax = 0.f;
+  float m[S::kSets][2], l[S::kSets][2];
+  float top[S::kSets][2];     // log2 of the row's largest p s^v so far, relative to 2^m (s^v as the power of two below it)
   uint64_t o[S::kSets][S::kTiles][2];  // sums of the columns (2 q4, 2 q4 + 1) for two head dims
   int cleft = 0, tok = 0, see_all = 0, see_from = 0;  // units of the tokens see_from < t <= see_all need no mask
   // and of a value tile: piece n (DP 64: half of piece n / 2) of row 2 q4
@@ -676,7 +682,6 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
       const Desc e = s_desc[w][cdesc];
       cleft = e.units;
       tok = e.token0;
-      vmax = 0.f;
       {
         const int r0 = e.tile * S::kRows, t0 = divide(r0, p.group, p.group_shift), t1 = divide(r0 + S::kRows - 1, p.group, p.group_shift);
         see_all = min(e.len - e.fresh + t0, e.hi - 1);
@@ -753,7 +758,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
         for (int k = 0; k < 2; ++k) {
           const int col = 2 * q4 + k;
           zf[s][k] = __shfl_sync(~0u, f, col * 4);
-          m[s][k] = -CUDART_INF_F;
+          m[s][k] = top[s][k] = -CUDART_INF_F;
           l[s][k] = 0.f;
         }
       }
@@ -839,44 +844,59 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
         }
     }
 
-    // the block scales of the values, relative to the largest so far
-    float vr[S::kGroups], vcorr = 1.f;
-    bool same = vmax > 0.f;
+    // the block scales of the values as vf 2^ve, 1 <= |vf| < 2 but for the ends of the range
+    float vf[S::kGroups];
+    int ve[S::kGroups];
+    bool alike = true;
 #pragma unroll
-    for (int g = 0; g < S::kGroups; ++g) same = same && vs[g] == vmax;
-    if (same) {
-#pragma unroll
-      for (int g = 0; g < S::kGroups; ++g) vr[g] = kWeight;
-    } else {
-      float vnew = vmax;
-#pragma unroll
-      for (int g = 0; g < S::kGroups; ++g)
-        if (fabsf(vs[g]) < CUDART_INF_F) vnew = fmaxf(vnew, fabsf(vs[g]));
-#pragma unroll
-      for (int g = 0; g < S::kGroups; ++g) vr[g] = vs[g] == 0.f ? 0.f : vs[g] / vnew * kWeight;
-      if (vnew != vmax) vcorr = vmax / vnew;
-      vmax = vnew;
+    for (int g = 0; g < S::kGroups; ++g) {
+      ve[g] = min((int)(__float_as_uint(vs[g]) >> 23 & 255), 253) - 127;
+      vf[g] = vs[g] * __uint_as_float((uint32_t)(127 - ve[g]) << 23);
+      alike = alike && ve[g] == ve[0];
     }
 
     uint32_t pf[S::kSets][S::kHalves][S::kGroups][2];
     uint64_t corr[S::kSets];
 #pragma unroll
     for (int s = 0; s < S::kSets; ++s) {
-      float cr[2], mu[2];
+      float cr[2], mu[2], vr[S::kGroups][2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        float mx = m[s][k];
+        float most[S::kGroups];  // of a group's z
 #pragma unroll
-        for (int g = 0; g < S::kGroups; ++g) mx = fmaxf(mx, fmaxf(z[s][g][k], z[s][g][2 + k]));
-        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 4));
-        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 8));
-        mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 16));
+        for (int g = 0; g < S::kGroups; ++g) {
+          most[g] = fmaxf(z[s][g][k], z[s][g][2 + k]);
+          if (g && alike) most[0] = fmaxf(most[0], most[g]);
+        }
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) most[0] = fmaxf(most[0], __shfl_xor_sync(~0u, most[0], o));
+        if (!alike)
+#pragma unroll
+          for (int g = 1; g < S::kGroups; ++g)
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) most[g] = fmaxf(most[g], __shfl_xor_sync(~0u, most[g], o));
+        float mx = fmaxf(m[s][k], most[0]);
+        if (!alike)
+#pragma unroll
+          for (int g = 1; g < S::kGroups; ++g) mx = fmaxf(mx, most[g]);
         mu[k] = mx == -CUDART_INF_F ? 0.f : mx;
-        cr[k] = exp2_fast(m[s][k] - mu[k]);
+        const float fall = m[s][k] - mu[k], held = exponent(top[s][k]);
+        float high = fmaxf(top[s][k] + fall, most[0] - mu[k] + ve[0]);
+        if (!alike)
+#pragma unroll
+          for (int g = 1; g < S::kGroups; ++g) high = fmaxf(high, most[g] - mu[k] + ve[g]);
         m[s][k] = mx;
-        l[s][k] *= cr[k];
+        top[s][k] = high;
+        const float hold = exponent(high);
+        l[s][k] *= exp2_fast(fall);
+        cr[k] = exp2_fast(fall + (held - hold));
+#pragma unroll
+        for (int g = 0; g < S::kGroups; ++g) {
+          const int ex = ve[g] + kWeight + 127 - exponent_bits(hold);
+          vr[g][k] = vf[g] * __uint_as_float((uint32_t)min(max(ex, 1), 254) << 23);
+        }
       }
-      corr[s] = f2_pack(cr[0] * vcorr, cr[1] * vcorr);
+      corr[s] = f2_pack(cr[0], cr[1]);
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g)
 #pragma unroll
@@ -886,7 +906,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
           for (int k = 0; k < 2; ++k) {
             const float zz = z[s][g][2 * t + k], pr = exp2_fast(zz - mu[k]);
             l[s][k] += pr;
-            wt[k] = pr * vr[g];
+            wt[k] = pr * vr[g][k];
             if (masked && zz == -CUDART_INF_F) wt[k] = 0.f;  // 0, whatever the scale is
           }
           uint32_t a, b;
@@ -952,7 +972,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
     const Desc e = s_desc[w][edesc];
     cdesc = cdesc == S::kStages ? 0 : cdesc + 1;
     const bool whole = e.whole, last = !more && it + 1 == copied;
-    float inv[S::kSets][2];
+    float inv[S::kSets][2], unit[S::kSets][2];
 #pragma unroll
     for (int s = 0; s < S::kSets; ++s)
 #pragma unroll
@@ -962,8 +982,10 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
         sum += __shfl_xor_sync(~0u, sum, 8);
         sum += __shfl_xor_sync(~0u, sum, 16);
         l[s][k] = sum;
-        // o / l first: the average code is small, the block scale may not be
-        inv[s][k] = sum == 0.f ? 0.f : __fdiv_rn(1.f / kWeight, sum);
+        // o / l first: that is small, the block scales may not be
+        inv[s][k] = sum == 0.f ? 0.f : __fdiv_rn(1.f / (1 << kWeight), sum);
+        const int ex = exponent_bits(exponent(top[s][k]));  // -127 to 126
+        unit[s][k] = __uint_as_float(ex == -127 ? 1u << 22 : (uint32_t)(ex + 127) << 23);
       }
     if (!whole) {
       // Its place: the ring if the warp is done, else a slot in the workspace.
@@ -981,7 +1003,8 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
         for (int j = 0; j < S::kTiles; ++j) {
           const float2 x = f2_unpack(o[s][j][0]), y = f2_unpack(o[s][j][1]);
           ((float4 *)(part + S::kStats))[(s * S::kTiles + j) * 32 + lane] =
-              make_float4(x.x * inv[s][0] * vmax, x.y * inv[s][1] * vmax, y.x * inv[s][0] * vmax, y.y * inv[s][1] * vmax);
+              make_float4(x.x * inv[s][0] * unit[s][0], x.y * inv[s][1] * unit[s][1], y.x * inv[s][0] * unit[s][0],
+                          y.y * inv[s][1] * unit[s][1]);
         }
       }
       continue;
@@ -993,7 +1016,8 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
 #pragma unroll
       for (int j = 0; j < S::kTiles; ++j) {
         const float2 a = f2_unpack(o[s][j][0]), b = f2_unpack(o[s][j][1]);
-        x[s * S::kTiles + j] = make_float4(a.x * inv[s][0] * vmax, a.y * inv[s][1] * vmax, b.x * inv[s][0] * vmax, b.y * inv[s][1] * vmax);
+        x[s * S::kTiles + j] = make_float4(a.x * inv[s][0] * unit[s][0], a.y * inv[s][1] * unit[s][1],
+                                              b.x * inv[s][0] * unit[s][0], b.y * inv[s][1] * unit[s][1]);
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) ml[s][k] = make_float2(m[s][k], l[s][k]);

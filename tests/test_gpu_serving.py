@@ -400,6 +400,62 @@ def test_attend_large_scores_and_scales(V):
     check_attend(V, c, "int8", [150, 20], [2, 1], 8, "f32", "f32", seed=2, scale=0.0)
 
 
+def check_rows_by_themselves(c, kind, lens, fresh, hq, table, q, window=0):
+    """Outputs against the definition, each row by its own terms alone: the bound
+    at the head of this file with the row's largest sum of p_j |v_jd| over sum p_j
+    in place of the largest |v|.  A weight in two binary16 halves, its row's
+    largest at 2^12 or more, adds half of 2^-24 per key, 2^-37 of the largest term:
+    below 2^-20 of that sum for a few hundred keys of codes up to 448."""
+    starts = np.concatenate([[0], np.cumsum(fresh)]).astype(np.int32)
+    n, D, P, h = int(starts[-1]), c.head_dim, c.page_size, c.n_kv_heads
+    out, lse = torch.zeros(n, hq, D, device="cuda"), torch.zeros(n, hq, device="cuda")
+    c.attend(q, out, dev(lens, torch.int32), dev(starts), dev(table), c.attend_workspace(hq, max(fresh)), max_new=max(fresh),
+             window=window, lse=lse)
+    (kc, vc), (ks, vs) = codes_of(c)
+    q64, got = q.double().cpu().numpy(), out.double().cpu().numpy()
+    for i, f in enumerate(fresh):
+        for t in range(f):
+            p = lens[i] - f + t
+            keys = np.arange(max(0, p - window + 1) if window else 0, p + 1)
+            b, o = table[i, keys // P], keys % P
+            k, v = (S.decode(x[b, :, o], kind) * s[b][:, :, None] for x, s in ((kc, ks), (vc, vs)))
+            for y in range(hq):
+                kv = y // (hq // h)
+                x = q64[starts[i] + t, y] * float(np.float32(D ** -0.5))
+                z = k[:, kv] @ x
+                e = np.exp(z - z.max())
+                own = (e @ np.abs(v[:, kv]) / e.sum()).max()
+                tol = (2.0 ** -17 * (np.abs(k[:, kv]) @ np.abs(x)).max() + 2.0 ** -16) * own
+                err = np.abs(got[starts[i] + t, y] - e @ v[:, kv] / e.sum()).max()
+                assert err <= tol, (i, t, y, err / own, tol / own)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("hq,fresh,d", [(1, 4, 64), (4, 1, 128), (4, 2, 128), (4, 7, 64), (2, 2, 256), (6, 2, 256), (3, 5, 80)])
+def test_attend_scales_far_apart(V, kind, hq, fresh, d):
+    """Value scales of the pages up to 2^100 apart.  A row is exact by its own
+    terms, whatever the scales of pages that it does not see (a later token's,
+    those before its window) and of pages that it weighs at almost nothing."""
+    c = new_cache(V, 30, 1, 16, d, kind)
+    fill_cache(c, d, kind)
+    g = torch.Generator("cuda").manual_seed(hq)
+    q = torch.randn(2 * fresh, hq, d, generator=g, device="cuda")
+    table = np.arange(30, dtype=np.int32).reshape(2, 15)
+    # the last token alone sees page 1; the pages of the window's first rows
+    c.v_scale[1] *= 2.0 ** 40
+    for lens in ([16 + fresh - 1, 16 + fresh], [17, 18 + fresh]):
+        check_rows_by_themselves(c, kind, [max(x, fresh) for x in lens], [fresh] * 2, hq, table, q)
+    c.v_scale.copy_(torch.pow(2.0, 8.0 * torch.arange(30, device="cuda").flip(0) - 120)[:, None])
+    check_rows_by_themselves(c, kind, [230, 37], [fresh] * 2, hq, table, q, window=17)
+    check_rows_by_themselves(c, kind, [230, 37], [fresh] * 2, hq, table, q)
+    # any order of scales, scores from -60 to 60
+    for seed in range(3):
+        c.v_scale.copy_(torch.pow(2.0, torch.randint(-50, 50, c.v_scale.shape, generator=g, device="cuda").float()))
+        size = 15 / float((q[0, 0] @ (c.k[0, 0].view(torch.int8).float() if kind == "int8" else
+                                      c.k[0, 0].view(torch.float8_e4m3fn).float()).T).abs().max()) / float(c.k_scale[0, 0])
+        check_rows_by_themselves(c, kind, [240, 100], [fresh] * 2, hq, table, q * size * d ** 0.5)
+
+
 def test_attend_query_zero_and_wide_range(V):
     c = new_cache(V, 12, 1, 16, 64, "int8")
     fill_cache(c, 6, "int8")
