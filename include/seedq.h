@@ -462,7 +462,8 @@ typedef struct {
   uint64_t workspace_bytes;
 } seedq_attend_args;
 
-/* 0 for arguments that seedq_kv_attend would refuse.  Host function. */
+/* Enough for any number of new tokens up to max_new; 0 for arguments that
+ * seedq_kv_attend would refuse.  Host function. */
 uint64_t seedq_kv_attend_workspace_bytes(const seedq_kv_cache *cache, int32_t n_heads,
                                          int32_t max_new);
 seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_args *args,

@@ -1208,7 +1208,13 @@ extern "C" {
 
 uint64_t seedq_kv_attend_workspace_bytes(const seedq_kv_cache *cache, int32_t n_heads, int32_t max_new) {
   if (check(cache, n_heads, max_new) != SEEDQ_OK) return 0;
-  return with_shape(shape_for(cache, n_heads, max_new), [](auto dp, auto mode) { return workspace_bytes<dp.value, mode.value>(); });
+  // The most that any number of new tokens up to max_new takes: tiles of 4 rows,
+  // with more warps, take more than tiles of 8.
+  uint64_t most = 0;
+  Plan s = shape_for(cache, n_heads, 1);
+  for (const int last = shape_for(cache, n_heads, max_new).mode; s.mode <= last; ++s.mode)
+    most = std::max(most, with_shape(s, [](auto dp, auto mode) { return workspace_bytes<dp.value, mode.value>(); }));
+  return most;
 }
 
 seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_args *args, void *cuda_stream) {

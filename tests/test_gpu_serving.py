@@ -456,6 +456,26 @@ def test_attend_scales_far_apart(V, kind, hq, fresh, d):
         check_rows_by_themselves(c, kind, [240, 100], [fresh] * 2, hq, table, q * size * d ** 0.5)
 
 
+@pytest.mark.parametrize("hq,h,d", [(32, 8, 128), (8, 8, 128), (4, 2, 64), (8, 1, 256)])
+def test_attend_workspace_for_more_tokens(V, hq, h, d):
+    """A workspace for up to n new tokens serves every smaller number, one after another."""
+    c = new_cache(V, 60, h, 16, d, "int8")
+    fill_cache(c, d, "int8")
+    lens, table = [400, 90], np.array([list(range(25)), list(range(25, 50))], np.int32)
+    for most in (2, 5, 16):
+        ws = c.attend_workspace(hq, most)
+        for n in (1, 2, 5, 16, 1):
+            if n > most:
+                continue
+            q = torch.randn(2 * n, hq, d, device="cuda")
+            res = []
+            for w in (ws, c.attend_workspace(hq, n)):
+                out = torch.zeros(2 * n, hq, d, device="cuda")
+                c.attend(q, out, dev(lens, torch.int32), dev([0, n, 2 * n], torch.int32), dev(table), w, max_new=n)
+                res.append(out)
+            assert torch.equal(*res), (most, n)
+
+
 def test_attend_query_zero_and_wide_range(V):
     c = new_cache(V, 12, 1, 16, 64, "int8")
     fill_cache(c, 6, "int8")

@@ -194,6 +194,14 @@ def test_attend_refuses(Q, kw, status):
     assert L.seedq_kv_attend(None, C.byref(_attend(Q)), None) == 1
 
 
+@pytest.mark.parametrize("dim", [16, 64, 80, 128, 144, 256])
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 8, 9, 17])
+def test_attend_workspace_serves_fewer_tokens(Q, dim, group):
+    d = _desc(Q, head_dim=dim, token_stride=dim, head_stride=16 * dim, page_stride=32 * dim)
+    n = [Q.lib().seedq_kv_attend_workspace_bytes(C.byref(d), 2 * group, m) for m in [*range(1, 34), 1000, (1 << 31) - 1]]
+    assert n[0] > 0 and n == sorted(n)
+
+
 @pytest.mark.parametrize("n,heads", [(1 << 30, 4), ((1 << 31) - 1, 2), (((1 << 31) - 32) // 8, 16)])
 def test_attend_refuses_more_rows_than_it_numbers(Q, n, heads):
     d = _desc(Q)
