@@ -4,8 +4,9 @@
 Like the rest of the binding it marshals arguments and computes nothing: every
 buffer is the caller's torch tensor, every length and page number stays on the
 device, and calls only enqueue work on the given stream (torch's current stream
-by default).  What the C ABI cannot see (shapes, types, devices) is checked
-here and raises ValueError; what it refuses itself raises SeedQError.
+by default).  The tensors' device must be the current one.  What the C ABI
+cannot see (shapes, types, devices) is checked here and raises ValueError; what it
+refuses itself raises SeedQError.
 """
 from __future__ import annotations
 
@@ -28,6 +29,9 @@ def _want(ok, what: str):
 
 
 def _stream(s, device) -> int:
+    # The library launches on the current device, whose kernels another device's pointers would reach.
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the current device ({torch.cuda.current_device()}) is not the tensors' ({device})")
     if s is None:
         return torch._C._cuda_getCurrentRawStream(device.index)
     return s if isinstance(s, int) else s.cuda_stream

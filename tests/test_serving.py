@@ -259,8 +259,39 @@ def test_plan_of_fewer_requests_hands_on_no_others(Q, monkeypatch):
     plan = V.BatchPlan(4, 16, device="cpu")
     base = [t.data_ptr() for t in (plan.seq_lens, plan.starts, plan.status)]
     monkeypatch.setattr(Q, "lib", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)  # as the CPU's tensors have it
     i = torch.zeros(4, dtype=torch.int32)
     for n in (4, 2, 2, 3, 1, 4):
         plan.build(i, i[:n], torch.zeros((4, 3), dtype=torch.int32), i, i[:1], 16, stream=0)
         assert (plan.seq_lens.shape[0], plan.starts.shape[0], plan.status.shape[0]) == (n, n + 1, n)
         assert [t.data_ptr() for t in (plan.seq_lens, plan.starts, plan.status)] == base
+
+
+@pytest.mark.parametrize("stream", [None, 0])
+def test_binding_refuses_another_device_than_the_current_one(Q, monkeypatch, stream):
+    """The library launches on the current device; tensors of another one never reach it."""
+    from paper_2609_38477_gb300 import serving as V
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: pytest.fail(f"{name} is called")
+
+    monkeypatch.setattr(Q, "lib", Library)
+    z = lambda *shape, dt=torch.int32: torch.zeros(shape, dtype=dt, device="meta")  # noqa: E731
+    cache = V.KVCache.__new__(V.KVCache)
+    cache.n_pages, cache.n_kv_heads, cache.page_size, cache.head_dim, cache.device, cache._ref = 4, 2, 16, 64, z(1).device, None
+    plan = V.BatchPlan(2, 4, device="meta")
+    f = lambda *shape: z(*shape, dt=torch.float32)  # noqa: E731
+    calls = [lambda: plan.build(z(2), z(2), z(2, 3), z(4), z(1), 16, stream=stream),
+             lambda: cache.append(f(3, 2, 64), f(3, 2, 64), z(3, dt=torch.int64), stream=stream),
+             lambda: cache.gather(z(3, dt=torch.int64), f(3, 2, 64), f(3, 2, 64), stream=stream),
+             lambda: cache.attend(f(2, 4, 64), f(2, 4, 64), z(2), z(3), z(2, 3), z(8, dt=torch.uint8), stream=stream)]
+    for current in (0, 1):
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+        for call in calls:
+            with pytest.raises(ValueError, match="current device"):
+                call()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current device"):  # where the log probabilities, for which no tensor can stand in, ask
+        V._stream(stream, torch.device("cuda", 1))
+    assert V._stream(7, torch.device("cuda", 0)) == 7
