@@ -79,14 +79,22 @@ class Decoder:
         Q.gemm_multi(layers, [x] * len(layers), x.shape[0], out)
         return out
 
+    def _advance(self):
+        self.seq_lens[:self.plan.n_requests].copy_(self.plan.seq_lens)
+        self.free_count.copy_(self.plan.free_count)
+
     def step(self, tokens, n_new):
         """The next tokens (int64, one request's after another's) of every
         request, n_new of each (int32; -1 ends a request); of fewer requests
         than the decoder was made for, the others wait.  Returns the logits
-        of every token; plan and seq_lens describe the step."""
+        of every token, none where requests only end; plan and seq_lens describe
+        the step."""
         s, n = self.spec, tokens.shape[0]
         p = self.plan
         p.build(self.seq_lens, n_new, self.table, self.free, self.free_count, self.page_size)
+        if n == 0:  # requests only end or wait
+            self._advance()
+            return torch.empty((0, s.vocab), device="cuda")
         x = self.embedding[tokens].float()
         angles = p.positions[:n, None].float() * self.freqs
         for block, cache in zip(self.blocks, self.caches):
@@ -101,8 +109,7 @@ class Decoder:
             gate, up = self._products(rms_norm(x, block["mlp_norm"]), ("gate", "up"), block)
             act = (torch.nn.functional.silu(gate) * up).bfloat16()
             x = x + self._products(act, ("down",), block)[0]
-        self.seq_lens[:p.n_requests].copy_(p.seq_lens)
-        self.free_count.copy_(p.free_count)
+        self._advance()
         return self._products(rms_norm(x, self.final_norm), ("head",), {"head": self.head})[0]
 
     def score(self, logits, targets=None, top_k: int = 1, temperature: float = 1.0):

@@ -136,3 +136,17 @@ def test_step_of_fewer_requests(G):
         a, b = (x.step(tokens[:sum(new)], t(*new)) for x in (d, e))
         assert float((a - b).abs().max()) <= 0.01 * float(b.abs().max())
     assert d.seq_lens.tolist() == [9, 13, 7] and e.seq_lens.tolist() == [9, 13]
+
+
+def test_step_that_only_ends_requests(G):
+    """The last requests of a batch end together, alone in a step; their pages are there again."""
+    d = G.synthetic_decoder("tiny", max_requests=2, n_pages=3)
+    t = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    for _ in range(3):
+        logits = d.step(torch.arange(12, device="cuda"), t(4, 8))
+        assert logits.shape == (12, d.spec.vocab) and int(d.free_count) == 1
+        assert d.step(none, t(0, 0)).shape == (0, d.spec.vocab) and d.seq_lens.tolist() == [4, 8] and int(d.free_count) == 1
+        assert d.step(none, t(-1, -1)).shape == (0, d.spec.vocab)
+        assert d.seq_lens.tolist() == [0, 0] and int(d.free_count) == 3
+        assert sorted(d.free.tolist()) == [0, 1, 2]
