@@ -88,14 +88,16 @@ class Decoder:
         request, n_new of each (int32; -1 ends a request); of fewer requests
         than the decoder was made for, the others wait.  Returns the logits
         of every token, none where requests only end; plan and seq_lens describe
-        the step."""
+        the step.  Tokens of a request that the plan could not serve (plan.status)
+        have logits of NaN, and the request is as it was before."""
         s, n = self.spec, tokens.shape[0]
         p = self.plan
         p.build(self.seq_lens, n_new, self.table, self.free, self.free_count, self.page_size)
         if n == 0:  # requests only end or wait
             self._advance()
             return torch.empty((0, s.vocab), device="cuda")
-        x = self.embedding[tokens].float()
+        # tokens without a slot have no keys to attend to: NaN, which stays in its row
+        x = self.embedding[tokens].float().masked_fill(p.slots[:n, None] < 0, float("nan"))
         angles = p.positions[:n, None].float() * self.freqs
         for block, cache in zip(self.blocks, self.caches):
             h = rms_norm(x, block["attn_norm"])
@@ -151,6 +153,8 @@ def main():
     tokens = torch.tensor(sum(prompts, []), device="cuda")
     for step in range(6):
         logits = d.step(tokens, n_new)
+        if any(d.plan.status.tolist()):
+            raise RuntimeError(f"step {step}: {[serving.STATUS[x] for x in d.plan.status.tolist()]}")
         last = (d.plan.starts[1:4] - 1).long()  # each request's newest token
         _, entropy, _, top, best = d.score(logits[last].contiguous(), top_k=3)
         tokens = best[:, 0].long()

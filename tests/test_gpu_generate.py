@@ -150,3 +150,32 @@ def test_step_that_only_ends_requests(G):
         assert d.step(none, t(-1, -1)).shape == (0, d.spec.vocab)
         assert d.seq_lens.tolist() == [0, 0] and int(d.free_count) == 3
         assert sorted(d.free.tolist()) == [0, 1, 2]
+
+
+def test_step_that_refuses_a_request(G):
+    """The logits of a request that got no pages are NaN, its neighbours' what they are without it."""
+    t = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    tokens = torch.arange(16, device="cuda")
+    got = []
+    for new in ((1, 12, 3), (1, 0, 3)):
+        d = G.synthetic_decoder("tiny", max_requests=3, n_pages=3)
+        d.step(tokens, t(12, 1, 3))
+        mine = tokens[:16] if new[1] else torch.cat([tokens[:1], tokens[13:]])
+        d.free_count.fill_(0)
+        d.seq_lens[1] = 16 if new[1] else 1  # a full page: the next tokens want another
+        got.append((d.step(mine, t(*new)), d))
+    (a, d), (b, _) = got
+    assert d.plan.status.tolist() == [0, 1, 0] and d.seq_lens.tolist() == [13, 16, 6]
+    assert bool(a[1:13].isnan().all()) and not bool(a[:1].isnan().any()) and not bool(a[13:].isnan().any())
+    own = torch.cat([a[:1], a[13:]])
+    assert float((own - b).abs().max()) <= 0.01 * float(b.abs().max())
+    logp, entropy, rank, top, _ = d.score(a, torch.zeros(16, dtype=torch.int64, device="cuda"), top_k=2)
+    assert bool(logp[1:13].isnan().all()) and bool(top[1:13].isnan().all()) and bool((rank[1:13] == -1).all())
+
+
+def test_example_says_what_the_plan_refused(G, monkeypatch):
+    """A page too few for the prompts: an error, and no token is taken from logits of NaN."""
+    make = G.synthetic_decoder
+    monkeypatch.setattr(G, "synthetic_decoder", lambda: make("tiny", n_pages=2))
+    with pytest.raises(RuntimeError, match="no pages"):
+        G.main()
