@@ -51,13 +51,18 @@ def _ints(t, n, dtype, device, name: str):
 
 
 def _table(t, n, device):
-    if not (t.dtype is torch.int32 and t.ndim == 2 and t.shape[0] >= n and t.stride(1) == 1 and t.device == device):
+    if not (t.dtype is torch.int32 and t.ndim == 2 and t.shape[0] >= n and (t.stride(1) == 1 or t.shape[1] == 1) and t.device == device):
         raise ValueError(f"block_table: int32, {n} or more rows with contiguous entries on {device} are wanted")
 
 
 def _row_stride(t) -> int:
     """The row stride of a matrix; torch leaves that of a single row open."""
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _same_strides(a, b) -> bool:
+    """Of tensors of one shape, but for those of single entries."""
+    return all(x == y or n < 2 for n, x, y in zip(a.shape, a.stride(), b.stride()))
 
 
 def _code_strides(t):
@@ -165,7 +170,7 @@ class KVCache:
     def _pair(self, k, v, slots):
         n, dev = k.shape[0], self.device
         dt, st = _rows(k, "k", n, self.n_kv_heads, self.head_dim, dev)
-        if v.shape != k.shape or v.dtype is not k.dtype or v.device != dev or v.stride() != st:
+        if v.shape != k.shape or v.dtype is not k.dtype or v.device != dev or (v.stride() != st and not _same_strides(k, v)):
             raise ValueError("v: the shape, type, strides and device of k are wanted")
         _ints(slots, n, torch.int64, dev, "slots")
         return n, dt, st
@@ -216,7 +221,7 @@ def token_logprobs(logits, targets, logprob, entropy, rank, top_logprob, top_ind
     and top_index (n, k) int32 are written.  Each of them may be None (logprob
     and rank only without targets, the two top tensors only together)."""
     dt, st = DTYPES.get(logits.dtype), logits.stride()
-    if len(st) != 2 or dt is None or st[1] != 1 or not logits.is_cuda:
+    if len(st) != 2 or dt is None or (st[1] != 1 and logits.shape[1] != 1) or not logits.is_cuda:
         raise ValueError("logits: (rows, vocab) float32, bfloat16 or float16 with contiguous rows on a CUDA device is wanted")
     (n, vocab), dev = logits.shape, logits.device
     pt = pl = pe = pr = px = pi = None

@@ -244,6 +244,31 @@ def test_append_strides_and_alignment(V):
         assert bool((o[:, 2 * h * d:] == 0).all()) and out[0] == 0
 
 
+def test_strides_of_single_entries(V):
+    """One token's or one head's keys and values with unlike strides there, a table of one page, logits of one token."""
+    for n, h in ((1, 4), (5, 1), (1, 1)):
+        x = torch.randn(2, n, h, 64, device="cuda")
+        k = x[0]
+        v = torch.zeros(4096, device="cuda").as_strided((n, h, 64), [y if m > 1 else 777 for m, y in zip(k.shape, k.stride())])
+        v.copy_(x[1])
+        slots = torch.arange(n, device="cuda")
+        a, b = (new_cache(V, 2, h, 16, 64, "int8") for _ in range(2))
+        a.append(k, x[1], slots)
+        b.append(k, v, slots)
+        assert torch.equal(a.k[0, :, :n], b.k[0, :, :n]) and torch.equal(a.v[0, :, :n], b.v[0, :, :n])
+        got = torch.zeros_like(k)
+        v.zero_()
+        b.gather(slots, got, v)
+        for i, y in enumerate((got, v)):
+            assert float((y - x[i]).abs().max()) < 0.05
+    table = torch.zeros(6, dtype=torch.int32, device="cuda").as_strided((3, 1), (1, 7))
+    table.fill_(-1)
+    plan, seq = V.BatchPlan(3, 8), torch.zeros(3, dtype=torch.int32, device="cuda")
+    plan.build(seq, dev([1, 2, 3], torch.int32), table, torch.arange(5, dtype=torch.int32, device="cuda"), dev([5], torch.int32), 16)
+    assert table[:, 0].tolist() == [4, 3, 2] and plan.slots.tolist() == [64, 48, 49, 32, 33, 34, -1, -1]
+    check_score(V, torch.randn(6, device="cuda").as_strided((3, 1), (1, 7)), [0, -1, 1], 1.0, 2)
+
+
 @pytest.mark.parametrize("kind", ["int8", "e4m3"])
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("heads,page,dim", [(3, 256, 128), (5, 256, 16), (2, 144, 256), (1, 240, 96), (7, 128, 64)])

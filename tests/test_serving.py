@@ -295,3 +295,40 @@ def test_binding_refuses_another_device_than_the_current_one(Q, monkeypatch, str
     with pytest.raises(ValueError, match="current device"):  # where the log probabilities, for which no tensor can stand in, ask
         V._stream(stream, torch.device("cuda", 1))
     assert V._stream(7, torch.device("cuda", 0)) == 7
+
+
+def test_strides_of_single_entries_do_not_matter(Q, monkeypatch):
+    """torch leaves the stride of a dimension of one entry open: keys and values of
+    one token or one head, a table of one page, whatever their strides there."""
+    from paper_2609_38477_gb300 import serving as V
+
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: calls.append((name, a)) or 0
+
+    monkeypatch.setattr(Q, "lib", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)
+    cache = V.KVCache.__new__(V.KVCache)
+    cache.page_size, cache.head_dim, cache.device, cache._ref = 16, 64, torch.device("cpu"), None
+    i64 = torch.zeros(9, dtype=torch.int64)
+    for n, h in ((1, 4), (5, 1), (1, 1), (0, 4)):
+        cache.n_kv_heads = h
+        k = torch.zeros(n, h, 64)
+        v = torch.zeros(4096).as_strided((n, h, 64), [x if m > 1 else 777 for m, x in zip(k.shape, k.stride())])
+        for a, b in ((k, v), (v, k)):
+            assert a.stride() != b.stride()
+            cache.append(a, b, i64, stream=0)
+            cache.gather(i64, a, b, stream=0)
+            for name, at in (("seedq_kv_append", 4), ("seedq_kv_gather", 6)):
+                args = next(c for f, c in reversed(calls) if f == name)
+                assert all(m < 2 or x == s for m, x, s in zip((n, h), args[at:at + 2], a.stride()))
+    cache.n_kv_heads = 4
+    with pytest.raises(ValueError, match="strides"):
+        cache.append(torch.zeros(2, 4, 64), torch.zeros(4, 2, 64).transpose(0, 1), i64, stream=0)
+    plan = V.BatchPlan(3, 4, device="cpu")
+    i = torch.zeros(4, dtype=torch.int32)
+    table = torch.zeros(6, dtype=torch.int32).as_strided((3, 1), (1, 7))
+    plan.build(i, i[:3], table, i, i[:1], 16, stream=0)
+    assert calls[-1][0] == "seedq_batch_plan" and calls[-1][1][5:7] == (1, 1)
