@@ -314,11 +314,12 @@ __device__ __forceinline__ T load_fresh(const float *x) {
 // Joins n parts of an entry into `to`, or, if to is null, writes the entry's
 // output.  A part holds m (in units of log2) and l of every column and the
 // columns' averages o = sum / l as the products' accumulators lie in the lanes;
-// it weighs l 2^m.  Averages, not sums, are kept, so nothing overflows on the
-// way.  The parts are from[0..n-1], or, without `from`, the second of the two
-// slots of the CTA at `slots` and the first ones of the n - 1 CTAs behind it.
-// The warp takes the tiles first, first + step, ...; a lane reads the statistics
-// of its two columns itself, so no barrier is needed.
+// it weighs l 2^m.  Averages, not sums, are kept, of the parts and of what is
+// joined so far, so nothing overflows on the way.  The parts are from[0..n-1],
+// or, without `from`, the second of the two slots of the CTA at `slots` and the
+// first ones of the n - 1 CTAs behind it.  The warp takes the tiles first, first +
+// step, ...; a lane reads the statistics of its two columns itself, so no barrier
+// is needed.
 template <typename S, int MODE>
 __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const float *const *from, const float *slots,
                                      float *to, int first, int step) {
@@ -348,24 +349,25 @@ __device__ __forceinline__ void join(const Args &p, const Desc &e, int n, const 
         m1 = fmaxf(m1, m[k].y);
       }
       const float u0 = m0 == -CUDART_INF_F ? 0.f : m0, u1 = m1 == -CUDART_INF_F ? 0.f : m1;
-      const float s0 = exp2_fast(was0 - u0), s1 = exp2_fast(was1 - u1);
-      l0 *= s0, c[0] *= s0, c[2] *= s0;
-      l1 *= s1, c[1] *= s1, c[3] *= s1;
+      const float s0 = l0 * exp2_fast(was0 - u0), s1 = l1 * exp2_fast(was1 - u1);
+      l0 = s0, l1 = s1;
 #pragma unroll
       for (int k = 0; k < kAtATime; ++k) {
-        const float w0 = l[k].x == 0.f ? 0.f : l[k].x * exp2_fast(m[k].x - u0);
-        const float w1 = l[k].y == 0.f ? 0.f : l[k].y * exp2_fast(m[k].y - u1);
-        l0 += w0;
-        l1 += w1;
+        l[k].x = l[k].x == 0.f ? 0.f : l[k].x * exp2_fast(m[k].x - u0);
+        l[k].y = l[k].y == 0.f ? 0.f : l[k].y * exp2_fast(m[k].y - u1);
+        l0 += l[k].x;
+        l1 += l[k].y;
+      }
+      const float i0 = l0 == 0.f ? 0.f : 1.f / l0, i1 = l1 == 0.f ? 0.f : 1.f / l1;
+      c[0] *= s0 * i0, c[2] *= s0 * i0;
+      c[1] *= s1 * i1, c[3] *= s1 * i1;
+#pragma unroll
+      for (int k = 0; k < kAtATime; ++k) {
+        const float w0 = l[k].x * i0, w1 = l[k].y * i1;
         if (w0 != 0.f) c[0] = fmaf(w0, o[k].x, c[0]), c[2] = fmaf(w0, o[k].z, c[2]);
         if (w1 != 0.f) c[1] = fmaf(w1, o[k].y, c[1]), c[3] = fmaf(w1, o[k].w, c[3]);
       }
     }
-    const float i0 = l0 == 0.f ? 0.f : 1.f / l0, i1 = l1 == 0.f ? 0.f : 1.f / l1;
-    c[0] *= i0;
-    c[1] *= i1;
-    c[2] *= i0;
-    c[3] *= i1;
     if (to) {
       if (tile == 0 && nn == 0) {
         *(float2 *)(to + col) = make_float2(m0, m1);

@@ -501,6 +501,15 @@ def test_attend_workspace_for_more_tokens(V, hq, h, d):
             assert torch.equal(*res), (most, n)
 
 
+def test_attend_joins_of_large_values(V):
+    """Values near float32's largest over a context of many parts: an average of them is no larger."""
+    for hq, h, d, lens in ((4, 1, 128, [9000]), (8, 1, 64, [5000, 40]), (16, 1, 256, [7000])):
+        c = new_cache(V, sum(S.cdiv(x, 64) for x in lens), h, 64, d, "int8")
+        fill_cache(c, d, "int8")
+        c.v_scale.fill_(2.0 ** 119)
+        check_attend(V, c, "int8", lens, [1] * len(lens), hq, "f32", "f32", seed=d, q_size=0.1)
+
+
 def test_attend_query_zero_and_wide_range(V):
     c = new_cache(V, 12, 1, 16, 64, "int8")
     fill_cache(c, 6, "int8")
