@@ -481,7 +481,8 @@ seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_arg
  * Logits of -inf count as excluded (p = 0); a row of nothing else has logprob
  * and top_logprob -inf and entropy 0.  A row with a NaN or +inf has NaN for
  * logprob, entropy and top_logprob (NaN counts as the largest for top_index;
- * the rank of a row with a NaN is -1).
+ * the rank of a row with a NaN is -1).  A scale below 2^-120 takes logits that lie
+ * further apart than float32 holds for infinitely far apart in lse and entropy.
  *   logits     device, row r at r * row_stride elements of type dtype.
  *   targets    device int64, n_rows, or NULL (then logprob and rank are not
  *              written and may be NULL).  entropy may be NULL.  top_k 0..32.

@@ -182,6 +182,12 @@ __device__ __noinline__ uint64_t sort_keys(uint64_t x, int lane) {
   return x;
 }
 
+// scale (x - m); by halves where the difference alone passes float32's largest.
+__device__ __forceinline__ float scaled_difference(float scale, float x, float m) {
+  const float d = x - m;
+  return d == -CUDART_INF_F && x > -CUDART_INF_F ? 2.f * (scale * (0.5f * x - 0.5f * m)) : scale * d;
+}
+
 // Writes a row's results: key is the lane's entry of the list, the rest is the
 // same in all lanes.
 __device__ __noinline__ void write_row(const ScoreArgs &a, int64_t row, float m, float s1, float s2, int count, uint64_t key,
@@ -196,14 +202,14 @@ __device__ __noinline__ void write_row(const ScoreArgs &a, int64_t row, float m,
       a.logprob[row] = t == -1          ? 0.f
                        : !has || bad    ? CUDART_NAN_F
                        : empty          ? -CUDART_INF_F
-                                        : a.scale * (xt - m) - ln_s1;
+                                        : scaled_difference(a.scale, xt, m) - ln_s1;
       a.rank[row] = has && !isnan(m) ? count : -1;
     }
   }
   if (lane < a.top_k) {
     const float x = key_value(key);
     a.top_index[row * a.top_k + lane] = key ? key_index(key) : -1;
-    a.top_logprob[row * a.top_k + lane] = !key || empty ? -CUDART_INF_F : bad ? CUDART_NAN_F : a.scale * (x - m) - ln_s1;
+    a.top_logprob[row * a.top_k + lane] = !key || empty ? -CUDART_INF_F : bad ? CUDART_NAN_F : scaled_difference(a.scale, x, m) - ln_s1;
   }
 }
 

@@ -740,6 +740,26 @@ def test_score_orders_in_long_batches(V, v):
                 assert torch.allclose(a[ok], b[ok], rtol=2e-5, atol=2e-5), name
 
 
+def test_score_logits_further_apart_than_float32(V):
+    """Logits whose difference passes float32's largest while the scaled one does not."""
+    x = (torch.rand(4, 3000, device="cuda") * 2 - 1) * 3e38
+    x[:, 5], x[:, 2500], x[1, 7] = 3.3e38, -3.3e38, -float("inf")
+    x[2] = torch.where(x[2] > 0, 3.0e38, -3.0e38)
+    for dt in (torch.float32, torch.bfloat16):
+        for scale in (0.25, 1e-3, 2.0 ** -100):
+            check_score(V, x.to(dt), [2500, 7, 2999, 5], scale, 32)
+        many = x.to(dt).repeat(2000, 1)
+        t = torch.tensor([2500, 7, 2999, 5], device="cuda")
+        few, all_ = (torch.empty(n, device="cuda") for n in (4, 8000))
+        rk = torch.empty(8000, dtype=torch.int32, device="cuda")
+        V.token_logprobs(many[:4], t, few, None, rk, None, None, V.score_workspace(4, 3000), scale=0.25)
+        V.token_logprobs(many, t.repeat(2000), all_, None, rk, None, None, V.score_workspace(8000, 3000), scale=0.25)
+        assert torch.equal(few.repeat(2000), all_)
+    low = torch.full((1, 3000), -3.3e38, device="cuda")  # the list reaches logits that far below its first
+    low[0, 9] = 3.3e38
+    check_score(V, low, [17], 0.25, 32)
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("n,v", [(1, 20000), (3, 20003), (2500, 1500), (2500, 2047), (2000, 9000)])
 def test_score_rank_of_a_negative_zero(V, dtype, n, v):
