@@ -401,7 +401,9 @@ typedef struct {
  * final scale.  A page that receives an infinity or a NaN gets the scale NaN:
  * whatever reads it is NaN.
  * Errors: INVALID_ARG (NULL pointer, n_tokens < 0, unknown dtype), UNSUPPORTED
- * (head_dim, page_size, strides or alignment outside the above), CUDA.
+ * (head_dim, page_size, strides or alignment outside the above; more than a
+ * grid takes: n_tokens x n_kv_heads of 2^37, or in seedq_kv_gather n_tokens x
+ * n_kv_heads x head_dim of 2^42), CUDA.
  * n_tokens = 0 is a no-op. */
 seedq_status seedq_kv_append(const seedq_kv_cache *cache, const void *k, const void *v,
                              int32_t dtype, int64_t token_stride, int64_t head_stride,

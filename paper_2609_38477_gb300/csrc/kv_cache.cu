@@ -375,11 +375,13 @@ int32_t rows_aligned(const void *k, const void *v, int32_t dtype, int64_t ts, in
   return all % 32 == 0 ? 2 : all % 16 == 0;
 }
 
+int64_t append_ctas(const CacheArgs &a) {
+  const int64_t groups = (a.n + (1 << a.group_shift) - 1) >> a.group_shift;
+  return groups * ((a.c.n_kv_heads * 2 + kAppendWarps - 1) / kAppendWarps);
+}
 template <int KIND, int DT>
 void launch_append(const CacheArgs &a, cudaStream_t st) {
-  const int64_t groups = (a.n + (1 << a.group_shift) - 1) >> a.group_shift;
-  const int ctas = (a.c.n_kv_heads * 2 + kAppendWarps - 1) / kAppendWarps;
-  k_kv_append<KIND, DT><<<(unsigned)(groups * ctas), kAppendWarps * 32, 0, st>>>(a);
+  k_kv_append<KIND, DT><<<(unsigned)append_ctas(a), kAppendWarps * 32, 0, st>>>(a);
 }
 template <int KIND, int DT>
 void launch_gather(const CacheArgs &a, cudaStream_t st) {
@@ -424,6 +426,7 @@ seedq_status seedq_kv_append(const seedq_kv_cache *cache, const void *k, const v
   // token per warp 100).
   a.group_shift = 0;
   while (a.group_shift < 5 && (n_tokens >> a.group_shift) * cache->n_kv_heads * 2 > 2 * 152 * 48) ++a.group_shift;
+  if (append_ctas(a) > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
   kAppend[cache->kind][dtype](a, (cudaStream_t)cuda_stream);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
@@ -434,6 +437,7 @@ seedq_status seedq_kv_gather(const seedq_kv_cache *cache, const int64_t *slots, 
   CacheArgs a;
   const seedq_status st = prepare(cache, k, v, dtype, token_stride, head_stride, slots, n_tokens, a);
   if (st != SEEDQ_OK || n_tokens == 0) return st;
+  if (n_tokens * cache->n_kv_heads * cache->head_dim / 2048 >= INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
   kGather[cache->kind][dtype](a, (cudaStream_t)cuda_stream);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);

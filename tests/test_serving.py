@@ -166,6 +166,14 @@ def test_append_and_gather_refuse(Q, a):
     assert L.seedq_kv_append(None, *a, None) == 1
 
 
+@pytest.mark.parametrize("n", [(1 << 31) - 1, 1 << 30, (1 << 28) + 1])
+def test_append_and_gather_refuse_more_than_a_grid_takes(Q, n):
+    """More CTAs than a launch counts (rows of stride 0 make such sizes possible): refused, not cut short."""
+    d = _desc(Q, n_kv_heads=1024, head_dim=256, token_stride=256, head_stride=16 * 256, page_stride=1024 * 16 * 256)
+    assert Q.lib().seedq_kv_append(C.byref(d), FAKE, FAKE, 0, 0, 0, FAKE, n, None) == 6
+    assert Q.lib().seedq_kv_gather(C.byref(d), FAKE, n, FAKE, FAKE, 0, 0, 0, None) == 6
+
+
 def test_nothing_to_do_is_ok(Q):
     L, r = Q.lib(), C.byref(_desc(Q))
     assert L.seedq_kv_append(r, None, None, 0, 0, 0, None, 0, None) == 0
