@@ -179,3 +179,40 @@ def test_example_says_what_the_plan_refused(G, monkeypatch):
     monkeypatch.setattr(G, "synthetic_decoder", lambda: make("tiny", n_pages=2))
     with pytest.raises(RuntimeError, match="no pages"):
         G.main()
+
+
+@pytest.mark.parametrize("name,kind", [("tiny", "int8"), ("tiny_odd", "e4m3")])
+def test_decode_loop_caches_values(G, name, kind):
+    """The cached values of every layer against their own product: one rounding
+    under the page's scale, at most its largest number / 63.5 (E4M3: a sixteenth of a
+    number at most), and neither the keys nor another layer's values."""
+    d = G.synthetic_decoder(name, max_requests=2, n_pages=6, kind=kind)
+    s = d.spec
+    weights = [{k: dense(b[k]) for k in ("q", "v", "o", "gate", "up", "down")} for b in d.blocks]
+    rng = np.random.RandomState(5)
+    history = [[], []]
+    for new in ([7, 9], [1, 1], [1, 15], [12, 1]):
+        fresh = [[int(t) for t in rng.randint(0, s.vocab, n)] for n in new]
+        d.step(torch.tensor(fresh[0] + fresh[1], device="cuda"), torch.tensor(new, dtype=torch.int32, device="cuda"))
+        for r, m in enumerate(new):
+            history[r] += fresh[r]
+            n = len(history[r])
+            at = torch.arange(n, device="cuda")
+            slots, pos = d.table[r, at // d.page_size].long() * d.page_size + at % d.page_size, at[n - m:]
+            x = d.embedding[torch.tensor(fresh[r], device="cuda")].double()
+            for block, cache, w in zip(d.blocks, d.caches, weights):
+                h = norm(x, block["attn_norm"])
+                k, v = (torch.empty((n, s.n_kv_heads, s.head_dim), device="cuda") for _ in range(2))
+                cache.gather(slots, k, v)
+                own = (h @ w["v"].T).view(m, s.n_kv_heads, s.head_dim)
+                step = max(float(own.abs().max()), float(v.abs().max())) / 63
+                off = float((v[n - m:].double() - own).abs().max())
+                assert off <= (step if kind == "int8" else 4 * step) < 0.2 * float((k[n - m:].double() - own).abs().max())
+                q = rope((h @ w["q"].T).view(m, s.n_heads, s.head_dim), pos, d.freqs)
+                g = s.n_heads // s.n_kv_heads
+                z = torch.einsum("thd,jhd->thj", q, k.double().repeat_interleave(g, 1)) * s.head_dim ** -0.5
+                z = z.masked_fill((at > pos[:, None])[:, None], -np.inf)
+                o = torch.einsum("thj,jhd->thd", z.softmax(2), v.double().repeat_interleave(g, 1))
+                x = x + bf(o).reshape(m, -1) @ w["o"].T
+                h = norm(x, block["mlp_norm"])
+                x = x + bf(torch.nn.functional.silu(h @ w["gate"].T) * (h @ w["up"].T)) @ w["down"].T
