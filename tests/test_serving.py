@@ -267,7 +267,7 @@ def test_plan_of_fewer_requests_hands_on_no_others(Q, monkeypatch):
     plan = V.BatchPlan(4, 16, device="cpu")
     base = [t.data_ptr() for t in (plan.seq_lens, plan.starts, plan.status)]
     monkeypatch.setattr(Q, "lib", Library)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)  # as the CPU's tensors have it
+    monkeypatch.setattr(V, "_current_device", lambda: None)  # as the CPU's tensors have it
     i = torch.zeros(4, dtype=torch.int32)
     for n in (4, 2, 2, 3, 1, 4):
         plan.build(i, i[:n], torch.zeros((4, 3), dtype=torch.int32), i, i[:1], 16, stream=0)
@@ -295,11 +295,11 @@ def test_binding_refuses_another_device_than_the_current_one(Q, monkeypatch, str
              lambda: cache.gather(z(3, dt=torch.int64), f(3, 2, 64), f(3, 2, 64), stream=stream),
              lambda: cache.attend(f(2, 4, 64), f(2, 4, 64), z(2), z(3), z(2, 3), z(8, dt=torch.uint8), stream=stream)]
     for current in (0, 1):
-        monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+        monkeypatch.setattr(V, "_current_device", lambda: current)
         for call in calls:
             with pytest.raises(ValueError, match="current device"):
                 call()
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(V, "_current_device", lambda: 0)
     with pytest.raises(ValueError, match="current device"):  # where the log probabilities, for which no tensor can stand in, ask
         V._stream(stream, torch.device("cuda", 1))
     assert V._stream(7, torch.device("cuda", 0)) == 7
@@ -317,7 +317,7 @@ def test_strides_of_single_entries_do_not_matter(Q, monkeypatch):
             return lambda *a: calls.append((name, a)) or 0
 
     monkeypatch.setattr(Q, "lib", Library)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)
+    monkeypatch.setattr(V, "_current_device", lambda: None)
     cache = V.KVCache.__new__(V.KVCache)
     cache.page_size, cache.head_dim, cache.device, cache._ref = 16, 64, torch.device("cpu"), None
     i64 = torch.zeros(9, dtype=torch.int64)
