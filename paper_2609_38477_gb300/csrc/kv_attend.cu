@@ -15,18 +15,18 @@
 // own into the same sums.  q is scaled by a power of two per row, the weights
 // p_j s^v_j of a row by one that brings the largest so far of its own (keys that it
 // does not see count for nothing, whatever their scale) to 2^13, so binary16's
-// range never cuts off more than 2^-37 of it.  Each unit's
-// products start from zero and are added to float32 registers, so a long
-// context is not accumulated inside the tensor cores, which truncate.
+// range never cuts off more than 2^-37 of it.  Each unit's products start from
+// zero and are added to float32 registers, so a long context is not accumulated
+// inside the tensor cores, which truncate.
 //
 // What bounds it: the bytes of the cache, 2 head_dim per key and key-value
 // head.  At 8 rows a byte costs 16 operations, far below the balance, but every
 // code has to be widened (about 1.5 instructions) and multiplied.  Measured, 128
-// head dims: 4 contexts of about 121000, 32 query on 8 key-value heads, 162 us (6.1
-// TB/s, 90% of the copy rate); 64 of 2048 on 8 heads, 66 us with 32 query heads
-// (4.0 TB/s) and 78 with 64, where the instructions bound it; 16 tokens of 32 heads
-// over 32768 keys 90 us (tiles of 16 rows read the keys four times, from L2); one
-// request of 1000 12 us, the latency of lengths, page numbers, keys and the joins.
+// head dims: 4 contexts of about 121000, 32 query on 8 key-value heads, 160 us (6.2
+// TB/s, 91% of the copy rate); 64 of 2048 on 8 heads, 66 us with 32 query heads
+// (4.0 TB/s) and 80 with 64, where the instructions bound it; 16 tokens of 32 heads
+// over 32768 keys 93 us (tiles of 16 rows read and widen the keys four times), of 64
+// heads 162 (eight times); one request of 1000 12 us, the latency of lengths, page numbers, keys and the joins.
 //
 // Layout.  For keys a product's row is a token and its inner index the head
 // dim; the order of the inner index is free as long as q uses the same, so each
@@ -90,8 +90,8 @@ struct Shape {
   static constexpr int kStage = kMetaAt + 128;       // meta: per group both scales and a flag
   // 12 warps with a ring of 2 units or 8 with 3: tiles of 4 rows, few registers, take
   // 12 (64 requests of 2048, 32 heads on 8: 66 us, 8 warps 73); the work of 8 rows
-  // is as fast either way (64 on 8 heads: 78 us) and leaves fewer parts to join (16
-  // ragged requests up to 8192: 19 us, 12 warps 22).
+  // is about as fast either way (64 on 8 heads: 80 us, 12 warps 77) and leaves fewer
+  // parts to join (16 ragged requests up to 8192: 19.6 us, 12 warps 21.4).
   static constexpr int kWarps = MODE == 0 && DP <= 128 ? 12 : 8;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kStages = DP == 64 ? 4 : kWarps == 12 ? 2 : 3;  // units in a warp's ring
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(Shape<DP, MODE, HALVES>::kThreads, 1) k_attend
   // to 4 warps per CTA, one per scheduler, and so to more SMs (one request of 1000:
   // 12 us, with all warps 15).  Entries of one length (one request, or a batch in
   // step) are each cut for the same number of CTAs, so that no CTA has parts of two
-  // (one request of 4096: 14 us, else 16).  Else, where no entry is longer than a
+  // (one request of 4096: 14.5 us, else 16).  Else, where no entry is longer than a
   // few units per warp and than a share by kOver, the shares' ends move to the
   // nearest entry's: a join between CTAs costs 3 to 4 us (40 ragged requests up to
   // 1000, 32 heads on 8: 19 us, without 22; 100: 26 and 30; but 16 up to 2048, whose
@@ -1139,10 +1139,10 @@ struct Plan {
 };
 // Tiles of 4 rows where they hold all rows that share a head's keys (a decode
 // step of up to 4 query heads per key-value head, half the products of 8 rows:
-// 66 us for 64 requests of 2048, 32 heads on 8, else 78), else of 8 (5 to 8 rows in
-// tiles of 16: 113 us instead of 78), and of 16 where more than 8 rows would read
-// the keys again (16 tokens of 32 heads on 8 over 32768 keys: 90 us, else 109); 256
-// head dims leave no registers for 16.
+// 66 us for 64 requests of 2048, 32 heads on 8, else 80), else of 8 (5 to 8 rows in
+// tiles of 16: 119 us instead of 80), and of 16 where more than 8 rows would read
+// the keys again (16 tokens of 32 heads on 8 over 32768 keys: 93 us, else 111; of 32
+// on 32 over a window of 3000 25, else 22); 256 head dims leave no registers for 16.
 Plan shape_for(const seedq_kv_cache *c, int32_t n_heads, int32_t max_new) {
   Plan s;
   s.dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
@@ -1250,8 +1250,8 @@ seedq_status seedq_kv_attend(const seedq_kv_cache *cache, const seedq_attend_arg
   p.ctas_inv = ~0ull / (uint64_t)p.ctas + 1;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   return with_shape(shape_for(cache, a.n_heads, a.max_new), [&](auto dp, auto mode) {
-    // One half of a q in 16 bits: 16 tokens of 32 heads on 8 over 32768 keys take 90
-    // us, with both halves 98.  Rows of 4 carry both anyway.
+    // One half of a q in 16 bits: 16 tokens of 32 heads on 8 over 32768 keys take 93
+    // us, with both halves 102.  Rows of 4 carry both anyway.
     constexpr int kShort = mode.value == 0 ? 2 : 1;
     if (a.q_dtype == SEEDQ_F32)
       return cache->kind == SEEDQ_KV_INT8 ? launch<SEEDQ_KV_INT8, dp.value, mode.value, 2>(p, dev, stream)

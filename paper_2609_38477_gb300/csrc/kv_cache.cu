@@ -122,7 +122,7 @@ __device__ __forceinline__ void four_values(uint32_t w, uint64_t &x01, uint64_t 
 // again, from cache.
 //
 // Measured, 128 head dims: 4 prompts of 1024 tokens, 32 heads, bfloat16, 24 us
-// (4.2 TB/s, 62% of the copy rate; float32 45 us, 3.7 TB/s); 16 single tokens of
+// (4.2 TB/s, 62% of the copy rate; float32 46 us, 3.7 TB/s); 16 single tokens of
 // 8 heads 3.4 us, launch and three dependent reads.  28 warps per SM: 24, with
 // more registers, take 28 and, for 256 single tokens of 32 heads, 12 us instead
 // of 10; 32 take 24 and 10.
@@ -420,10 +420,10 @@ seedq_status seedq_kv_append(const seedq_kv_cache *cache, const void *k, const v
   const seedq_status st = prepare(cache, k, v, dtype, token_stride, head_stride, slots, n_tokens, a);
   if (st != SEEDQ_OK || n_tokens == 0) return st;
   // One token per warp until the warps fill the GPU twice over, then more.  Each may
-  // be a page of its own (32 heads, 256 single tokens: 10 us; measured before the
-  // shared memory, 13, and 14 with one token per warp, 17 at half the threshold, 57
-  // with 32), or all on a page (4 prompts of 1024, pages of 64: then 39 us, with one
-  // token per warp 100).
+  // be a page of its own (32 heads, 256 single tokens: 10.4 us, with one token per
+  // warp 11.5, with 32 38; 512: 17, 21 and 40), or all on a page (4 prompts of 1024,
+  // pages of 64: 23 us, with one token per warp 77, with 32 24).  At half the
+  // threshold 256 single tokens take 9.5 and the prompts as long, at twice 11.6 and 28.
   a.group_shift = 0;
   while (a.group_shift < 5 && (n_tokens >> a.group_shift) * cache->n_kv_heads * 2 > 2 * 152 * 48) ++a.group_shift;
   if (append_ctas(a) > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;

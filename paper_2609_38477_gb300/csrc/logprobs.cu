@@ -23,8 +23,8 @@
 // one 2^x per logit leave the SMs at half their rate for float32); few rows, the
 // latency of the joins.  Measured, 128256 logits: 2048 rows of float32 153 us
 // without targets and alternatives (6.9 TB/s, 101% of the copy rate), 171 with
-// targets and 5 alternatives (90%), 212 with 20; of bfloat16 86 us (90%), 117 with
-// targets, 190 with 20 alternatives as well, where instructions bound it; 16 rows
+// targets and 5 alternatives (90%), 213 with 20; of bfloat16 86 us (90%), 117 with
+// targets, 191 with 20 alternatives as well, where instructions bound it; 16 rows
 // of float32 with 20 alternatives 12 us.
 //
 // Split.  All rows' tiles form one sequence, cut into equal ranges, one per warp
