@@ -303,12 +303,16 @@ seedq_status seedq_fp64_fma_probe(int64_t iters, int32_t blocks_per_sm, double *
  * an 8-bit key/value cache each new token goes to (seedq_batch_plan), the
  * cache write and its inverse (seedq_kv_append, seedq_kv_gather), the
  * attention that reads the cache (seedq_kv_attend), and what a row of logits
- * says about a token (seedq_token_logprobs).  No paper counterpart: the paper
+ * says about a token (seedq_token_logprobs); rotary positions, also on the way
+ * into the cache (seedq_rotary_angles, seedq_rotate, seedq_kv_append_rotary);
+ * and beam search's choice with the pages of the chosen beams
+ * (seedq_beam_select, seedq_beam_reorder).  No paper counterpart: the paper
  * covers the weights only.
  *
- * All calls are hot calls: they validate on the host, enqueue one launch,
- * allocate nothing and do not synchronize; every length, slot and
- * page number stays on the device, so a step can be captured in a CUDA graph.
+ * All calls are hot calls: they validate on the host, enqueue one launch
+ * (seedq_beam_reorder two or more), allocate nothing and do not synchronize;
+ * every length, slot and page number stays on the device, so a step can be
+ * captured in a CUDA graph.
  * Kernels check what they read from device memory (pages, slots, offsets)
  * against the sizes given here and skip what is out of range. */
 
@@ -416,6 +420,70 @@ seedq_status seedq_kv_gather(const seedq_kv_cache *cache, const int64_t *slots, 
                              void *k, void *v, int32_t dtype, int64_t token_stride,
                              int64_t head_stride, void *cuda_stream);
 
+/* Rotary positions.  A pair (u, v) of a head's numbers at position p becomes
+ *   (u c - v s, v c + u s),  c = scale * cos(p w), s = scale * sin(p w)
+ * with a frequency w (radians per position) of each of rot_dim / 2 pairs: numbers
+ * i and i + rot_dim / 2 of the head (SEEDQ_ROPE_HALF), or 2i and 2i + 1
+ * (SEEDQ_ROPE_PAIRS).  Numbers from rot_dim on stay as they are.  Stretched and
+ * mixed frequencies for long contexts are the caller's (the binding's
+ * rotary_frequencies makes the usual ones). */
+enum { SEEDQ_ROPE_HALF = 0, SEEDQ_ROPE_PAIRS = 1 };
+#define SEEDQ_ROPE_MAX_DIM 1024
+#define SEEDQ_ROPE_MAX_HEADS 65536
+
+/* cos and sin of a step's tokens, made once for all layers:
+ * cos_sin[t][i] = (c, s) of positions[t] and pair i.
+ *   turns      device, half entries: w / (2 pi) in units of 2^-64, rounded (mod
+ *              2^64).  The angle is taken in whole numbers, so that any int32
+ *              position, negative ones too, is as exact as position 1.
+ *   positions  device int32, n_tokens (seedq_batch_plan's).
+ *   cos_sin    device, 8-byte aligned, n_tokens x half x 2 float32.
+ * Errors: INVALID_ARG (NULL pointer, half outside 1..SEEDQ_ROPE_MAX_DIM/2,
+ * n_tokens < 0, scale not finite), UNSUPPORTED (more than a grid takes), CUDA.
+ * n_tokens = 0 is a no-op. */
+seedq_status seedq_rotary_angles(const uint64_t *turns, int32_t half, float scale,
+                                 const int32_t *positions, int64_t n_tokens, float *cos_sin,
+                                 void *cuda_stream);
+
+/* Rotate every head of n_tokens tokens; computed in float32, rounded once to
+ * out_dtype.  x, out: device, token t of head h at t * token_stride + h *
+ * head_stride (elements), head_dim elements in a row.  out may be x itself (the
+ * same type and strides); other overlaps are not allowed.  cos_sin: n_tokens x
+ * rot_dim / 2 x 2, of seedq_rotary_angles.
+ * Errors: INVALID_ARG (NULL pointer, unknown type or layout, rot_dim odd or
+ * outside 2..head_dim, head_dim above SEEDQ_ROPE_MAX_DIM, n_tokens < 0, n_heads
+ * outside 0..SEEDQ_ROPE_MAX_HEADS, out = x of another type or strides),
+ * UNSUPPORTED (more than a grid takes), CUDA.  Without tokens or heads a no-op. */
+seedq_status seedq_rotate(const void *x, int32_t x_dtype, int64_t x_token_stride,
+                          int64_t x_head_stride, int64_t n_tokens, int32_t n_heads,
+                          int32_t head_dim, int32_t rot_dim, int32_t layout, const float *cos_sin,
+                          void *out, int32_t out_dtype, int64_t out_token_stride,
+                          int64_t out_head_stride, void *cuda_stream);
+
+/* seedq_kv_append of rotated keys: k is rotated as by seedq_rotate before the
+ * scales are taken (in float32: no rounding between), v is written as it is.
+ * With n_heads > 0 the step's queries are rotated by the same launch: q
+ * (n_tokens tokens, head_dim as the cache, the type of k) to q_out.
+ * Errors: as seedq_kv_append and seedq_rotate. */
+typedef struct {
+  const float *cos_sin;
+  int32_t rot_dim;
+  int32_t layout;
+  int32_t n_heads;   /* of q; 0: no queries, the rest is not read */
+  int32_t out_dtype;
+  const void *q;
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  void *q_out;
+  int64_t out_token_stride;
+  int64_t out_head_stride;
+} seedq_append_rotary_args;
+
+seedq_status seedq_kv_append_rotary(const seedq_kv_cache *cache, const void *k, const void *v,
+                                    int32_t dtype, int64_t token_stride, int64_t head_stride,
+                                    const int64_t *slots, int64_t n_tokens,
+                                    const seedq_append_rotary_args *args, void *cuda_stream);
+
 /* Attention of the newest tokens over the cache, causal.  Request i owns the
  * query tokens starts[i] .. starts[i+1]-1 of q (n_tokens rows in all) and
  * seq_lens[i] cached tokens, its own newest among them: its query token t sits
@@ -500,6 +568,122 @@ seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_r
                                   float *logprob, float *entropy, int32_t *rank, int32_t top_k,
                                   float *top_logprob, int32_t *top_index, void *workspace,
                                   uint64_t workspace_bytes, void *cuda_stream);
+
+/* Beam search's choice.  n_groups requests have n_beams beams each; beam b of
+ * request g is row g * n_beams + b of logits, scores, done and weights.  With z =
+ * scale * x over a row's logits, a beam brings the candidates
+ *   live  (b, v), total scores[b] + z_v - log sum exp z, for every token v;
+ *   done  (b, end_token), total scores[b]: a finished hypothesis, kept as it is;
+ * none where its score is -inf, and no token whose logit is -inf.  The first n_out
+ * of a request, by weights[b] * total (lengths differ: a hypothesis' length to some
+ * negative power), larger first, lower beam first among equals, then as
+ * seedq_token_logprobs orders:
+ *   out_score[g][i]  the total, not weighted; out_beam[g][i] the beam b;
+ *   out_token[g][i]  the token.  Past the candidates -inf, -1 and -1.
+ * Beams are compared in float64, their log sums are float32's.  A request with a
+ * score of NaN or +inf, a weight that is not positive and finite (both only of
+ * beams that bring anything) or a NaN or +inf among a live beam's logits gets NaN,
+ * -1 and -1 everywhere.  Logits of done beams and of those with score -inf are not
+ * read.
+ *   logits     device, row r at r * row_stride elements of type dtype.
+ *   scores     device, n_groups x n_beams float32.
+ *   done       device, as many bytes, not 0 where the beam has ended, or NULL.
+ *   weights    device, as many float32, or NULL (all 1).
+ *   out_*      device, n_groups x n_out.
+ *   workspace  device, 16-byte aligned, seedq_beam_select_workspace_bytes(n_groups,
+ *              n_beams, vocab) bytes, zeroed once before its first use, good for
+ *              any call that asks for no more; calls that may overlap need one each.
+ * Errors: INVALID_ARG (NULL pointer, unknown type, n_groups < 0, n_beams or n_out
+ * outside 1..SEEDQ_MAX_BEAMS, n_groups x n_beams above SEEDQ_MAX_REQUESTS, vocab
+ * outside 1..SEEDQ_BEAM_MAX_VOCAB, row_stride < vocab, logits not aligned to their
+ * type, end_token outside the vocabulary where done is given, scale outside
+ * 2^-64..2^64, workspace too small), CUDA.  n_groups = 0 is a no-op. */
+#define SEEDQ_MAX_BEAMS 32
+#define SEEDQ_BEAM_MAX_VOCAB (1 << 27)
+typedef struct {
+  const void *logits;
+  int64_t row_stride;
+  int32_t dtype;
+  int32_t n_beams;
+  int64_t n_groups;
+  int64_t vocab;
+  float scale;
+  int32_t end_token;
+  const float *scores;
+  const uint8_t *done;
+  const float *weights;
+  int32_t n_out;
+  float *out_score;
+  int32_t *out_beam;
+  int32_t *out_token;
+  void *workspace;
+  uint64_t workspace_bytes;
+} seedq_beam_select_args;
+
+uint64_t seedq_beam_select_workspace_bytes(int64_t n_groups, int32_t n_beams, int64_t vocab);
+seedq_status seedq_beam_select(const seedq_beam_select_args *args, void *cuda_stream);
+
+/* The pages of the chosen beams.  Row r = g * n_beams + b of the block table goes
+ * on from beam parents[r] of its request (0..n_beams-1; -1: it ends): it gets
+ * that beam's length and list of pages.  Full pages are shared.  A partly filled
+ * last page stays with the first row that goes on from its beam; every further one
+ * gets a page of its own off the free stack, into which the tokens of all caches
+ * are copied.  Pages that no row of the request holds any more are returned.
+ *
+ * So a prompt in one row is forked by parents of that row's number, a request ends
+ * by parents of -1, and seedq_batch_plan serves the rows in between: it adds tokens
+ * to pages that are the row's own, since shared ones are full.  Rows that may
+ * share pages must not end through seedq_batch_plan (n_new = -1), which returns a
+ * page once for every row that holds it.  A shared page stands in the lists of
+ * one request alone, at the same place in each.
+ *
+ * Returned pages are pushed first, by request, then place in the list, then row;
+ * copies' pages are then popped off the end, in row order.  A row whose copy the
+ * stack cannot cover is empty afterwards, as are rows of a bad parent.
+ *   caches        host array of n_caches layers, equal but for their addresses
+ *                 (and kind): page p of each holds the same tokens.
+ *   parents, seq_lens  device int32, n_groups x n_beams.
+ *   block_table   device, rows of table_width int32 at table_stride.
+ *   table_out     the same with out_stride, or block_table itself; entries past a
+ *                 row's pages, and rows that end, are not written.
+ *   free_pages    free_capacity int32, at least n_pages of the caches, the first
+ *                 *free_count of them free.  Updated in place (popped entries stay).
+ *   seq_lens_out, status  n_groups x n_beams: SEEDQ_REQ_OK, _NO_PAGES, or _BAD (a
+ *                 parent outside the request, or one whose length is negative or
+ *                 longer than a table row holds).
+ *   free_count_out  entries left.
+ *   workspace     device, 16-byte aligned, seedq_beam_reorder_workspace_bytes
+ *                 (n_groups, n_beams) bytes; calls that may overlap need one each.
+ * Outputs must not alias parents, seq_lens or free_count.
+ * Errors: INVALID_ARG (NULL or aliased pointer, n_caches outside
+ * 1..SEEDQ_BEAM_MAX_CACHES, caches that differ, n_beams outside
+ * 1..SEEDQ_MAX_BEAMS, rows outside 1..SEEDQ_MAX_REQUESTS, table_width outside
+ * 1..2^20 or above a stride, free_capacity below n_pages, workspace too small),
+ * UNSUPPORTED (as the cache calls), CUDA. */
+#define SEEDQ_BEAM_MAX_CACHES 4096
+typedef struct {
+  int32_t n_groups;
+  int32_t n_beams;
+  const int32_t *parents;
+  const int32_t *seq_lens;
+  const int32_t *block_table;
+  int64_t table_stride;
+  int32_t *table_out;
+  int64_t out_stride;
+  int32_t table_width;
+  int32_t free_capacity;
+  int32_t *free_pages;
+  const int32_t *free_count;
+  int32_t *seq_lens_out;
+  int32_t *status;
+  int32_t *free_count_out;
+  void *workspace;
+  uint64_t workspace_bytes;
+} seedq_beam_reorder_args;
+
+uint64_t seedq_beam_reorder_workspace_bytes(int32_t n_groups, int32_t n_beams);
+seedq_status seedq_beam_reorder(const seedq_kv_cache *caches, int32_t n_caches,
+                                const seedq_beam_reorder_args *args, void *cuda_stream);
 
 /* -------------------------------------------------------------- container
  * A file holding a compressed model: the global decoder table (Sec. 3.6, as

@@ -1,9 +1,12 @@
 """CPU oracle of the serving calls (numpy, fp64); test infrastructure only.
 
-Page bookkeeping, the 8-bit cache's append and gather, attention over it, and
-token log probabilities, each written from its definition in include/seedq.h
+Page bookkeeping, the 8-bit cache's append and gather, attention over it, token
+log probabilities, rotary positions, and beam search's choice and pages, each written from its definition in include/seedq.h
 and sharing nothing with the CUDA library.
 """
+import math
+from fractions import Fraction
+
 import numpy as np
 
 OK, NO_PAGES, BAD, NO_ROOM = 0, 1, 2, 3
@@ -216,3 +219,126 @@ def token_logprobs(x, targets, scale, top_k):
         for k, c in enumerate(order[:top_k]):
             tl[r, k], ti[r, k] = logp[c], c
     return lp, en, rk, tl, ti
+
+
+# ---------------------------------------------------------------- rotary positions
+
+TWO_PI = Fraction(6283185307179586476925286766559005768394338798750211641949889184615632812572, 10 ** 75)
+
+
+def rotary_angles(positions, frequencies, scale):
+    """(tokens, pairs, 2) of cos and sin, the angle reduced in whole fractions."""
+    out = np.zeros((len(positions), len(frequencies), 2))
+    for t, p in enumerate(positions):
+        for i, w in enumerate(frequencies):
+            a = float(int(p) * Fraction(float(w)) % TWO_PI)
+            out[t, i] = scale * math.cos(a), scale * math.sin(a)
+    return out
+
+
+def rotate(x, cos_sin, layout):
+    """x (tokens, heads, dim) as float64, by complex numbers; also the sum of the products' magnitudes."""
+    r = 2 * cos_sin.shape[1]
+    i = np.arange(r // 2)
+    a, b = (i, i + r // 2) if layout == "half" else (2 * i, 2 * i + 1)
+    c = (cos_sin[..., 0] + 1j * cos_sin[..., 1])[:, None]
+    y, size = x.copy(), np.zeros_like(x)
+    z = (x[..., a] + 1j * x[..., b]) * c
+    y[..., a], y[..., b] = z.real, z.imag
+    size[..., a] = np.abs(x[..., a] * c.real) + np.abs(x[..., b] * c.imag)
+    size[..., b] = np.abs(x[..., b] * c.real) + np.abs(x[..., a] * c.imag)
+    return y, size
+
+
+# ---------------------------------------------------------------- beams
+
+def beam_select(x, scores, scale, n_out, done=None, end=-1, weights=None):
+    """x (groups, beams, vocab) as float64.  Returns (score, beam, token, room): room
+    is the smallest distance between neighbours of different beams in the order, as a
+    share of their weighted totals' rounding unknowns (inf where none are compared)."""
+    g, b, v = x.shape
+    score, beam, token = np.full((g, n_out), -np.inf), np.full((g, n_out), -1, np.int32), np.full((g, n_out), -1, np.int32)
+    room = np.inf
+    for i in range(g):
+        cand, spoiled = [], False
+        for j in range(b):
+            s, w = float(scores[i, j]), 1.0 if weights is None else float(weights[i, j])
+            if s == -np.inf:
+                continue
+            if not s < np.inf or not 0 < w < np.inf:
+                spoiled = True
+                continue
+            if done is not None and done[i, j]:
+                cand.append((-(w * s), j, 0.0, end, s))
+                continue
+            row = np.where(x[i, j] == 0, 0.0, x[i, j])
+            if np.isnan(row).any() or np.isposinf(row).any():
+                spoiled = True
+                continue
+            if np.isneginf(row).all():
+                continue
+            z = scale * row
+            m = z.max()
+            log_sum = np.log(np.exp(z - m).sum())
+            for t in np.argsort(-row, kind="stable")[:n_out]:
+                if row[t] > -np.inf:
+                    total = s - log_sum + (z[t] - m)
+                    cand.append((-(w * total), j, -row[t], int(t), total))
+        if spoiled:
+            score[i] = np.nan
+            continue
+        cand.sort()
+        for k, (key, j, _, t, total) in enumerate(cand[:n_out]):
+            score[i, k], beam[i, k], token[i, k] = total, j, t
+            if k + 1 < len(cand) and cand[k + 1][1] != j and cand[k + 1][0] != key:
+                room = min(room, (cand[k + 1][0] - key) / (1.0 if weights is None else float(np.max(weights[i]))))
+    return score, beam, token, room
+
+
+def beam_reorder(parents, lens, table, out, free, count, page):
+    """Returns (table_out, seq_lens, status, free, free_count, copies) with copies
+    (src, dst, tokens) in row order; out holds what table_out held."""
+    table, out, free = np.array(table), np.array(out), np.array(free, np.int32)
+    g, b = parents.shape
+    width, n = table.shape[1], g * b
+    count = min(max(int(count), 0), free.size)
+    ok = lambda x: x >= 0 and cdiv(x, page) <= width  # noqa: E731
+    lens = [int(x) for x in lens]
+    new, status, wants = [0] * n, [OK] * n, []
+    for r in range(n):
+        p = int(parents[r // b, r % b])
+        q = r // b * b + p
+        if p < -1 or p >= b or (p >= 0 and not ok(lens[q])):
+            status[r] = BAD
+        elif p >= 0:
+            new[r] = lens[q]
+            if lens[q] % page and p in parents[r // b, :r % b].tolist():
+                wants.append(r)
+    returned = []
+    for i in range(g):
+        rows = range(i * b, i * b + b)
+        live = {int(p) for r, p in zip(rows, parents[i]) if status[r] == OK and p >= 0}
+        held = {r: cdiv(lens[r], page) if ok(lens[r]) else 0 for r in rows}
+        for c in range(max(held.values())):
+            kept = {int(table[r, c]) for r in rows if r - i * b in live and c < held[r]}
+            for r in rows:
+                if c < held[r] and table[r, c] >= 0 and int(table[r, c]) not in kept:
+                    kept.add(int(table[r, c]))
+                    returned.append(int(table[r, c]))
+    returned = returned[:free.size - count]
+    free[count:count + len(returned)] = returned
+    total = count + len(returned)
+    short = set(wants[total:])
+    copies = []
+    for r in range(n):
+        if r in short:
+            new[r], status[r] = 0, NO_PAGES
+        if new[r] <= 0:
+            continue
+        m = cdiv(new[r], page)
+        out[r, :m] = table[r // b * b + int(parents[r // b, r % b]), :m]
+        if r in wants:
+            dst = int(free[total - 1 - wants.index(r)])
+            copies.append((int(out[r, m - 1]), dst, new[r] % page))
+            out[r, m - 1] = dst
+    return out, np.array(new, np.int32), np.array(status, np.int32), free, np.int32(total - len(copies)), copies

@@ -1,0 +1,357 @@
+// The pages of chosen beams (seedq_beam_reorder): a beam that goes on from another
+// takes over its list of pages, full pages are shared, and the partly filled last
+// one is copied for every child but the first.
+//
+// What the beams of a request share lies at the same place of their lists, so no
+// page needs a count of its holders: page p at column c is kept if a beam that has
+// children holds it there, and goes back to the stack once if none does.  Work is
+// cut into tiles of 32 columns of a request, a warp each, a lane per column.  The
+// first pass counts the pages that go back, a sum over the tiles gives each its
+// place on the stack, and the second writes lists and stack; a row's old entries
+// are read by the warp that writes the new ones, so lists may be changed in place.
+//
+// The copies are the second launch: units of one head and tensor of one layer and
+// page, dealt to all warps.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "device_once.h"
+#include "serve.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace seedq {
+namespace {
+
+constexpr int kWarps = 16, kThreads = kWarps * 32;
+constexpr int kMaxBeams = SEEDQ_MAX_BEAMS;
+constexpr int kMaxCluster = 8;
+constexpr int kLayersAtOnce = 64;  // whose pointers go in a launch's parameters
+
+// One copy: tokens [0, used) of page src to page dst.
+struct Copy {
+  int32_t src, dst, used;
+};
+struct Workspace {
+  int32_t n, pad[3];
+  Copy copy[1];  // one per row
+};
+
+struct PagesArgs {
+  int32_t groups, beams, page, page_shift, width, capacity;
+  int64_t table_stride, out_stride;
+  const int32_t *parents, *seq_lens, *table, *free_count;
+  int32_t *table_out, *free_pages, *seq_out, *status, *count_out;
+  Workspace *work;
+};
+
+__device__ __forceinline__ int pages_of(int tokens, const PagesArgs &a) {  // tokens >= 0
+  const uint32_t x = (uint32_t)tokens + (uint32_t)a.page - 1;
+  return (int)(a.page_shift >= 0 ? x >> a.page_shift : x / (uint32_t)a.page);
+}
+
+// Exclusive sum of v over the CTA, and the total.
+__device__ __forceinline__ int cta_sum(int v, int *warp_sums, int &total) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(~0u, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) warp_sums[w] = x;
+  __syncthreads();
+  int s = lane < kWarps ? warp_sums[lane] : 0;
+#pragma unroll
+  for (int o = 1; o < kWarps; o <<= 1) {
+    const int y = __shfl_up_sync(~0u, s, o);
+    if (lane >= o) s += y;
+  }
+  total = __shfl_sync(~0u, s, kWarps - 1);
+  const int before = __shfl_sync(~0u, s, max(w - 1, 0));
+  __syncthreads();
+  return (w ? before : 0) + x - v;
+}
+
+// What the kernel keeps of a row: the row of its group that it goes on from (-1:
+// none), its new length (-1: refused), its pages before, its place among the rows
+// that want a copy (-1: none).
+struct Rows {
+  int *from, *len, *held, *nth, *first_tile;  // first_tile: per group, and their number
+};
+
+__global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__ PagesArgs a) {
+  extern __shared__ int sm[];
+  const int n = a.groups * a.beams, B = a.beams;
+  const Rows r{sm, sm + n, sm + 2 * n, sm + 3 * n, sm + 4 * n};
+  int *tiles = sm + 4 * n + a.groups + 1 + (threadIdx.x >> 5) * B * 32;  // the warp's tile
+  __shared__ int s_warp[kWarps], s_back[kWarps], s_cta_back;
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks();
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int count = min(max(*a.free_count, 0), a.capacity);
+
+  // rows: every CTA makes the same tables
+  int copies = 0;
+  for (int base = 0; base < n; base += kThreads) {
+    const int i = base + threadIdx.x;
+    int wants = 0, len = 0, held = 0, p = -1;
+    if (i < n) {
+      const int g = i / B, b = i - g * B, old = a.seq_lens[i];
+      p = a.parents[i];
+      // a length that makes no sense: the row holds nothing that can be told
+      held = old < 0 || pages_of(old, a) > a.width ? 0 : pages_of(old, a);
+      if (p < -1 || p >= B) {
+        len = -1;
+      } else if (p >= 0) {
+        len = a.seq_lens[g * B + p];
+        if (len < 0 || pages_of(len, a) > a.width) len = -1;
+        if (len > 0 && len % a.page)
+          for (int q = 0; q < b && !wants; ++q) wants = a.parents[g * B + q] == p;
+      }
+    }
+    int total;
+    const int at = copies + cta_sum(wants, s_warp, total);
+    copies += total;
+    if (i < n) r.from[i] = len >= 0 ? p : -1, r.len[i] = len, r.held[i] = held, r.nth[i] = wants ? at : -1;
+  }
+  __syncthreads();
+  // tiles: as many of a group as its longest list has
+  int n_tiles = 0;
+  for (int base = 0; base < a.groups; base += kThreads) {
+    const int g = base + threadIdx.x;
+    int most = 0;
+    if (g < a.groups)
+      for (int b = 0; b < B; ++b) most = max(most, r.held[g * B + b]);
+    int total;
+    const int at = n_tiles + cta_sum((most + 31) / 32, s_warp, total);
+    n_tiles += total;
+    if (g < a.groups) r.first_tile[g] = at;
+  }
+  if (threadIdx.x == 0) r.first_tile[a.groups] = n_tiles;
+  __syncthreads();
+
+  const int64_t workers = (int64_t)ranks * kWarps, me = (int64_t)rank * kWarps + w;
+  const int t0 = (int)(n_tiles * me / workers), t1 = (int)(n_tiles * (me + 1) / workers);
+  int g0 = 0;
+  if (t0 < t1) {
+    int lo = 0, hi = a.groups;  // last group with first_tile <= t0
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (r.first_tile[mid] <= t0) lo = mid;
+      else hi = mid;
+    }
+    g0 = lo;
+  }
+  // Reads a tile; bit b of the result: row b's page at the lane's column goes back here.
+  auto read_tile = [&](int g, int col) -> uint32_t {
+    uint32_t held = 0, live = 0;
+    for (int b = 0; b < B; ++b) {
+      const int i = g * B + b;
+      const int id = col < r.held[i] ? a.table[(int64_t)i * a.table_stride + col] : -1;
+      tiles[b * 32 + lane] = id;
+      if (id >= 0) held |= 1u << b;
+      if (r.from[i] >= 0) live |= 1u << r.from[i];
+    }
+    uint32_t back = 0;
+    for (uint32_t dead = held & ~live; dead; dead &= dead - 1) {
+      const int q = __ffs(dead) - 1, id = tiles[q * 32 + lane];
+      bool stays = false;
+      for (uint32_t other = held & (live | ((1u << q) - 1)); other && !stays; other &= other - 1)
+        stays = tiles[(__ffs(other) - 1) * 32 + lane] == id;
+      if (!stays) back |= 1u << q;
+    }
+    return back;
+  };
+
+  int mine = 0;
+  for (int t = t0, g = g0; t < t1; ++t) {
+    while (t >= r.first_tile[g + 1]) ++g;
+    mine += __popc(read_tile(g, (t - r.first_tile[g]) * 32 + lane));
+  }
+  mine = __reduce_add_sync(~0u, mine);
+  if (lane == 0) s_back[w] = mine;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int x = 0;
+    for (int k = 0; k < kWarps; ++k) x += s_back[k];
+    s_cta_back = x;
+  }
+  cluster.sync();
+  int before = 0, all = 0;
+  for (int k = 0; k < ranks; ++k) {
+    const int x = *cluster.map_shared_rank(&s_cta_back, k);
+    if (k < rank) before += x;
+    all += x;
+  }
+  for (int k = 0; k < w; ++k) before += s_back[k];
+  const int total = (int)min((int64_t)count + all, (int64_t)a.capacity);
+
+  int place = count + before;
+  for (int t = t0, g = g0; t < t1; ++t) {
+    while (t >= r.first_tile[g + 1]) ++g;
+    const int col = (t - r.first_tile[g]) * 32 + lane;
+    const uint32_t back = read_tile(g, col);
+    int x = __popc(back);
+    const int c = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(~0u, x, o);
+      if (lane >= o) x += y;
+    }
+    int at = place + x - c;
+    for (uint32_t rest = back; rest; rest &= rest - 1, ++at)
+      if (at < a.capacity) a.free_pages[at] = tiles[(__ffs(rest) - 1) * 32 + lane];
+    place += __shfl_sync(~0u, x, 31);
+    for (int b = 0; b < B; ++b) {
+      const int i = g * B + b, len = r.len[i], nth = r.nth[i];
+      if (len <= 0 || nth >= total || col >= pages_of(len, a)) continue;
+      const int id = tiles[r.from[i] * 32 + lane];
+      if (nth >= 0 && col == pages_of(len, a) - 1) a.work->copy[nth].src = id;  // gets a page of its own
+      else a.table_out[(int64_t)i * a.out_stride + col] = id;
+    }
+  }
+  cluster.sync();  // the stack is whole, and no CTA's counts are read any more
+
+  for (int i = rank * kThreads + threadIdx.x; i < n; i += ranks * kThreads) {
+    const int len = r.len[i], nth = r.nth[i];
+    const bool fits = nth < total;
+    a.seq_out[i] = len > 0 && fits ? len : 0;
+    a.status[i] = len < 0 ? SEEDQ_REQ_BAD : fits ? SEEDQ_REQ_OK : SEEDQ_REQ_NO_PAGES;
+    if (nth >= 0 && fits) {
+      const int dst = __ldcg(a.free_pages + (total - 1 - nth));
+      a.table_out[(int64_t)i * a.out_stride + pages_of(len, a) - 1] = dst;
+      a.work->copy[nth].dst = dst;
+      a.work->copy[nth].used = len % a.page;
+    }
+  }
+  if (rank == 0 && threadIdx.x == 0) {
+    a.work->n = min(copies, total);
+    *a.count_out = total - min(copies, total);
+  }
+}
+
+// ---------------------------------------------------------------- copies
+
+struct CopyArgs {
+  const Workspace *work;
+  int32_t layers, heads, pieces;  // pieces of 16 codes of a token
+  int64_t pages, page_stride, head_stride, token_stride;
+  uint8_t *codes[kLayersAtOnce][2];
+  float *scales[kLayersAtOnce][2];
+};
+
+constexpr int kCopyThreads = 256;
+
+__global__ void __launch_bounds__(kCopyThreads) k_beam_copy(const __grid_constant__ CopyArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int of_copy = a.layers * 2 * a.heads;
+  const int64_t units = (int64_t)a.work->n * of_copy, warps = (int64_t)gridDim.x * (kCopyThreads / 32);
+  for (int64_t u = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); u < units; u += warps) {
+    const int c = (int)(u / of_copy), rest = (int)(u - (int64_t)c * of_copy), lt = rest / a.heads, h = rest - lt * a.heads;
+    const Copy y = a.work->copy[c];
+    if (y.src < 0 || y.src >= a.pages || y.dst < 0 || y.dst >= a.pages) continue;
+    uint8_t *base = a.codes[lt >> 1][lt & 1] + h * a.head_stride;
+    const uint8_t *src = base + y.src * a.page_stride;
+    uint8_t *dst = base + y.dst * a.page_stride;
+    const int n = y.used * a.pieces;
+#pragma unroll 4
+    for (int i = lane; i < n; i += 32) {
+      const int t = i / a.pieces;
+      const int64_t at = t * a.token_stride + (i - t * a.pieces) * 16;
+      *(uint4 *)(dst + at) = *(const uint4 *)(src + at);
+    }
+    if (lane == 0) {
+      float *s = a.scales[lt >> 1][lt & 1];
+      s[(int64_t)y.dst * a.heads + h] = s[(int64_t)y.src * a.heads + h];
+    }
+  }
+}
+
+DeviceOnce g_pages_smem;
+
+size_t pages_smem(int groups, int beams) {
+  return sizeof(int) * ((size_t)4 * groups * beams + groups + 1 + (size_t)kWarps * beams * 32);
+}
+
+}  // namespace
+}  // namespace seedq
+
+using namespace seedq;
+
+extern "C" {
+
+uint64_t seedq_beam_reorder_workspace_bytes(int32_t n_groups, int32_t n_beams) {
+  if (n_groups < 1 || n_beams < 1 || n_beams > kMaxBeams || (int64_t)n_groups * n_beams > SEEDQ_MAX_REQUESTS) return 0;
+  return sizeof(Workspace) + (uint64_t)n_groups * n_beams * sizeof(Copy);
+}
+
+seedq_status seedq_beam_reorder(const seedq_kv_cache *caches, int32_t n_caches, const seedq_beam_reorder_args *args, void *cuda_stream) {
+  if (!caches || !args || n_caches < 1 || n_caches > SEEDQ_BEAM_MAX_CACHES) return SEEDQ_ERR_INVALID_ARG;
+  const seedq_kv_cache &c = caches[0];
+  for (int i = 0; i < n_caches; ++i) {
+    const seedq_kv_cache &x = caches[i];
+    const seedq_status st = kv_check(&x);
+    if (st != SEEDQ_OK) return st;
+    if (x.n_kv_heads != c.n_kv_heads || x.head_dim != c.head_dim || x.page_size != c.page_size || x.n_pages != c.n_pages ||
+        x.page_stride != c.page_stride || x.head_stride != c.head_stride || x.token_stride != c.token_stride)
+      return SEEDQ_ERR_INVALID_ARG;
+  }
+  const seedq_beam_reorder_args &p = *args;
+  const uint64_t bytes = seedq_beam_reorder_workspace_bytes(p.n_groups, p.n_beams);
+  if (bytes == 0 || !p.parents || !p.seq_lens || !p.block_table || !p.table_out || !p.free_pages || !p.free_count || !p.seq_lens_out ||
+      !p.status || !p.free_count_out || !p.workspace || (uintptr_t)p.workspace % 16 || p.workspace_bytes < bytes)
+    return SEEDQ_ERR_INVALID_ARG;
+  if (p.table_width < 1 || p.table_width > (1 << 20) || p.table_width > p.table_stride || p.table_width > p.out_stride ||
+      p.free_capacity < c.n_pages || p.free_capacity == INT32_MAX)
+    return SEEDQ_ERR_INVALID_ARG;
+  if (p.table_out == p.block_table && p.out_stride != p.table_stride) return SEEDQ_ERR_INVALID_ARG;
+  for (const int32_t *o : {p.seq_lens_out, p.status, p.free_count_out})
+    if (o == p.parents || o == p.seq_lens || o == p.free_count) return SEEDQ_ERR_INVALID_ARG;
+  PagesArgs a{p.n_groups, p.n_beams, c.page_size, log2_of(c.page_size), p.table_width, p.free_capacity, p.table_stride, p.out_stride,
+              p.parents, p.seq_lens, p.block_table, p.free_count, p.table_out, p.free_pages, p.seq_lens_out, p.status, p.free_count_out,
+              (Workspace *)p.workspace};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_fail(e);
+  const int rc = g_pages_smem.run(dev, [] {
+    return (int)cudaFuncSetAttribute(k_beam_pages, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)std::max(pages_smem(SEEDQ_MAX_REQUESTS, 1), pages_smem(SEEDQ_MAX_REQUESTS / kMaxBeams, kMaxBeams)));
+  });
+  if (rc) return cuda_fail((cudaError_t)rc);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const int64_t tiles = (int64_t)p.n_groups * ((p.table_width + 31) / 32);
+  int ranks = 1;
+  while (ranks < kMaxCluster && tiles > ranks * kWarps) ranks *= 2;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)ranks, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)ranks), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = pages_smem(p.n_groups, p.n_beams);
+  cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, k_beam_pages, a);
+  if (e != cudaSuccess) return cuda_fail(e);
+
+  CopyArgs y{};
+  y.work = a.work, y.heads = c.n_kv_heads, y.pieces = c.head_dim / 16, y.pages = c.n_pages;
+  y.page_stride = c.page_stride, y.head_stride = c.head_stride, y.token_stride = c.token_stride;
+  for (int first = 0; first < n_caches; first += kLayersAtOnce) {
+    y.layers = std::min(n_caches - first, kLayersAtOnce);
+    for (int i = 0; i < y.layers; ++i) {
+      const seedq_kv_cache &x = caches[first + i];
+      y.codes[i][0] = (uint8_t *)x.k, y.codes[i][1] = (uint8_t *)x.v;
+      y.scales[i][0] = x.k_scale, y.scales[i][1] = x.v_scale;
+    }
+    const int64_t most = (int64_t)p.n_groups * p.n_beams * y.layers * 2 * y.heads, per = kCopyThreads / 32;
+    const unsigned ctas = (unsigned)std::min<int64_t>((most + per - 1) / per, 152 * 8);
+    k_beam_copy<<<ctas, kCopyThreads, 0, st>>>(y);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e);
+  }
+  return SEEDQ_OK;
+}
+
+}  // extern "C"

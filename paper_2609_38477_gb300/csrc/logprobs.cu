@@ -42,6 +42,7 @@
 #include "cp_async.cuh"
 #include "device_once.h"
 #include "f32x2.cuh"
+#include "order.cuh"
 #include "serve.cuh"
 
 namespace seedq {
@@ -89,44 +90,11 @@ struct Part {
   uint64_t key[kMaxTop];
 };
 
-// A logit's place in the order as a whole number: larger logits first, NaN
-// before all, -0 equal to +0, the lower index first among equals.  Never 0.
-__device__ __forceinline__ uint32_t order_word(float x) {
-  const uint32_t b = __float_as_uint(x + 0.f);
-  return isnan(x) ? 0xffffffffu : (b >> 31) ? ~b : (b | 0x80000000u);
-}
-__device__ __forceinline__ uint64_t order_key(float x, int i) { return ((uint64_t)order_word(x) << 32) | (uint32_t)~i; }
-__device__ __forceinline__ float key_value(uint64_t key) {
-  const uint32_t u = (uint32_t)(key >> 32);
-  return u == 0xffffffffu ? CUDART_NAN_F : __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u);
-}
-__device__ __forceinline__ int key_index(uint64_t key) { return (int)~(uint32_t)key; }
-
-__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
-__device__ __forceinline__ float max_nan(float a, float b, float c) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-  return y;
-}
 // x >= xt as x > the number before xt; for -inf every x: no x is <= NaN.
 __device__ __forceinline__ float number_before(float xt) {
   if (xt == -CUDART_INF_F) return CUDART_NAN_F;
   return xt == 0.f ? __uint_as_float(0x80000001u) : __uint_as_float(__float_as_uint(xt) + (xt > 0.f ? -1 : 1));
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// A load past the L1 cache: sees what other SMs wrote.
-template <typename T>
-__device__ __forceinline__ T fresh_load(const T *x) { return *(const volatile T *)x; }
-
 // A target's logit, -0 as +0: count_above would take every +0 for larger than -0.
 __device__ __forceinline__ float target_logit(const void *p, int dt, int64_t i) { return load_elem(p, dt, i) + 0.f; }
 
@@ -154,32 +122,6 @@ __device__ __forceinline__ void rebase(float &m, float &s1, float &s2, float to,
   s2 = (s2 + d * s1) * e;
   s1 *= e;
   m = to;
-}
-
-// Both lists' first 32 keys in order: of two descending lists, the larger of a's
-// i-th and b's (31 - i)-th are the 32 largest, a bitonic sequence.
-__device__ __noinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane) {
-  b = __shfl_sync(~0u, b, 31 - lane);
-  uint64_t x = a > b ? a : b;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const uint64_t y = __shfl_xor_sync(~0u, x, o);
-    x = (lane & o) == 0 ? (x > y ? x : y) : (x < y ? x : y);
-  }
-  return x;
-}
-
-// A warp's keys in descending order (bitonic).
-__device__ __noinline__ uint64_t sort_keys(uint64_t x, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-    for (int o = size >> 1; o; o >>= 1) {
-      const uint64_t y = __shfl_xor_sync(~0u, x, o);
-      const bool larger = ((lane & o) == 0) == ((lane & size) == 0);
-      x = (x > y) == larger ? x : y;
-    }
-  return x;
 }
 
 // scale (x - m); by halves where the difference alone passes float32's largest.

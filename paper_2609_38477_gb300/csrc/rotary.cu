@@ -1,0 +1,98 @@
+// Rotary positions: cos and sin of a step's positions (seedq_rotary_angles), and
+// queries and keys turned by them (seedq_rotate).
+//
+// An angle is position * frequency, of which only the fraction of a turn matters.
+// Frequencies are kept in turns as whole numbers F = round(w / 2 pi * 2^64), so the
+// fraction is the product modulo 2^64: exact at any position, where a float32
+// product of position 131072 is off by 2^-8.
+#include "rotary.cuh"
+
+#include <algorithm>
+
+namespace seedq {
+namespace {
+
+// cos and sin of f turns, f in units of 2^-64: the nearest eighth of a turn but
+// one comes off as a whole number, so the rest is exact in float32 to 2^-25 of
+// its size and sincospif sees at most a quarter.
+__device__ __forceinline__ float2 cos_sin_of(uint64_t f) {
+  const uint32_t h = (uint32_t)(f >> 32);
+  const uint32_t quarter = (h + 0x20000000u) >> 30;
+  const int32_t rest = (int32_t)(h - (quarter << 30));  // -2^29 .. 2^29 - 1 of 2^32 to the turn
+  float s, c;
+  sincospif((float)rest * 0x1p-31f, &s, &c);
+  switch (quarter & 3) {
+    case 0: return make_float2(c, s);
+    case 1: return make_float2(-s, c);
+    case 2: return make_float2(-c, -s);
+    default: return make_float2(s, -c);
+  }
+}
+
+__global__ void __launch_bounds__(256) k_rotary_angles(const uint64_t *__restrict__ turns, int half, float scale,
+                                                       const int32_t *__restrict__ positions, int64_t n, float2 *__restrict__ cs) {
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int64_t t = i >> 32 ? i / half : (int64_t)((uint32_t)i / (uint32_t)half);
+  if (t >= n) return;
+  const float2 y = cos_sin_of((uint64_t)(int64_t)positions[t] * turns[i - t * half]);
+  cs[i] = make_float2(scale * y.x, scale * y.y);
+}
+
+template <int IN, int OUT, int N>
+__global__ void __launch_bounds__(256) k_rotate(const __grid_constant__ RotateArgs a, const __grid_constant__ RotateSplit s) {
+  rotate_item<IN, OUT, N>(a, s, (int64_t)blockIdx.x * blockDim.x + threadIdx.x);
+}
+
+template <int IN, int OUT>
+seedq_status launch(const RotateArgs &a, cudaStream_t st) {
+  RotateSplit s{};
+  const bool wide = rotate_split(a, IN, OUT, s);
+  const int64_t ctas = (a.n * s.pieces * s.groups + 255) / 256;
+  if (ctas > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
+  if (wide) k_rotate<IN, OUT, kRotateWide><<<(unsigned)ctas, 256, 0, st>>>(a, s);
+  else k_rotate<IN, OUT, 1><<<(unsigned)ctas, 256, 0, st>>>(a, s);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
+}
+
+}  // namespace
+}  // namespace seedq
+
+using namespace seedq;
+
+extern "C" {
+
+seedq_status seedq_rotary_angles(const uint64_t *turns, int32_t half, float scale, const int32_t *positions, int64_t n_tokens,
+                                 float *cos_sin, void *cuda_stream) {
+  if (half < 1 || half > SEEDQ_ROPE_MAX_DIM / 2 || n_tokens < 0 || n_tokens > INT32_MAX || !(scale - scale == 0.f))
+    return SEEDQ_ERR_INVALID_ARG;
+  if (n_tokens == 0) return SEEDQ_OK;
+  if (!turns || !positions || !cos_sin || (uintptr_t)cos_sin % 8) return SEEDQ_ERR_INVALID_ARG;
+  const int64_t ctas = (n_tokens * half + 255) / 256;
+  if (ctas > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
+  k_rotary_angles<<<(unsigned)ctas, 256, 0, (cudaStream_t)cuda_stream>>>(turns, half, scale, positions, n_tokens, (float2 *)cos_sin);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
+}
+
+seedq_status seedq_rotate(const void *x, int32_t x_dtype, int64_t x_token_stride, int64_t x_head_stride, int64_t n_tokens,
+                          int32_t n_heads, int32_t head_dim, int32_t rot_dim, int32_t layout, const float *cos_sin, void *out,
+                          int32_t out_dtype, int64_t out_token_stride, int64_t out_head_stride, void *cuda_stream) {
+  if (!dtype_ok(x_dtype) || !dtype_ok(out_dtype) || !rope_ok(layout, rot_dim, head_dim) || n_tokens < 0 || n_tokens > INT32_MAX ||
+      n_heads < 0 || n_heads > SEEDQ_ROPE_MAX_HEADS)
+    return SEEDQ_ERR_INVALID_ARG;
+  if (n_tokens == 0 || n_heads == 0) return SEEDQ_OK;
+  if (!x || !out || !cos_sin || (uintptr_t)cos_sin % 8) return SEEDQ_ERR_INVALID_ARG;
+  // turned where it lies: a thread writes what it alone has read
+  if (x == out && (x_dtype != out_dtype || x_token_stride != out_token_stride || x_head_stride != out_head_stride))
+    return SEEDQ_ERR_INVALID_ARG;
+  const RotateArgs a{x, out, x_token_stride, x_head_stride, out_token_stride, out_head_stride, n_tokens, n_heads, head_dim,
+                     rot_dim / 2, layout, out_dtype, (const float2 *)cos_sin};
+  using Launch = seedq_status (*)(const RotateArgs &, cudaStream_t);
+  static constexpr Launch kLaunch[3][3] = {{launch<0, 0>, launch<0, 1>, launch<0, 2>},
+                                           {launch<1, 0>, launch<1, 1>, launch<1, 2>},
+                                           {launch<2, 0>, launch<2, 1>, launch<2, 2>}};
+  return kLaunch[x_dtype][out_dtype](a, (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"

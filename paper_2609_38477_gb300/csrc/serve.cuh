@@ -63,6 +63,11 @@ __device__ __forceinline__ float block_scale(uint32_t abits) {
   return __uint_as_float((uint32_t)e << 23);
 }
 
+inline bool rope_ok(int32_t layout, int32_t rot_dim, int32_t head_dim) {
+  return (layout == SEEDQ_ROPE_HALF || layout == SEEDQ_ROPE_PAIRS) && head_dim <= SEEDQ_ROPE_MAX_DIM && rot_dim >= 2 &&
+         rot_dim <= head_dim && rot_dim % 2 == 0;
+}
+
 inline int log2_of(int x) {  // -1 if x is no power of two
   if (x & (x - 1)) return -1;
   int n = 0;

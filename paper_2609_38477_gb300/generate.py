@@ -1,15 +1,18 @@
-"""A decode loop over compressed layers: page bookkeeping, the 8-bit cache, its
-attention and token log probabilities around the fused products.
+"""A decode loop over compressed layers: page bookkeeping, rotary positions, the
+8-bit cache, its attention, token log probabilities and beam search around the
+fused products.
 
 Decoder.step takes the next tokens of a batch of requests (single tokens, or
 pieces of prompts; at most 16 in all, the widest product), and everything after
-the token ids stays on the device.  RMSNorm, rotary positions, SiLU and the
-residual sums are plain torch operations.
+the token ids stays on the device; Decoder.beam_search follows several
+hypotheses of each prompt.  RMSNorm, SiLU and the residual sums are plain torch
+operations.
 
     python -m paper_2609_38477_gb300.generate
 
 compresses the small synthetic checkpoint (2 layers, 4 query and 2 key-value
-heads) by the seed search and continues three prompts of different lengths.
+heads) by the seed search, continues three prompts of different lengths, and
+searches the likeliest continuations of one of them.
 """
 from __future__ import annotations
 
@@ -42,13 +45,6 @@ def rms_norm(x, gain):
     return (x * torch.rsqrt((x * x).mean(1, keepdim=True) + 1e-5) * gain).bfloat16()
 
 
-def rotate(x, angles):
-    """Rotary positions: x (tokens, heads, dim), angles (tokens, dim / 2)."""
-    c, s = torch.cos(angles)[:, None], torch.sin(angles)[:, None]
-    a, b = x.chunk(2, 2)
-    return torch.cat([a * c - b * s, b * c + a * s], 2)
-
-
 class Decoder:
     """A Llama-shaped decoder over compressed layers.
 
@@ -70,6 +66,7 @@ class Decoder:
         self.seq_lens = torch.zeros(max_requests, dtype=torch.int32, device="cuda")
         half = spec.head_dim // 2
         self.freqs = 10000.0 ** (-torch.arange(half, device="cuda") / half)
+        self.rotary = serving.Rotary(self.freqs.tolist())
         self.score_work = serving.score_workspace(MAX_COLUMNS, spec.vocab)
 
     def _products(self, x, names, block):
@@ -98,13 +95,14 @@ class Decoder:
             return torch.empty((0, s.vocab), device="cuda")
         # tokens without a slot have no keys to attend to: NaN, which stays in its row
         x = self.embedding[tokens].float().masked_fill(p.slots[:n, None] < 0, float("nan"))
-        angles = p.positions[:n, None].float() * self.freqs
+        cos_sin = torch.empty((n, self.rotary.half, 2), device="cuda")
+        self.rotary.angles(p.positions, cos_sin)
         for block, cache in zip(self.blocks, self.caches):
             h = rms_norm(x, block["attn_norm"])
             q, k, v = self._products(h, ("q", "k", "v"), block)
-            q = rotate(q.view(n, s.n_heads, s.head_dim), angles)
-            k = rotate(k.view(n, s.n_kv_heads, s.head_dim), angles)
-            cache.append(k, v.view(n, s.n_kv_heads, s.head_dim).contiguous(), p.slots)
+            q = q.view(n, s.n_heads, s.head_dim)
+            k, v = (y.view(n, s.n_kv_heads, s.head_dim) for y in (k, v))
+            cache.append_rotary(k, v, p.slots, self.rotary, cos_sin, q=q, q_out=q)
             out = torch.empty((n, s.n_heads, s.head_dim), dtype=torch.bfloat16, device="cuda")
             cache.attend(q, out, p.seq_lens, p.starts, self.table, self.work, max_new=n)
             x = x + self._products(out.view(n, -1), ("o",), block)[0]
@@ -122,6 +120,60 @@ class Decoder:
                torch.empty((n, top_k), **i))
         serving.token_logprobs(logits, targets, *out, self.score_work, scale=1.0 / temperature)
         return out
+
+    def beam_search(self, prompts, n_beams: int, max_new: int, end_token: int = -1, length_power: float = 0.0):
+        """The likeliest continuations of every prompt (lists of tokens; no request
+        may be under way, and prompts x n_beams be at most 16): tokens (prompts,
+        n_beams, max_new), likeliest first, with -1 where there is no hypothesis,
+        and the sums of their log probabilities.  A hypothesis that has chosen
+        end_token keeps its sum and repeats it.  Sums are compared after division
+        by the number of chosen tokens to the length_power.  Where the pages do not
+        last, a prompt's sums are NaN and its tokens -1 from there on."""
+        g, b, vocab = len(prompts), n_beams, self.spec.vocab
+        rows = g * b
+        if not 1 <= rows <= min(MAX_COLUMNS, self.plan.max_requests) or not all(prompts) or max_new < 1:
+            raise ValueError("1..16 beams in all and no more than max_requests, prompts of a token or more and max_new >= 1 are wanted")
+        i32 = dict(dtype=torch.int32, device="cuda")
+        pages = serving.BeamPages(self.caches, g, b)
+        work = serving.beam_workspace(g, b, vocab)
+
+        def reorder(parents):
+            pages.reorder(parents, self.seq_lens, self.table, self.free, self.free_count)
+            self.seq_lens[:rows].copy_(pages.seq_lens)
+            self.free_count.copy_(pages.free_count)
+
+        # prompts in the first row of each request, which its beams then fork
+        logits = torch.zeros((rows, vocab), device="cuda")
+        for i, prompt in enumerate(prompts):
+            for at in range(0, len(prompt), MAX_COLUMNS):
+                piece = torch.tensor(prompt[at:at + MAX_COLUMNS], device="cuda")
+                n_new = torch.zeros(rows, **i32)
+                n_new[i * b] = piece.shape[0]
+                logits[i * b] = self.step(piece, n_new)[-1]
+        scores = torch.full((g, b), float("-inf"), device="cuda")
+        scores[:, 0] = 0.0
+        done = torch.zeros((g, b), dtype=torch.bool, device="cuda")
+        chosen = torch.zeros((g, b), device="cuda")
+        history = torch.full((g, b, max_new), -1, dtype=torch.int64, device="cuda")
+        for i in range(max_new):
+            new_scores, beam, token = torch.empty_like(scores), torch.empty((g, b), **i32), torch.empty((g, b), **i32)
+            weights = (chosen + ~done) ** -length_power if length_power else None
+            serving.beam_select(logits, scores, new_scores, beam, token, work, done=done if end_token >= 0 else None,
+                                end_token=end_token, weights=weights)
+            source = beam.clamp(min=0).long()
+            history = history.gather(1, source[..., None].expand_as(history))
+            history[..., i] = token
+            history.masked_fill_(beam[..., None] < 0, -1)
+            chosen, done = (chosen + ~done).gather(1, source), done.gather(1, source) | (token == end_token)
+            if i + 1 == max_new:
+                scores = new_scores
+                break
+            reorder(beam)
+            # a beam whose copy found no page has no context any more: NaN, which the next choice passes on
+            scores = new_scores.masked_fill(pages.status.view(g, b) != 0, float("nan"))
+            logits = self.step(token.flatten().clamp(min=0).long(), torch.ones(rows, **i32))
+        reorder(torch.full((g, b), -1, **i32))
+        return history, scores
 
 
 def synthetic_decoder(name: str = "tiny", max_requests: int = 4, n_pages: int = 64, page_size: int = 16, kind: str = "int8"):
@@ -161,6 +213,10 @@ def main():
         n_new = torch.tensor([1, 1, 1, 0], dtype=torch.int32, device="cuda")
         print(f"step {step}: lengths {d.seq_lens[:3].tolist()}, next {tokens.tolist()}, "
               f"logprob {[round(x, 3) for x in top[:, 0].tolist()]}, entropy {[round(x, 3) for x in entropy.tolist()]}")
+    d.step(torch.empty(0, dtype=torch.int64, device="cuda"), torch.full((4,), -1, dtype=torch.int32, device="cuda"))
+    found, scores = d.beam_search(prompts[:1], 4, 6)
+    for hypothesis, score in zip(found[0].tolist(), scores[0].tolist()):
+        print(f"beam: {hypothesis}, logprob {score:.3f}")
 
 
 if __name__ == "__main__":

@@ -108,6 +108,40 @@ ATTEND_ARGS = struct.Struct("@iiqPqqPqqiiPPPPqiiifPQ")
 assert ATTEND_ARGS.size == C.sizeof(AttendArgs)
 
 
+class AppendRotaryArgs(C.Structure):
+    _fields_ = [("cos_sin", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("n_heads", C.c_int32),
+                ("out_dtype", C.c_int32), ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("q_out", C.c_void_p), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64)]
+
+
+APPEND_ROTARY_ARGS = struct.Struct("@PiiiiPqqPqq")
+assert APPEND_ROTARY_ARGS.size == C.sizeof(AppendRotaryArgs)
+
+
+class BeamSelectArgs(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("row_stride", C.c_int64), ("dtype", C.c_int32), ("n_beams", C.c_int32),
+                ("n_groups", C.c_int64), ("vocab", C.c_int64), ("scale", C.c_float), ("end_token", C.c_int32),
+                ("scores", C.c_void_p), ("done", C.c_void_p), ("weights", C.c_void_p), ("n_out", C.c_int32),
+                ("out_score", C.c_void_p), ("out_beam", C.c_void_p), ("out_token", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+BEAM_SELECT_ARGS = struct.Struct("@PqiiqqfiPPPiPPPPQ")
+assert BEAM_SELECT_ARGS.size == C.sizeof(BeamSelectArgs)
+
+
+class BeamReorderArgs(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("n_beams", C.c_int32), ("parents", C.c_void_p), ("seq_lens", C.c_void_p),
+                ("block_table", C.c_void_p), ("table_stride", C.c_int64), ("table_out", C.c_void_p), ("out_stride", C.c_int64),
+                ("table_width", C.c_int32), ("free_capacity", C.c_int32), ("free_pages", C.c_void_p),
+                ("free_count", C.c_void_p), ("seq_lens_out", C.c_void_p), ("status", C.c_void_p),
+                ("free_count_out", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+BEAM_REORDER_ARGS = struct.Struct("@iiPPPqPqiiPPPPPPQ")
+assert BEAM_REORDER_ARGS.size == C.sizeof(BeamReorderArgs)
+
+
 # Every symbol include/seedq.h declares, with its ctypes signature.
 SIGNATURES = {
     "seedq_layer_prepare": (C.c_int, [C.POINTER(LayerDesc), C.POINTER(Schedule), C.c_void_p,
@@ -176,6 +210,15 @@ SIGNATURES = {
                                        C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64,
                                        C.c_void_p]),
+    "seedq_rotary_angles": (C.c_int, [C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "seedq_rotate": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                               C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p]),
+    "seedq_kv_append_rotary": (C.c_int, [C.POINTER(KvCacheDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64,
+                                         C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "seedq_beam_select_workspace_bytes": (C.c_uint64, [C.c_int64, C.c_int32, C.c_int64]),
+    "seedq_beam_select": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "seedq_beam_reorder_workspace_bytes": (C.c_uint64, [C.c_int32, C.c_int32]),
+    "seedq_beam_reorder": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
     "seedq_status_string": (C.c_char_p, [C.c_int]),
     "seedq_last_cuda_error_string": (C.c_char_p, []),
 }

@@ -1,5 +1,6 @@
 """Python binding of the serving calls of libseedq.so: page bookkeeping, the
-8-bit key/value cache, the attention that reads it, and token log probabilities.
+8-bit key/value cache, the attention that reads it, rotary positions, token log
+probabilities, and beam search's choice with the pages of the chosen beams.
 
 Like the rest of the binding it marshals arguments and computes nothing: every
 buffer is the caller's torch tensor, every length and page number stays on the
@@ -11,7 +12,9 @@ refuses itself raises SeedQError.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import struct
+from fractions import Fraction
 
 import torch
 
@@ -19,6 +22,7 @@ from . import seedq as Q
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 KINDS = {"int8": 0, "e4m3": 1}
+LAYOUTS = {"half": 0, "pairs": 1}
 STATUS = {0: "ok", 1: "no pages", 2: "bad lengths", 3: "no room"}
 _CODE_TYPES = (torch.int8, torch.uint8, torch.float8_e4m3fn)
 
@@ -179,6 +183,27 @@ class KVCache:
         _ints(slots, n, torch.int64, dev, "slots")
         return n, dt, st
 
+    def append_rotary(self, k, v, slots, rotary, cos_sin, q=None, q_out=None, stream=None):
+        """seedq_kv_append_rotary: k (n_tokens, n_kv_heads, head_dim) rotated as
+        by rotary.rotate, then written with v at slots; q (n_tokens, n_heads,
+        head_dim) of k's type, if given, is rotated to q_out in the same launch."""
+        n, dt, st = self._pair(k, v, slots)
+        rotary._want_angles(cos_sin, n, self.device)
+        heads, ot, qs, os, qp, op = 0, dt, (0, 0), (0, 0), 0, 0
+        if q is not None:
+            heads = q.shape[1] if q.ndim == 3 else 0
+            qt, qs = _rows(q, "q", n, heads, self.head_dim, self.device)
+            if qt != dt or q_out is None:
+                raise ValueError("q: the type of k, and q_out beside it are wanted")
+            ot, os = _rows(q_out, "q_out", n, heads, self.head_dim, self.device)
+            _want_apart(q_out, "q_out")
+            qp, op = q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise ValueError("q_out: wanted beside q alone")
+        a = Q.APPEND_ROTARY_ARGS.pack(cos_sin.data_ptr(), rotary.rot_dim, rotary.layout, heads, ot, qp, qs[0], qs[1], op, os[0], os[1])
+        _check(Q.lib().seedq_kv_append_rotary(self._ref, k.data_ptr(), v.data_ptr(), dt, st[0], st[1], slots.data_ptr(), n, a,
+                                              _stream(stream, self.device)), "seedq_kv_append_rotary")
+
     def attend_workspace(self, n_heads: int, max_new: int = 1):
         """A zeroed workspace for attend() with that many query heads and, per
         request, up to max_new query tokens."""
@@ -211,6 +236,95 @@ class KVCache:
         except struct.error as e:
             raise ValueError(f"max_new, window: 32-bit integers, scale: a number are wanted ({e})") from None
         _check(Q.lib().seedq_kv_attend(self._ref, a, _stream(stream, dev)), "seedq_kv_attend")
+
+
+def _want_apart(t, name: str):
+    """Rows that are written must not lie on one another."""
+    if any(n > 1 and st < t.shape[2] for n, st in zip(t.shape, t.stride()[:2])):
+        raise ValueError(f"{name}: rows that overlap")
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, rule: str = "none", factor: float = 1.0, original: int = 8192,
+                       low: float = 1.0, high: float = 4.0):
+    """(frequencies, scale) for Rotary: radians per position of the rot_dim / 2
+    pairs, w_i = base^(-2 i / rot_dim), and the factor of cos and sin, for contexts
+    `factor` times as long as the `original` ones:
+      "none"    w_i
+      "linear"  w_i / factor
+      "base"    w_i of base * factor^(rot_dim / (rot_dim - 2)): the slowest pair is
+                stretched by factor, the fastest not at all
+      "bands"   by the turns t that a pair makes over the original context: w_i where
+                t >= high, w_i / factor where t <= low, between them both, mixed in
+                proportion to t
+      "ramp"    the same, mixed in proportion to the pair's number between the
+                (whole) numbers at which pairs make high and low turns (32 and 1
+                are usual); scale 1 + 0.1 ln factor"""
+    _want(rot_dim >= 2 and rot_dim % 2 == 0, f"rot_dim: an even number is wanted, got {rot_dim}")
+    _want(base > 1 and factor >= 1 and original >= 1 and 0 < low < high, "base > 1, factor >= 1, original >= 1, 0 < low < high are wanted")
+    half, scale = rot_dim // 2, 1.0
+    if rule == "base" and half > 1:
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    w = [base ** (-2.0 * i / rot_dim) for i in range(half)]
+    if rule == "linear":
+        keep = [0.0] * half
+    elif rule == "bands":
+        keep = [min(max((original * x / (2 * math.pi) - low) / (high - low), 0.0), 1.0) for x in w]
+    elif rule == "ramp":
+        at = lambda turns: rot_dim * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(base))  # noqa: E731
+        first, last = max(math.floor(at(high)), 0), min(math.ceil(at(low)), rot_dim - 1)
+        keep = [1.0 - min(max((i - first) / max(last - first, 0.001), 0.0), 1.0) for i in range(half)]
+        scale = 1.0 + 0.1 * math.log(factor)
+    else:
+        _want(rule in ("none", "base"), f"rule: none, linear, base, bands or ramp is wanted, got {rule!r}")
+        keep = [1.0] * half
+    return [x * k + x / factor * (1.0 - k) if k < 1.0 else x for x, k in zip(w, keep)], scale
+
+
+_TWO_PI = Fraction(6283185307179586476925286766559005768394, 10 ** 39)
+
+
+class Rotary:
+    """Rotary positions of one kind (see seedq_rotary_angles and seedq_rotate).
+
+    frequencies: radians per position of each pair (rot_dim / 2 numbers, as
+    rotary_frequencies gives them).  layout: "half" (numbers i and i + rot_dim / 2
+    of a head are a pair) or "pairs" (2i and 2i + 1).  scale: factor of cos and
+    sin.  Keeps the frequencies on the device in whole parts of a turn."""
+
+    def __init__(self, frequencies, layout: str = "half", scale: float = 1.0, device="cuda"):
+        _want(layout in LAYOUTS, f"layout: one of {sorted(LAYOUTS)} is wanted, got {layout!r}")
+        w = [float(x) for x in frequencies]
+        _want(w and all(math.isfinite(x) for x in w), "frequencies: one or more finite numbers are wanted")
+        self.half, self.rot_dim, self.layout, self.scale = len(w), 2 * len(w), LAYOUTS[layout], float(scale)
+        whole = [round(Fraction(x) / _TWO_PI * 2 ** 64) % 2 ** 64 for x in w]
+        self.turns = torch.tensor([x - 2 ** 64 if x >= 2 ** 63 else x for x in whole], dtype=torch.int64, device=device)
+        self.device = self.turns.device
+
+    def _want_angles(self, cos_sin, n, device):
+        if not (cos_sin.dtype is torch.float32 and cos_sin.shape == (n, self.half, 2) and cos_sin.is_contiguous()
+                and cos_sin.device == device):
+            raise ValueError(f"cos_sin: contiguous float32 ({n}, {self.half}, 2) on {device} is wanted")
+
+    def angles(self, positions, cos_sin, stream=None):
+        """seedq_rotary_angles: cos_sin (n_tokens, rot_dim / 2, 2) float32 of
+        positions (int32, at least n_tokens)."""
+        n = cos_sin.shape[0]
+        self._want_angles(cos_sin, n, self.device)
+        _ints(positions, n, torch.int32, self.device, "positions")
+        _check(Q.lib().seedq_rotary_angles(self.turns.data_ptr(), self.half, self.scale, positions.data_ptr(), n, cos_sin.data_ptr(),
+                                           _stream(stream, self.device)), "seedq_rotary_angles")
+
+    def rotate(self, x, cos_sin, out, stream=None):
+        """seedq_rotate: x, out (n_tokens, n_heads, head_dim); out may be x."""
+        if x.ndim != 3:
+            raise ValueError("x: (n_tokens, n_heads, head_dim) is wanted")
+        n, heads, dim = x.shape
+        self._want_angles(cos_sin, n, x.device)
+        xt, xs = _rows(x, "x", n, heads, dim, x.device)
+        ot, os = _rows(out, "out", n, heads, dim, x.device)
+        _want_apart(out, "out")
+        _check(Q.lib().seedq_rotate(x.data_ptr(), xt, xs[0], xs[1], n, heads, dim, self.rot_dim, self.layout, cos_sin.data_ptr(),
+                                    out.data_ptr(), ot, os[0], os[1], _stream(stream, x.device)), "seedq_rotate")
 
 
 def score_workspace(n_rows: int, vocab: int, device="cuda"):
@@ -258,3 +372,90 @@ def token_logprobs(logits, targets, logprob, entropy, rank, top_logprob, top_ind
     _check(Q.lib().seedq_token_logprobs(
         logits.data_ptr(), dt, n, vocab, st[0] if n > 1 else vocab, scale, pt, pl, pe, pr, k, px, pi, workspace.data_ptr(),
         workspace.nbytes, _stream(stream, dev)), "seedq_token_logprobs")
+
+
+def beam_workspace(n_groups: int, n_beams: int, vocab: int, device="cuda"):
+    """A zeroed workspace for beam_select over that many rows and tokens or fewer."""
+    n = Q.lib().seedq_beam_select_workspace_bytes(n_groups, n_beams, vocab)
+    _want(n > 0, "beam_workspace: 1..32 beams, up to 8192 rows and a vocabulary of up to 2^27 are wanted")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def _beams(t, name, dtype, shape, device):
+    if not (t.dtype in dtype and t.shape == shape and t.is_contiguous() and t.device == device):
+        raise ValueError(f"{name}: contiguous {' or '.join(map(str, dtype))} {tuple(shape)} on {device} is wanted")
+    return t.data_ptr()
+
+
+_F32, _I32, _BYTES = (torch.float32,), (torch.int32,), (torch.bool, torch.uint8)
+
+
+def beam_select(logits, scores, out_score, out_beam, out_token, workspace, scale: float = 1.0, done=None, end_token: int = -1,
+                weights=None, stream=None):
+    """seedq_beam_select: logits (n_groups * n_beams, vocab); scores, done (bool or
+    uint8, or None) and weights (or None) (n_groups, n_beams); out_score,
+    out_beam and out_token (n_groups, n_out) are written."""
+    dt, st = DTYPES.get(logits.dtype), logits.stride()
+    if len(st) != 2 or dt is None or (st[1] != 1 and logits.shape[1] != 1) or not logits.is_cuda:
+        raise ValueError("logits: (rows, vocab) float32, bfloat16 or float16 with contiguous rows on a CUDA device is wanted")
+    if scores.ndim != 2 or out_score.ndim != 2:
+        raise ValueError("scores, out_score: (n_groups, n_beams) and (n_groups, n_out) are wanted")
+    (rows, vocab), (groups, beams), n_out, dev = logits.shape, scores.shape, out_score.shape[1], logits.device
+    if rows != groups * beams:
+        raise ValueError(f"logits: a row for each of {groups} x {beams} beams is wanted, got {rows}")
+    shape, out = (groups, beams), (groups, n_out)
+    if not workspace.is_contiguous() or workspace.device != dev:
+        raise ValueError("workspace: a tensor of beam_workspace is wanted")
+    try:
+        a = Q.BEAM_SELECT_ARGS.pack(
+            logits.data_ptr(), st[0] if rows > 1 else vocab, dt, beams, groups, vocab, scale, end_token,
+            _beams(scores, "scores", _F32, shape, dev), 0 if done is None else _beams(done, "done", _BYTES, shape, dev),
+            0 if weights is None else _beams(weights, "weights", _F32, shape, dev), n_out,
+            _beams(out_score, "out_score", _F32, out, dev), _beams(out_beam, "out_beam", _I32, out, dev),
+            _beams(out_token, "out_token", _I32, out, dev), workspace.data_ptr(), workspace.nbytes)
+    except struct.error as e:
+        raise ValueError(f"end_token: a 32-bit integer, scale: a number are wanted ({e})") from None
+    _check(Q.lib().seedq_beam_select(a, _stream(stream, dev)), "seedq_beam_select")
+
+
+class BeamPages:
+    """The outputs of seedq_beam_reorder for n_groups requests of n_beams beams
+    over the caches of all layers (KVCache, alike but for their tensors):
+    seq_lens, status (per row) and free_count.  Allocated once, so a captured
+    graph keeps its addresses."""
+
+    def __init__(self, caches, n_groups: int, n_beams: int):
+        caches = list(caches)
+        _want(caches and all(isinstance(c, KVCache) and c.device == caches[0].device for c in caches),
+              "caches: KVCache objects of one device are wanted")
+        self.caches, self.n_groups, self.n_beams, self.device = caches, int(n_groups), int(n_beams), caches[0].device
+        n = Q.lib().seedq_beam_reorder_workspace_bytes(self.n_groups, self.n_beams)
+        _want(n > 0, "n_groups, n_beams: 1..32 beams and 1..8192 rows are wanted")
+        self.descs = (Q.KvCacheDesc * len(caches))(*(c.desc for c in caches))
+        self.rows = self.n_groups * self.n_beams
+        ints = torch.zeros(2 * self.rows + 1, dtype=torch.int32, device=self.device)
+        self.seq_lens, self.status, self.free_count = ints.split([self.rows, self.rows, 1])
+        self.workspace = torch.zeros(n, dtype=torch.uint8, device=self.device)
+
+    def reorder(self, parents, seq_lens, block_table, free_pages, free_count, out=None, stream=None):
+        """seedq_beam_reorder: parents (n_groups, n_beams) int32, seq_lens int32 of
+        at least as many rows; block_table changes in place, or out (the same
+        shape) gets the new one; free_pages changes in place."""
+        n, dev = self.rows, self.device
+        _ints(seq_lens, n, torch.int32, dev, "seq_lens")
+        _ints(free_pages, 0, torch.int32, dev, "free_pages")
+        _ints(free_count, 1, torch.int32, dev, "free_count")
+        _table(block_table, n, dev)
+        to = block_table if out is None else out
+        if out is not None:
+            _table(out, n, dev)
+            if out.shape[1] != block_table.shape[1]:
+                raise ValueError("out: as wide as block_table is wanted")
+        if n > 1 and to.stride(0) < to.shape[1]:
+            raise ValueError("out: rows that overlap")
+        a = Q.BEAM_REORDER_ARGS.pack(
+            self.n_groups, self.n_beams, _beams(parents, "parents", _I32, (self.n_groups, self.n_beams), dev), seq_lens.data_ptr(),
+            block_table.data_ptr(), _row_stride(block_table), to.data_ptr(), _row_stride(to), block_table.shape[1],
+            free_pages.shape[0], free_pages.data_ptr(), free_count.data_ptr(), self.seq_lens.data_ptr(), self.status.data_ptr(),
+            self.free_count.data_ptr(), self.workspace.data_ptr(), self.workspace.nbytes)
+        _check(Q.lib().seedq_beam_reorder(self.descs, len(self.caches), a, _stream(stream, dev)), "seedq_beam_reorder")

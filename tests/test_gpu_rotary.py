@@ -1,0 +1,352 @@
+"""Rotary positions and the rotating cache write on the GPU against the fp64 oracle.
+
+Tolerances, with u = 2^-24.  Angles: the fraction of a turn is cut to 2^-32 of one
+and its rest, at most an eighth, rounded to 25 bits (2^-28 of a turn at most):
+together 2 pi 2^-27.9 < 0.42 u' with u' = 2^-24; sincospif is within 2 units in the
+last place of numbers up to 1 (2 u), and the factor `scale` rounds once more (u): at
+most 4 u scale.  Rotation: a product and a fused sum, each rounded once: 2 u times
+the sum of the two products' magnitudes, then half a step of the output's type.
+"""
+import os
+import sys
+
+import numpy as np
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+sys.path.insert(0, ROOT)
+sys.path.insert(0, os.path.join(ROOT, "oracle"))
+
+import serving as S  # noqa: E402
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def V():
+    from paper_2609_38477_gb300 import build
+
+    build.build()
+    from paper_2609_38477_gb300 import seedq, serving
+
+    seedq.lib()
+    return serving
+
+
+def angles_of(V, rotary, positions):
+    cs = torch.empty((len(positions), rotary.half, 2), device="cuda")
+    rotary.angles(torch.tensor(positions, dtype=torch.int32, device="cuda"), cs)
+    return cs
+
+
+# ---------------------------------------------------------------- angles
+
+@pytest.mark.parametrize("rot,rule,factor", [(2, "none", 1.0), (24, "linear", 4.0), (128, "bands", 8.0), (96, "ramp", 4.0), (64, "base", 2.0),
+                                             (1024, "none", 1.0)])
+def test_angles(V, rot, rule, factor):
+    w, scale = V.rotary_frequencies(rot, 500000.0 if rot == 128 else 10000.0, rule, factor)
+    positions = [0, 1, 2, 7, 1000, 131071, 10 ** 6 + 3, 2 ** 24 + 1, 2 ** 31 - 1, -1, -5, -131071, -2 ** 31]
+    cs = angles_of(V, V.Rotary(w, scale=scale), positions)
+    want = S.rotary_angles(positions, w, scale)
+    assert np.abs(cs.double().cpu().numpy() - want).max() <= 4 * U * scale
+    assert bool((cs[0, :, 0] == torch.tensor(scale, dtype=torch.float32)).all()) and bool((cs[0, :, 1] == 0).all())
+
+
+def test_angles_of_frequencies_above_a_turn_and_below_zero(V):
+    """Whole turns vanish, negative frequencies turn backwards; and a factor of any size."""
+    w = [2 * np.pi * 5, -0.3, 100.0, 0.0, 1e-12, 3.0]
+    positions = [0, 1, 3, -7, 12345, 2 ** 30]
+    for scale in (1.0, -2.5, 0.0, 1e30):
+        cs = angles_of(V, V.Rotary(w, scale=scale), positions)
+        assert np.abs(cs.double().cpu().numpy() - S.rotary_angles(positions, w, scale)).max() <= 4 * U * abs(scale)
+
+
+# ---------------------------------------------------------------- rotation
+
+def check_rotate(V, x, cs, rotary, layout, out, inplace=False):
+    want, size = S.rotate(x.double().cpu().numpy(), cs.double().cpu().numpy(), layout)
+    rotary.rotate(x, cs, out)
+    got = out.double().cpu().numpy()
+    info = torch.finfo(out.dtype)
+    # half a step of the type (of its subnormals: half their distance) on what the sums may be off by
+    off = 2 * U * size
+    tol = off + (np.abs(want) + off) * info.eps / 2 + info.tiny * info.eps / 2
+    tol = np.where(size > 0, tol, np.abs(want) * info.eps / 2 + info.tiny * info.eps / 2)
+    assert np.all(np.abs(got - want) <= tol)
+    return got
+
+
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("ti,to", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("f32", "bf16"), ("bf16", "f32"), ("f16", "bf16"), ("f32", "f16")])
+@pytest.mark.parametrize("n,heads,dim,rot", [(1, 1, 2, 2), (1, 40, 128, 128), (16, 5, 32, 32), (333, 3, 96, 24), (7, 4, 80, 20), (65, 2, 64, 6),
+                                             (5, 9, 256, 128), (3, 1, 99, 50), (2, 3, 1000, 998), (1100, 33, 64, 64)])
+def test_rotate(V, layout, ti, to, n, heads, dim, rot):
+    rng = np.random.RandomState(n + heads + dim + rot)
+    rotary = V.Rotary(V.rotary_frequencies(rot)[0], layout, scale=1.25)
+    cs = angles_of(V, rotary, rng.randint(0, 200000, n).tolist())
+    x = torch.from_numpy(rng.randn(n, heads, dim).astype(np.float32)).to(DT[ti]).cuda()
+    out = torch.full((n, heads, dim), 9.0, dtype=DT[to], device="cuda")
+    check_rotate(V, x, cs, rotary, layout, out)
+    if ti == to:  # where it lies: the same numbers
+        y = x.clone()
+        rotary.rotate(y, cs, y)
+        assert torch.equal(y, out)
+
+
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("dtype", list(DT))
+def test_rotate_strides(V, layout, dtype):
+    """Heads of a fused projection at odd offsets, heads before tokens, one row for all tokens; neighbours stay."""
+    n, h, d, r = 9, 4, 64, 48
+    rng = np.random.RandomState(1)
+    rotary = V.Rotary(V.rotary_frequencies(r)[0], layout)
+    cs = angles_of(V, rotary, rng.randint(0, 5000, n).tolist())
+    for shift, width in ((0, 3 * h * d), (1, 3 * h * d + 1), (4, 3 * h * d + 4), (2, 3 * h * d + 2)):
+        flat = torch.from_numpy(rng.randn(shift + n * width).astype(np.float32)).to(DT[dtype]).cuda()
+        before = flat.clone()
+        x = flat[shift:].view(n, width)[:, h * d:2 * h * d].view(n, h, d)
+        out = torch.empty((n, h, d), dtype=DT[dtype], device="cuda")
+        check_rotate(V, x, cs, rotary, layout, out)
+        rotary.rotate(x, cs, x)  # in its place
+        assert torch.equal(x, out)
+        x.copy_(before[shift:].view(n, width)[:, h * d:2 * h * d].view(n, h, d))
+        assert torch.equal(flat, before)
+    x = torch.from_numpy(rng.randn(h, n, d).astype(np.float32)).to(DT[dtype]).cuda().transpose(0, 1)
+    out = torch.empty((h, n, d), dtype=DT[dtype], device="cuda").transpose(0, 1)
+    check_rotate(V, x, cs, rotary, layout, out)
+    x = x[:1].expand(n, h, d)
+    check_rotate(V, x, cs, rotary, layout, out)
+
+
+def test_rotate_not_a_number_stays_in_its_pair(V):
+    rotary = V.Rotary(V.rotary_frequencies(32)[0])
+    cs = angles_of(V, rotary, [5, 6])
+    x = torch.randn(2, 2, 48, device="cuda")
+    clean, out = torch.empty_like(x), torch.empty_like(x)
+    rotary.rotate(x, cs, clean)
+    x[0, 1, 3], x[1, 0, 40], x[1, 1, 20] = float("nan"), float("inf"), float("nan")
+    rotary.rotate(x, cs, out)
+    bad = torch.zeros_like(x, dtype=torch.bool)
+    bad[0, 1, [3, 19]] = bad[1, 1, [4, 20]] = True
+    assert bool(out[bad].isnan().all()) and out[1, 0, 40] == float("inf")
+    bad[1, 0, 40] = True
+    assert torch.equal(out[~bad], clean[~bad])
+
+
+def test_nothing_to_rotate(V):
+    rotary = V.Rotary([1.0])
+    cs = torch.empty((0, 1, 2), device="cuda")
+    rotary.angles(torch.empty(0, dtype=torch.int32, device="cuda"), cs)
+    rotary.rotate(torch.empty((0, 3, 2), device="cuda"), cs, torch.empty((0, 3, 2), device="cuda"))
+    cs = angles_of(V, rotary, [1, 2])
+    rotary.rotate(torch.empty((2, 0, 2), device="cuda"), cs, torch.empty((2, 0, 2), device="cuda"))
+
+
+# ---------------------------------------------------------------- on the way into the cache
+
+def new_cache(V, pages, heads, page, dim, kind, order="head"):
+    shape = (pages, heads, page, dim) if order == "head" else (pages, page, heads, dim)
+    t = [torch.full(shape, 0x55, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    if order == "token":
+        t = [x.transpose(1, 2) for x in t]
+    return V.KVCache(*t, *(torch.full((pages, heads), 77.0, device="cuda") for _ in range(2)), kind)
+
+
+def same(a, b):
+    for x, y in ((a.k, b.k), (a.v, b.v)):
+        assert torch.equal(x, y)
+    for x, y in ((a.k_scale, b.k_scale), (a.v_scale, b.v_scale)):
+        assert torch.equal(x.nan_to_num(-1), y.nan_to_num(-1))
+
+
+def both_ways(V, a, b, k, v, slots, rotary, cs, q=None, q_out=None):
+    """The call, and its two halves: keys rotated in float32, then appended."""
+    a.append_rotary(k, v, slots, rotary, cs, q=q, q_out=q_out)
+    turned = torch.empty(k.shape, device="cuda")
+    rotary.rotate(k, cs, turned)
+    b.append(turned, v.float().contiguous(), slots)
+    same(a, b)
+    if q is not None:
+        want = torch.empty_like(q_out)
+        rotary.rotate(q, cs, want)
+        assert torch.equal(q_out, want)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("heads,page,dim,rot,order", [(1, 16, 16, 16, "head"), (3, 32, 80, 80, "token"), (8, 16, 128, 128, "head"),
+                                                      (2, 256, 64, 32, "token"), (5, 48, 256, 64, "head"), (3, 64, 96, 24, "head"),
+                                                      (4, 256, 128, 128, "token"), (2, 32, 48, 38, "head"), (7, 128, 32, 2, "token"),
+                                                      (2, 240, 112, 112, "head")])
+def test_append_rotary_in_steps(V, kind, dtype, layout, heads, page, dim, rot, order):
+    """Runs of every length and offset, pages that fill up and are reused, slots outside; queries of another type out."""
+    rng = np.random.RandomState(heads * page + dim)
+    a, b = (new_cache(V, 6, heads, page, dim, kind, order) for _ in range(2))
+    rotary = V.Rotary(V.rotary_frequencies(rot)[0], layout, scale=1.1)
+    at = {}
+    for step in range(7):
+        slots = []
+        for p in rng.permutation(6)[:rng.randint(1, 6)]:
+            o = at.get(p, 0)
+            if o >= page or rng.rand() < 0.2:
+                o = 0
+            m = min(page - o, int(rng.choice([1, 2, 3, 15, 16, 17, 33, page])))
+            slots += list(range(p * page + o, p * page + o + m))
+            at[p] = o + m
+            if rng.rand() < 0.3:
+                slots.append(int(rng.choice([-1, 6 * page, 2 ** 40, -2 ** 40])))
+        n = len(slots)
+        size = 2.0 ** rng.randint(-9, 9, (2, n, 1, 1))
+        odd = step % 2  # rows that begin at an odd element
+        flat = torch.zeros(2 * n * heads * dim + odd, dtype=DT[dtype], device="cuda")
+        x = flat[odd:].view(2, n, heads, dim)
+        x.copy_(torch.from_numpy((size * rng.randn(2, n, heads, dim)).astype(np.float32)))
+        cs = angles_of(V, rotary, rng.randint(0, 100000, n).tolist())
+        q = torch.from_numpy(rng.randn(n, 3 * heads, dim).astype(np.float32)).to(DT[dtype]).cuda() if step != 3 else None
+        q_out = torch.full((n, 3 * heads, dim), 5.0, dtype=list(DT.values())[step % 3], device="cuda") if q is not None else None
+        both_ways(V, a, b, x[0], x[1], torch.tensor(slots, device="cuda"), rotary, cs, q, q_out)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("layout,rot", [("half", 64), ("pairs", 64), ("half", 32), ("half", 20)])
+def test_append_rotary_against_the_oracle(V, kind, layout, rot):
+    """Codes of keys turned in fp64: equal, or where the number lies within the rotation's
+    rounding of the border between two codes, one of the two."""
+    rng = np.random.RandomState(rot)
+    P, H, D, n = 16, 3, 64, 40
+    rotary = V.Rotary(V.rotary_frequencies(rot)[0], layout)
+    c = new_cache(V, 4, H, P, D, kind)
+    slots = list(range(16, 56))
+    cs = angles_of(V, rotary, (3000 + np.arange(n)).tolist())
+    x = torch.from_numpy(rng.randn(2, n, H, D).astype(np.float32)).bfloat16().cuda()
+    c.append_rotary(x[0], x[1], torch.tensor(slots, device="cuda"), rotary, cs)
+    turned, size = S.rotate(x[0].double().cpu().numpy(), cs.double().cpu().numpy(), layout)
+    for codes, scales, want, off in ((c.k, c.k_scale, turned, 2 * U * size), (c.v, c.v_scale, x[1].double().cpu().numpy(), 0 * size)):
+        wc, ws = np.zeros((4, H, P, D), np.uint8), np.zeros((4, H))
+        S.append(wc, ws, want, slots, P, kind)
+        got, gs = codes.cpu().numpy().view(np.uint8), scales.double().cpu().numpy()
+        for t, s in enumerate(slots):
+            b, o = s // P, s % P
+            assert np.array_equal(gs[b], ws[b])
+            g, w = S.decode(got[b, :, o], kind), S.decode(wc[b, :, o], kind)
+            border = (g + w) / 2 * ws[b][:, None]
+            assert np.all((g == w) | (np.abs(want[t] - border) <= off[t]))
+        assert np.mean(got[1:3] == wc[1:3]) > 0.999
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_append_rotary_extremes(V, kind):
+    """Zeros, numbers at the type's ends, NaN and infinities; scales that are no powers of two, as a caller may have."""
+    rotary = V.Rotary(V.rotary_frequencies(16)[0])
+    for first in (0.0, 3.0, float("nan"), 0.3):
+        a, b = (new_cache(V, 12, 1, 16, 16, kind) for _ in range(2))
+        rows = [0.0, 1e-45, 1e-39, 1.1754944e-38, 1e38, 127.0, 448.0, -0.0, float("inf"), float("-inf"), float("nan"), 5.0]
+        if first == 0.3:
+            for c in (a, b):
+                c.k_scale.fill_(0.3)
+                c.v_scale.fill_(0.3)
+                c.k.fill_(3)
+                c.v.fill_(3)
+        else:
+            x = torch.full((12, 1, 16), first, device="cuda")
+            cs = angles_of(V, rotary, [3] * 12)
+            both_ways(V, a, b, x, x, torch.arange(12, device="cuda") * 16, rotary, cs)
+        x = torch.zeros((12, 1, 16), device="cuda")
+        x[:, 0, 5] = torch.tensor(rows)
+        cs = angles_of(V, rotary, list(range(12)))
+        both_ways(V, a, b, x, x, torch.arange(12, device="cuda") * 16 + 1, rotary, cs)
+
+
+def test_append_rotary_without_tokens(V):
+    rotary = V.Rotary([1.0, 0.5])
+    c = new_cache(V, 2, 2, 16, 16, "int8")
+    e = torch.empty((0, 2, 16), device="cuda")
+    c.append_rotary(e, e, torch.empty(0, dtype=torch.int64, device="cuda"), rotary, torch.empty((0, 2, 2), device="cuda"), q=e, q_out=e)
+    assert bool((c.k == 0x55).all())
+
+
+def test_append_rotary_of_many_single_tokens(V):
+    """Every token a page of its own, more than the warps of a launch's first wave, queries in place."""
+    rotary = V.Rotary(V.rotary_frequencies(128)[0])
+    n, h = 700, 9
+    a, b = (new_cache(V, n, h, 16, 128, "int8") for _ in range(2))
+    x = torch.randn((2, n, h, 128), device="cuda")
+    cs = angles_of(V, rotary, list(range(n)))
+    q = torch.randn((n, 2 * h, 128), device="cuda")
+    want = torch.empty_like(q)
+    rotary.rotate(q, cs, want)
+    slots = torch.randperm(n, device="cuda") * 16
+    a.append_rotary(x[0], x[1], slots, rotary, cs, q=q, q_out=q)
+    assert torch.equal(q, want)
+    k = torch.empty_like(x[0])
+    rotary.rotate(x[0], cs, k)
+    b.append(k, x[1], slots)
+    for y, z in ((a.k, b.k), (a.v, b.v)):
+        assert torch.equal(y[:, :, 0], z[:, :, 0])
+
+
+@pytest.mark.parametrize("page", [16, 64])
+def test_rotation_captured_and_replayed(V, page):
+    """A step's angles, rotation and cache write in a graph, replayed with other positions and numbers."""
+    n, h, d = 5, 3, 64
+    rotary = V.Rotary(V.rotary_frequencies(d)[0])
+    a, b = (new_cache(V, 8, h, page, d, "int8") for _ in range(2))
+    for c in (a, b):
+        c.k.zero_()
+        c.v.zero_()
+    pos = torch.zeros(n, dtype=torch.int32, device="cuda")
+    slots = torch.zeros(n, dtype=torch.int64, device="cuda")
+    x, q = torch.randn((2, n, h, d), device="cuda"), torch.randn((n, 2 * h, d), device="cuda")
+    cs, q_out, direct = torch.empty((n, d // 2, 2), device="cuda"), torch.empty_like(q), torch.empty_like(q)
+
+    def step():
+        rotary.angles(pos, cs)
+        a.append_rotary(x[0], x[1], slots, rotary, cs, q=q, q_out=q_out)
+        rotary.rotate(q, cs, direct)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for i in range(3):
+        pos.copy_(torch.randint(0, 50000, (n,)))
+        slots.copy_(torch.arange(n) + i * n + page)
+        x.normal_()
+        q.normal_()
+        graph.replay()
+        cs2 = torch.empty_like(cs)
+        rotary.angles(pos, cs2)
+        assert torch.equal(cs, cs2) and torch.equal(q_out, direct)
+        k = torch.empty_like(x[0])
+        rotary.rotate(x[0], cs2, k)
+        b.append(k, x[1], slots)
+        same(a, b)
+
+
+def test_other_streams(V):
+    """Calls on a stream of their own, given and current."""
+    rotary = V.Rotary(V.rotary_frequencies(64)[0])
+    x = torch.randn((300, 8, 64), device="cuda")
+    pos = torch.arange(300, dtype=torch.int32, device="cuda")
+    want = torch.empty_like(x)
+    rotary.rotate(x, angles_of(V, rotary, list(range(300))), want)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for given in (True, False):
+        cs, out = torch.empty((300, 32, 2), device="cuda"), torch.empty_like(x)
+        s.wait_stream(torch.cuda.current_stream())
+        if given:
+            rotary.angles(pos, cs, stream=s)
+            rotary.rotate(x, cs, out, stream=s)
+        else:
+            with torch.cuda.stream(s):
+                rotary.angles(pos, cs)
+                rotary.rotate(x, cs, out)
+        s.synchronize()
+        assert torch.equal(out, want)
