@@ -1,11 +1,11 @@
-// The 8-bit paged key/value cache: append (seedq_kv_append, seedq_kv_append_rotary)
-// and its inverse (seedq_kv_gather).
+// The 8-bit paged key/value cache: append (seedq_kv_append) and its inverse
+// (seedq_kv_gather).
 #include <cuda_runtime.h>
 #include <stdint.h>
 
 #include "cp_async.cuh"
 #include "f32x2.cuh"
-#include "rotary.cuh"
+#include "kv_codes.cuh"
 #include "serve.cuh"
 
 namespace seedq {
@@ -19,18 +19,6 @@ struct CacheArgs {
   int32_t vec;         // 2 or 1 where rows of x allow accesses of 32 or 16 bytes, else 0
   int32_t group_shift; // append: log2 of the tokens of a CTA
   int32_t page_shift;  // log2 of the page size, -1 if it is no power of two
-};
-
-// What the rotating append adds: the keys' cos and sin, and queries that CTAs
-// behind those of the append turn.
-struct RopeArgs {
-  const float2 *cs;
-  int32_t half, layout;
-  bool whole;       // pieces of 8 elements hold whole pairs, or one element of 8 pairs
-  bool wide;        // queries: by kRotateWide pairs
-  unsigned ctas;    // of the append
-  RotateArgs q;
-  RotateSplit split;
 };
 
 __device__ __forceinline__ int64_t page_of(const CacheArgs &a, int64_t slot) {  // -1 for a negative slot
@@ -88,37 +76,6 @@ struct Eight {
   }
 };
 
-// Four codes of the products x times a number, where none is past the largest code.
-// int8: 1.5 * 2^23 has unit 1, so adding it rounds to an integer in the low bits.
-template <int KIND>
-__device__ __forceinline__ uint32_t four_codes(uint64_t x01, uint64_t x23, uint64_t by2) {
-  if (KIND == SEEDQ_KV_INT8) {
-    const uint64_t one = f2_pack(12582912.f, 12582912.f);
-    const float2 a = f2_unpack(f2_add(f2_mul(x01, by2), one)), b = f2_unpack(f2_add(f2_mul(x23, by2), one));
-    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
-                       __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
-  }
-  const uint32_t lo = __nv_cvt_float2_to_fp8x2(f2_unpack(f2_mul(x01, by2)), __NV_SATFINITE, __NV_E4M3);
-  const uint32_t hi = __nv_cvt_float2_to_fp8x2(f2_unpack(f2_mul(x23, by2)), __NV_SATFINITE, __NV_E4M3);
-  return lo | hi << 16;
-}
-// The numbers of four codes, in pairs.  int8: byte + 128 in the low bits of 2^23.
-template <int KIND>
-__device__ __forceinline__ void four_values(uint32_t w, uint64_t &x01, uint64_t &x23) {
-  if (KIND == SEEDQ_KV_INT8) {
-    const uint32_t y = w ^ 0x80808080u;
-    const uint64_t off = f2_pack(-8388736.f, -8388736.f);
-    auto wide = [&](int sel) { return __uint_as_float(__byte_perm(y, 0x4b000000u, sel)); };
-    x01 = f2_add(f2_pack(wide(0x7440), wide(0x7441)), off);
-    x23 = f2_add(f2_pack(wide(0x7442), wide(0x7443)), off);
-  } else {
-    const uint32_t lo = e4m3x2_to_half2(w), hi = e4m3x2_to_half2(w >> 16);
-    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&lo));
-    const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
-    x01 = f2_pack(a.x, a.y), x23 = f2_pack(b.x, b.y);
-  }
-}
-
 // ---------------------------------------------------------------- append
 //
 // A page's tokens are read, their largest magnitude is found, and the codes are
@@ -143,57 +100,8 @@ constexpr int kAppendWarps = 4;
 constexpr int kAppendBlocks = 7;  // per SM: 28 warps of up to 73 registers
 constexpr int kKeptPieces = 14;   // of a lane in shared memory: 7 KB per warp
 
-//
-// With ROT the keys are turned by their token's cos and sin before their largest
-// magnitude is taken: a piece's partners in their pairs are its own elements, or
-// the same lanes' of a piece half the rotated dims away, read from the token
-// itself or, where the token was kept, from the lane that kept it.
-template <int DT>
-__device__ __forceinline__ Eight<SEEDQ_F32> widened(const Eight<DT> &e) {
-  Eight<SEEDQ_F32> y;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) y.w[k] = __float_as_uint(e.get(k));
-  return y;
-}
-// The piece at dim d of token t's key; e holds it, other(...) gives the piece with its partners.
-template <int DT, typename Other>
-__device__ __forceinline__ Eight<SEEDQ_F32> turned_piece(const RopeArgs &r, const Eight<DT> &e, const void *x, int64_t at, int64_t t,
-                                                         int d, Other &&other) {
-  Eight<SEEDQ_F32> y = widened(e);
-  if (d >= 2 * r.half) return y;
-  const float2 *cs = r.cs + t * r.half;
-  if (r.layout == SEEDQ_ROPE_PAIRS) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (d / 2 + k < r.half) {
-        const float2 z = turned(e.get(2 * k), e.get(2 * k + 1), cs[d / 2 + k]);
-        y.w[2 * k] = __float_as_uint(z.x), y.w[2 * k + 1] = __float_as_uint(z.y);
-      }
-  } else if (r.whole) {
-    const bool second = d >= r.half;
-    const Eight<DT> o = other(second ? -r.half : r.half);
-    const float2 *c = cs + (second ? d - r.half : d);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float2 z = second ? turned(o.get(k), e.get(k), c[k]) : turned(e.get(k), o.get(k), c[k]);
-      y.w[k] = __float_as_uint(second ? z.y : z.x);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int i = d + k;
-      if (i >= 2 * r.half) continue;
-      const bool second = i >= r.half;
-      const float o = load_elem(x, DT, at + k + (second ? -r.half : r.half));
-      const float2 z = second ? turned(o, e.get(k), cs[i - r.half]) : turned(e.get(k), o, cs[i]);
-      y.w[k] = __float_as_uint(second ? z.y : z.x);
-    }
-  }
-  return y;
-}
-
-template <int KIND, int DT, bool ROT>
-__device__ __forceinline__ void append_body(const CacheArgs &a, const RopeArgs &rope) {
+template <int KIND, int DT>
+__global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(const __grid_constant__ CacheArgs a) {
   constexpr int kHeld = 1, kPieces = DT == SEEDQ_F32 ? 2 : 1;  // 16-byte pieces of a lane and step
   constexpr int kKept = kKeptPieces / kPieces;
   __shared__ uint4 s_kept[kAppendWarps][kKeptPieces][32];
@@ -246,25 +154,8 @@ __device__ __forceinline__ void append_body(const CacheArgs &a, const RopeArgs &
         const void *x = a.x[which];
         uint8_t *code = (uint8_t *)(which ? a.c.v : a.c.k) + page * a.c.page_stride + h * a.c.head_stride + d;
         const int64_t at = t0 * a.ts + h * a.hs + d;
-        using Piece = Eight<ROT ? (int)SEEDQ_F32 : DT>;
-        Piece held[kHeld];
+        Eight<DT> held[kHeld];
         uint32_t amax = 0;
-        // as it lies in memory, or turned
-        auto load = [&](int t) {
-          Eight<DT> e;
-          e.load(x, at + t * a.ts, a.vec);
-          if constexpr (ROT) {
-            if (which == 0)
-              return turned_piece(rope, e, x, at + t * a.ts, t0 + t, d, [&](int by) {
-                Eight<DT> o;
-                o.load(x, at + t * a.ts + by, a.vec);
-                return o;
-              });
-            return widened(e);
-          } else {
-            return e;
-          }
-        };
         const int kept = a.vec ? kKept : 0;
         if (kHeld * stride < m)
           for (int k = 0; k < kept; ++k) {
@@ -274,40 +165,32 @@ __device__ __forceinline__ void append_body(const CacheArgs &a, const RopeArgs &
               for (int y = 0; y < kPieces; ++y)
                 cp_async16(&s_kept[w][k * kPieces + y][lane], (const char *)x + (at + t * a.ts) * (kPieces * 2) + 16 * y);
           }
-        auto kept_piece = [&](int k, int from) {
+        auto from_kept = [&](int k) {
           Eight<DT> e;
 #pragma unroll
           for (int y = 0; y < kPieces; ++y) {
-            const uint4 v = s_kept[w][k * kPieces + y][from];
+            const uint4 v = s_kept[w][k * kPieces + y][lane];
             e.w[4 * y] = v.x, e.w[4 * y + 1] = v.y, e.w[4 * y + 2] = v.z, e.w[4 * y + 3] = v.w;
           }
           return e;
         };
-        auto from_kept = [&](int k) {
-          if constexpr (ROT) {
-            const Eight<DT> e = kept_piece(k, lane);
-            const int t = first + (kHeld + k) * stride;
-            if (which == 0)
-              return turned_piece(rope, e, x, at + t * a.ts, t0 + t, d, [&](int by) { return kept_piece(k, lane + by / 8); });
-            return widened(e);
-          } else {
-            return kept_piece(k, lane);
-          }
-        };
 #pragma unroll
         for (int k = 0; k < kHeld; ++k)
-          if (first + k * stride < mine) held[k] = load(first + k * stride);
+          if (first + k * stride < mine) held[k].load(x, at + (first + k * stride) * a.ts, a.vec);
 #pragma unroll
         for (int k = 0; k < kHeld; ++k)
           if (first + k * stride < mine) held[k].largest(amax);
 #pragma unroll 2
-        for (int t = first + (kHeld + kept) * stride; t < mine; t += stride) load(t).largest(amax);
+        for (int t = first + (kHeld + kept) * stride; t < mine; t += stride) {
+          Eight<DT> e;
+          e.load(x, at + t * a.ts, a.vec);
+          e.largest(amax);
+        }
         cp_async_commit();
         cp_async_wait<0>();
-        if (ROT) __syncwarp();  // other lanes' pieces
 #pragma unroll 2
         for (int k = 0; k < kept && first + (kHeld + k) * stride < mine; ++k) from_kept(k).largest(amax);
-        amax = __reduce_max_sync(~0u, Piece::largest_bits(amax));
+        amax = __reduce_max_sync(~0u, Eight<DT>::largest_bits(amax));
         float was = old;
         if (together) {  // what is written here was last read before another pair's barrier
           if (lane == 0) s_max[p][w] = amax;
@@ -338,22 +221,17 @@ __device__ __forceinline__ void append_body(const CacheArgs &a, const RopeArgs &
         const bool exact = (nb & 0x7fffffu) == 0 && nb < 0x7f000000u && nb != 0;
         const float inv = exact ? __uint_as_float(0x7f000000u - nb) : 0.f;
         const uint64_t inv2 = f2_pack(inv, inv);
-        auto write = [&](const Piece &e, int t) {
+        auto write = [&](const Eight<DT> &e, int t) {
           uint32_t z[2] = {0, 0};
           if (exact) {
             z[0] = four_codes<KIND>(e.pair(0), e.pair(1), inv2);
             z[1] = four_codes<KIND>(e.pair(2), e.pair(3), inv2);
           } else if (now > 0.f) {
-            if constexpr (ROT) {
-#pragma unroll
-              for (int k = 0; k < 8; ++k) z[k / 4] |= value_code<KIND>(__fdiv_rn(e.get(k), now)) << 8 * (k & 3);
-            } else {
 #pragma unroll 1
-              for (int k = 0; k < 8; ++k) {
-                const uint32_t c = value_code<KIND>(__fdiv_rn(load_elem(x, DT, at + t * a.ts + k), now)) << 8 * (k & 3);
-                if (k < 4) z[0] |= c;
-                else z[1] |= c;
-              }
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t c = value_code<KIND>(__fdiv_rn(load_elem(x, DT, at + t * a.ts + k), now)) << 8 * (k & 3);
+              if (k < 4) z[0] |= c;
+              else z[1] |= c;
             }
           }
           *(uint2 *)(code + (off + t) * ts) = make_uint2(z[0], z[1]);
@@ -364,9 +242,12 @@ __device__ __forceinline__ void append_body(const CacheArgs &a, const RopeArgs &
 #pragma unroll 2
         for (int k = 0; k < kept && first + (kHeld + k) * stride < mine; ++k) write(from_kept(k), first + (kHeld + k) * stride);
 #pragma unroll 2
-        for (int t = first + (kHeld + kept) * stride; t < mine; t += stride) write(load(t), t);
+        for (int t = first + (kHeld + kept) * stride; t < mine; t += stride) {
+          Eight<DT> e;
+          e.load(x, at + t * a.ts, a.vec);
+          write(e, t);
+        }
         if (p == w) old = now;
-        if (ROT) __syncwarp();  // what the other lanes kept is read
       }
       t0 += m;
       slot = t0 < a.n ? a.slots[t0] : -1;
@@ -374,31 +255,6 @@ __device__ __forceinline__ void append_body(const CacheArgs &a, const RopeArgs &
       else __syncwarp();
     } while (page_of(a, slot) == page);
     if (owner && lane == 0) *scale = old;
-  }
-}
-
-template <int KIND, int DT>
-__global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks) k_kv_append(const __grid_constant__ CacheArgs a) {
-  append_body<KIND, DT, false>(a, RopeArgs());
-}
-
-template <int DT, int N>
-__device__ __forceinline__ void rotate_query(const RopeArgs &r, int64_t i) {
-  switch (r.q.out_dtype) {
-    case SEEDQ_F32: rotate_item<DT, SEEDQ_F32, N>(r.q, r.split, i); break;
-    case SEEDQ_BF16: rotate_item<DT, SEEDQ_BF16, N>(r.q, r.split, i); break;
-    default: rotate_item<DT, SEEDQ_F16, N>(r.q, r.split, i);
-  }
-}
-template <int KIND, int DT>
-__global__ void __launch_bounds__(kAppendWarps * 32, kAppendBlocks)
-    k_kv_append_rotary(const __grid_constant__ CacheArgs a, const __grid_constant__ RopeArgs rope) {
-  if (blockIdx.x < rope.ctas) {
-    append_body<KIND, DT, true>(a, rope);
-  } else {
-    const int64_t i = (int64_t)(blockIdx.x - rope.ctas) * blockDim.x + threadIdx.x;
-    if (rope.wide) rotate_query<DT, kRotateWide>(rope, i);
-    else rotate_query<DT, 1>(rope, i);
   }
 }
 
@@ -493,15 +349,6 @@ int64_t append_ctas(const CacheArgs &a) {
   const int64_t groups = (a.n + (1 << a.group_shift) - 1) >> a.group_shift;
   return groups * ((a.c.n_kv_heads * 2 + kAppendWarps - 1) / kAppendWarps);
 }
-void set_groups(CacheArgs &a) {
-  // One token per warp until the warps fill the GPU twice over, then more.  Each may
-  // be a page of its own (32 heads, 256 single tokens: 10.4 us, with one token per
-  // warp 11.5, with 32 38; 512: 17, 21 and 40), or all on a page (4 prompts of 1024,
-  // pages of 64: 23 us, with one token per warp 77, with 32 24).  At half the
-  // threshold 256 single tokens take 9.5 and the prompts as long, at twice 11.6 and 28.
-  a.group_shift = 0;
-  while (a.group_shift < 5 && (a.n >> a.group_shift) * a.c.n_kv_heads * 2 > 2 * 152 * 48) ++a.group_shift;
-}
 template <int KIND, int DT>
 void launch_append(const CacheArgs &a, cudaStream_t st) {
   k_kv_append<KIND, DT><<<(unsigned)append_ctas(a), kAppendWarps * 32, 0, st>>>(a);
@@ -512,13 +359,6 @@ void launch_gather(const CacheArgs &a, cudaStream_t st) {
   if (pieces <= kGatherSmall) k_kv_gather<KIND, DT, 16><<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(a);
   else k_kv_gather<KIND, DT, 32><<<(unsigned)((pieces / 2 + 255) / 256), 256, 0, st>>>(a);
 }
-template <int KIND, int DT>
-void launch_append_rotary(const CacheArgs &a, const RopeArgs &r, unsigned more, cudaStream_t st) {
-  k_kv_append_rotary<KIND, DT><<<r.ctas + more, kAppendWarps * 32, 0, st>>>(a, r);
-}
-using LaunchRotary = void (*)(const CacheArgs &, const RopeArgs &, unsigned, cudaStream_t);
-constexpr LaunchRotary kAppendRotary[2][3] = {{launch_append_rotary<0, 0>, launch_append_rotary<0, 1>, launch_append_rotary<0, 2>},
-                                              {launch_append_rotary<1, 0>, launch_append_rotary<1, 1>, launch_append_rotary<1, 2>}};
 using Launch = void (*)(const CacheArgs &, cudaStream_t);
 constexpr Launch kAppend[2][3] = {
     {launch_append<0, 0>, launch_append<0, 1>, launch_append<0, 2>}, {launch_append<1, 0>, launch_append<1, 1>, launch_append<1, 2>}};
@@ -549,45 +389,9 @@ seedq_status seedq_kv_append(const seedq_kv_cache *cache, const void *k, const v
   CacheArgs a;
   const seedq_status st = prepare(cache, k, v, dtype, token_stride, head_stride, slots, n_tokens, a);
   if (st != SEEDQ_OK || n_tokens == 0) return st;
-  set_groups(a);
+  a.group_shift = append_group_shift(n_tokens, cache->n_kv_heads);
   if (append_ctas(a) > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
   kAppend[cache->kind][dtype](a, (cudaStream_t)cuda_stream);
-  const cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
-}
-
-seedq_status seedq_kv_append_rotary(const seedq_kv_cache *cache, const void *k, const void *v, int32_t dtype,
-                                    int64_t token_stride, int64_t head_stride, const int64_t *slots, int64_t n_tokens,
-                                    const seedq_append_rotary_args *args, void *cuda_stream) {
-  CacheArgs a;
-  const seedq_status st = prepare(cache, k, v, dtype, token_stride, head_stride, slots, n_tokens, a);
-  if (st != SEEDQ_OK) return st;
-  if (!args || !rope_ok(args->layout, args->rot_dim, cache->head_dim)) return SEEDQ_ERR_INVALID_ARG;
-  const bool queries = args->n_heads > 0;
-  if (args->n_heads < 0 || args->n_heads > SEEDQ_ROPE_MAX_HEADS || (queries && !dtype_ok(args->out_dtype))) return SEEDQ_ERR_INVALID_ARG;
-  if (n_tokens == 0) return SEEDQ_OK;
-  if (!args->cos_sin || (uintptr_t)args->cos_sin % 8) return SEEDQ_ERR_INVALID_ARG;
-  if (queries) {
-    if (!args->q || !args->q_out) return SEEDQ_ERR_INVALID_ARG;
-    if (args->q == args->q_out && (args->out_dtype != dtype || args->q_token_stride != args->out_token_stride ||
-                                   args->q_head_stride != args->out_head_stride))
-      return SEEDQ_ERR_INVALID_ARG;
-  }
-  set_groups(a);
-  RopeArgs r{};
-  r.cs = (const float2 *)args->cos_sin, r.half = args->rot_dim / 2, r.layout = args->layout;
-  r.whole = r.half % 8 == 0;
-  int64_t more = 0;
-  if (queries) {
-    const int32_t out = args->out_dtype;
-    r.q = RotateArgs{args->q, args->q_out, args->q_token_stride, args->q_head_stride, args->out_token_stride, args->out_head_stride,
-                     n_tokens, args->n_heads, cache->head_dim, r.half, r.layout, out, r.cs};
-    r.wide = rotate_split(r.q, dtype, out, r.split);
-    more = (n_tokens * r.split.pieces * r.split.groups + kAppendWarps * 32 - 1) / (kAppendWarps * 32);
-  }
-  if (append_ctas(a) + more > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
-  r.ctas = (unsigned)append_ctas(a);
-  kAppendRotary[cache->kind][dtype](a, r, (unsigned)more, (cudaStream_t)cuda_stream);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
 }

@@ -45,17 +45,26 @@ __global__ void __launch_bounds__(256) k_rotate(const __grid_constant__ RotateAr
 
 template <int IN, int OUT>
 seedq_status launch(const RotateArgs &a, cudaStream_t st) {
-  RotateSplit s{};
-  const bool wide = rotate_split(a, IN, OUT, s);
+  const RotateSplit s = rotate_split(a, IN, OUT);
   const int64_t ctas = (a.n * s.pieces * s.groups + 255) / 256;
   if (ctas > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
-  if (wide) k_rotate<IN, OUT, kRotateWide><<<(unsigned)ctas, 256, 0, st>>>(a, s);
+  if (s.wide == 8) k_rotate<IN, OUT, 8><<<(unsigned)ctas, 256, 0, st>>>(a, s);
+  else if (s.wide == 4) k_rotate<IN, OUT, 4><<<(unsigned)ctas, 256, 0, st>>>(a, s);
   else k_rotate<IN, OUT, 1><<<(unsigned)ctas, 256, 0, st>>>(a, s);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
 }
 
 }  // namespace
+
+seedq_status rotate_launch(const RotateArgs &a, int32_t in, cudaStream_t st) {
+  using Launch = seedq_status (*)(const RotateArgs &, cudaStream_t);
+  static constexpr Launch kLaunch[3][3] = {{launch<0, 0>, launch<0, 1>, launch<0, 2>},
+                                           {launch<1, 0>, launch<1, 1>, launch<1, 2>},
+                                           {launch<2, 0>, launch<2, 1>, launch<2, 2>}};
+  return kLaunch[in][a.out_dtype](a, st);
+}
+
 }  // namespace seedq
 
 using namespace seedq;
@@ -88,11 +97,7 @@ seedq_status seedq_rotate(const void *x, int32_t x_dtype, int64_t x_token_stride
     return SEEDQ_ERR_INVALID_ARG;
   const RotateArgs a{x, out, x_token_stride, x_head_stride, out_token_stride, out_head_stride, n_tokens, n_heads, head_dim,
                      rot_dim / 2, layout, out_dtype, (const float2 *)cos_sin};
-  using Launch = seedq_status (*)(const RotateArgs &, cudaStream_t);
-  static constexpr Launch kLaunch[3][3] = {{launch<0, 0>, launch<0, 1>, launch<0, 2>},
-                                           {launch<1, 0>, launch<1, 1>, launch<1, 2>},
-                                           {launch<2, 0>, launch<2, 1>, launch<2, 2>}};
-  return kLaunch[x_dtype][out_dtype](a, (cudaStream_t)cuda_stream);
+  return rotate_launch(a, x_dtype, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

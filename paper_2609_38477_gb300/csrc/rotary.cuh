@@ -78,6 +78,9 @@ __device__ __forceinline__ float2 turned(float x, float y, float2 cs) {
   return make_float2(fmaf(x, cs.x, -(y * cs.y)), fmaf(y, cs.x, x * cs.y));
 }
 
+constexpr int kRotateHeads = 4;                  // of a thread, where there is work for all SMs
+constexpr int64_t kRotateMany = 152 * 2048 * 4;  // threads from which on one takes several heads
+
 struct RotateArgs {
   const void *x;
   void *out;
@@ -88,25 +91,34 @@ struct RotateArgs {
   const float2 *cs;        // n x half
 };
 
-// Work on a token and head: `pieces` threads, of which the first take N pairs each
-// and the others copy 2 N of the dims behind the rotated ones.
+// Work on a token: `pieces` threads to a head, of which the first take N pairs each
+// and the others copy 2 N of the dims behind the rotated ones; `groups` such rows of
+// threads, each with the heads that lie `groups` apart, whose cos and sin it reads once.
 struct RotateSplit {
-  int32_t turns, pieces;
-  int32_t groups;  // threads of a token are pieces x groups, each with heads of distance `groups`
+  int32_t turns, pieces, groups, wide;  // wide: N
 };
-// Sets the split; true where the call's rows allow N = kRotateWide, else N is 1.
-constexpr int kRotateWide = 4;
-inline bool rotate_split(const RotateArgs &a, int32_t in, int32_t out, RotateSplit &s) {
+// The widest N whose accesses are whole.
+inline int rotate_wide(const RotateArgs &a, int32_t in, int32_t out) {
   const int ib = dtype_bytes(in), ob = dtype_bytes(out), rest = a.dim - 2 * a.half;
   const uint64_t all = (uint64_t)(uintptr_t)a.x | (uint64_t)(uintptr_t)a.out | (uint64_t)(a.xt * ib) | (uint64_t)(a.xh * ib) |
                        (uint64_t)(a.ot * ob) | (uint64_t)(a.oh * ob);
-  const bool wide = all % 16 == 0 && a.half % kRotateWide == 0 && rest % (2 * kRotateWide) == 0;
-  const int n = wide ? kRotateWide : 1;
+  for (int n : {8, 4})
+    if (all % 16 == 0 && a.half % n == 0 && rest % (2 * n) == 0) return n;
+  return 1;
+}
+inline RotateSplit rotate_split(const RotateArgs &a, int32_t in, int32_t out) {
+  RotateSplit s{};
+  const int n = rotate_wide(a, in, out), rest = a.dim - 2 * a.half;
+  s.wide = n;
   s.turns = (a.half + n - 1) / n;
   s.pieces = s.turns + (rest + 2 * n - 1) / (2 * n);
-  s.groups = a.heads;
-  return wide;
+  const int each = a.n * s.pieces * a.heads >= kRotateMany ? kRotateHeads : 1;
+  s.groups = (a.heads + each - 1) / each;
+  return s;
 }
+
+// Enqueues the rotation (rotary.cu).
+seedq_status rotate_launch(const RotateArgs &a, int32_t in, cudaStream_t st);
 
 // The work of thread i of the call.  N = 1 takes any sizes and strides; larger N
 // wants half and dim - 2 half in multiples of N and 2 N, and rows whose accesses of
@@ -123,7 +135,7 @@ __device__ __forceinline__ void rotate_item(const RotateArgs &a, const RotateSpl
     float2 cs[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) cs[k] = a.cs[t * a.half + p0 + k];
-#pragma unroll 4
+#pragma unroll kRotateHeads
     for (int h = g; h < a.heads; h += s.groups) {
       const int64_t at = t * a.xt + h * a.xh, to = t * a.ot + h * a.oh;
       if (a.layout == SEEDQ_ROPE_HALF) {
