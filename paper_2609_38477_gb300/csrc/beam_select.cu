@@ -7,17 +7,21 @@
 // the score and the log sum, so candidates that lie close together are not swapped by
 // a float32 sum.
 //
-// One pass over the logits keeps the sums and, per segment of 256 logits, the
-// largest.  The first n candidates lie in the n segments whose largest logits come
-// first in the same order: each of those n alone brings a candidate that precedes
-// all of the others.  So the last CTA to arrive for a request chooses n segments
-// from the maxima, reads them again, and chooses from their logits.
+// One pass over the logits keeps, per chunk of a row, the sum and the largest, and the
+// largest per segment of 256 logits.  The first n candidates lie in the n segments
+// whose largest logits come first in the same order: each of those n alone brings a
+// candidate that precedes all of the others.  So the last CTA to arrive for a request
+// chooses n segments from the maxima (of the chunks that can hold them), reads them
+// again, and chooses from their logits.  Each choice is by a float32 bound that at
+// least n reach, then by counting, for each of the few that do, how many precede it.
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <stdint.h>
 
 #include <cmath>
 
+#include "cp_async.cuh"
+#include "device_once.h"
 #include "f32x2.cuh"
 #include "order.cuh"
 #include "serve.cuh"
@@ -32,12 +36,15 @@ static_assert(kMaxBeams == 32, "a lane per beam and per candidate");
 constexpr int kTokenBits = 27;
 constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr uint64_t kHeader = SEEDQ_MAX_REQUESTS * 4;  // arrival counters
+constexpr uint64_t kHeader = 2 * SEEDQ_MAX_REQUESTS * 4;  // arrival counters of requests and of rows
+// Logits from which on warps stream: 512 rows of 128256 bfloat16 (131 MB) take 42 us
+// so and 45 by a CTA per chunk, 128 of float32 (66 MB) 27.5 and 24.
+constexpr int64_t kStreamBytes = 96 << 20, kStreamVocab = 16384;
 
 struct SelectArgs {
   const void *x;
   int64_t stride;
-  int32_t vocab, beams, groups, segments, chunks;  // segments, chunks: of a row
+  int32_t vocab, beams, groups, segments, chunks, chunk_segments;  // of a row, and of a chunk
   float scale, c;                                  // c = scale * log2(e)
   const float *scores, *weights;
   const uint8_t *done;
@@ -122,81 +129,347 @@ __device__ __forceinline__ int rest_beam(uint64_t rest) { return 31 - (int)(rest
 __device__ __forceinline__ float rest_logit(uint64_t rest) { return key_value((rest >> kTokenBits) << 32); }
 __device__ __forceinline__ int rest_index(uint64_t rest) { return (int)(kTokenMask - ((uint32_t)rest & kTokenMask)); }
 
-__device__ __forceinline__ Item shuffled(const Item &x, int from) { return {__shfl_sync(~0u, x.key, from), __shfl_sync(~0u, x.rest, from)}; }
-// The first 32 of two lists in order, as merge_lists.
-__device__ __noinline__ Item merge_items(Item a, Item b, int lane) {
-  b = shuffled(b, 31 - lane);
-  Item x = a.before(b) ? a : b;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const Item y = shuffled(x, lane ^ o);
-    if (y.before(x) == ((lane & o) == 0)) x = y;
-  }
-  return x;
-}
+constexpr int kMaxFound = 256;   // candidates of a choice: one of each thread
+constexpr int kMaxChunks = 1024; // of a request, that the first look takes
+constexpr int kAhead = 8;        // maxima that a thread has under way
+constexpr int kLanesOfRow = 8;
 
 struct Join {
   // total = base + scale * (logit - most): the difference first, or a large common part would take the sum's digits
   double base[kMaxBeams], weight[kMaxBeams], most[kMaxBeams];
+  float4 line[kMaxBeams];  // the same weighted, in float32: x * (logit - y) + z, and w = 2^-21 |z|; -inf of a beam that brings nothing
   int kind[kMaxBeams];
-  uint32_t reach[kMaxBeams];  // the row's n-th largest segment maximum, as a word: no smaller logit is chosen
-  Item list[kWarps][32];
-  Item chosen[32];
-  uint64_t keys[kWarps][kSegment];
-  int spoiled;
+  alignas(16) float group[64];
+  uint32_t words[kWarps];
+  float chunk_most[kMaxChunks];
+  uint32_t chunk[kMaxChunks];  // those that are looked at: beam << 16 and number
+  Item found[kMaxFound], chosen[32];
+  float found_x[kMaxFound];
+  uint32_t found_at[kMaxFound];  // beam << 27 and index
+  int n_chunks, n_found, n_chosen, spoiled, slow;  // slow: numbers too large for float32 bounds
 };
 
 __device__ __forceinline__ double total_of(const SelectArgs &a, const Join &s, int b, float x) {
   return s.kind[b] == kDone ? s.base[b] : s.base[b] + (double)a.scale * ((double)x - s.most[b]);
 }
-__device__ __forceinline__ Item item_of(const SelectArgs &a, const Join &s, int b, uint64_t key) {  // of an order_key
-  if (!key) return {0, 0};
-  return {order_double(s.weight[b] * total_of(a, s, b, key_value(key))), rest_word(b, (uint32_t)(key >> 32), key_index(key))};
+__device__ __forceinline__ Item item_of(const SelectArgs &a, const Join &s, int b, float x, int index) {
+  return {order_double(s.weight[b] * total_of(a, s, b, x)), rest_word(b, order_word(x), index)};
 }
-// The CTA's lists, one per warp, as one; in warp 0.
-__device__ __forceinline__ Item join_lists(Join &s, Item mine, int w, int lane) {
-  s.list[w][lane] = mine;
+// The weighted total in float32, and how far it may be off: a few roundings of its
+// parts, here 2^-21 of them.  What is far down is cut off, for all beams alike (their
+// offsets are at most 1e29).
+__device__ __forceinline__ float about(const Join &s, int b, float x, float &off) {
+  const float4 l = s.line[b];
+  const float d = fmaxf(l.x * (x - l.y), -1e37f);
+  off = fmaf(-0x1p-21f, fminf(d, 0.f), l.w);  // d is at most 0 but for roundings
+  return d + l.z;
+}
+// Which of 256 items in a row a thread takes: such that the first 64 fall into 64
+// different groups of four threads.
+__device__ __forceinline__ int item_slot() { return (threadIdx.x & 3) * 64 + (threadIdx.x >> 2); }
+// Of the threads' values (lower bounds of candidates' totals) the largest of every four:
+// the n-th largest of those 64, -inf if fewer have any.  At least n candidates reach it.
+__device__ __forceinline__ float nth_bound(Join &s, float mine, int n) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  mine = fmaxf(mine, __shfl_xor_sync(~0u, mine, 1));
+  mine = fmaxf(mine, __shfl_xor_sync(~0u, mine, 2));
+  if (tid % 4 == 0) s.group[tid / 4] = mine;
+  __syncthreads();
+  int above = 0;  // each of the four looks at 16
 #pragma unroll
-  for (int n = kWarps / 2; n; n >>= 1) {
-    __syncthreads();
-    if (w < n) {
-      mine = merge_items(mine, s.list[w + n][lane], lane);
-      s.list[w][lane] = mine;
-    }
+  for (int k = 0; k < 16; k += 4) {
+    const float4 v = *(const float4 *)(s.group + (tid & 3) * 16 + k);
+    above += (v.x > mine) + (v.y > mine) + (v.z > mine) + (v.w > mine);
   }
-  return mine;
+  above += __shfl_xor_sync(~0u, above, 1);
+  above += __shfl_xor_sync(~0u, above, 2);
+  const uint32_t word = __reduce_min_sync(~0u, above < n ? order_word(mine) : ~0u);
+  if (lane == 0) s.words[tid / 32] = word;
+  __syncthreads();
+  const uint32_t least = __reduce_min_sync(~0u, s.words[lane % kWarps]);
+  return key_value((uint64_t)least << 32);
+}
+// The first n of the found candidates, in order, to chosen.  False if more were
+// found than fit.
+__device__ __forceinline__ bool rank_found(const SelectArgs &a, Join &s, int n) {
+  __syncthreads();
+  const int m = s.n_found;
+  if (m > kMaxFound) return false;
+  Item mine{0, 0};
+  if (threadIdx.x < m) {
+    const uint32_t at = s.found_at[threadIdx.x];
+    mine = item_of(a, s, at >> kTokenBits, s.found_x[threadIdx.x], at & kTokenMask);
+    s.found[threadIdx.x] = mine;
+  }
+  __syncthreads();
+  if (threadIdx.x < m) {
+    int before = 0;
+#pragma unroll 8
+    for (int k = 0; k < m; ++k) before += s.found[k].before(mine);
+    if (before < n) s.chosen[before] = mine;
+  }
+  if (threadIdx.x == 0) s.n_chosen = min(m, n);
+  __syncthreads();
+  return true;
+}
+__device__ __forceinline__ void push(Join &s, int b, float x, int index) {
+  const int at = atomicAdd(&s.n_found, 1);
+  if (at < kMaxFound) s.found_x[at] = x, s.found_at[at] = (uint32_t)b << kTokenBits | (uint32_t)index;
+}
+
+// For rows in which more than fit are about equal, or numbers too large for the
+// bounds: the n first one after another.  each(f) calls f(beam, logit, index) for
+// all that the thread sees.
+template <typename Each>
+__device__ __forceinline__ void choose_slowly(const SelectArgs &a, Join &s, Each each) {
+  Item last = {~0ull, ~0ull};
+  __syncthreads();
+  if (threadIdx.x == 0) s.n_chosen = 0;
+#pragma unroll 1
+  for (int i = 0; i < a.n_out; ++i) {
+    Item best = {0, 0};
+    each([&](int b, float x, int index) {
+      const Item y = item_of(a, s, b, x, index);
+      if (last.before(y) && y.before(best)) best = y;
+    });
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      const Item y{__shfl_xor_sync(~0u, best.key, o), __shfl_xor_sync(~0u, best.rest, o)};
+      if (y.before(best)) best = y;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s.found[threadIdx.x >> 5] = best;
+    __syncthreads();
+    best = s.found[0];
+    for (int k = 1; k < kWarps; ++k)
+      if (s.found[k].before(best)) best = s.found[k];
+    if (!best.key) break;
+    if (threadIdx.x == 0) s.chosen[i] = best, s.n_chosen = i + 1;
+    last = best;
+  }
+  __syncthreads();
 }
 
 template <int DT, bool VEC>
-__device__ __forceinline__ void join_group(const SelectArgs &a, Join &s, int64_t g) {
+__device__ __noinline__ void join_slowly(const SelectArgs &a, Join &s, int64_t g) {
   using Seg = Segment<DT, VEC>;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  if (threadIdx.x == 0) s.spoiled = 0;
+  choose_slowly(a, s, [&](auto &&f) {
+    for (int b = 0; b < a.beams; ++b) {
+      if (s.kind[b] == kDone && threadIdx.x == 0) f(b, 0.f, a.end_token);
+      if (s.kind[b] != kLive) continue;
+      for (int i = threadIdx.x; i < a.segments; i += kThreads) {
+        const float x = __ldcg(a.most + (g * a.beams + b) * a.segments + i);
+        if (x > -CUDART_INF_F) f(b, x, i);
+      }
+    }
+  });
+  const Item mine = s.chosen[lane];
+  const int n_chosen = s.n_chosen;
+  choose_slowly(a, s, [&](auto &&f) {
+    for (int i = w; i < n_chosen; i += kWarps) {
+      const uint64_t rest = __shfl_sync(~0u, mine.rest, i);
+      const int b = rest_beam(rest), first = rest_index(rest) * kSegment;
+      if (s.kind[b] == kDone) {
+        if (lane == 0) f(b, 0.f, a.end_token);
+        continue;
+      }
+      Seg seg;
+      seg.load((const char *)a.x + (g * a.beams + b) * a.stride * Seg::kSize, first, a.vocab, lane);
+      float x[8];
+      seg.get(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (x[e] > -CUDART_INF_F) f(b, x[e], first + Seg::place(e, lane));
+    }
+  });
+}
+
+__device__ __forceinline__ bool by_chunks(const SelectArgs &a) {
+  return a.beams * a.chunks <= kMaxChunks && a.beams * a.segments > kThreads * kAhead;
+}
+// The first segments' maxima, of all rows.
+__device__ __forceinline__ void load_first(const SelectArgs &a, int64_t g, float (&ahead)[kAhead]) {
+  const int total = a.beams * a.segments, slot = item_slot();
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) ahead[k] = k * kThreads + slot < total ? __ldcg(a.most + g * total + k * kThreads + slot) : -CUDART_INF_F;
+}
+
+template <int DT, bool VEC>
+__device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t g, float (&ahead)[kAhead]) {
+  using Seg = Segment<DT, VEC>;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, slot = item_slot();
+  const int chunks = a.beams * a.chunks, of_chunk = a.chunk_segments;
+  float bound = -CUDART_INF_F, off;
+  // chunks, by their largest logits: of those whose upper bound reaches the n-th lower one the segments are looked at
+  const bool few = by_chunks(a);
+  if (few) {
+    for (int k = slot; k < chunks; k += kThreads) {
+      const int b = (unsigned)k / (unsigned)a.chunks;
+      const float x = s.chunk_most[k];
+      if (s.kind[b] == kLive && x > -CUDART_INF_F) bound = fmaxf(bound, about(s, b, x, off) - off);
+    }
+    bound = nth_bound(s, bound, a.n_out);
+    for (int k = tid; k < chunks; k += kThreads) {
+      const int b = (unsigned)k / (unsigned)a.chunks;
+      const float x = s.chunk_most[k];
+      if (s.kind[b] == kLive && x > -CUDART_INF_F && about(s, b, x, off) + off >= bound)
+        s.chunk[atomicAdd(&s.n_chunks, 1)] = (uint32_t)b << 16 | (uint32_t)(k - b * a.chunks);
+    }
+    __syncthreads();
+  }
+  // segments, by their largest logits; a finished beam is a segment of its one candidate
+  const int total = few ? s.n_chunks * of_chunk : a.beams * a.segments;
+  int beam[kAhead], number[kAhead];
+  const int step_b = kThreads / a.segments, step_i = kThreads - step_b * a.segments;
+  auto load = [&](int first) {
+    int b = 0, i = 0;  // of the item that k comes to
+    if (!few) b = (first + slot) / a.segments, i = first + slot - b * a.segments;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int at = first + k * kThreads + slot;
+      beam[k] = number[k] = 0;
+      if (few) {
+        const uint32_t c = at < total ? s.chunk[at / of_chunk] : 0;
+        beam[k] = c >> 16, number[k] = (c & 0xffffu) * of_chunk + at % of_chunk;
+        ahead[k] = at < total && number[k] < a.segments ? __ldcg(a.most + (g * a.beams + beam[k]) * a.segments + number[k]) : -CUDART_INF_F;
+      } else if (at < total) {
+        beam[k] = b, number[k] = i;
+        if (first) ahead[k] = __ldcg(a.most + g * a.beams * a.segments + at);
+      } else {
+        ahead[k] = -CUDART_INF_F;
+      }
+      b += step_b, i += step_i;
+      if (i >= a.segments) i -= a.segments, ++b;
+    }
+  };
+  const bool ends = tid < a.beams && s.kind[tid] == kDone;
+  bound = ends ? about(s, tid, 0.f, off) - off : -CUDART_INF_F;
+  for (int first = 0; first < total; first += kThreads * kAhead) {
+    load(first);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (ahead[k] > -CUDART_INF_F && s.kind[beam[k]] == kLive) bound = fmaxf(bound, about(s, beam[k], ahead[k], off) - off);
+  }
+  bound = nth_bound(s, bound, a.n_out);
+  if (ends && about(s, tid, 0.f, off) + off >= bound) push(s, tid, 0.f, a.end_token);
+  for (int first = 0; first < total; first += kThreads * kAhead) {
+    if (total > kThreads * kAhead) {
+      if (!few && first == 0) load_first(a, g, ahead);
+      load(first);
+    }
+    uint32_t in = 0;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (ahead[k] > -CUDART_INF_F && about(s, beam[k], ahead[k], off) + off >= bound) in |= 1u << k;
+    while (in) {
+      const int k = __ffs(in) - 1;
+      in &= in - 1;
+      float x = ahead[0];
+      int b = beam[0], i = number[0];
+#pragma unroll
+      for (int z = 1; z < kAhead; ++z)
+        if (k == z) x = ahead[z], b = beam[z], i = number[z];
+      if (s.kind[b] == kLive) push(s, b, x, i);  // a finished beam's row holds anything
+    }
+  }
+  if (!rank_found(a, s, a.n_out)) return join_slowly<DT, VEC>(a, s, g);
+
+  // their logits
+  const int n_chosen = s.n_chosen;
+  bound = -CUDART_INF_F;
+  if (n_chosen == a.n_out) {  // no candidate comes behind the last segment's best
+    const Item last = s.chosen[n_chosen - 1];
+    const int b = rest_beam(last.rest);
+    bound = about(s, b, rest_logit(last.rest), off) - off;
+  }
+  constexpr int kEach = kMaxTop / kWarps;
+  Seg seg[kEach];
+  int of[kEach], at[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int i = w + k * kWarps;
+    of[k] = -1;
+    if (i < n_chosen) {
+      const uint64_t rest = s.chosen[i].rest;
+      of[k] = rest_beam(rest), at[k] = rest_index(rest) * kSegment;
+      if (s.kind[of[k]] == kLive) seg[k].load((const char *)a.x + (g * a.beams + of[k]) * a.stride * Seg::kSize, at[k], a.vocab, lane);
+    }
+  }
   __syncthreads();
-  // the sums of the beams
-  Item best = {0, 0};
-  for (int b = w; b < a.beams; b += kWarps) {
-    const int64_t row = g * a.beams + b;
-    const float score = a.scores[row];
-    const float weight = a.weights ? a.weights[row] : 1.f;
-    int kind = row_kind(a, row);
-    double base = (double)score, most_logit = 0.0;
+  if (tid == 0) s.n_found = 0;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    if (of[k] < 0) continue;
+    const int b = of[k];
+    if (s.kind[b] == kDone) {
+      if (lane == 0) push(s, b, 0.f, a.end_token);
+      continue;
+    }
+    float x[8];
+    seg[k].get(x);
+    uint32_t in = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (x[e] > -CUDART_INF_F && about(s, b, x[e], off) + off >= bound) in |= 1u << e;
+    while (in) {
+      const int e = __ffs(in) - 1;
+      in &= in - 1;
+      float y = x[0];
+#pragma unroll
+      for (int z = 1; z < 8; ++z) y = e == z ? x[z] : y;
+      push(s, b, y, at[k] + Seg::place(e, lane));
+    }
+  }
+  if (!rank_found(a, s, a.n_out)) return join_slowly<DT, VEC>(a, s, g);
+}
+
+template <int DT, bool VEC>
+__device__ __noinline__ void join_group(const SelectArgs &a, Join &s, int64_t g) {
+  const int tid = threadIdx.x;
+  if (tid == 0) s.spoiled = s.slow = s.n_found = s.n_chosen = s.n_chunks = 0;
+  __syncthreads();
+  // the sums of the beams, 8 lanes each: all at once
+  static_assert(kThreads / kLanesOfRow == kMaxBeams, "");
+  const int b = tid / kLanesOfRow, part = tid % kLanesOfRow;
+  const bool there = b < a.beams;
+  const int64_t row = g * a.beams + (there ? b : 0);
+  const float score = a.scores[row];
+  const float weight = a.weights ? a.weights[row] : 1.f;
+  int kind = there ? row_kind(a, row) : kNone;
+  const bool keep = a.beams * a.chunks <= kMaxChunks;
+  float ahead[kAhead];
+  if (!by_chunks(a)) load_first(a, g, ahead);  // on their way while the sums are made
+  constexpr int kEarly = 4;  // parts under way before the beam's kind is known
+  float2 early[kEarly];
+#pragma unroll
+  for (int k = 0; k < kEarly; ++k)
+    if (part + k * kLanesOfRow < a.chunks) early[k] = __ldcg(a.parts + row * a.chunks + part + k * kLanesOfRow);
+  float m = -CUDART_INF_F, sum = 0.f;
+  if (kind == kLive) {
+#pragma unroll 4
+    for (int k = 0, i = part; i < a.chunks; i += kLanesOfRow, ++k) {
+      float2 p = early[0];
+      early[0] = early[1], early[1] = early[2], early[2] = early[3];
+      if (k >= kEarly) p = __ldcg(a.parts + row * a.chunks + i);
+      if (keep) s.chunk_most[b * a.chunks + i] = p.x;
+      const float to = max_nan(m, p.x);
+      if (to != -CUDART_INF_F) sum = sum * exp2_fast((m - to) * a.c) + p.y * exp2_fast((p.x - to) * a.c);
+      m = to;
+    }
+  }
+  float to = m;
+#pragma unroll
+  for (int o = kLanesOfRow / 2; o; o >>= 1) to = max_nan(to, __shfl_xor_sync(~0u, to, o));
+  if (to != -CUDART_INF_F) sum *= exp2_fast((m - to) * a.c);
+#pragma unroll
+  for (int o = kLanesOfRow / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+  if (there && part == 0) {
+    double base = (double)score;
+    float high = 0.f;
     bool bad = isnan(score) || (kind != kNone && !(score < CUDART_INF_F && weight > 0.f && weight < CUDART_INF_F));
     if (kind == kLive) {
-      float m = -CUDART_INF_F, sum = 0.f;
-      for (int i = lane; i < a.chunks; i += 32) {
-        const float2 *p = a.parts + row * a.chunks + i;
-        const float pm = fresh_load(&p->x), ps = fresh_load(&p->y);
-        const float to = max_nan(m, pm);
-        if (to != -CUDART_INF_F) sum = sum * exp2_fast((m - to) * a.c) + ps * exp2_fast((pm - to) * a.c);
-        m = to;
-      }
-      float to = m;
-#pragma unroll
-      for (int o = 16; o; o >>= 1) to = max_nan(to, __shfl_xor_sync(~0u, to, o));
-      if (to != -CUDART_INF_F) sum *= exp2_fast((m - to) * a.c);
-#pragma unroll
-      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
       if (to == -CUDART_INF_F) {
         kind = kNone;  // no token is allowed
       } else if (!(sum < CUDART_INF_F)) {
@@ -206,85 +479,37 @@ __device__ __forceinline__ void join_group(const SelectArgs &a, Join &s, int64_t
         const int e = (int)(__float_as_uint(sum * 1.41421356f) >> 23) - 127;
         const float f = sum * __uint_as_float((uint32_t)(127 - e) << 23);
         base -= (double)e * 0.69314718055994531 + (double)logf(f);
-        most_logit = (double)to;
+        high = to;
       }
     }
-    if (lane == 0) {
-      s.base[b] = base, s.weight[b] = (double)weight, s.most[b] = most_logit, s.kind[b] = kind;
-      if (bad) s.spoiled = 1;
-    }
-    __syncwarp();
-    // the beam's first segments
-    uint64_t key = 0;
-    if (kind == kLive && !bad) {
-      const float *most = a.most + row * a.segments;
-      uint64_t last = 0;
-      for (int s0 = 0; s0 < a.segments; s0 += 32) {
-        const int i = s0 + lane;
-        const float x = i < a.segments ? fresh_load(most + i) : -CUDART_INF_F;
-        const uint64_t k = x > -CUDART_INF_F ? order_key(x, i) : 0;
-        if (!__any_sync(~0u, k > last)) continue;
-        key = merge_lists(key, sort_keys(k, lane), lane);
-        last = __shfl_sync(~0u, key, a.n_out - 1);
-      }
-      if (lane == 0) s.reach[b] = (uint32_t)(last >> 32);
-    } else if (kind == kDone && !bad && lane == 0) {
-      key = order_key(0.f, a.end_token);
-    }
-    best = merge_items(best, item_of(a, s, b, key), lane);
+    const double offset = (double)weight * base;
+    s.base[b] = base, s.weight[b] = (double)weight, s.most[b] = (double)high, s.kind[b] = kind;
+    s.line[b] = kind == kNone ? make_float4(0.f, 0.f, -CUDART_INF_F, 0.f)
+                              : make_float4(kind == kLive ? weight * a.scale : 0.f, high, (float)offset, 0x1p-21f * fabsf((float)offset));
+    if (kind != kNone && !(fabs(offset) <= 1e29)) s.slow = 1;
+    if (bad) s.spoiled = 1;
   }
-  best = join_lists(s, best, w, lane);
-  if (w == 0) s.chosen[lane] = lane < a.n_out ? best : Item{0, 0};
   __syncthreads();
-
-  // the chosen segments' logits
-  best = {0, 0};
-  if (!s.spoiled) {
-    for (int i = w; i < a.n_out; i += kWarps) {
-      const Item at = s.chosen[i];
-      if (!at.key) break;  // the same in all lanes
-      const int b = rest_beam(at.rest);
-      if (s.kind[b] == kDone) {
-        best = merge_items(best, lane == 0 ? at : Item{0, 0}, lane);
-        continue;
-      }
-      const int64_t row = g * a.beams + b;
-      const char *base = (const char *)a.x + row * a.stride * Seg::kSize;
-      const int first = rest_index(at.rest) * kSegment;
-      Seg seg;
-      seg.load(base, first, a.vocab, lane);
-      float x[8];
-      seg.get(x);
-      const uint32_t reach = s.reach[b];
-      int n = 0;
-      __syncwarp();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint64_t k = order_key(x[e], first + Seg::place(e, lane));
-        const bool in = x[e] > -CUDART_INF_F && (uint32_t)(k >> 32) >= reach;
-        const uint32_t all = __ballot_sync(~0u, in);
-        if (in) s.keys[w][n + __popc(all & ((1u << lane) - 1))] = k;
-        n += __popc(all);
-      }
-      __syncwarp();
-      uint64_t key = 0;
-      for (int o = 0; o < n; o += 32) key = merge_lists(key, sort_keys(o + lane < n ? s.keys[w][o + lane] : 0, lane), lane);
-      best = merge_items(best, item_of(a, s, b, key), lane);
-    }
+  const bool spoiled = s.spoiled;  // the same in all threads
+  if (!spoiled) {
+    if (s.slow) join_slowly<DT, VEC>(a, s, g);
+    else join_fast<DT, VEC>(a, s, g, ahead);
   }
-  best = join_lists(s, best, w, lane);
-  if (w == 0 && lane < a.n_out) {
-    const int64_t o = g * a.n_out + lane;
-    const bool there = best.key && !s.spoiled;
-    const int b = rest_beam(best.rest);
-    a.out_score[o] = s.spoiled ? CUDART_NAN_F : there ? (float)total_of(a, s, b, rest_logit(best.rest)) : -CUDART_INF_F;
-    a.out_beam[o] = there ? b : -1;
-    a.out_token[o] = there ? rest_index(best.rest) : -1;
+  if (tid < a.n_out) {
+    const int64_t o = g * a.n_out + tid;
+    const bool has = !spoiled && tid < s.n_chosen;
+    const Item x = has ? s.chosen[tid] : Item{0, 0};
+    const int from = rest_beam(x.rest);
+    a.out_score[o] = spoiled ? CUDART_NAN_F : has ? (float)total_of(a, s, from, rest_logit(x.rest)) : -CUDART_INF_F;
+    a.out_beam[o] = has ? from : -1;
+    a.out_token[o] = has ? rest_index(x.rest) : -1;
   }
+  __syncthreads();
 }
 
+// Few logits: a CTA per chunk of a row, all of it read at once.
 template <int DT, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_beam_select(const __grid_constant__ SelectArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) k_beam_select(const __grid_constant__ SelectArgs a) {
   using Seg = Segment<DT, VEC>;
   constexpr int kEach = Seg::kSize == 4 ? 4 : 8;  // segments of a warp
   __shared__ Join s_join;
@@ -299,7 +524,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_select(const __grid_constant_
     Seg seg[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) seg[j].load(base, (s0 + j * kWarps) * kSegment, a.vocab, lane);
-    uint32_t word = 0;
+    float m = -CUDART_INF_F;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
       float x[8];
@@ -307,11 +532,10 @@ __global__ void __launch_bounds__(kThreads) k_beam_select(const __grid_constant_
       float mx = max_nan(x[0], x[1]);
 #pragma unroll
       for (int e = 2; e < 8; e += 2) mx = max_nan(mx, x[e], x[e + 1]);
-      const uint32_t most = __reduce_max_sync(~0u, order_word(mx));
-      word = max(word, most);
-      if (lane == 0 && s0 + j * kWarps < a.segments) a.most[row * a.segments + s0 + j * kWarps] = key_value((uint64_t)most << 32);
+      mx = warp_max_nan(mx);
+      m = max_nan(m, mx);
+      if (lane == 0 && s0 + j * kWarps < a.segments) a.most[row * a.segments + s0 + j * kWarps] = mx;
     }
-    const float m = key_value((uint64_t)word << 32);
     const float off = m == -CUDART_INF_F ? 0.f : -m;
     const uint64_t off2 = f2_pack(off, off), c2 = f2_pack(a.c, a.c);
     uint64_t sums = 0;
@@ -353,13 +577,211 @@ __global__ void __launch_bounds__(kThreads) k_beam_select(const __grid_constant_
   if (s_last) join_group<DT, VEC>(a, s_join, g);
 }
 
-int chunk_segments(int32_t dtype) { return dtype == SEEDQ_F32 ? 4 * kWarps : 8 * kWarps; }
+// Many logits: warps stream through equal ranges of the live rows' chunks, a ring of
+// copies ahead; a row's chunks are the same for all rows, so that equal rows have
+// equal sums.  A row counts its chunks, a request its rows; the CTA of the warp that
+// brings the last joins the request once its own range is done.
+constexpr int kStages = 3;          // tiles in a warp's ring
+constexpr int kTileBytes = 2048;    // 64 bytes of each lane
+constexpr int kChunkTiles = 4;
+constexpr int kMaxJoins = 128;
+constexpr int kStreamCtas = 2;      // per SM
+template <int DT>
+__global__ void __launch_bounds__(kThreads, kStreamCtas) k_beam_stream(const __grid_constant__ SelectArgs a) {
+  using Seg = Segment<DT, true>;
+  constexpr int kSize = Seg::kSize, kVec = Seg::kVec, kTile = kTileBytes / kSize, kSegs = kTile / kSegment;
+  extern __shared__ __align__(128) uint8_t s_ring[];
+  uint16_t *live = (uint16_t *)(s_ring + kWarps * kStages * kTileBytes);  // the live rows
+  __shared__ Join s_join;
+  __shared__ int s_count[kWarps], s_joins[kMaxJoins], s_n_joins;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  if (tid == 0) s_n_joins = 0;
+  int n_live = 0;
+  const int rows = a.groups * a.beams;
+  constexpr int kRounds = 2;  // whose rows are looked at together
+  bool ahead[kRounds];
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) ahead[k] = k * kThreads + tid < rows && row_kind(a, k * kThreads + tid) == kLive;
+  for (int r0 = 0, k = 0; r0 < rows; r0 += kThreads, ++k) {
+    const bool is = k < kRounds ? ahead[0] : r0 + tid < rows && row_kind(a, r0 + tid) == kLive;
+    ahead[0] = ahead[1];
+    const uint32_t mask = __ballot_sync(~0u, is);
+    if (lane == 0) s_count[w] = __popc(mask);
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int k = 0; k < kWarps; ++k) {
+      before += k < w ? s_count[k] : 0;
+      all += s_count[k];
+    }
+    if (is) live[n_live + before + __popc(mask & ((1u << lane) - 1))] = (uint16_t)(r0 + tid);
+    n_live += all;
+    __syncthreads();
+  }
+  auto live_of_group = [&](int g) { return __popc(__ballot_sync(~0u, lane < a.beams && row_kind(a, (int64_t)g * a.beams + lane) == kLive)); };
+  // requests without a live beam are nobody's last
+  for (int g = blockIdx.x; g < a.groups; g += gridDim.x)
+    if (w == 0 && live_of_group(g) == 0 && lane == 0) s_joins[s_n_joins++] = g;
+  __syncthreads();
+
+  const int64_t tasks = (int64_t)n_live * a.chunks, warps = (int64_t)gridDim.x * kWarps, me = (int64_t)blockIdx.x * kWarps + w;
+  const int64_t t0 = tasks * me / warps, t1 = tasks * (me + 1) / warps;
+  const int tiles = (a.vocab + kTile - 1) / kTile;  // of a row
+  uint8_t *ring = s_ring + w * (kStages * kTileBytes) + lane * 16;
+  // where the copies are: live row, tile
+  int li = (int)(t0 / a.chunks), pi = li, ptile = (int)(t0 - (int64_t)li * a.chunks) * kChunkTiles, chunk = ptile / kChunkTiles, pstage = 0, stage = 0;
+  // tiles left to copy
+  int64_t pleft = 0;
+  if (t0 < t1) {
+    const int le = (int)((t1 - 1) / a.chunks), ce = (int)(t1 - 1 - (int64_t)le * a.chunks);
+    pleft = (int64_t)(le - li) * tiles + min((ce + 1) * kChunkTiles, tiles) - ptile;
+  }
+  const char *psrc = t0 < t1 ? (const char *)a.x + (int64_t)live[pi] * a.stride * kSize : nullptr;
+  auto issue = [&]() {
+    if (pleft > 0) {
+      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring + pstage * kTileBytes);
+      if ((ptile + 1) * kTile <= a.vocab) {
+        const char *from = psrc + ptile * kTileBytes + lane * 16;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + v * 512), "l"(from + v * 512) : "memory");
+      } else
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int i = ptile * kTile + v * (32 * kVec) + lane * kVec;
+        const int bytes = min(max(a.vocab - i, 0) * kSize, 16);  // what lies past the row's end is not read
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + v * 512),
+                     "l"(bytes ? psrc + (int64_t)i * kSize : (const char *)a.x), "r"(bytes)
+                     : "memory");
+      }
+      --pleft;
+      pstage = pstage + 1 == kStages ? 0 : pstage + 1;
+      if (++ptile == tiles && pleft > 0) {
+        ptile = 0;
+        psrc = (const char *)a.x + (int64_t)live[++pi] * a.stride * kSize;
+      }
+    }
+    cp_async_commit();
+  };
+  for (int k = 0; k < kStages - 1; ++k) issue();
+  int pending = 0;  // chunks of the row that nobody knows of yet
+  auto arrive = [&](int64_t row) {
+    __syncwarp();
+    const int g = (int)(row / a.beams), n = live_of_group(g);
+    if (lane == 0) {
+      __threadfence();
+      if (atomicAdd(a.counters + SEEDQ_MAX_REQUESTS + row, pending) + pending == a.chunks) {
+        a.counters[SEEDQ_MAX_REQUESTS + row] = 0;
+        __threadfence();
+        if (atomicAdd(a.counters + g, 1) + 1 == n) {
+          a.counters[g] = 0;
+          s_joins[atomicAdd(&s_n_joins, 1)] = g;
+        }
+      }
+    }
+    pending = 0;
+  };
+  const uint64_t c2 = f2_pack(a.c, a.c);
+  for (int64_t t = t0; t < t1; ++t) {
+    const int64_t row = live[li];
+    float m = -CUDART_INF_F;
+    float sum = 0.f;
+    const int last = min((chunk + 1) * kChunkTiles, tiles);
+    for (int tile = chunk * kChunkTiles; tile < last; ++tile) {
+      issue();
+      cp_async_wait<kStages - 1>();
+      const uint8_t *src = ring + stage * kTileBytes;
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+      Seg seg[kSegs];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const uint4 y = *(const uint4 *)(src + v * 512);
+        uint32_t *to = seg[v / Seg::kPieces].w + (v % Seg::kPieces) * 4;
+        to[0] = y.x, to[1] = y.y, to[2] = y.z, to[3] = y.w;
+      }
+      float x[kSegs][8];
+#pragma unroll
+      for (int k = 0; k < kSegs; ++k) seg[k].get(x[k]);
+      if ((tile + 1) * kTile > a.vocab) {
+#pragma unroll
+        for (int k = 0; k < kSegs; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (tile * kTile + k * kSegment + Seg::place(e, lane) >= a.vocab) x[k][e] = -CUDART_INF_F;
+      }
+      float to = m, mine = 0.f;
+#pragma unroll
+      for (int k = 0; k < kSegs; ++k) {
+        float mx = max_nan(x[k][0], x[k][1]);
+#pragma unroll
+        for (int e = 2; e < 8; e += 2) mx = max_nan(mx, x[k][e], x[k][e + 1]);
+        mx = warp_max_nan(mx);
+        to = max_nan(to, mx);
+        if (lane == k) mine = mx;
+      }
+      if (lane < kSegs && tile * kSegs + lane < a.segments) a.most[row * a.segments + tile * kSegs + lane] = mine;
+      if (to != -CUDART_INF_F) sum *= exp2_fast((m - to) * a.c);
+      m = to;
+      const float off = to == -CUDART_INF_F ? 0.f : -to;
+      const uint64_t off2 = f2_pack(off, off);
+      uint64_t sums = 0;
+#pragma unroll
+      for (int k = 0; k < kSegs; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const float2 d = f2_unpack(f2_mul(f2_add(f2_pack(x[k][e], x[k][e + 1]), off2), c2));
+          sums = f2_add(sums, f2_pack(exp2_fast(d.x), exp2_fast(d.y)));
+        }
+      sum += f2_unpack(sums).x + f2_unpack(sums).y;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (lane == 0) a.parts[row * a.chunks + chunk] = make_float2(m, sum);
+    ++pending;
+    if (++chunk == a.chunks) {
+      arrive(row);
+      chunk = 0;
+      ++li;
+    }
+  }
+  if (pending) arrive(live[li]);
+  cp_async_wait<0>();
+  __syncthreads();
+  const int joins = s_n_joins;
+  __threadfence();
+  for (int k = 0; k < joins; ++k) join_group<DT, true>(a, s_join, s_joins[k]);
+}
+
+int few_chunk_logits(int32_t dtype) { return (dtype == SEEDQ_F32 ? 4 : 8) * kWarps * kSegment; }
+int stream_chunk_logits(int32_t dtype) { return kChunkTiles * kTileBytes / dtype_bytes(dtype); }
 int64_t segments_of(int64_t vocab) { return (vocab + kSegment - 1) / kSegment; }
 
+DeviceOnce g_stream[3];
+
 template <int DT>
-void launch(const SelectArgs &a, bool vec, unsigned ctas, cudaStream_t st) {
-  if (vec) k_beam_select<DT, true><<<ctas, kThreads, 0, st>>>(a);
-  else k_beam_select<DT, false><<<ctas, kThreads, 0, st>>>(a);
+cudaError_t launch(SelectArgs &a, bool vec, cudaStream_t st) {
+  const int64_t rows = (int64_t)a.groups * a.beams;
+  if (vec && rows * a.vocab * dtype_bytes(DT) >= kStreamBytes && a.vocab >= kStreamVocab) {
+    constexpr size_t kSmem = kWarps * kStages * kTileBytes + SEEDQ_MAX_REQUESTS * sizeof(uint16_t);
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    const int rc = g_stream[DT].run(dev, [] {
+      return (int)cudaFuncSetAttribute(k_beam_stream<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    });
+    if (rc) return (cudaError_t)rc;
+    a.chunks = (a.vocab + stream_chunk_logits(DT) - 1) / stream_chunk_logits(DT);
+    a.chunk_segments = stream_chunk_logits(DT) / kSegment;
+    a.most = (float *)(a.parts + rows * a.chunks);
+    k_beam_stream<DT><<<sms * kStreamCtas, kThreads, kSmem, st>>>(a);
+  } else {
+    a.chunks = (a.vocab + few_chunk_logits(DT) - 1) / few_chunk_logits(DT);
+    a.chunk_segments = few_chunk_logits(DT) / kSegment;
+    a.most = (float *)(a.parts + rows * a.chunks);
+    const unsigned ctas = (unsigned)(rows * a.chunks);  // at most 2^13 * 2^14
+    if (vec) k_beam_select<DT, true><<<ctas, kThreads, 0, st>>>(a);
+    else k_beam_select<DT, false><<<ctas, kThreads, 0, st>>>(a);
+  }
+  return cudaGetLastError();
 }
 
 bool sizes_ok(int64_t groups, int32_t beams, int64_t vocab) {
@@ -377,7 +799,7 @@ extern "C" {
 uint64_t seedq_beam_select_workspace_bytes(int64_t n_groups, int32_t n_beams, int64_t vocab) {
   if (!sizes_ok(n_groups, n_beams, vocab)) return 0;
   const uint64_t rows = (uint64_t)n_groups * n_beams, segments = (uint64_t)segments_of(vocab);
-  const uint64_t chunks = (segments + chunk_segments(SEEDQ_F32) - 1) / chunk_segments(SEEDQ_F32);
+  const uint64_t chunks = ((uint64_t)vocab + stream_chunk_logits(SEEDQ_F32) - 1) / stream_chunk_logits(SEEDQ_F32);  // the smallest
   return kHeader + rows * (chunks * sizeof(float2) + segments * sizeof(float));
 }
 
@@ -397,20 +819,14 @@ seedq_status seedq_beam_select(const seedq_beam_select_args *args, void *cuda_st
   a.scale = p.scale, a.c = p.scale * kLog2e, a.scores = p.scores, a.weights = p.weights, a.done = p.done, a.end_token = p.end_token;
   a.n_out = p.n_out, a.out_score = p.out_score, a.out_beam = p.out_beam, a.out_token = p.out_token;
   a.segments = (int32_t)segments_of(p.vocab);
-  a.chunks = (a.segments + chunk_segments(p.dtype) - 1) / chunk_segments(p.dtype);
   const int64_t rows = p.n_groups * p.n_beams;
   a.counters = (int *)p.workspace;
   a.parts = (float2 *)((char *)p.workspace + kHeader);
-  a.most = (float *)(a.parts + rows * a.chunks);
-  const unsigned ctas = (unsigned)(rows * a.chunks);  // at most 2^13 * 2^14
   const bool vec = (uintptr_t)p.logits % 16 == 0 && (rows == 1 || p.row_stride * dtype_bytes(p.dtype) % 16 == 0);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  switch (p.dtype) {
-    case SEEDQ_F32: launch<SEEDQ_F32>(a, vec, ctas, st); break;
-    case SEEDQ_BF16: launch<SEEDQ_BF16>(a, vec, ctas, st); break;
-    default: launch<SEEDQ_F16>(a, vec, ctas, st);
-  }
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = p.dtype == SEEDQ_F32    ? launch<SEEDQ_F32>(a, vec, st)
+                        : p.dtype == SEEDQ_BF16 ? launch<SEEDQ_BF16>(a, vec, st)
+                                                : launch<SEEDQ_F16>(a, vec, st);
   return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
 }
 

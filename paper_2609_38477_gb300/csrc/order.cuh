@@ -36,6 +36,12 @@ __device__ __forceinline__ float min_nan(float a, float b, float c) {
   asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
+// The largest of a warp's, in all lanes; NaN if any is.
+__device__ __forceinline__ float warp_max_nan(float x) {
+  float y;
+  asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

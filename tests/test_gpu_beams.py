@@ -74,7 +74,7 @@ def some(check):
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("g,b,v,n", [(1, 1, 1, 1), (1, 1, 1, 32), (1, 3, 2, 5), (2, 4, 77, 8), (1, 1, 300, 32), (3, 32, 40, 32),
                                      (1, 4, 8192, 4), (2, 2, 8193, 20), (1, 5, 32000, 32), (7, 8, 4097, 16), (2, 3, 128256, 6),
-                                     (1, 2, 100003, 32), (65, 1, 513, 2)])
+                                     (1, 2, 100003, 32), (65, 1, 513, 2), (60, 5, 32000, 12), (400, 1, 33000, 3), (9, 32, 50004, 32)])
 def test_select(V, dtype, g, b, v, n):
     def check(seed):
         rng = np.random.RandomState(g * 7 + b + v + n + 1000 * seed)
@@ -140,6 +140,44 @@ def test_select_equal_logits(V):
     got = select(V, x, torch.zeros((1, 8), device="cuda"), 32)
     order = torch.sort(row, descending=True, stable=True).indices.tolist()
     assert got[1][0].tolist() == list(range(8)) * 4 and got[2][0].tolist() == [t for t in order[:4] for _ in range(8)]
+
+
+def test_select_equal_rows_of_many(V):
+    """Equal rows in a large batch, dealt to the SMs at other places each: sums equal to the bit, ties by the beam."""
+    for v, dtype in ((40000, "f32"), (128256, "bf16")):
+        row = (3 * torch.randn(v, generator=torch.Generator("cuda").manual_seed(v), device="cuda")).to(DT[dtype])
+        x = row.expand(200, v).contiguous()
+        scores = torch.zeros((40, 5), device="cuda")
+        scores[7], scores[8, :4], scores[9, 0] = -float("inf"), -float("inf"), -float("inf")
+        got = select(V, x, scores, 10)
+        order = torch.sort(row.float(), descending=True, stable=True)
+        ties = [order.indices[order.values == y].tolist() for y in torch.unique(order.values).flip(0)[:10]]
+        for g in range(40):
+            beams = [] if g == 7 else [4] if g == 8 else [1, 2, 3, 4] if g == 9 else list(range(5))
+            want = [(b, t) for same in ties for b in beams for t in same][:10]
+            assert list(zip(got[1][g].tolist(), got[2][g].tolist())) == (want or [(-1, -1)] * 10)
+            assert len(set(got[0][g].tolist())) <= 10 and bool((got[0][g] == got[0][0])[:2].all()) or g in (7, 8)
+
+
+def test_select_nothing_alive_in_a_large_batch(V):
+    x = torch.randn((300, 32768), device="cuda")
+    done = torch.zeros((100, 3), dtype=torch.bool, device="cuda")
+    done[::3] = True
+    scores = torch.randn((100, 3), device="cuda")
+    scores[::5] = -float("inf")
+    x[3:6], x[299] = -float("inf"), float("nan")
+    for _ in range(3):
+        got = select(V, x, scores, 2, done=done, end=9)
+        for g in range(100):
+            if g % 5 == 0 or g == 1:
+                assert got[1][g].tolist() == [-1, -1] and bool((got[0][g] == -float("inf")).all())
+            elif g == 99:
+                assert g % 3 == 0 and not bool(got[0][g].isnan().any())
+            elif g % 3 == 0:
+                assert sorted(got[0][g].tolist(), reverse=True) == got[0][g].tolist() == torch.sort(scores[g], descending=True).values[:2].tolist()
+                assert got[2][g].tolist() == [9, 9]
+            else:
+                assert not bool(got[0][g].isnan().any()) and min(got[1][g].tolist()) >= 0
 
 
 def test_select_all_candidates_in_one_segment(V):
