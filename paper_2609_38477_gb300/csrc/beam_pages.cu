@@ -10,13 +10,14 @@
 // place on the stack, and the second writes lists and stack; a row's old entries
 // are read by the warp that writes the new ones, so lists may be changed in place.
 //
-// The copies are the second launch: units of one head and tensor of one layer and
-// page, dealt to all warps.
+// The copies are units of one head and tensor of one layer and page, dealt to all
+// warps: of a second launch, or, where they are small, of the first.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_once.h"
 #include "serve.cuh"
@@ -29,11 +30,14 @@ namespace {
 constexpr int kWarps = 16, kThreads = kWarps * 32;
 constexpr int kMaxBeams = SEEDQ_MAX_BEAMS;
 constexpr int kMaxCluster = 8;
+constexpr int kAtOnce = 8;        // rows of a tile under way
 constexpr int kLayersAtOnce = 64;  // whose pointers go in a launch's parameters
+// What may have to be copied, up to which the first launch does it.
+constexpr int64_t kFewBytes = 1 << 20;
 
 // One copy: tokens [0, used) of page src to page dst.
-struct Copy {
-  int32_t src, dst, used;
+struct alignas(16) Copy {
+  int32_t src, dst, used, none;
 };
 struct Workspace {
   int32_t n, pad[3];
@@ -53,27 +57,67 @@ __device__ __forceinline__ int pages_of(int tokens, const PagesArgs &a) {  // to
   return (int)(a.page_shift >= 0 ? x >> a.page_shift : x / (uint32_t)a.page);
 }
 
-// Exclusive sum of v over the CTA, and the total.
-__device__ __forceinline__ int cta_sum(int v, int *warp_sums, int &total) {
+struct CopyArgs {
+  const Workspace *work;
+  int32_t layers, heads, pieces;  // pieces of 16 codes of a token
+  int64_t pages, page_stride, head_stride, token_stride;
+  uint8_t *codes[kLayersAtOnce][2];
+  float *scales[kLayersAtOnce][2];
+};
+constexpr int kCopyAhead = 8;  // loads of 16 bytes that a lane has under way
+
+// What warp `me` of `warps` copies of the first n entries of the list.
+__device__ __forceinline__ void copy_pages(const CopyArgs &a, int n, int64_t me, int64_t warps) {
+  const int lane = threadIdx.x & 31;
+  const int of_copy = a.layers * 2 * a.heads;
+  const int step = 32 / a.pieces, first = lane / a.pieces;  // tokens of a warp's step; the lane's
+  const int64_t lane_at = first * a.token_stride + (lane - first * a.pieces) * 16, step_at = step * a.token_stride;
+  const int64_t units = (int64_t)n * of_copy;
+  for (int64_t u = me; u < units; u += warps) {
+    const int c = (int)(u / of_copy), rest = (int)(u - (int64_t)c * of_copy), lt = rest / a.heads, h = rest - lt * a.heads;
+    const int4 entry = __ldcg((const int4 *)(a.work->copy + c));
+    const Copy y{entry.x, entry.y, entry.z, 0};
+    if (y.src < 0 || y.src >= a.pages || y.dst < 0 || y.dst >= a.pages) continue;
+    uint8_t *base = a.codes[lt >> 1][lt & 1] + h * a.head_stride + lane_at;
+    const uint8_t *src = base + y.src * a.page_stride;
+    uint8_t *dst = base + y.dst * a.page_stride;
+    float *s = a.scales[lt >> 1][lt & 1];
+    const float scale = lane == 0 ? s[(int64_t)y.src * a.heads + h] : 0.f;
+    const int used = first < step ? y.used : 0;  // lanes that are left over copy nothing
+    for (int t = first; t < used; t += kCopyAhead * step, src += kCopyAhead * step_at, dst += kCopyAhead * step_at) {
+      uint4 v[kCopyAhead];
+#pragma unroll
+      for (int k = 0; k < kCopyAhead; ++k)
+        if (t + k * step < used) v[k] = *(const uint4 *)(src + k * step_at);
+#pragma unroll
+      for (int k = 0; k < kCopyAhead; ++k)
+        if (t + k * step < used) *(uint4 *)(dst + k * step_at) = v[k];
+    }
+    if (lane == 0) s[(int64_t)y.dst * a.heads + h] = scale;
+  }
+}
+
+// Exclusive sums of v over the CTA, two at once, and the totals.
+__device__ __forceinline__ int2 cta_sum(int2 v, int2 *warp_sums, int2 &total) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  int x = v;
+  int2 x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(~0u, x, o);
-    if (lane >= o) x += y;
+    const int y = __shfl_up_sync(~0u, x.x, o), z = __shfl_up_sync(~0u, x.y, o);
+    if (lane >= o) x.x += y, x.y += z;
   }
   if (lane == 31) warp_sums[w] = x;
   __syncthreads();
-  int s = lane < kWarps ? warp_sums[lane] : 0;
+  int2 before = make_int2(0, 0);
+  total = make_int2(0, 0);
 #pragma unroll
-  for (int o = 1; o < kWarps; o <<= 1) {
-    const int y = __shfl_up_sync(~0u, s, o);
-    if (lane >= o) s += y;
+  for (int k = 0; k < kWarps; ++k) {
+    const int2 y = warp_sums[k];
+    if (k < w) before.x += y.x, before.y += y.y;
+    total.x += y.x, total.y += y.y;
   }
-  total = __shfl_sync(~0u, s, kWarps - 1);
-  const int before = __shfl_sync(~0u, s, max(w - 1, 0));
   __syncthreads();
-  return (w ? before : 0) + x - v;
+  return make_int2(before.x + x.x - v.x, before.y + x.y - v.y);
 }
 
 // What the kernel keeps of a row: the row of its group that it goes on from (-1:
@@ -83,56 +127,65 @@ struct Rows {
   int *from, *len, *held, *nth, *first_tile;  // first_tile: per group, and their number
 };
 
-__global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__ PagesArgs a) {
+// COPY: the copies as well.
+template <bool COPY>
+__global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__ PagesArgs a, const __grid_constant__ std::conditional_t<COPY, CopyArgs, char> y) {
   extern __shared__ int sm[];
   const int n = a.groups * a.beams, B = a.beams;
   const Rows r{sm, sm + n, sm + 2 * n, sm + 3 * n, sm + 4 * n};
   int *tiles = sm + 4 * n + a.groups + 1 + (threadIdx.x >> 5) * B * 32;  // the warp's tile
-  __shared__ int s_warp[kWarps], s_back[kWarps], s_cta_back;
+  __shared__ int2 s_warp[kWarps];
+  __shared__ int s_back[kWarps], s_cta_back;
   const cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  if (!COPY) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int count = min(max(*a.free_count, 0), a.capacity);
 
-  // rows: every CTA makes the same tables
-  int copies = 0;
+  // rows: every CTA makes the same tables.  First as they are given.
+  for (int i = threadIdx.x; i < n; i += kThreads) r.from[i] = a.parents[i], r.nth[i] = a.seq_lens[i];
+  __syncthreads();
+  auto pages_held = [&](int len) { return len < 0 || pages_of(len, a) > a.width ? -1 : pages_of(len, a); };  // -1: makes no sense
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int g0 = i / B * B, p = r.from[i], old = pages_held(r.nth[i]);
+    const int from = p >= 0 && p < B ? r.nth[g0 + p] : 0;
+    r.held[i] = max(old, 0);
+    r.len[i] = p < -1 || p >= B || pages_held(from) < 0 ? -1 : p < 0 ? 0 : from;
+  }
+  __syncthreads();
+  // The rows that want a copy: those with an earlier sibling and a partly filled page.
+  // Tiles: as many of a group as its longest list has.
+  int copies = 0, n_tiles = 0;
   for (int base = 0; base < n; base += kThreads) {
     const int i = base + threadIdx.x;
-    int wants = 0, len = 0, held = 0, p = -1;
+    int2 mine = make_int2(0, 0), total;
     if (i < n) {
-      const int g = i / B, b = i - g * B, old = a.seq_lens[i];
-      p = a.parents[i];
-      // a length that makes no sense: the row holds nothing that can be told
-      held = old < 0 || pages_of(old, a) > a.width ? 0 : pages_of(old, a);
-      if (p < -1 || p >= B) {
-        len = -1;
-      } else if (p >= 0) {
-        len = a.seq_lens[g * B + p];
-        if (len < 0 || pages_of(len, a) > a.width) len = -1;
-        if (len > 0 && len % a.page)
-          for (int q = 0; q < b && !wants; ++q) wants = a.parents[g * B + q] == p;
+      const int g0 = i / B * B, p = r.from[i], len = r.len[i];
+      if (len > 0 && len % a.page)
+#pragma unroll 4
+        for (int q = g0; q < i; ++q) mine.x |= r.from[q] == p;
+      if (i < a.groups) {
+        int most = 0;
+#pragma unroll 4
+        for (int b = 0; b < B; ++b) most = max(most, r.held[i * B + b]);
+        mine.y = (most + 31) / 32;
       }
     }
-    int total;
-    const int at = copies + cta_sum(wants, s_warp, total);
-    copies += total;
-    if (i < n) r.from[i] = len >= 0 ? p : -1, r.len[i] = len, r.held[i] = held, r.nth[i] = wants ? at : -1;
+    const int2 at = cta_sum(mine, s_warp, total);
+    if (i < n) {
+      r.nth[i] = mine.x ? copies + at.x : -1;
+      if (i < a.groups) r.first_tile[i] = n_tiles + at.y;
+    }
+    copies += total.x, n_tiles += total.y;
   }
-  __syncthreads();
-  // tiles: as many of a group as its longest list has
-  int n_tiles = 0;
-  for (int base = 0; base < a.groups; base += kThreads) {
-    const int g = base + threadIdx.x;
-    int most = 0;
-    if (g < a.groups)
-      for (int b = 0; b < B; ++b) most = max(most, r.held[g * B + b]);
-    int total;
-    const int at = n_tiles + cta_sum((most + 31) / 32, s_warp, total);
-    n_tiles += total;
-    if (g < a.groups) r.first_tile[g] = at;
-  }
+  for (int i = threadIdx.x; i < n; i += kThreads)
+    if (r.len[i] < 0) r.from[i] = -1;  // refused: goes on from none
   if (threadIdx.x == 0) r.first_tile[a.groups] = n_tiles;
   __syncthreads();
+
+  // The entry that the thread's row gets if no page comes back, on its way.
+  const int my_row = rank * kThreads + threadIdx.x, my_nth = my_row < n ? r.nth[my_row] : -1;
+  const int top = my_nth >= 0 && my_nth < count ? a.free_pages[count - 1 - my_nth] : -1;
 
   const int64_t workers = (int64_t)ranks * kWarps, me = (int64_t)rank * kWarps + w;
   const int t0 = (int)(n_tiles * me / workers), t1 = (int)(n_tiles * (me + 1) / workers);
@@ -149,12 +202,21 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
   // Reads a tile; bit b of the result: row b's page at the lane's column goes back here.
   auto read_tile = [&](int g, int col) -> uint32_t {
     uint32_t held = 0, live = 0;
-    for (int b = 0; b < B; ++b) {
-      const int i = g * B + b;
-      const int id = col < r.held[i] ? a.table[(int64_t)i * a.table_stride + col] : -1;
-      tiles[b * 32 + lane] = id;
-      if (id >= 0) held |= 1u << b;
-      if (r.from[i] >= 0) live |= 1u << r.from[i];
+    for (int b0 = 0; b0 < B; b0 += kAtOnce) {
+      int id[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int i = g * B + b0 + k;
+        id[k] = b0 + k < B && col < r.held[i] ? a.table[(int64_t)i * a.table_stride + col] : -1;
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+        if (b0 + k < B) {
+          tiles[(b0 + k) * 32 + lane] = id[k];
+          if (id[k] >= 0) held |= 1u << (b0 + k);
+          const int p = r.from[g * B + b0 + k];
+          if (p >= 0) live |= 1u << p;
+        }
     }
     uint32_t back = 0;
     for (uint32_t dead = held & ~live; dead; dead &= dead - 1) {
@@ -168,9 +230,11 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
   };
 
   int mine = 0;
+  uint32_t back = 0;  // of the tile that was read last
   for (int t = t0, g = g0; t < t1; ++t) {
     while (t >= r.first_tile[g + 1]) ++g;
-    mine += __popc(read_tile(g, (t - r.first_tile[g]) * 32 + lane));
+    back = read_tile(g, (t - r.first_tile[g]) * 32 + lane);
+    mine += __popc(back);
   }
   mine = __reduce_add_sync(~0u, mine);
   if (lane == 0) s_back[w] = mine;
@@ -194,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
   for (int t = t0, g = g0; t < t1; ++t) {
     while (t >= r.first_tile[g + 1]) ++g;
     const int col = (t - r.first_tile[g]) * 32 + lane;
-    const uint32_t back = read_tile(g, col);
+    if (t1 - t0 > 1) back = read_tile(g, col);
     int x = __popc(back);
     const int c = x;
 #pragma unroll
@@ -222,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
     a.seq_out[i] = len > 0 && fits ? len : 0;
     a.status[i] = len < 0 ? SEEDQ_REQ_BAD : fits ? SEEDQ_REQ_OK : SEEDQ_REQ_NO_PAGES;
     if (nth >= 0 && fits) {
-      const int dst = __ldcg(a.free_pages + (total - 1 - nth));
+      const int dst = total == count && i == my_row ? top : __ldcg(a.free_pages + (total - 1 - nth));
       a.table_out[(int64_t)i * a.out_stride + pages_of(len, a) - 1] = dst;
       a.work->copy[nth].dst = dst;
       a.work->copy[nth].used = len % a.page;
@@ -232,43 +296,17 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
     a.work->n = min(copies, total);
     *a.count_out = total - min(copies, total);
   }
+  if constexpr (COPY) {
+    cluster.sync();  // the list is whole
+    copy_pages(y, min(copies, total), me, workers);
+  }
 }
 
-// ---------------------------------------------------------------- copies
+constexpr int kCopyThreads = 256, kCopyCtas = 4;  // per SM
 
-struct CopyArgs {
-  const Workspace *work;
-  int32_t layers, heads, pieces;  // pieces of 16 codes of a token
-  int64_t pages, page_stride, head_stride, token_stride;
-  uint8_t *codes[kLayersAtOnce][2];
-  float *scales[kLayersAtOnce][2];
-};
-
-constexpr int kCopyThreads = 256;
-
-__global__ void __launch_bounds__(kCopyThreads) k_beam_copy(const __grid_constant__ CopyArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int of_copy = a.layers * 2 * a.heads;
-  const int64_t units = (int64_t)a.work->n * of_copy, warps = (int64_t)gridDim.x * (kCopyThreads / 32);
-  for (int64_t u = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); u < units; u += warps) {
-    const int c = (int)(u / of_copy), rest = (int)(u - (int64_t)c * of_copy), lt = rest / a.heads, h = rest - lt * a.heads;
-    const Copy y = a.work->copy[c];
-    if (y.src < 0 || y.src >= a.pages || y.dst < 0 || y.dst >= a.pages) continue;
-    uint8_t *base = a.codes[lt >> 1][lt & 1] + h * a.head_stride;
-    const uint8_t *src = base + y.src * a.page_stride;
-    uint8_t *dst = base + y.dst * a.page_stride;
-    const int n = y.used * a.pieces;
-#pragma unroll 4
-    for (int i = lane; i < n; i += 32) {
-      const int t = i / a.pieces;
-      const int64_t at = t * a.token_stride + (i - t * a.pieces) * 16;
-      *(uint4 *)(dst + at) = *(const uint4 *)(src + at);
-    }
-    if (lane == 0) {
-      float *s = a.scales[lt >> 1][lt & 1];
-      s[(int64_t)y.dst * a.heads + h] = s[(int64_t)y.src * a.heads + h];
-    }
-  }
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) k_beam_copy(const __grid_constant__ CopyArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // for the list of copies
+  copy_pages(a, a.work->n, (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5), (int64_t)gridDim.x * (kCopyThreads / 32));
 }
 
 DeviceOnce g_pages_smem;
@@ -318,8 +356,9 @@ seedq_status seedq_beam_reorder(const seedq_kv_cache *caches, int32_t n_caches, 
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_fail(e);
   const int rc = g_pages_smem.run(dev, [] {
-    return (int)cudaFuncSetAttribute(k_beam_pages, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)std::max(pages_smem(SEEDQ_MAX_REQUESTS, 1), pages_smem(SEEDQ_MAX_REQUESTS / kMaxBeams, kMaxBeams)));
+    const int most = (int)std::max(pages_smem(SEEDQ_MAX_REQUESTS, 1), pages_smem(SEEDQ_MAX_REQUESTS / kMaxBeams, kMaxBeams));
+    const cudaError_t e = cudaFuncSetAttribute(k_beam_pages<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return (int)(e == cudaSuccess ? cudaFuncSetAttribute(k_beam_pages<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) : e);
   });
   if (rc) return cuda_fail((cudaError_t)rc);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -329,26 +368,39 @@ seedq_status seedq_beam_reorder(const seedq_kv_cache *caches, int32_t n_caches, 
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = (unsigned)ranks, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)ranks), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = pages_smem(p.n_groups, p.n_beams);
-  cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, k_beam_pages, a);
-  if (e != cudaSuccess) return cuda_fail(e);
-
   CopyArgs y{};
   y.work = a.work, y.heads = c.n_kv_heads, y.pieces = c.head_dim / 16, y.pages = c.n_pages;
   y.page_stride = c.page_stride, y.head_stride = c.head_stride, y.token_stride = c.token_stride;
-  for (int first = 0; first < n_caches; first += kLayersAtOnce) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)ranks), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = pages_smem(p.n_groups, p.n_beams);
+  cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  auto layers = [&](int first) {
     y.layers = std::min(n_caches - first, kLayersAtOnce);
     for (int i = 0; i < y.layers; ++i) {
       const seedq_kv_cache &x = caches[first + i];
       y.codes[i][0] = (uint8_t *)x.k, y.codes[i][1] = (uint8_t *)x.v;
       y.scales[i][0] = x.k_scale, y.scales[i][1] = x.v_scale;
     }
+  };
+  layers(0);
+  const int64_t tensors = (int64_t)p.n_groups * p.n_beams * n_caches * 2 * y.heads;
+  if (tensors * (c.page_size - 1) * c.head_dim <= kFewBytes && n_caches <= kLayersAtOnce) {
+    e = cudaLaunchKernelEx(&cfg, k_beam_pages<true>, a, y);
+    return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);
+  }
+  e = cudaLaunchKernelEx(&cfg, k_beam_pages<false>, a, char(0));
+  if (e != cudaSuccess) return cuda_fail(e);
+  for (int first = 0; first < n_caches; first += kLayersAtOnce) {
+    if (first) layers(first);
     const int64_t most = (int64_t)p.n_groups * p.n_beams * y.layers * 2 * y.heads, per = kCopyThreads / 32;
-    const unsigned ctas = (unsigned)std::min<int64_t>((most + per - 1) / per, 152 * 8);
-    k_beam_copy<<<ctas, kCopyThreads, 0, st>>>(y);
-    e = cudaGetLastError();
+    // Its CTAs may start while the pages are being handed out; they wait for that before they read.
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t copy{};
+    copy.gridDim = dim3((unsigned)std::min<int64_t>((most + per - 1) / per, 152 * kCopyCtas));
+    copy.blockDim = dim3(kCopyThreads), copy.stream = st, copy.attrs = &early, copy.numAttrs = 1;
+    e = cudaLaunchKernelEx(&copy, k_beam_copy, y);
     if (e != cudaSuccess) return cuda_fail(e);
   }
   return SEEDQ_OK;

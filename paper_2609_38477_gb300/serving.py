@@ -191,12 +191,11 @@ class KVCache:
         rotary._want_angles(cos_sin, n, self.device)
         heads, ot, qs, os, qp, op = 0, dt, (0, 0), (0, 0), 0, 0
         if q is not None:
-            heads = q.shape[1] if q.ndim == 3 else 0
-            qt, qs = _rows(q, "q", n, heads, self.head_dim, self.device)
-            if qt != dt or q_out is None:
-                raise ValueError("q: the type of k, and q_out beside it are wanted")
-            ot, os = _rows(q_out, "q_out", n, heads, self.head_dim, self.device)
-            _want_apart(q_out, "q_out")
+            shape = q.shape
+            if q_out is None or q.dtype is not k.dtype or len(shape) != 3 or shape[0] != n or shape[2] != self.head_dim or q.device != self.device:
+                raise ValueError(f"q: ({n}, n_heads, {self.head_dim}) of the type and device of k, and q_out beside it are wanted")
+            heads = shape[1]
+            _, qs, ot, os = _turned_rows(q, q_out, "q_out")
             qp, op = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out: wanted beside q alone")
@@ -238,10 +237,14 @@ class KVCache:
         _check(Q.lib().seedq_kv_attend(self._ref, a, _stream(stream, dev)), "seedq_kv_attend")
 
 
-def _want_apart(t, name: str):
-    """Rows that are written must not lie on one another."""
-    if any(n > 1 and st < t.shape[2] for n, st in zip(t.shape, t.stride()[:2])):
-        raise ValueError(f"{name}: rows that overlap")
+def _turned_rows(x, out, name: str):
+    """Types and strides of (tokens, heads, dim) rows and of those that they are rotated to, which must not lie on one another."""
+    shape, xt, ot, xs, os = x.shape, DTYPES.get(x.dtype), DTYPES.get(out.dtype), x.stride(), out.stride()
+    if (xt is None or ot is None or len(shape) != 3 or out.shape != shape or xs[2] != 1 or os[2] != 1 or out.device != x.device
+            or (os[1] < shape[2] and shape[1] > 1) or (os[0] < shape[2] and shape[0] > 1)):
+        raise ValueError(f"{name}: (tokens, heads, dim) float32, bfloat16 or float16 in and out, of one shape and device, with contiguous "
+                         f"last dimension and no rows of {name} on one another are wanted, got {tuple(shape)} {x.dtype} and {tuple(out.shape)} {out.dtype}")
+    return xt, xs, ot, os
 
 
 def rotary_frequencies(rot_dim: int, base: float = 10000.0, rule: str = "none", factor: float = 1.0, original: int = 8192,
@@ -316,13 +319,9 @@ class Rotary:
 
     def rotate(self, x, cos_sin, out, stream=None):
         """seedq_rotate: x, out (n_tokens, n_heads, head_dim); out may be x."""
-        if x.ndim != 3:
-            raise ValueError("x: (n_tokens, n_heads, head_dim) is wanted")
+        xt, xs, ot, os = _turned_rows(x, out, "out")
         n, heads, dim = x.shape
         self._want_angles(cos_sin, n, x.device)
-        xt, xs = _rows(x, "x", n, heads, dim, x.device)
-        ot, os = _rows(out, "out", n, heads, dim, x.device)
-        _want_apart(out, "out")
         _check(Q.lib().seedq_rotate(x.data_ptr(), xt, xs[0], xs[1], n, heads, dim, self.rot_dim, self.layout, cos_sin.data_ptr(),
                                     out.data_ptr(), ot, os[0], os[1], _stream(stream, x.device)), "seedq_rotate")
 
