@@ -114,9 +114,9 @@ struct Segment {
 // A candidate as two words that sort as candidates do: the weighted total as an
 // ordered double; then beam, logit and token, each such that what comes first is
 // larger.  No candidate is (0, 0).
-struct Item {
+struct alignas(16) Item {
   uint64_t key, rest;
-  __device__ __forceinline__ bool before(const Item &o) const { return key > o.key || (key == o.key && rest > o.rest); }
+  __device__ __forceinline__ bool before(const Item &o) const { return (key > o.key) | ((key == o.key) & (rest > o.rest)); }
 };
 __device__ __forceinline__ uint64_t order_double(double x) {
   const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
@@ -137,7 +137,7 @@ constexpr int kLanesOfRow = 8;
 struct Join {
   // total = base + scale * (logit - most): the difference first, or a large common part would take the sum's digits
   double base[kMaxBeams], weight[kMaxBeams], most[kMaxBeams];
-  float4 line[kMaxBeams];  // the same weighted, in float32: x * (logit - y) + z, and w = 2^-21 |z|; -inf of a beam that brings nothing
+  float4 line[kMaxBeams];  // the same weighted, in float32: x * (logit - y) + z, and w = 2^-21 |z|; for a finished beam z alone
   int kind[kMaxBeams];
   alignas(16) float group[64];
   uint32_t words[kWarps];
@@ -155,14 +155,16 @@ __device__ __forceinline__ double total_of(const SelectArgs &a, const Join &s, i
 __device__ __forceinline__ Item item_of(const SelectArgs &a, const Join &s, int b, float x, int index) {
   return {order_double(s.weight[b] * total_of(a, s, b, x)), rest_word(b, order_word(x), index)};
 }
-// The weighted total in float32, and how far it may be off: a few roundings of its
-// parts, here 2^-21 of them.  What is far down is cut off, for all beams alike (their
-// offsets are at most 1e29).
-__device__ __forceinline__ float about(const Join &s, int b, float x, float &off) {
-  const float4 l = s.line[b];
-  const float d = fmaxf(l.x * (x - l.y), -1e37f);
-  off = fmaf(-0x1p-21f, fminf(d, 0.f), l.w);  // d is at most 0 but for roundings
-  return d + l.z;
+// Bounds of the weighted total in float32: of its parts' few roundings, here 2^-21 of
+// them.  What is far down is cut off, for all beams alike (their offsets are at most
+// 1e29).  -inf of what is no candidate.
+__device__ __forceinline__ float lower(const float4 l, float x) {
+  const float d = fmaxf(l.x * (x - l.y), -1e37f), y = fmaf(fminf(d, 0.f), 0x1p-21f, d) + (l.z - l.w);  // d is at most 0 but for roundings
+  return x > -CUDART_INF_F ? y : -CUDART_INF_F;
+}
+__device__ __forceinline__ float upper(const float4 l, float x) {
+  const float d = fmaxf(l.x * (x - l.y), -1e37f), y = fmaf(fminf(d, 0.f), -0x1p-21f, d) + (l.z + l.w);
+  return x > -CUDART_INF_F ? y : -CUDART_INF_F;
 }
 // Which of 256 items in a row a thread takes: such that the first 64 fall into 64
 // different groups of four threads.
@@ -202,12 +204,19 @@ __device__ __forceinline__ bool rank_found(const SelectArgs &a, Join &s, int n) 
     s.found[threadIdx.x] = mine;
   }
   __syncthreads();
-  if (threadIdx.x < m) {
-    int before = 0;
-#pragma unroll 8
-    for (int k = 0; k < m; ++k) before += s.found[k].before(mine);
-    if (before < n) s.chosen[before] = mine;
+  // several threads count for one candidate
+  const int share = m <= 32 ? 8 : m <= 64 ? 4 : m <= 128 ? 2 : 1, i = threadIdx.x / share;
+  mine = s.found[min(i, kMaxFound - 1)];
+  int before = 0;
+  if (i < m) {
+#pragma unroll 4
+    for (int k = threadIdx.x % share; k < m; k += share) {
+      const ulonglong2 y = *(const ulonglong2 *)&s.found[k];
+      before += Item{y.x, y.y}.before(mine);
+    }
   }
+  for (int o = share / 2; o; o >>= 1) before += __shfl_xor_sync(~0u, before, o);
+  if (i < m && before < n && threadIdx.x % share == 0) s.chosen[before] = mine;
   if (threadIdx.x == 0) s.n_chosen = min(m, n);
   __syncthreads();
   return true;
@@ -251,7 +260,7 @@ __device__ __forceinline__ void choose_slowly(const SelectArgs &a, Join &s, Each
 }
 
 template <int DT, bool VEC>
-__device__ __noinline__ void join_slowly(const SelectArgs &a, Join &s, int64_t g) {
+__device__ __noinline__ void join_slowly(const SelectArgs a, Join &s, int64_t g) {  // by value: the kernel's own stay in constant memory
   using Seg = Segment<DT, VEC>;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   choose_slowly(a, s, [&](auto &&f) {
@@ -300,20 +309,18 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
   using Seg = Segment<DT, VEC>;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, slot = item_slot();
   const int chunks = a.beams * a.chunks, of_chunk = a.chunk_segments;
-  float bound = -CUDART_INF_F, off;
+  float bound = -CUDART_INF_F;
   // chunks, by their largest logits: of those whose upper bound reaches the n-th lower one the segments are looked at
   const bool few = by_chunks(a);
   if (few) {
     for (int k = slot; k < chunks; k += kThreads) {
       const int b = (unsigned)k / (unsigned)a.chunks;
-      const float x = s.chunk_most[k];
-      if (s.kind[b] == kLive && x > -CUDART_INF_F) bound = fmaxf(bound, about(s, b, x, off) - off);
+      if (s.kind[b] == kLive) bound = fmaxf(bound, lower(s.line[b], s.chunk_most[k]));
     }
     bound = nth_bound(s, bound, a.n_out);
-    for (int k = tid; k < chunks; k += kThreads) {
+    for (int k = slot; k < chunks; k += kThreads) {
       const int b = (unsigned)k / (unsigned)a.chunks;
-      const float x = s.chunk_most[k];
-      if (s.kind[b] == kLive && x > -CUDART_INF_F && about(s, b, x, off) + off >= bound)
+      if (s.kind[b] == kLive && s.chunk_most[k] > -CUDART_INF_F && upper(s.line[b], s.chunk_most[k]) >= bound)
         s.chunk[atomicAdd(&s.n_chunks, 1)] = (uint32_t)b << 16 | (uint32_t)(k - b * a.chunks);
     }
     __syncthreads();
@@ -336,6 +343,7 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
       } else if (at < total) {
         beam[k] = b, number[k] = i;
         if (first) ahead[k] = __ldcg(a.most + g * a.beams * a.segments + at);
+        if (s.kind[b] != kLive) ahead[k] = -CUDART_INF_F;  // the row holds anything
       } else {
         ahead[k] = -CUDART_INF_F;
       }
@@ -344,15 +352,15 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
     }
   };
   const bool ends = tid < a.beams && s.kind[tid] == kDone;
-  bound = ends ? about(s, tid, 0.f, off) - off : -CUDART_INF_F;
+  bound = ends ? s.line[tid].z - s.line[tid].w : -CUDART_INF_F;
   for (int first = 0; first < total; first += kThreads * kAhead) {
     load(first);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-      if (ahead[k] > -CUDART_INF_F && s.kind[beam[k]] == kLive) bound = fmaxf(bound, about(s, beam[k], ahead[k], off) - off);
+      bound = fmaxf(bound, lower(s.line[beam[k]], ahead[k]));
   }
   bound = nth_bound(s, bound, a.n_out);
-  if (ends && about(s, tid, 0.f, off) + off >= bound) push(s, tid, 0.f, a.end_token);
+  if (ends && s.line[tid].z + s.line[tid].w >= bound) push(s, tid, 0.f, a.end_token);
   for (int first = 0; first < total; first += kThreads * kAhead) {
     if (total > kThreads * kAhead) {
       if (!few && first == 0) load_first(a, g, ahead);
@@ -361,7 +369,7 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
     uint32_t in = 0;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-      if (ahead[k] > -CUDART_INF_F && about(s, beam[k], ahead[k], off) + off >= bound) in |= 1u << k;
+      in |= (uint32_t)((upper(s.line[beam[k]], ahead[k]) >= bound) & (ahead[k] > -CUDART_INF_F)) << k;
     while (in) {
       const int k = __ffs(in) - 1;
       in &= in - 1;
@@ -370,7 +378,7 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
 #pragma unroll
       for (int z = 1; z < kAhead; ++z)
         if (k == z) x = ahead[z], b = beam[z], i = number[z];
-      if (s.kind[b] == kLive) push(s, b, x, i);  // a finished beam's row holds anything
+      push(s, b, x, i);
     }
   }
   if (!rank_found(a, s, a.n_out)) return join_slowly<DT, VEC>(a, s, g);
@@ -381,7 +389,7 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
   if (n_chosen == a.n_out) {  // no candidate comes behind the last segment's best
     const Item last = s.chosen[n_chosen - 1];
     const int b = rest_beam(last.rest);
-    bound = about(s, b, rest_logit(last.rest), off) - off;
+    bound = s.kind[b] == kDone ? s.line[b].z - s.line[b].w : lower(s.line[b], rest_logit(last.rest));
   }
   constexpr int kEach = kMaxTop / kWarps;
   Seg seg[kEach];
@@ -409,10 +417,10 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
     }
     float x[8];
     seg[k].get(x);
+    const float4 line = s.line[b];
     uint32_t in = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (x[e] > -CUDART_INF_F && about(s, b, x[e], off) + off >= bound) in |= 1u << e;
+    for (int e = 0; e < 8; ++e) in |= (uint32_t)((upper(line, x[e]) >= bound) & (x[e] > -CUDART_INF_F)) << e;
     while (in) {
       const int e = __ffs(in) - 1;
       in &= in - 1;
@@ -426,7 +434,7 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
 }
 
 template <int DT, bool VEC>
-__device__ __noinline__ void join_group(const SelectArgs &a, Join &s, int64_t g) {
+__device__ __forceinline__ void join_group(const SelectArgs &a, Join &s, int64_t g) {
   const int tid = threadIdx.x;
   if (tid == 0) s.spoiled = s.slow = s.n_found = s.n_chosen = s.n_chunks = 0;
   __syncthreads();
