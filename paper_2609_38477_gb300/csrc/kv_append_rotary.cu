@@ -204,12 +204,12 @@ __device__ __forceinline__ void write_run(const AppendArgs &a, const Lane &l, co
   uint4 *ring = s_ring + threadIdx.x;
   const int second_x = (l.d1 - l.d0) * U::kSize, second_c = l.d1 - l.d0;
   // The lane's kept tokens; where the run has fewer, its last once more: the same numbers to the same place.
-  uint32_t x_kept[STEPS], c_kept[STEPS];  // what a page's tokens span is below 4 GB
+  int64_t x_kept[STEPS], c_kept[STEPS];
 #pragma unroll
   for (int k = 0; k < STEPS; ++k) {
     const int t = min(team.first + k * team.stride, run.m - 1);
-    x_kept[k] = (uint32_t)(t * a.ts + l.d0) * U::kSize;
-    c_kept[k] = (uint32_t)(t * a.c.token_stride) + l.d0;
+    x_kept[k] = (t * a.ts + l.d0) * U::kSize;
+    c_kept[k] = t * a.c.token_stride + l.d0;
   }
   const int64_t x_head = a.hs * U::kSize;
   const char *x = (const char *)a.x[TENSOR] + (run.t0 * a.ts + team.h0 * a.hs) * U::kSize;
@@ -481,7 +481,7 @@ DeviceOnce g_once[2][3][3];
 
 template <int KIND, int DT, int PAIRS>
 cudaError_t launch_as(const AppendArgs &a, unsigned ctas, cudaStream_t st) {
-  if (ring_bytes<DT>() > 40 * 1024) {
+  if (ring_bytes<DT>() > 40 * 1024) {  // of 48 without being asked for, the static part among them
     int dev = 0;
     const cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;

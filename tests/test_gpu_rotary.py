@@ -350,3 +350,60 @@ def test_other_streams(V):
                 rotary.rotate(x, cs, out)
         s.synchronize()
         assert torch.equal(out, want)
+
+
+def test_offsets_past_32_bits(V):
+    """Tokens that lie gigabytes apart, in the numbers, in the cache and between tokens of one page."""
+    rotary = V.Rotary(V.rotary_frequencies(64)[0])
+    n, h, d = 17, 2, 64
+    cs = angles_of(V, rotary, list(range(n)))
+    near = torch.randn((2, n, h, d), device="cuda").bfloat16()
+    far = torch.empty(17 * (1 << 28) + 4096, dtype=torch.bfloat16, device="cuda")  # 9 GB
+    x = far.as_strided((n, h, d), ((1 << 28) + 16, d, 1))
+    x.copy_(near[0])
+    out, want = torch.empty((n, h, d), device="cuda"), torch.empty((n, h, d), device="cuda")
+    rotary.rotate(x, cs, out)
+    rotary.rotate(near[0], cs, want)
+    assert torch.equal(out, want)
+    rotary.rotate(x, cs, x)
+    assert torch.equal(x.float(), want.bfloat16().float())
+    x.copy_(near[0])
+    v = x.as_strided((n, h, d), ((1 << 28) + 16, d, 1), 2048)
+    v.copy_(near[1])
+    # a cache whose tokens lie 512 MB apart: a page spans 16 GB
+    codes = torch.empty(32 * (1 << 29), dtype=torch.int8, device="cuda")
+    page = lambda at: codes.as_strided((2, h, 32, d), (4096, 256, 1 << 29, 1), at)  # noqa: E731
+    a = V.KVCache(page(0), page(1 << 20), *(torch.zeros((2, h), device="cuda") for _ in range(2)))
+    b = new_cache(V, 2, h, 32, d, "int8")
+    for c in (a, b):
+        for t in (c.k, c.v, c.k_scale, c.v_scale):
+            t.zero_()
+    slots = torch.arange(n, device="cuda") + 32 + 13
+    for keys, values in ((x, v), (near[0], near[1])):
+        a.append_rotary(keys, values, slots, rotary, cs)
+        assert a.k.stride(2) == 1 << 29
+    turned = torch.empty((n, h, d), device="cuda")
+    rotary.rotate(near[0], cs, turned)
+    for _ in range(2):
+        b.append(turned, near[1].float(), slots)
+    assert torch.equal(a.k.view(torch.uint8), b.k) and torch.equal(a.v.view(torch.uint8), b.v)
+    assert torch.equal(a.k_scale[1], b.k_scale[1]) and torch.equal(a.v_scale[1], b.v_scale[1])
+
+
+def test_cache_pages_of_every_order(V):
+    """Pages whose heads or tokens lie outermost, as views of one buffer."""
+    rotary = V.Rotary(V.rotary_frequencies(48)[0], "pairs")
+    n, h, d, P = 50, 3, 48, 16
+    x = torch.randn((2, n, h, d), device="cuda")
+    cs = angles_of(V, rotary, list(range(100, 100 + n)))
+    slots = torch.arange(n, device="cuda") + 5
+    want = new_cache(V, 4, h, P, d, "e4m3")
+    k = torch.empty_like(x[0])
+    rotary.rotate(x[0], cs, k)
+    want.append(k, x[1], slots)
+    for order in ((0, 1, 2), (0, 2, 1), (1, 0, 2), (1, 2, 0), (2, 0, 1), (2, 1, 0)):
+        shape = (4, h, P)
+        t = [torch.full([shape[i] for i in order] + [d], 0x55, dtype=torch.uint8, device="cuda").permute(*[order.index(i) for i in range(3)], 3) for _ in range(2)]
+        c = V.KVCache(*t, *(torch.full((4, h), 77.0, device="cuda") for _ in range(2)), "e4m3")
+        c.append_rotary(x[0], x[1], slots, rotary, cs)
+        same(c, want)
