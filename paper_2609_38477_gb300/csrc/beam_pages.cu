@@ -245,13 +245,9 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
     s_cta_back = x;
   }
   cluster.sync();
-  int before = 0, all = 0;
-  for (int k = 0; k < ranks; ++k) {
-    const int x = *cluster.map_shared_rank(&s_cta_back, k);
-    if (k < rank) before += x;
-    all += x;
-  }
-  for (int k = 0; k < w; ++k) before += s_back[k];
+  const int of_rank = lane < ranks ? *cluster.map_shared_rank(&s_cta_back, lane) : 0;
+  const int all = __reduce_add_sync(~0u, of_rank);
+  const int before = __reduce_add_sync(~0u, (lane < rank ? of_rank : 0) + (lane < w ? s_back[lane] : 0));
   const int total = (int)min((int64_t)count + all, (int64_t)a.capacity);
 
   int place = count + before;
