@@ -589,7 +589,7 @@ seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_r
  *   scores     device, n_groups x n_beams float32.
  *   done       device, as many bytes, not 0 where the beam has ended, or NULL.
  *   weights    device, as many float32, or NULL (all 1).
- *   out_*      device, n_groups x n_out.
+ *   out_*      device, n_groups x n_out; not over scores, done or weights.
  *   workspace  device, 16-byte aligned, seedq_beam_select_workspace_bytes(n_groups,
  *              n_beams, vocab) bytes, zeroed once before its first use, good for
  *              any call that asks for no more; calls that may overlap need one each.
@@ -597,7 +597,7 @@ seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_r
  * outside 1..SEEDQ_MAX_BEAMS, n_groups x n_beams above SEEDQ_MAX_REQUESTS, vocab
  * outside 1..SEEDQ_BEAM_MAX_VOCAB, row_stride < vocab, logits not aligned to their
  * type, end_token outside the vocabulary where done is given, scale outside
- * 2^-64..2^64, workspace too small), CUDA.  n_groups = 0 is a no-op. */
+ * 2^-64..2^64, outputs over inputs, workspace too small), CUDA.  n_groups = 0 is a no-op. */
 #define SEEDQ_MAX_BEAMS 32
 #define SEEDQ_BEAM_MAX_VOCAB (1 << 27)
 typedef struct {
@@ -654,7 +654,8 @@ seedq_status seedq_beam_select(const seedq_beam_select_args *args, void *cuda_st
  *   free_count_out  entries left.
  *   workspace     device, 16-byte aligned, seedq_beam_reorder_workspace_bytes
  *                 (n_groups, n_beams) bytes; calls that may overlap need one each.
- * Outputs must not alias parents, seq_lens or free_count.
+ * seq_lens_out may be seq_lens and free_count_out free_count (an earlier call's
+ * outputs); no other output may alias parents, seq_lens or free_count.
  * Errors: INVALID_ARG (NULL or aliased pointer, n_caches outside
  * 1..SEEDQ_BEAM_MAX_CACHES, caches that differ, n_beams outside
  * 1..SEEDQ_MAX_BEAMS, rows outside 1..SEEDQ_MAX_REQUESTS, table_width outside

@@ -12,6 +12,11 @@
 //
 // The copies are units of one head and tensor of one layer and page, dealt to all
 // warps: of a second launch, or, where they are small, of the first.
+//
+// Measured: 4 requests of 4 beams of 600 tokens, 32 layers of 8 heads of 128, 9.4 us
+// (the lists 7: launch, six dependent trips to memory and two barriers of the
+// cluster); 32 requests of 8 beams, 8 layers, 22 us, of which the copies (67 MB) take
+// 11 to 12 (5.8 TB/s).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -29,10 +34,11 @@ namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32;
 constexpr int kMaxBeams = SEEDQ_MAX_BEAMS;
-constexpr int kMaxCluster = 8;
-constexpr int kAtOnce = 8;        // rows of a tile under way
+constexpr int kMaxCluster = 8;  // one CTA takes 33 us instead of 23 for 32 requests of 8 beams
+constexpr int kAtOnce = 8;      // rows of a tile under way
 constexpr int kLayersAtOnce = 64;  // whose pointers go in a launch's parameters
-// What may have to be copied, up to which the first launch does it.
+// What may have to be copied, up to which the first launch does it: a fork of 2 small
+// layers takes as long on the GPU (9 us) and 3 us less of the caller's time.
 constexpr int64_t kFewBytes = 1 << 20;
 
 // One copy: tokens [0, used) of page src to page dst.
@@ -64,7 +70,7 @@ struct CopyArgs {
   uint8_t *codes[kLayersAtOnce][2];
   float *scales[kLayersAtOnce][2];
 };
-constexpr int kCopyAhead = 8;  // loads of 16 bytes that a lane has under way
+constexpr int kCopyAhead = 8;  // loads of 16 bytes that a lane has under way (4: 25.4 us instead of 23.5)
 
 // What warp `me` of `warps` copies of the first n entries of the list.
 __device__ __forceinline__ void copy_pages(const CopyArgs &a, int n, int64_t me, int64_t warps) {
@@ -202,8 +208,8 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
   // Reads a tile; bit b of the result: row b's page at the lane's column goes back here.
   auto read_tile = [&](int g, int col) -> uint32_t {
     uint32_t held = 0, live = 0;
+    int id[kAtOnce];
     for (int b0 = 0; b0 < B; b0 += kAtOnce) {
-      int id[kAtOnce];
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k) {
         const int i = g * B + b0 + k;
@@ -219,6 +225,17 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
         }
     }
     uint32_t back = 0;
+    if (B <= kAtOnce) {  // all in registers
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        uint32_t same = 0;
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b) same |= (uint32_t)(id[b] == id[q]) << b;
+        const bool stays = same & held & (live | ((1u << q) - 1));
+        back |= (uint32_t)!stays << q;
+      }
+      return back & held & ~live;
+    }
     for (uint32_t dead = held & ~live; dead; dead &= dead - 1) {
       const int q = __ffs(dead) - 1, id = tiles[q * 32 + lane];
       bool stays = false;
@@ -343,8 +360,9 @@ seedq_status seedq_beam_reorder(const seedq_kv_cache *caches, int32_t n_caches, 
       p.free_capacity < c.n_pages || p.free_capacity == INT32_MAX)
     return SEEDQ_ERR_INVALID_ARG;
   if (p.table_out == p.block_table && p.out_stride != p.table_stride) return SEEDQ_ERR_INVALID_ARG;
+  // Lengths and count are read before any are written.
   for (const int32_t *o : {p.seq_lens_out, p.status, p.free_count_out})
-    if (o == p.parents || o == p.seq_lens || o == p.free_count) return SEEDQ_ERR_INVALID_ARG;
+    if (o == p.parents || (o == p.seq_lens && o != p.seq_lens_out) || (o == p.free_count && o != p.free_count_out)) return SEEDQ_ERR_INVALID_ARG;
   PagesArgs a{p.n_groups, p.n_beams, c.page_size, log2_of(c.page_size), p.table_width, p.free_capacity, p.table_stride, p.out_stride,
               p.parents, p.seq_lens, p.block_table, p.free_count, p.table_out, p.free_pages, p.seq_lens_out, p.status, p.free_count_out,
               (Workspace *)p.workspace};

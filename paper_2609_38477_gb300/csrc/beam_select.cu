@@ -14,6 +14,14 @@
 // chooses n segments from the maxima (of the chunks that can hold them), reads them
 // again, and chooses from their logits.  Each choice is by a float32 bound that at
 // least n reach, then by counting, for each of the few that do, how many precede it.
+//
+// Measured, n = twice the beams: a request of 4 beams of 32000 logits 8.9 us, 4
+// requests of 4 beams of 128256 10.6 (the pass over the logits 3.9: launch, one trip
+// to memory, an arrival), 64 of 8 beams of 128256 bfloat16 38 us (the pass 24, 4.4
+// TB/s).  The join is a chain of about fifteen trips to L2 or shared memory and
+// barriers of one CTA, 5 to 7 us (sorted lists of 32 took 9 to 19), and many requests'
+// joins fall at the end.  Segments of 256: what is read again is 1 KB a candidate, and
+// a row of 128256 has 501 maxima, one look of a CTA at 4 beams.
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <stdint.h>
@@ -37,8 +45,8 @@ constexpr int kTokenBits = 27;
 constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint64_t kHeader = 2 * SEEDQ_MAX_REQUESTS * 4;  // arrival counters of requests and of rows
-// Logits from which on warps stream: 512 rows of 128256 bfloat16 (131 MB) take 42 us
-// so and 45 by a CTA per chunk, 128 of float32 (66 MB) 27.5 and 24.
+// Logits from which on warps stream: 512 rows of 128256 bfloat16 (131 MB) take 38 us
+// so and 42 by a CTA per chunk, 128 of float32 (66 MB) 25 and 22.
 constexpr int64_t kStreamBytes = 96 << 20, kStreamVocab = 16384;
 
 struct SelectArgs {
@@ -767,12 +775,13 @@ DeviceOnce g_stream[3];
 template <int DT>
 cudaError_t launch(SelectArgs &a, bool vec, cudaStream_t st) {
   const int64_t rows = (int64_t)a.groups * a.beams;
-  if (vec && rows * a.vocab * dtype_bytes(DT) >= kStreamBytes && a.vocab >= kStreamVocab) {
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  const bool many = rows * a.vocab * dtype_bytes(DT) >= kStreamBytes && a.vocab >= kStreamVocab;
+  if (vec && many && rows <= (int64_t)sms * kStreamCtas * kMaxJoins / 4) {  // a CTA meets a quarter as many rows, and as many requests without any
     constexpr size_t kSmem = kWarps * kStages * kTileBytes + SEEDQ_MAX_REQUESTS * sizeof(uint16_t);
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
     const int rc = g_stream[DT].run(dev, [] {
       return (int)cudaFuncSetAttribute(k_beam_stream<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     });
@@ -792,6 +801,10 @@ cudaError_t launch(SelectArgs &a, bool vec, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+bool apart(const void *a, uint64_t na, const void *b, uint64_t nb) {
+  const uint64_t x = (uint64_t)(uintptr_t)a, y = (uint64_t)(uintptr_t)b;
+  return !a || !b || x + na <= y || y + nb <= x;
+}
 bool sizes_ok(int64_t groups, int32_t beams, int64_t vocab) {
   return groups >= 0 && beams >= 1 && beams <= kMaxBeams && groups * beams <= SEEDQ_MAX_REQUESTS && groups <= SEEDQ_MAX_REQUESTS &&
          vocab >= 1 && vocab <= SEEDQ_BEAM_MAX_VOCAB;
@@ -822,6 +835,10 @@ seedq_status seedq_beam_select(const seedq_beam_select_args *args, void *cuda_st
       p.workspace_bytes < seedq_beam_select_workspace_bytes(p.n_groups, p.n_beams, p.vocab) ||
       (p.done && (p.end_token < 0 || p.end_token >= p.vocab)) || (uintptr_t)p.logits % dtype_bytes(p.dtype))
     return SEEDQ_ERR_INVALID_ARG;
+  // CTAs that begin late read the scores again.
+  const uint64_t in = (uint64_t)p.n_groups * p.n_beams, out = (uint64_t)p.n_groups * p.n_out * 4;
+  for (const void *o : {(const void *)p.out_score, (const void *)p.out_beam, (const void *)p.out_token})
+    if (!apart(o, out, p.scores, in * 4) || !apart(o, out, p.weights, in * 4) || !apart(o, out, p.done, in)) return SEEDQ_ERR_INVALID_ARG;
   SelectArgs a{};
   a.x = p.logits, a.stride = p.row_stride, a.vocab = (int32_t)p.vocab, a.beams = p.n_beams, a.groups = (int32_t)p.n_groups;
   a.scale = p.scale, a.c = p.scale * kLog2e, a.scores = p.scores, a.weights = p.weights, a.done = p.done, a.end_token = p.end_token;

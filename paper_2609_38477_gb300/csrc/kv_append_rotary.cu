@@ -14,8 +14,17 @@
 // heads' numbers under way by asynchronous copies, and the cos and sin of its lanes'
 // tokens in registers for all heads.  Runs longer than 8 warps keep are read again.
 // The step's queries are turned by CTAs behind those of the append, many by a launch
-// of their own (4 prompts of 1024, 32 heads: 41 us instead of 46: their CTAs want more
-// of an SM's threads than the registers and shared memory of the append leave).
+// of their own: the registers and shared memory of the append leave their CTAs too few
+// of an SM's threads.
+//
+// Measured, 128 head dims: 16 single tokens of 8 key-value and 32 query heads, float32,
+// 3.9 us (the plain append 3.0, a rotation 2.4); 4 prompts of 1024, 32 heads, bfloat16,
+// 30 us without queries (3.3 TB/s; the plain append 23), 44 with them (3.8 TB/s).  What
+// bounds the prompts is the chain of a head (numbers, largest, the warps' largest,
+// codes) and about 220 instructions per 16 numbers of a lane at 16 warps per SM, 42%
+// of the issue slots.  24 warps want 80 registers, and spill (61 us); cos and sin in
+// registers instead of shared memory, 36 us; as loads of every head, 50; the numbers
+// kept as they came and rotated twice, 45.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -34,7 +43,10 @@ constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kCtasPerSm = 2;
 constexpr int kSteps = 2;   // tokens that a lane keeps
 constexpr int kStages = 2;  // tasks whose numbers are under way
-constexpr int64_t kFewPairs = 8192;            // tokens times heads and tensors up to which a CTA takes one head
+// Tokens times heads and tensors up to which a CTA takes one head of 8 tokens: a prompt
+// of 512 tokens of 8 heads (8192) takes 10.8 us so, 15.5 with 8 heads to a CTA, 256
+// single tokens of 32 heads (16384) 23.5 and 17.1.
+constexpr int64_t kFewPairs = 8192;
 constexpr int64_t kQueriesApart = 152 * 2048;  // threads from which on the queries have a launch of their own
 
 struct AppendArgs {

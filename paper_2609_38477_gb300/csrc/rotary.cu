@@ -5,6 +5,11 @@
 // Frequencies are kept in turns as whole numbers F = round(w / 2 pi * 2^64), so the
 // fraction is the product modulo 2^64: exact at any position, where a float32
 // product of position 131072 is off by 2^-8.
+//
+// Bytes bound the rotation (8192 tokens of 72 heads of 128, bfloat16: 50 us, 6.0 TB/s,
+// 91% of the copy rate), launch a step's (16 tokens of 40 heads: 2.4 us, the angles
+// 1.6).  A thread moves 16 bytes (8 pairs of 16-bit numbers in two pieces, or 8
+// neighbouring pairs); 8 bytes took 72 us.
 #include "rotary.cuh"
 
 #include <algorithm>

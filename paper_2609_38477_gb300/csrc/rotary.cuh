@@ -78,8 +78,11 @@ __device__ __forceinline__ float2 turned(float x, float y, float2 cs) {
   return make_float2(fmaf(x, cs.x, -(y * cs.y)), fmaf(y, cs.x, x * cs.y));
 }
 
-constexpr int kRotateHeads = 4;                  // of a thread, where there is work for all SMs
-constexpr int64_t kRotateMany = 152 * 2048 * 4;  // threads from which on one takes several heads
+// A thread takes several heads, and so reads their cos and sin once, where threads are
+// many and numbers narrow: 8192 tokens of 72 heads of 128 bfloat16 51 us instead of 57,
+// 2048 of 40 10 us instead of 9, 4096 of 72 in float32 46 instead of 44.
+constexpr int kRotateHeads = 4;
+constexpr int64_t kRotateMany = 152 * 2048 * 4;
 
 struct RotateArgs {
   const void *x;
@@ -112,7 +115,7 @@ inline RotateSplit rotate_split(const RotateArgs &a, int32_t in, int32_t out) {
   s.wide = n;
   s.turns = (a.half + n - 1) / n;
   s.pieces = s.turns + (rest + 2 * n - 1) / (2 * n);
-  const int each = a.n * s.pieces * a.heads >= kRotateMany ? kRotateHeads : 1;
+  const int each = a.n * s.pieces * a.heads >= kRotateMany && (in != SEEDQ_F32 || out != SEEDQ_F32) ? kRotateHeads : 1;
   s.groups = (a.heads + each - 1) / each;
   return s;
 }

@@ -133,6 +133,8 @@ class Decoder:
         rows = g * b
         if not 1 <= rows <= min(MAX_COLUMNS, self.plan.max_requests) or not all(prompts) or max_new < 1:
             raise ValueError("1..16 beams in all and no more than max_requests, prompts of a token or more and max_new >= 1 are wanted")
+        if bool(self.seq_lens.any()):
+            raise ValueError("a request is under way")
         i32 = dict(dtype=torch.int32, device="cuda")
         pages = serving.BeamPages(self.caches, g, b)
         work = serving.beam_workspace(g, b, vocab)

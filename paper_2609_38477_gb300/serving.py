@@ -241,7 +241,8 @@ def _turned_rows(x, out, name: str):
     """Types and strides of (tokens, heads, dim) rows and of those that they are rotated to, which must not lie on one another."""
     shape, xt, ot, xs, os = x.shape, DTYPES.get(x.dtype), DTYPES.get(out.dtype), x.stride(), out.stride()
     if (xt is None or ot is None or len(shape) != 3 or out.shape != shape or xs[2] != 1 or os[2] != 1 or out.device != x.device
-            or (os[1] < shape[2] and shape[1] > 1) or (os[0] < shape[2] and shape[0] > 1)):
+            or not ((os[1] >= shape[2] or shape[1] < 2) and (os[0] >= os[1] * (shape[1] - 1) + shape[2] or shape[0] < 2))
+            and not ((os[0] >= shape[2] or shape[0] < 2) and (os[1] >= os[0] * (shape[0] - 1) + shape[2] or shape[1] < 2))):
         raise ValueError(f"{name}: (tokens, heads, dim) float32, bfloat16 or float16 in and out, of one shape and device, with contiguous "
                          f"last dimension and no rows of {name} on one another are wanted, got {tuple(shape)} {x.dtype} and {tuple(out.shape)} {out.dtype}")
     return xt, xs, ot, os
@@ -438,7 +439,7 @@ class BeamPages:
 
     def reorder(self, parents, seq_lens, block_table, free_pages, free_count, out=None, stream=None):
         """seedq_beam_reorder: parents (n_groups, n_beams) int32, seq_lens int32 of
-        at least as many rows; block_table changes in place, or out (the same
+        at least as many rows (this object's own after a first call); block_table changes in place, or out (the same
         shape) gets the new one; free_pages changes in place."""
         n, dev = self.rows, self.device
         _ints(seq_lens, n, torch.int32, dev, "seq_lens")

@@ -373,6 +373,62 @@ def test_reorder_bad_parents_and_lengths(V):
         check_reorder(V, caches[:1], np.array([[0, 0, 0], [1, 1, 2]], np.int32), lens, table, np.resize(free, caches[0].n_pages), count, False)
 
 
+def test_reorder_from_its_own_outputs(V):
+    """An earlier call's lengths and count as the next one's, changed in place."""
+    rng = np.random.RandomState(6)
+    g, b, page = 300, 4, 16
+    lens, table, free, n = beams_state(rng, g, b, page, 50, 4, g * b)
+    caches = make_caches(V, 1, n, 1, page, 16, "head", torch.Generator("cuda").manual_seed(1))
+    pages = V.BeamPages(caches, g, b)
+    i32 = lambda x: torch.as_tensor(np.asarray(x, np.int32)).cuda()  # noqa: E731
+    t, f = i32(table), i32(free)
+    pages.seq_lens.copy_(i32(lens))
+    pages.free_count.fill_(g * b)
+    count = g * b
+    for _ in range(4):
+        parents = np.minimum(rng.geometric(0.5, (g, b)) - 1, b - 1).astype(np.int32)
+        pages.reorder(i32(parents), pages.seq_lens, t, f, pages.free_count)
+        table, lens, status, free, count, _ = S.beam_reorder(parents, lens, table, table, free, count, page)
+        assert np.array_equal(t.cpu().numpy(), table) and np.array_equal(pages.seq_lens.cpu().numpy(), lens)
+        assert np.array_equal(f.cpu().numpy(), free) and int(pages.free_count) == count and not status.any()
+
+
+def test_two_searches_at_once(V):
+    """Choices and pages of two batches on two streams, each with a workspace of its own, as they are alone."""
+    gen = torch.Generator("cuda").manual_seed(8)
+    rng = np.random.RandomState(8)
+    i32 = lambda x: torch.as_tensor(np.asarray(x, np.int32)).cuda()  # noqa: E731
+    cases = []
+    for g, b, v in ((3, 5, 90000), (64, 4, 128256)):
+        lens, table, free, n = beams_state(rng, g, b, 16, 60, 4, g * b)
+        caches = make_caches(V, 2, n, 2, 16, 32, "head", gen)
+        x = (3 * torch.randn((g * b, v), generator=gen, device="cuda")).bfloat16()
+        cases.append(dict(x=x, scores=torch.randn((g, b), generator=gen, device="cuda"), work=V.beam_workspace(g, b, v), pages=V.BeamPages(caches, g, b),
+                          lens=i32(lens), table=i32(table), free=i32(free), count=i32([g * b]), caches=caches, g=g, b=b, start=[c.k.clone() for c in caches]))
+    done = []
+    for together in (False, True):
+        out = [[] for _ in cases]
+        streams = [torch.cuda.Stream() for _ in cases]
+        for c in cases:
+            for k, s in zip(c["caches"], c["start"]):
+                k.k.copy_(s)
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for i, (c, s) in enumerate(zip(cases, streams)):
+                with torch.cuda.stream(s):
+                    res = select(V, c["x"], c["scores"], c["b"], work=c["work"])
+                    t, f = c["table"].clone(), c["free"].clone()
+                    c["pages"].reorder(res[1], c["lens"], t, f, c["count"])
+                    out[i].append([*res, t, f, c["pages"].seq_lens.clone()] + [k.k.clone() for k in c["caches"]])
+                if not together:
+                    s.synchronize()
+        torch.cuda.synchronize()
+        done.append(out)
+    for one, two in zip(*done):
+        for p, q in zip(one, two):
+            assert all(torch.equal(y, z) for y, z in zip(p, q))
+
+
 def test_reorder_steps_with_the_plan(V):
     """Forks, steps of the plan and choices in turn: pages are neither lost nor held twice, shared ones are full, and
     every row reads back the tokens of its own history."""

@@ -179,8 +179,8 @@ def test_append_rotary_refuses_what_append_does(Q, a, status):
 
 
 def _select(Q, **kw):
-    a = dict(logits=FAKE, stride=100, dtype=0, beams=4, groups=2, vocab=100, scale=1.0, end=3, scores=FAKE, done=FAKE, weights=None, n_out=4,
-             score=FAKE, beam=FAKE, token=FAKE, work=FAKE, bytes=1 << 40)
+    a = dict(logits=FAKE, stride=100, dtype=0, beams=4, groups=8, vocab=100, scale=1.0, end=3, scores=FAKE, done=FAKE, weights=None, n_out=4,
+             score=3 * FAKE, beam=4 * FAKE, token=5 * FAKE, work=FAKE, bytes=1 << 40)
     a.update(kw)
     return Q.BeamSelectArgs(*a.values())
 
@@ -189,6 +189,7 @@ def _select(Q, **kw):
     dict(logits=None), dict(logits=FAKE + 2), dict(stride=99), dict(dtype=3), dict(beams=0), dict(beams=33), dict(groups=-1),
     dict(groups=2049), dict(groups=1 << 40), dict(vocab=0), dict(vocab=(1 << 27) + 1, stride=1 << 28), dict(scale=0.0), dict(scale=-1.0),
     dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2.0 ** -65), dict(scale=2.0 ** 65), dict(end=-1), dict(end=100),
+    dict(scores=3 * FAKE + 4 * 31), dict(weights=3 * FAKE - 4 * 7), dict(done=4 * FAKE + 127), dict(scores=5 * FAKE),
     dict(scores=None), dict(n_out=0), dict(n_out=33), dict(score=None), dict(beam=None), dict(token=None), dict(work=None),
     dict(work=FAKE + 8), dict(bytes=1000)])
 def test_select_refuses(Q, kw):
@@ -216,7 +217,8 @@ def _reorder(Q, **kw):
     dict(groups=0), dict(beams=0), dict(beams=33), dict(groups=2049), dict(parents=None), dict(lens=None), dict(table=None), dict(out=None),
     dict(width=0), dict(width=9), dict(width=(1 << 20) + 1, stride=1 << 21, ostride=1 << 21), dict(out=FAKE + 256, ostride=7),
     dict(ostride=9), dict(cap=3), dict(cap=(1 << 31) - 1), dict(free=None), dict(count=None), dict(lens_out=None), dict(status=None),
-    dict(left=None), dict(lens_out=FAKE + 64), dict(status=FAKE), dict(left=FAKE + 768), dict(work=None), dict(work=FAKE + 8), dict(bytes=100)])
+    dict(left=None), dict(lens_out=FAKE), dict(lens_out=FAKE + 768), dict(status=FAKE), dict(status=FAKE + 64), dict(status=FAKE + 768),
+    dict(left=FAKE + 64), dict(left=FAKE), dict(work=None), dict(work=FAKE + 8), dict(bytes=100)])
 def test_reorder_refuses(Q, kw):
     caches = (Q.KvCacheDesc * 2)(_desc(Q), _desc(Q, kind=1))
     assert Q.lib().seedq_beam_reorder(caches, 2, C.byref(_reorder(Q, **kw)), None) == 1
@@ -269,7 +271,8 @@ def test_binding_refuses_rotary(Q, V, monkeypatch):
             r.angles(pos, out, stream=0)
     x = z(3, 4, 64)
     for a, c, o in ((x[0], cs, x), (x, cs[:2], x), (x, cs, z(3, 4, 63)), (x, cs, x.double()), (z(3, 64, 4).transpose(1, 2), cs, x),
-                    (x, cs, z(3, 1, 64).expand(3, 4, 64)), (x, cs, _meta(3, 4, 64)), (x, cs, z(64 * 12).as_strided((3, 4, 64), (32, 192, 1)))):
+                    (x, cs, z(3, 1, 64).expand(3, 4, 64)), (x, cs, z(999).as_strided((3, 4, 64), (64, 64, 1))),
+                    (x, cs, z(999).as_strided((3, 4, 64), (128, 64, 1))), (x, cs, z(999).as_strided((3, 4, 64), (64, 128, 1))), (x, cs, _meta(3, 4, 64)), (x, cs, z(64 * 12).as_strided((3, 4, 64), (32, 192, 1)))):
         with pytest.raises(ValueError):
             r.rotate(a, c, o, stream=0)
     cache = _cache(V, "cpu")
