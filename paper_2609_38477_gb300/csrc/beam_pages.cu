@@ -145,6 +145,10 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
   const cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  auto meet = [&]() {  // all CTAs of the cluster
+    if (ranks == 1) __syncthreads();
+    else cluster.sync();
+  };
   if (!COPY) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int count = min(max(*a.free_count, 0), a.capacity);
 
@@ -261,7 +265,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
     for (int k = 0; k < kWarps; ++k) x += s_back[k];
     s_cta_back = x;
   }
-  cluster.sync();
+  meet();
   const int of_rank = lane < ranks ? *cluster.map_shared_rank(&s_cta_back, lane) : 0;
   const int all = __reduce_add_sync(~0u, of_rank);
   const int before = __reduce_add_sync(~0u, (lane < rank ? of_rank : 0) + (lane < w ? s_back[lane] : 0));
@@ -291,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
       else a.table_out[(int64_t)i * a.out_stride + col] = id;
     }
   }
-  cluster.sync();  // the stack is whole, and no CTA's counts are read any more
+  meet();  // the stack is whole, and no CTA's counts are read any more
 
   for (int i = rank * kThreads + threadIdx.x; i < n; i += ranks * kThreads) {
     const int len = r.len[i], nth = r.nth[i];
@@ -310,7 +314,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_pages(const __grid_constant__
     *a.count_out = total - min(copies, total);
   }
   if constexpr (COPY) {
-    cluster.sync();  // the list is whole
+    meet();  // the list is whole
     copy_pages(y, min(copies, total), me, workers);
   }
 }
@@ -387,7 +391,7 @@ seedq_status seedq_beam_reorder(const seedq_kv_cache *caches, int32_t n_caches, 
   y.page_stride = c.page_stride, y.head_stride = c.head_stride, y.token_stride = c.token_stride;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ranks), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = pages_smem(p.n_groups, p.n_beams);
-  cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = ranks > 1;
   auto layers = [&](int first) {
     y.layers = std::min(n_caches - first, kLayersAtOnce);
     for (int i = 0; i < y.layers; ++i) {
