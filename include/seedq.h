@@ -310,9 +310,9 @@ seedq_status seedq_fp64_fma_probe(int64_t iters, int32_t blocks_per_sm, double *
  * covers the weights only.
  *
  * All calls are hot calls: they validate on the host, enqueue one launch
- * (seedq_beam_reorder two or more), allocate nothing and do not synchronize;
- * every length, slot and page number stays on the device, so a step can be
- * captured in a CUDA graph.
+ * (seedq_kv_append_rotary one or two, seedq_beam_reorder one or more), allocate
+ * nothing and do not synchronize; every length, slot and page number stays on the
+ * device, so a step can be captured in a CUDA graph.
  * Kernels check what they read from device memory (pages, slots, offsets)
  * against the sizes given here and skip what is out of range. */
 

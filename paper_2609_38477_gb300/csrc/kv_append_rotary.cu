@@ -4,8 +4,8 @@
 // keys within the codes' range, so every key is rotated before the first code is
 // written.  Between the two a lane keeps the rotated numbers in registers, two tokens
 // of 16 numbers each: two pieces of 8 that hold whole pairs, with SEEDQ_ROPE_HALF
-// piece i of the first half of the rotated dims and piece i of the second, else
-// neighbours.
+// piece i of the first half of the rotated dims and piece i of the second, else of the
+// head's halves.
 //
 // A CTA owns `share` heads of the keys or of the values, for the stretches of tokens on
 // one page that begin among 2^group_shift tokens.  Its 8 warps form teams, the
@@ -60,7 +60,7 @@ struct AppendArgs {
   bool wide_cs;         // pairs of cos and sin two at a time
   int32_t group_shift, page_shift;
   int32_t share;           // heads of a CTA
-  unsigned ctas, ctas_of_group;  // of the append, and of a group of tokens
+  unsigned ctas, ctas_of_group;  // of the append, and of a group of tokens and a tensor
   RotateArgs q;
   RotateSplit split;
 };
@@ -100,35 +100,40 @@ struct Unit {
 // pieces of any lanes.
 enum { kAcross = 0, kBeside = 1, kOdd = 2 };
 
-// What a lane does to every token: its pieces begin at dims d0 and d1, and hold
-// the pairs from p0 on, n of 8.
+// What a lane does to every token: its pieces begin at dims d0 and d1 (lanes of a token
+// read each of them side by side), and hold n0 pairs from p0 on and n1 from p1 on, up
+// to 4 each.
 struct Lane {
-  int d0, d1, p0, n;
+  int d0, d1, p0, p1, n0, n1;
 };
 
 template <int PAIRS>
 __device__ __forceinline__ Lane lane_of(const AppendArgs &a, int u) {
-  if (PAIRS == kBeside) return {16 * u, 16 * u + 8, 8 * u, min(max(a.half - 8 * u, 0), 8)};
-  if (PAIRS == kOdd) return {16 * u, 16 * u + 8, 0, 0};
+  const int D = a.c.head_dim;
+  if (PAIRS == kOdd) return {8 * u, D / 2 + 8 * u, 0, 0, 0, 0};
+  if (PAIRS == kBeside) {
+    const int p0 = 4 * u, p1 = D / 4 + 4 * u;
+    return {8 * u, D / 2 + 8 * u, p0, p1, min(max(a.half - p0, 0), 4), min(max(a.half - p1, 0), 4)};
+  }
   const int turns = a.half / 8;
-  if (u < turns) return {8 * u, a.half + 8 * u, 8 * u, 8};
-  const int d = 2 * a.half + 16 * (u - turns);
-  return {d, d + 8, 0, 0};
+  if (u < turns) return {8 * u, a.half + 8 * u, 8 * u, 8 * u + 4, 4, 4};
+  const int d = 2 * a.half + 8 * (u - turns);
+  return {d, d + (D - 2 * a.half) / 2, 0, 0, 0, 0};
 }
 
 // cos and sin of the lane's pairs of token t; 1 and 0 where it has none, which leaves
 // numbers as they are (one that is not finite makes its page's scale a NaN anyway).
 __device__ __forceinline__ void load_angles(const AppendArgs &a, const Lane &l, int64_t t, float2 (&c)[8]) {
-  const float2 *cs = a.cs + t * a.half + l.p0;
-  if (a.wide_cs && l.n == 8) {
+  const float2 *cs = a.cs + t * a.half;
+  if (a.wide_cs && l.n0 == 4 && l.n1 == 4) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float4 v = __ldg((const float4 *)cs + k);
+      const float4 v = __ldg((const float4 *)(cs + (k < 2 ? l.p0 : l.p1)) + k % 2);
       c[2 * k] = make_float2(v.x, v.y), c[2 * k + 1] = make_float2(v.z, v.w);
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) c[k] = k < l.n ? __ldg(cs + k) : make_float2(1.f, 0.f);
+    for (int k = 0; k < 8; ++k) c[k] = k % 4 < (k < 4 ? l.n0 : l.n1) ? __ldg(cs + (k < 4 ? l.p0 : l.p1) + k % 4) : make_float2(1.f, 0.f);
   }
 }
 
@@ -139,7 +144,7 @@ __device__ __forceinline__ void turn(const AppendArgs &a, const Lane &l, const f
     const float2 *cs = a.cs + t * a.half;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      const int i = l.d0 + k;
+      const int i = k < 8 ? l.d0 + k : l.d1 + k - 8;
       if (i < 2 * a.half) {
         const bool second = i >= a.half;
         const float o = load_elem(x, DT, i + (second ? -a.half : a.half));
@@ -147,7 +152,7 @@ __device__ __forceinline__ void turn(const AppendArgs &a, const Lane &l, const f
         y[k] = second ? z.y : z.x;
       }
     }
-  } else if (l.n > 0) {
+  } else if (l.n0 > 0) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int i = PAIRS == kBeside ? 2 * k : k, j = PAIRS == kBeside ? 2 * k + 1 : 8 + k;
@@ -476,9 +481,11 @@ __device__ __forceinline__ void rotate_query(const AppendArgs &a, int64_t i) {
 template <int KIND, int DT, int PAIRS>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_kv_append_rotary(const __grid_constant__ AppendArgs a) {
   if (blockIdx.x < a.ctas) {
-    const unsigned of_group = a.ctas_of_group, i = blockIdx.x % of_group, tensor = i >= of_group / 2;
-    const int64_t group = blockIdx.x / of_group;
-    const int h0 = (int)(tensor ? i - of_group / 2 : i) * a.share;
+    // the keys first: they take longer
+    const bool tensor = blockIdx.x >= a.ctas / 2;
+    const unsigned i = tensor ? blockIdx.x - a.ctas / 2 : blockIdx.x;
+    const int64_t group = i / a.ctas_of_group;
+    const int h0 = (int)(i - (unsigned)group * a.ctas_of_group) * a.share;
     if (tensor) append<KIND, DT, PAIRS, 1>(a, group, h0);
     else append<KIND, DT, PAIRS, 0>(a, group, h0);
   } else {
@@ -541,8 +548,8 @@ extern "C" seedq_status seedq_kv_append_rotary(const seedq_kv_cache *cache, cons
   a.group_shift = work <= kFewPairs ? 3 : append_group_shift(n_tokens, cache->n_kv_heads);
   a.page_shift = log2_of(cache->page_size);
   const int64_t groups = (n_tokens + (1 << a.group_shift) - 1) >> a.group_shift;
-  a.ctas_of_group = 2 * (unsigned)((cache->n_kv_heads + a.share - 1) / a.share);
-  const int64_t ctas = groups * a.ctas_of_group;
+  a.ctas_of_group = (unsigned)((cache->n_kv_heads + a.share - 1) / a.share);
+  const int64_t ctas = 2 * groups * a.ctas_of_group;
   if (ctas > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
   int64_t more = 0;
   if (queries) {

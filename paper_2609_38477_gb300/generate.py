@@ -128,11 +128,13 @@ class Decoder:
         and the sums of their log probabilities.  A hypothesis that has chosen
         end_token keeps its sum and repeats it.  Sums are compared after division
         by the number of chosen tokens to the length_power.  Where the pages do not
-        last, a prompt's sums are NaN and its tokens -1 from there on."""
+        last, a prompt's sums are NaN and its tokens -1."""
         g, b, vocab = len(prompts), n_beams, self.spec.vocab
         rows = g * b
         if not 1 <= rows <= min(MAX_COLUMNS, self.plan.max_requests) or not all(prompts) or max_new < 1:
             raise ValueError("1..16 beams in all and no more than max_requests, prompts of a token or more and max_new >= 1 are wanted")
+        if not all(0 <= t < vocab for prompt in prompts for t in prompt) or end_token >= vocab:
+            raise ValueError(f"prompts, end_token: tokens below {vocab} are wanted")
         if bool(self.seq_lens.any()):
             raise ValueError("a request is under way")
         i32 = dict(dtype=torch.int32, device="cuda")

@@ -623,5 +623,9 @@ def test_beam_search_without_pages(G):
     assert int(d.free_count) == 3 and sorted(d.free[:3].tolist()) == [0, 1, 2]
     with pytest.raises(ValueError, match="max_requests"):
         d.beam_search([[1]], 5, 2)
-    with pytest.raises(ValueError):
-        d.beam_search([[]], 2, 2)
+    for bad in (([[]], 2, 2), ([[1]], 0, 2), ([[1]], 2, 0), ([], 2, 2), ([[1], [300]], 2, 2), ([[-1]], 2, 2), ([[1]], 2, 2, 300)):
+        with pytest.raises(ValueError):
+            d.beam_search(*bad)
+    d.step(torch.tensor([5], device="cuda"), torch.tensor([1], dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError, match="under way"):
+        d.beam_search([[1]], 2, 2)
