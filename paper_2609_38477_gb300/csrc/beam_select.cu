@@ -3,9 +3,9 @@
 // Mathematics.  With m the largest of a live beam's logits x, candidate (b, v) has
 // the total score_b - ln sum exp(scale (x - m)) + scale (x_v - m), and a request's
 // first n candidates by weight_b * total are wanted.  Within a beam the order is that of
-// the logits themselves; between beams it is that of doubles made from the logit,
-// the score and the log sum, so candidates that lie close together are not swapped by
-// a float32 sum.
+// the logits themselves; between beams it is that of pairs of floats made from the
+// logit, the score and the log sum, so candidates that lie close together are not
+// swapped by a float32 sum.
 //
 // One pass over the logits keeps, per chunk of a row, the sum and the largest, and the
 // largest per segment of 256 logits.  The first n candidates lie in the n segments
@@ -15,9 +15,9 @@
 // again, and chooses from their logits.  Each choice is by a float32 bound that at
 // least n reach, then by counting, for each of the few that do, how many precede it.
 //
-// Measured, n = twice the beams: a request of 4 beams of 32000 logits 8.9 us, 4
-// requests of 4 beams of 128256 10.6 (the pass over the logits 3.9: launch, one trip
-// to memory, an arrival), 64 of 8 beams of 128256 bfloat16 38 us (the pass 24, 4.4
+// Measured, n = twice the beams: a request of 4 beams of 32000 logits 8.5 us, 4
+// requests of 4 beams of 128256 10.4 (the pass over the logits 3.9: launch, one trip
+// to memory, an arrival), 64 of 8 beams of 128256 bfloat16 37 us (the pass 24, 4.4
 // TB/s).  The join is a chain of about fifteen trips to L2 or shared memory and
 // barriers of one CTA, 5 to 7 us (sorted lists of 32 took 9 to 19), and many requests'
 // joins fall at the end.  Segments of 256: what is read again is 1 KB a candidate, and
@@ -119,13 +119,41 @@ struct Segment {
 
 // ---------------------------------------------------------------- candidates
 //
-// A candidate as two words that sort as candidates do: the weighted total as an
-// ordered double; then beam, logit and token, each such that what comes first is
-// larger.  No candidate is (0, 0).
+// A candidate as two words that sort as candidates do: the weighted total as ordered
+// numbers; then beam, logit and token, each such that what comes first is larger.  No
+// candidate is (0, 0).
+//
+// Totals are pairs of floats, the nearest and the rest (46 bits; by the error-free
+// sums and products of Knuth and Dekker): float64 instructions, few as they are, made
+// the join 0.3 to 1 us longer.  Where a pair would overflow or underflow, the choice is
+// made again in float64.
 struct alignas(16) Item {
   uint64_t key, rest;
   __device__ __forceinline__ bool before(const Item &o) const { return (key > o.key) | ((key == o.key) & (rest > o.rest)); }
 };
+struct Pair {
+  float hi, lo;
+};
+__device__ __forceinline__ Pair quick_sum(float a, float b) {  // |a| >= |b|
+  const float s = __fadd_rn(a, b);
+  return {s, __fsub_rn(b, __fsub_rn(s, a))};
+}
+__device__ __forceinline__ Pair exact_sum(float a, float b) {
+  const float s = __fadd_rn(a, b), c = __fsub_rn(s, a);
+  return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, c)), __fsub_rn(b, c))};
+}
+__device__ __forceinline__ Pair exact_product(float a, float b) {
+  const float p = __fmul_rn(a, b);
+  return {p, __fmaf_rn(a, b, -p)};
+}
+__device__ __forceinline__ Pair sum(Pair a, Pair b) {
+  const Pair s = exact_sum(a.hi, b.hi);
+  return quick_sum(s.hi, __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo)));
+}
+__device__ __forceinline__ Pair product(float a, Pair b) {
+  const Pair p = exact_product(a, b.hi);
+  return quick_sum(p.hi, __fmaf_rn(a, b.lo, p.lo));
+}
 __device__ __forceinline__ uint64_t order_double(double x) {
   const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
   return b >> 63 ? ~b : b | (1ull << 63);
@@ -144,7 +172,8 @@ constexpr int kLanesOfRow = 8;
 
 struct Join {
   // total = base + scale * (logit - most): the difference first, or a large common part would take the sum's digits
-  double base[kMaxBeams], weight[kMaxBeams], most[kMaxBeams];
+  Pair base[kMaxBeams];
+  float weight[kMaxBeams], most[kMaxBeams];
   float4 line[kMaxBeams];  // the same weighted, in float32: x * (logit - y) + z, and w = 2^-21 |z|; for a finished beam z alone
   int kind[kMaxBeams];
   alignas(16) float group[64];
@@ -158,10 +187,21 @@ struct Join {
 };
 
 __device__ __forceinline__ double total_of(const SelectArgs &a, const Join &s, int b, float x) {
-  return s.kind[b] == kDone ? s.base[b] : s.base[b] + (double)a.scale * ((double)x - s.most[b]);
+  const double base = (double)s.base[b].hi + (double)s.base[b].lo;
+  return s.kind[b] == kDone ? base : base + (double)a.scale * ((double)x - (double)s.most[b]);
 }
 __device__ __forceinline__ Item item_of(const SelectArgs &a, const Join &s, int b, float x, int index) {
-  return {order_double(s.weight[b] * total_of(a, s, b, x)), rest_word(b, order_word(x), index)};
+  return {order_double((double)s.weight[b] * total_of(a, s, b, x)), rest_word(b, order_word(x), index)};
+}
+__device__ __forceinline__ Pair quick_total(const SelectArgs &a, const Join &s, int b, float x) {
+  const Pair base = s.base[b];
+  return s.kind[b] == kDone ? base : sum(base, product(a.scale, exact_sum(x, -s.most[b])));
+}
+// fine: false where a pair has no room, by its size or its smallness.
+__device__ __forceinline__ Item quick_item(const SelectArgs &a, const Join &s, int b, float x, int index, bool &fine) {
+  const Pair total = quick_total(a, s, b, x), y = product(s.weight[b], total);
+  fine = fabsf(y.hi) < CUDART_INF_F && fabsf(y.lo) < CUDART_INF_F && (fabsf(y.hi) > 0x1p-70f || total.hi == 0.f);
+  return {(uint64_t)order_word(y.hi) << 32 | order_word(y.lo), rest_word(b, order_word(x), index)};
 }
 // Bounds of the weighted total in float32: of its parts' few roundings, here 2^-21 of
 // them.  What is far down is cut off, for all beams alike (their offsets are at most
@@ -200,7 +240,7 @@ __device__ __forceinline__ float nth_bound(Join &s, float mine, int n) {
   return key_value((uint64_t)least << 32);
 }
 // The first n of the found candidates, in order, to chosen.  False if more were
-// found than fit.
+// found than fit, or pairs do not hold some.
 __device__ __forceinline__ bool rank_found(const SelectArgs &a, Join &s, int n) {
   __syncthreads();
   const int m = s.n_found;
@@ -208,10 +248,13 @@ __device__ __forceinline__ bool rank_found(const SelectArgs &a, Join &s, int n) 
   Item mine{0, 0};
   if (threadIdx.x < m) {
     const uint32_t at = s.found_at[threadIdx.x];
-    mine = item_of(a, s, at >> kTokenBits, s.found_x[threadIdx.x], at & kTokenMask);
+    bool fine;
+    mine = quick_item(a, s, at >> kTokenBits, s.found_x[threadIdx.x], at & kTokenMask, fine);
     s.found[threadIdx.x] = mine;
+    if (!fine) s.slow = 1;
   }
   __syncthreads();
+  if (s.slow) return false;
   // several threads count for one candidate
   const int share = m <= 32 ? 8 : m <= 64 ? 4 : m <= 128 ? 2 : 1, i = threadIdx.x / share;
   mine = s.found[min(i, kMaxFound - 1)];
@@ -271,6 +314,8 @@ template <int DT, bool VEC>
 __device__ __noinline__ void join_slowly(const SelectArgs a, Join &s, int64_t g) {  // by value: the kernel's own stay in constant memory
   using Seg = Segment<DT, VEC>;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  __syncthreads();
+  if (threadIdx.x == 0) s.slow = 1;  // for who writes the results
   choose_slowly(a, s, [&](auto &&f) {
     for (int b = 0; b < a.beams; ++b) {
       if (s.kind[b] == kDone && threadIdx.x == 0) f(b, 0.f, a.end_token);
@@ -482,7 +527,7 @@ __device__ __forceinline__ void join_group(const SelectArgs &a, Join &s, int64_t
 #pragma unroll
   for (int o = kLanesOfRow / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
   if (there && part == 0) {
-    double base = (double)score;
+    Pair base{score, 0.f};
     float high = 0.f;
     bool bad = isnan(score) || (kind != kNone && !(score < CUDART_INF_F && weight > 0.f && weight < CUDART_INF_F));
     if (kind == kLive) {
@@ -494,15 +539,19 @@ __device__ __forceinline__ void join_group(const SelectArgs &a, Join &s, int64_t
         // ln sum = e ln 2 + ln f, f within 0.7 and 1.42: float32 errors of the small logarithm alone
         const int e = (int)(__float_as_uint(sum * 1.41421356f) >> 23) - 127;
         const float f = sum * __uint_as_float((uint32_t)(127 - e) << 23);
-        base -= (double)e * 0.69314718055994531 + (double)logf(f);
+        constexpr float kLn2 = 0.693147182f, kLn2Rest = -1.9046543e-9f;  // together ln 2 to 2^-50
+        const Pair log_sum = seedq::sum(product((float)e, Pair{kLn2, kLn2Rest}), Pair{logf(f), 0.f});
+        base = seedq::sum(base, Pair{-log_sum.hi, -log_sum.lo});
         high = to;
       }
     }
-    const double offset = (double)weight * base;
-    s.base[b] = base, s.weight[b] = (double)weight, s.most[b] = (double)high, s.kind[b] = kind;
+    const float offset = weight * base.hi;
+    s.base[b] = base, s.weight[b] = weight, s.most[b] = high, s.kind[b] = kind;
     s.line[b] = kind == kNone ? make_float4(0.f, 0.f, -CUDART_INF_F, 0.f)
-                              : make_float4(kind == kLive ? weight * a.scale : 0.f, high, (float)offset, 0x1p-21f * fabsf((float)offset));
-    if (kind != kNone && !(fabs(offset) <= 1e29)) s.slow = 1;
+                              : make_float4(kind == kLive ? weight * a.scale : 0.f, high, offset, 0x1p-21f * fabsf(offset));
+    // the bounds' margins need room at both ends
+    const float smallest = fminf(weight, kind == kLive ? weight * a.scale : weight);
+    if (kind != kNone && !(fabsf(offset) <= 1e29f && smallest >= 0x1p-80f)) s.slow = 1;
     if (bad) s.spoiled = 1;
   }
   __syncthreads();
@@ -516,7 +565,8 @@ __device__ __forceinline__ void join_group(const SelectArgs &a, Join &s, int64_t
     const bool has = !spoiled && tid < s.n_chosen;
     const Item x = has ? s.chosen[tid] : Item{0, 0};
     const int from = rest_beam(x.rest);
-    a.out_score[o] = spoiled ? CUDART_NAN_F : has ? (float)total_of(a, s, from, rest_logit(x.rest)) : -CUDART_INF_F;
+    const float total = !has ? -CUDART_INF_F : s.slow ? (float)total_of(a, s, from, rest_logit(x.rest)) : quick_total(a, s, from, rest_logit(x.rest)).hi;
+    a.out_score[o] = spoiled ? CUDART_NAN_F : total;
     a.out_beam[o] = has ? from : -1;
     a.out_token[o] = has ? rest_index(x.rest) : -1;
   }

@@ -208,6 +208,22 @@ def test_select_values_at_the_ends(V):
         assert abs(float(got[0][0, 2]) + np.log(600)) < 1e-5
 
 
+@pytest.mark.parametrize("vocab", [300, 40000])
+def test_select_weights_of_any_size(V, vocab):
+    """Weights of powers of two leave the choice as it is, from denormals to the largest."""
+    rng = np.random.RandomState(vocab)
+    x = torch.from_numpy(rng.randn(9, vocab).astype(np.float32)).cuda()
+    scores = torch.from_numpy(-rng.rand(3, 3).astype(np.float32)).cuda()
+    weights = torch.tensor([[1.0, 0.5, 1.0], [2.0, 1.0, 1.0], [1.0, 1.0, 1.0]], device="cuda")
+    done = torch.tensor([[0, 0, 0], [0, 1, 0], [0, 0, 1]], dtype=torch.uint8, device="cuda")
+    want = select(V, x, scores, 12, 1.5, done, 7, weights)
+    for power in (-140, -100, -78, -60, 60, 100, 125):
+        got = select(V, x, scores, 12, 1.5, done, 7,
+                     torch.from_numpy(np.ldexp(weights.cpu().numpy(), power)).cuda())
+        assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+        assert torch.all((got[0] - want[0]).abs() <= want[0].abs() * 2.0 ** -23)  # pairs or float64: roundings of neighbours
+
+
 def test_select_spoiled_requests(V):
     """NaN or infinity in a live beam, its score or its weight: that request alone."""
     nan, inf = float("nan"), float("inf")
