@@ -13,8 +13,8 @@
 // The copies are units of one head and tensor of one layer and page, dealt to all
 // warps: of a second launch, or, where they are small, of the first.
 //
-// Measured: 4 requests of 4 beams of 600 tokens, 32 layers of 8 heads of 128, 9.4 us
-// (the lists 7: launch, six dependent trips to memory and two barriers of the
+// Measured: 4 requests of 4 beams of 600 tokens, 32 layers of 8 heads of 128, 8.5 us
+// (the lists 6: launch, six dependent trips to memory and two barriers of the
 // cluster); 32 requests of 8 beams, 8 layers, 22 us, of which the copies (67 MB) take
 // 11 to 12 (5.8 TB/s).
 #include <cooperative_groups.h>
@@ -38,7 +38,7 @@ constexpr int kMaxCluster = 8;  // one CTA takes 33 us instead of 23 for 32 requ
 constexpr int kAtOnce = 8;      // rows of a tile under way
 constexpr int kLayersAtOnce = 64;  // whose pointers go in a launch's parameters
 // What may have to be copied, up to which the first launch does it: a fork of 2 small
-// layers takes as long on the GPU (9 us) and 3 us less of the caller's time.
+// layers takes as long on the GPU (8 us) and 3 us less of the caller's time.
 constexpr int64_t kFewBytes = 1 << 20;
 
 // One copy: tokens [0, used) of page src to page dst.

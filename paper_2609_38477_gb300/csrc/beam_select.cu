@@ -17,7 +17,7 @@
 //
 // Measured, n = twice the beams: a request of 4 beams of 32000 logits 8.5 us, 4
 // requests of 4 beams of 128256 10.4 (the pass over the logits 3.9: launch, one trip
-// to memory, an arrival), 64 of 8 beams of 128256 bfloat16 37 us (the pass 24, 4.4
+// to memory, an arrival), 64 of 8 beams of 128256 bfloat16 35 us (the pass 24, 4.4
 // TB/s).  The join is a chain of about fifteen trips to L2 or shared memory and
 // barriers of one CTA, 5 to 7 us (sorted lists of 32 took 9 to 19), and many requests'
 // joins fall at the end.  Segments of 256: what is read again is 1 KB a candidate, and
@@ -44,8 +44,8 @@ static_assert(kMaxBeams == 32, "a lane per beam and per candidate");
 constexpr int kTokenBits = 27;
 constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr uint64_t kHeader = 2 * SEEDQ_MAX_REQUESTS * 4;  // arrival counters of requests and of rows
-// Logits from which on warps stream: 512 rows of 128256 bfloat16 (131 MB) take 38 us
+constexpr uint64_t kHeader = 2 * SEEDQ_MAX_REQUESTS * 4 + 16;  // arrival counters of requests and of rows, a request on offer
+// Logits from which on warps stream: 512 rows of 128256 bfloat16 (131 MB) take 35 us
 // so and 42 by a CTA per chunk, 128 of float32 (66 MB) 25 and 22.
 constexpr int64_t kStreamBytes = 96 << 20, kStreamVocab = 16384;
 
@@ -646,7 +646,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_beam_select(const __grid_consta
 // Many logits: warps stream through equal ranges of the live rows' chunks, a ring of
 // copies ahead; a row's chunks are the same for all rows, so that equal rows have
 // equal sums.  A row counts its chunks, a request its rows; the CTA of the warp that
-// brings the last joins the request once its own range is done.
+// brings the last joins the request once its own range is done.  A CTA that has two
+// to join, which would end 7 us after the others, offers one to those whose range ends
+// later, and takes back what is still there after its own.
 constexpr int kStages = 3;          // tiles in a warp's ring
 constexpr int kTileBytes = 2048;    // 64 bytes of each lane
 constexpr int kChunkTiles = 4;
@@ -659,7 +661,7 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) k_beam_stream(const __g
   extern __shared__ __align__(128) uint8_t s_ring[];
   uint16_t *live = (uint16_t *)(s_ring + kWarps * kStages * kTileBytes);  // the live rows
   __shared__ Join s_join;
-  __shared__ int s_count[kWarps], s_joins[kMaxJoins], s_n_joins;
+  __shared__ int s_count[kWarps], s_joins[kMaxJoins], s_n_joins, s_offers;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   if (tid == 0) s_n_joins = 0;
   int n_live = 0;
@@ -811,9 +813,26 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) k_beam_stream(const __g
   if (pending) arrive(live[li]);
   cp_async_wait<0>();
   __syncthreads();
-  const int joins = s_n_joins;
+  int *const offer = a.counters + 2 * SEEDQ_MAX_REQUESTS;  // a request + 1, or 0
+  if (tid == 0) {
+    __threadfence();
+    const int n = s_n_joins;
+    s_offers = n > 1 && atomicCAS(offer, 0, s_joins[n - 1] + 1) == 0;
+    if (s_offers) s_n_joins = n - 1;
+    if (n == 0 && (s_joins[0] = atomicExch(offer, 0) - 1) >= 0) s_n_joins = 1;
+  }
+  __syncthreads();
   __threadfence();
-  for (int k = 0; k < joins; ++k) join_group<DT, true>(a, s_join, s_joins[k]);
+  const int joins = s_n_joins, offers = s_offers;
+  for (int k = 0; k < joins + offers; ++k) {
+    if (k == joins) {
+      if (tid == 0) s_joins[k] = atomicExch(offer, 0) - 1;  // its own, another's or none
+      __syncthreads();
+      if (s_joins[k] < 0) break;
+      __threadfence();
+    }
+    join_group<DT, true>(a, s_join, s_joins[k]);
+  }
 }
 
 int few_chunk_logits(int32_t dtype) { return (dtype == SEEDQ_F32 ? 4 : 8) * kWarps * kSegment; }

@@ -19,12 +19,14 @@
 //
 // Measured, 128 head dims: 16 single tokens of 8 key-value and 32 query heads, float32,
 // 3.9 us (the plain append 3.0, a rotation 2.4); 4 prompts of 1024, 32 heads, bfloat16,
-// 30 us without queries (3.3 TB/s; the plain append 23), 44 with them (3.8 TB/s).  What
-// bounds the prompts is the chain of a head (numbers, largest, the warps' largest,
-// codes) and about 220 instructions per 16 numbers of a lane at 16 warps per SM, 42%
-// of the issue slots.  24 warps want 80 registers, and spill (61 us); cos and sin in
-// registers instead of shared memory, 36 us; as loads of every head, 50; the numbers
-// kept as they came and rotated twice, 45.
+// 27.5 us without queries (3.7 TB/s; the plain append 23), 43 with them (3.9 TB/s).
+// What bounds the prompts is the chain of a head (numbers, largest, the warps' largest,
+// codes) and about 200 instructions per 16 numbers of a lane at 16 warps per SM, 43%
+// of the issue slots of an active SM, and CTAs that begin apart: 3.4 to a place, 54
+// thousand cycles on average of the longest SM's 59.  4 heads to a CTA instead of 8
+// level that, and read cos and sin twice as often, 33 us; 16, 37.  24 warps want 80
+// registers, and spill (61 us); cos and sin in registers instead of shared memory, 36
+// us; as loads of every head, 50; the numbers kept as they came and rotated twice, 45.
 #include <cuda_runtime.h>
 #include <stdint.h>
 

@@ -159,6 +159,26 @@ def test_select_equal_rows_of_many(V):
             assert len(set(got[0][g].tolist())) <= 10 and bool((got[0][g] == got[0][0])[:2].all()) or g in (7, 8)
 
 
+def test_select_of_a_large_batch_repeats(V):
+    """Whoever joins a request, the results are the same bits, and the workspace is left as it was."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    g, b, v = 70, 6, 128256
+    x = torch.randn((g * b, v), device="cuda", generator=gen).bfloat16()
+    scores = -torch.rand((g, b), device="cuda", generator=gen)
+    scores[3] = scores[40:44] = -np.inf
+    work = V.beam_workspace(g, b, v)
+    first = select(V, x, scores, 12, work=work)
+    head = work[: 2 * 8192 * 4 + 16]  # the counters
+    assert int(head.max()) == 0
+    for i in (0, 3, 33, 69):  # alone, other chunks: both sums may be off, and totals of less than 16 round
+        score, beam, token = select(V, x[i * b:(i + 1) * b], scores[i:i + 1], 12)
+        assert torch.allclose(score, first[0][i:i + 1], rtol=0, atol=2 * OFF + 32 * U)
+        assert i != 3 or (bool((first[1][3] == -1).all()) and bool((first[2][3] == -1).all()))
+    for _ in range(60):
+        assert all(torch.equal(p, q) for p, q in zip(select(V, x, scores, 12, work=work), first))
+    assert int(head.max()) == 0
+
+
 def test_select_nothing_alive_in_a_large_batch(V):
     x = torch.randn((300, 32768), device="cuda")
     done = torch.zeros((100, 3), dtype=torch.bool, device="cuda")
