@@ -52,7 +52,7 @@ constexpr int64_t kStreamBytes = 96 << 20, kStreamVocab = 16384;
 struct SelectArgs {
   const void *x;
   int64_t stride;
-  int32_t vocab, beams, groups, segments, chunks, chunk_segments;  // of a row, and of a chunk
+  int32_t vocab, beams, groups, segments, chunks, chunk_shift;  // of a row; segments of a chunk, a power of two
   float scale, c;                                  // c = scale * log2(e)
   const float *scores, *weights;
   const uint8_t *done;
@@ -361,25 +361,27 @@ template <int DT, bool VEC>
 __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t g, float (&ahead)[kAhead]) {
   using Seg = Segment<DT, VEC>;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, slot = item_slot();
-  const int chunks = a.beams * a.chunks, of_chunk = a.chunk_segments;
+  const int chunks = a.beams * a.chunks, shift = a.chunk_shift;
+  const float per_chunk = 1.f / (float)a.chunks;
+  auto beam_of = [&](int k) { return (int)(((float)k + 0.5f) * per_chunk); };  // off by 2^-17 at most, and 2^-11 from the next beam
   float bound = -CUDART_INF_F;
   // chunks, by their largest logits: of those whose upper bound reaches the n-th lower one the segments are looked at
   const bool few = by_chunks(a);
   if (few) {
     for (int k = slot; k < chunks; k += kThreads) {
-      const int b = (unsigned)k / (unsigned)a.chunks;
+      const int b = beam_of(k);
       if (s.kind[b] == kLive) bound = fmaxf(bound, lower(s.line[b], s.chunk_most[k]));
     }
     bound = nth_bound(s, bound, a.n_out);
     for (int k = slot; k < chunks; k += kThreads) {
-      const int b = (unsigned)k / (unsigned)a.chunks;
+      const int b = beam_of(k);
       if (s.kind[b] == kLive && s.chunk_most[k] > -CUDART_INF_F && upper(s.line[b], s.chunk_most[k]) >= bound)
         s.chunk[atomicAdd(&s.n_chunks, 1)] = (uint32_t)b << 16 | (uint32_t)(k - b * a.chunks);
     }
     __syncthreads();
   }
   // segments, by their largest logits; a finished beam is a segment of its one candidate
-  const int total = few ? s.n_chunks * of_chunk : a.beams * a.segments;
+  const int total = few ? s.n_chunks << shift : a.beams * a.segments;
   int beam[kAhead], number[kAhead];
   const int step_b = kThreads / a.segments, step_i = kThreads - step_b * a.segments;
   auto load = [&](int first) {
@@ -390,8 +392,8 @@ __device__ __forceinline__ void join_fast(const SelectArgs &a, Join &s, int64_t 
       const int at = first + k * kThreads + slot;
       beam[k] = number[k] = 0;
       if (few) {
-        const uint32_t c = at < total ? s.chunk[at / of_chunk] : 0;
-        beam[k] = c >> 16, number[k] = (c & 0xffffu) * of_chunk + at % of_chunk;
+        const uint32_t c = at < total ? s.chunk[at >> shift] : 0;
+        beam[k] = c >> 16, number[k] = (int)(c & 0xffffu) << shift | (at & ((1 << shift) - 1));
         ahead[k] = at < total && number[k] < a.segments ? __ldcg(a.most + (g * a.beams + beam[k]) * a.segments + number[k]) : -CUDART_INF_F;
       } else if (at < total) {
         beam[k] = b, number[k] = i;
@@ -856,12 +858,12 @@ cudaError_t launch(SelectArgs &a, bool vec, cudaStream_t st) {
     });
     if (rc) return (cudaError_t)rc;
     a.chunks = (a.vocab + stream_chunk_logits(DT) - 1) / stream_chunk_logits(DT);
-    a.chunk_segments = stream_chunk_logits(DT) / kSegment;
+    a.chunk_shift = __builtin_ctz(stream_chunk_logits(DT) / kSegment);
     a.most = (float *)(a.parts + rows * a.chunks);
     k_beam_stream<DT><<<sms * kStreamCtas, kThreads, kSmem, st>>>(a);
   } else {
     a.chunks = (a.vocab + few_chunk_logits(DT) - 1) / few_chunk_logits(DT);
-    a.chunk_segments = few_chunk_logits(DT) / kSegment;
+    a.chunk_shift = __builtin_ctz(few_chunk_logits(DT) / kSegment);
     a.most = (float *)(a.parts + rows * a.chunks);
     const unsigned ctas = (unsigned)(rows * a.chunks);  // at most 2^13 * 2^14
     if (vec) k_beam_select<DT, true><<<ctas, kThreads, 0, st>>>(a);
