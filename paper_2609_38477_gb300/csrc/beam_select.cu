@@ -547,13 +547,12 @@ __device__ __forceinline__ void join_group(const SelectArgs &a, Join &s, int64_t
         high = to;
       }
     }
-    const float offset = weight * base.hi;
+    const float offset = weight * base.hi, slope = kind == kLive ? weight * a.scale : 0.f;
     s.base[b] = base, s.weight[b] = weight, s.most[b] = high, s.kind[b] = kind;
-    s.line[b] = kind == kNone ? make_float4(0.f, 0.f, -CUDART_INF_F, 0.f)
-                              : make_float4(kind == kLive ? weight * a.scale : 0.f, high, offset, 0x1p-21f * fabsf(offset));
-    // the bounds' margins need room at both ends
-    const float smallest = fminf(weight, kind == kLive ? weight * a.scale : weight);
-    if (kind != kNone && !(fabsf(offset) <= 1e29f && smallest >= 0x1p-80f)) s.slow = 1;
+    s.line[b] = kind == kNone ? make_float4(0.f, 0.f, -CUDART_INF_F, 0.f) : make_float4(slope, high, offset, 0x1p-21f * fabsf(offset));
+    // the bounds' margins need room at both ends, and an infinite slope times no difference is no number
+    const float smallest = kind == kLive ? fminf(weight, slope) : weight;
+    if (kind != kNone && !(fabsf(offset) <= 1e29f && smallest >= 0x1p-80f && slope < CUDART_INF_F)) s.slow = 1;
     if (bad) s.spoiled = 1;
   }
   __syncthreads();

@@ -665,3 +665,22 @@ def test_beam_search_without_pages(G):
     d.step(torch.tensor([5], device="cuda"), torch.tensor([1], dtype=torch.int32, device="cuda"))
     with pytest.raises(ValueError, match="under way"):
         d.beam_search([[1]], 2, 2)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("b,vocab", [(2, 40), (8, 128256)])
+def test_select_slope_past_float32(V, dtype, b, vocab):
+    """A weight times a scale above the largest float32: the beam's best token, whose total is 0 whatever they are,
+    comes first, and its others last."""
+    for weight, scale in ((2.0 ** 120, 2.0 ** 20), (3e38, 1.25), (2.0 ** 64, 2.0 ** 64)):
+        x = torch.full((b, vocab), -200.0, dtype=DT[dtype], device="cuda")
+        x[0, 7], x[1, 30] = 3.0, 4.0
+        scores = torch.full((1, b), -float("inf"), device="cuda")
+        scores[0, 0], scores[0, 1] = 0.0, -5.0
+        weights = torch.ones((1, b), device="cuda")
+        weights[0, 0] = weight
+        for n in (1, 3):
+            got = select(V, x, scores, n, scale, weights=weights)
+            down = float(np.float32(-5 - scale * 204))
+            assert got[1][0].tolist() == [0, 1, 1][:n] and got[2][0].tolist() == [7, 30, 0][:n]
+            assert got[0][0].tolist() == [0.0, -5.0, down][:n]
