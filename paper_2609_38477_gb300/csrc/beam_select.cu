@@ -550,9 +550,10 @@ __device__ __forceinline__ void join_group(const SelectArgs &a, Join &s, int64_t
     const float offset = weight * base.hi, slope = kind == kLive ? weight * a.scale : 0.f;
     s.base[b] = base, s.weight[b] = weight, s.most[b] = high, s.kind[b] = kind;
     s.line[b] = kind == kNone ? make_float4(0.f, 0.f, -CUDART_INF_F, 0.f) : make_float4(slope, high, offset, 0x1p-21f * fabsf(offset));
-    // the bounds' margins need room at both ends, and an infinite slope times no difference is no number
+    // the bounds' margins need room at both ends, an infinite slope times no difference is no number, and a logit
+    // of -float32's largest must not lie infinitely far below the beam's own largest
     const float smallest = kind == kLive ? fminf(weight, slope) : weight;
-    if (kind != kNone && !(fabsf(offset) <= 1e29f && smallest >= 0x1p-80f && slope < CUDART_INF_F)) s.slow = 1;
+    if (kind != kNone && !(fabsf(offset) <= 1e29f && smallest >= 0x1p-80f && slope < CUDART_INF_F && high <= 0x1p100f)) s.slow = 1;
     if (bad) s.spoiled = 1;
   }
   __syncthreads();

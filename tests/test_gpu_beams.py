@@ -684,3 +684,20 @@ def test_select_slope_past_float32(V, dtype, b, vocab):
             down = float(np.float32(-5 - scale * 204))
             assert got[1][0].tolist() == [0, 1, 1][:n] and got[2][0].tolist() == [7, 30, 0][:n]
             assert got[0][0].tolist() == [0.0, -5.0, down][:n]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,vocab", [(2, 4000), (8, 128256)])
+def test_select_logits_further_apart_than_float32(V, dtype, b, vocab):
+    """A beam's logits at both ends of the type, under a small weight: -6e35 of it comes before another's -1e36."""
+    x = torch.full((b, vocab), -float("inf"), dtype=DT[dtype], device="cuda")
+    x[0, 1], x[0, 300] = 3e38, -3e38
+    x[1, 1], x[1, 300:2701:300] = 0.0, -1e37 * torch.arange(1, 10, device="cuda")  # segments of their own
+    scores = torch.full((1, b), -float("inf"), device="cuda")
+    scores[0, :2] = 0.0
+    weights = torch.ones((1, b), device="cuda")
+    weights[0, 0] = 0.01
+    got = select(V, x, scores, 5, 0.1, weights=weights)
+    assert list(zip(got[1][0].tolist(), got[2][0].tolist())) == [(0, 1), (1, 1), (0, 300), (1, 300), (1, 600)]
+    want = torch.tensor([0.0, 0.0, 2 * float(x[0, 300]), float(x[1, 300]), float(x[1, 600])], dtype=torch.float64) * float(np.float32(0.1))
+    assert bool(((got[0][0].double().cpu() - want).abs() <= want.abs() * U * (1 + 2.0 ** -20)).all())
