@@ -17,15 +17,14 @@
 namespace seedq {
 namespace {
 
-// cos and sin of f turns, f in units of 2^-64: the nearest eighth of a turn but
-// one comes off as a whole number, so the rest is exact in float32 to 2^-25 of
-// its size and sincospif sees at most a quarter.
+// cos and sin of f turns, f in units of 2^-64: the nearest quarter of a turn comes off as a
+// whole number, and the rest, at most an eighth, rounds to float32 once: the sine of a small
+// angle is as exact, relative to itself, as that of a large one.
 __device__ __forceinline__ float2 cos_sin_of(uint64_t f) {
-  const uint32_t h = (uint32_t)(f >> 32);
-  const uint32_t quarter = (h + 0x20000000u) >> 30;
-  const int32_t rest = (int32_t)(h - (quarter << 30));  // -2^29 .. 2^29 - 1 of 2^32 to the turn
+  const uint32_t quarter = (uint32_t)((f + (1ull << 61)) >> 62);
+  const int64_t rest = (int64_t)(f - ((uint64_t)quarter << 62));  // -2^61 .. 2^61 - 1 of 2^64 to the turn
   float s, c;
-  sincospif((float)rest * 0x1p-31f, &s, &c);
+  sincospif((float)rest * 0x1p-63f, &s, &c);
   switch (quarter & 3) {
     case 0: return make_float2(c, s);
     case 1: return make_float2(-s, c);

@@ -407,3 +407,18 @@ def test_cache_pages_of_every_order(V):
         c = V.KVCache(*t, *(torch.full((4, h), 77.0, device="cuda") for _ in range(2)), "e4m3")
         c.append_rotary(x[0], x[1], slots, rotary, cs)
         same(c, want)
+
+
+@pytest.mark.parametrize("base", [10000.0, 5e5, 1e7])
+def test_sines_of_small_angles(V, base):
+    """Angles of less than an eighth of a turn, however small: sines within a few roundings of themselves.  The
+    frequency is a whole number of 2^-64 turns (off by 2^-65 of w / 2 pi > 2^-26), the phase rounds to 24 bits (u),
+    sincospif is within 2 units in the last place (4 u of the number at most), the scale rounds once more (u)."""
+    w = V.rotary_frequencies(128, base)[0]
+    positions = [1, -1, 3, -7, 1000, -131071, 2 ** 24 + 1]
+    for scale in (1.0, 1.4):
+        got = angles_of(V, V.Rotary(w, scale=scale), positions)[..., 1].double().cpu().numpy()
+        angle = np.array(positions, np.float64)[:, None] * np.array(w)
+        want = scale * np.sin(angle)
+        small = np.abs(angle) < np.pi / 4
+        assert small.sum() > 100 and np.all(np.abs(got - want)[small] <= 6.1 * U * np.abs(want)[small])
