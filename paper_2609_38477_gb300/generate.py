@@ -141,9 +141,10 @@ class Decoder:
         pages = serving.BeamPages(self.caches, g, b)
         work = serving.beam_workspace(g, b, vocab)
 
-        def reorder(parents):
+        def reorder(parents, length=0):
+            """The chosen beams' pages; rows that go on from none get that length."""
             pages.reorder(parents, self.seq_lens, self.table, self.free, self.free_count)
-            self.seq_lens[:rows].copy_(pages.seq_lens)
+            self.seq_lens[:rows].copy_(torch.where(parents.view(-1) < 0, length, pages.seq_lens))
             self.free_count.copy_(pages.free_count)
 
         # prompts in the first row of each request, which its beams then fork
@@ -172,7 +173,9 @@ class Decoder:
             if i + 1 == max_new:
                 scores = new_scores
                 break
-            reorder(beam)
+            # A hypothesis that has ended needs no context, and a row without one has none.  Their rows are given
+            # up; a negative length makes the plan refuse their tokens, so the others' stay at their rows' places.
+            reorder(beam.masked_fill(done, -1), -1)
             # a beam whose copy found no page has no context any more: NaN, which the next choice passes on
             scores = new_scores.masked_fill(pages.status.view(g, b) != 0, float("nan"))
             logits = self.step(token.flatten().clamp(min=0).long(), torch.ones(rows, **i32))

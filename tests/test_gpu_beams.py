@@ -701,3 +701,48 @@ def test_select_logits_further_apart_than_float32(V, dtype, b, vocab):
     assert list(zip(got[1][0].tolist(), got[2][0].tolist())) == [(0, 1), (1, 1), (0, 300), (1, 300), (1, 600)]
     want = torch.tensor([0.0, 0.0, 2 * float(x[0, 300]), float(x[1, 300]), float(x[1, 600])], dtype=torch.float64) * float(np.float32(0.1))
     assert bool(((got[0][0].double().cpu() - want).abs() <= want.abs() * U * (1 + 2.0 ** -20)).all())
+
+
+def test_beam_search_steps_live_beams_alone(G, monkeypatch):
+    """Ended hypotheses take part in no step and hold no page: as many tokens a step as there are hypotheses
+    that go on, and as many pages as their rows list."""
+    d = G.synthetic_decoder("tiny", max_requests=8, n_pages=60)
+    prompts, b, steps = [[5, 17, 42, 7, 99, 3, 8, 21, 6, 5, 4, 3, 2, 1, 9, 11, 13, 30], [200]], 4, 16
+    plain, _ = d.beam_search(prompts, b, steps)
+    end = int(plain[0, 0, 6])  # a token that a good hypothesis chooses early
+    live = []
+    for n in range(1, steps):
+        last = d.beam_search(prompts, b, n, end_token=end)[0][..., -1]
+        live.append(int(((last != end) & (last >= 0)).sum()))
+    assert min(live) < 2 * b  # some end
+    taken, step = [], d.step
+
+    def counted(tokens, n_new):
+        out = step(tokens, n_new)
+        pages = {p for row, n in zip(d.table.tolist(), d.seq_lens.tolist()) for p in row[:-(-max(n, 0) // d.page_size)]}
+        taken.append((int((d.plan.slots >= 0).sum()), 60 - int(d.free_count), len(pages), int((d.seq_lens > 0).sum())))
+        return out
+
+    monkeypatch.setattr(d, "step", counted)
+    d.beam_search(prompts, b, steps, end_token=end)
+    assert [t[0] for t in taken[3:]] == live  # behind the prompts' three steps
+    assert all(held == listed for _, held, listed, _ in taken)
+    assert [t[3] for t in taken[3:]] == live
+    assert int(d.free_count) == 60 and not bool(d.seq_lens.any())
+
+
+@pytest.mark.parametrize("first,n_pages", [(30, 5)])
+def test_beam_search_of_a_prompt_beside_one_without_pages(G, first, n_pages):
+    """A prompt that finds no pages, for the tokens behind its own, gives back what it has, and its
+    neighbour is searched as if alone: the sums are those of the same tokens decoded one by one."""
+    d = G.synthetic_decoder("tiny", max_requests=4, n_pages=n_pages)
+    long, short, steps = [int(x) for x in np.random.RandomState(1).randint(0, 300, first)], [7, 30, 2, 41, 5, 99, 8], 14
+    found, scores = d.beam_search([long, short], 2, steps)
+    assert bool(scores[0].isnan().all()) and bool((found[0, :, -1] == -1).all())
+    assert bool(scores[1].isfinite().all()) and bool((found[1] >= 0).all())
+    assert int(d.free_count) == n_pages and not bool(d.seq_lens.any())
+    for r in range(2):
+        tokens = found[1, r].tolist()
+        rows = follow(d, short, tokens)
+        want = sum(row[t] for row, t in zip(rows, tokens))
+        assert abs(float(scores[1, r]) - want) <= 0.02 * sum(np.abs(row).max() for row in rows)
