@@ -147,14 +147,16 @@ class Decoder:
             self.seq_lens[:rows].copy_(torch.where(parents.view(-1) < 0, length, pages.seq_lens))
             self.free_count.copy_(pages.free_count)
 
-        # prompts in the first row of each request, which its beams then fork
+        # prompts in the first row of each request, which its beams then fork; one that finds no pages ends at once
         logits = torch.zeros((rows, vocab), device="cuda")
+        lost = torch.zeros(rows, dtype=torch.bool, device="cuda")
         for i, prompt in enumerate(prompts):
             for at in range(0, len(prompt), MAX_COLUMNS):
                 piece = torch.tensor(prompt[at:at + MAX_COLUMNS], device="cuda")
                 n_new = torch.zeros(rows, **i32)
                 n_new[i * b] = piece.shape[0]
-                logits[i * b] = self.step(piece, n_new)[-1]
+                logits[i * b] = self.step(piece, n_new.masked_fill_(lost, -1))[-1]
+                lost |= self.plan.status != 0
         scores = torch.full((g, b), float("-inf"), device="cuda")
         scores[:, 0] = 0.0
         done = torch.zeros((g, b), dtype=torch.bool, device="cuda")

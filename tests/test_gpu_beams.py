@@ -731,9 +731,9 @@ def test_beam_search_steps_live_beams_alone(G, monkeypatch):
     assert int(d.free_count) == 60 and not bool(d.seq_lens.any())
 
 
-@pytest.mark.parametrize("first,n_pages", [(30, 5)])
+@pytest.mark.parametrize("first,n_pages", [(70, 4), (30, 5)])
 def test_beam_search_of_a_prompt_beside_one_without_pages(G, first, n_pages):
-    """A prompt that finds no pages, for the tokens behind its own, gives back what it has, and its
+    """A prompt that finds no pages, for its own tokens or for those behind it, gives back what it has, and its
     neighbour is searched as if alone: the sums are those of the same tokens decoded one by one."""
     d = G.synthetic_decoder("tiny", max_requests=4, n_pages=n_pages)
     long, short, steps = [int(x) for x in np.random.RandomState(1).randint(0, 300, first)], [7, 30, 2, 41, 5, 99, 8], 14
