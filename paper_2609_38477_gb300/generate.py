@@ -16,6 +16,8 @@ searches the likeliest continuations of one of them.
 """
 from __future__ import annotations
 
+import math
+
 import torch
 
 from . import seedq as Q
@@ -135,6 +137,8 @@ class Decoder:
             raise ValueError("1..16 beams in all and no more than max_requests, prompts of a token or more and max_new >= 1 are wanted")
         if not all(0 <= t < vocab for prompt in prompts for t in prompt) or end_token >= vocab:
             raise ValueError(f"prompts, end_token: tokens below {vocab} are wanted")
+        if not abs(length_power) * math.log2(max_new) <= 126:
+            raise ValueError("length_power: max_new to this power passes float32")
         if bool(self.seq_lens.any()):
             raise ValueError("a request is under way")
         i32 = dict(dtype=torch.int32, device="cuda")

@@ -357,3 +357,19 @@ def test_strides_of_single_entries_do_not_matter(Q, V, monkeypatch):
     i = torch.zeros(1, dtype=torch.int32)
     pages.reorder(i.view(1, 1), i, torch.zeros(9, dtype=torch.int32).as_strided((1, 5), (2, 1)), torch.zeros(9, dtype=torch.int32), i, stream=0)
     assert calls[-1][0] == "seedq_beam_reorder" and Q.BEAM_REORDER_ARGS.unpack(calls[-1][1][2])[5] == 5
+
+
+def test_search_refuses_powers_past_float32(monkeypatch):
+    """Lengths to a power that float32 cannot hold would make a weight of 0 or infinity: refused before any work."""
+    from types import SimpleNamespace
+
+    from paper_2609_38477_gb300 import generate
+
+    d = generate.Decoder.__new__(generate.Decoder)
+    d.spec, d.plan, d.seq_lens = SimpleNamespace(vocab=50), SimpleNamespace(max_requests=4), torch.ones(4)
+    for power, steps in ((64.0, 4), (-64.0, 4), (20.0, 100), (float("nan"), 4), (float("inf"), 4), (-float("inf"), 2)):
+        with pytest.raises(ValueError, match="length_power"):
+            d.beam_search([[1]], 2, steps, length_power=power)
+    for power, steps in ((63.0, 4), (-63.0, 4), (1.0, 10 ** 6), (1e30, 1)):
+        with pytest.raises(ValueError, match="under way"):
+            d.beam_search([[1]], 2, steps, length_power=power)
