@@ -66,9 +66,9 @@ class Decoder:
         self.free = torch.arange(n_pages, dtype=torch.int32, device="cuda")
         self.free_count = torch.full((1,), n_pages, dtype=torch.int32, device="cuda")
         self.seq_lens = torch.zeros(max_requests, dtype=torch.int32, device="cuda")
-        half = spec.head_dim // 2
-        self.freqs = 10000.0 ** (-torch.arange(half, device="cuda") / half)
-        self.rotary = serving.Rotary(self.freqs.tolist())
+        freqs, scale = serving.rotary_frequencies(spec.head_dim)
+        self.freqs = torch.tensor(freqs, device="cuda")
+        self.rotary = serving.Rotary(freqs, scale=scale)
         self.score_work = serving.score_workspace(MAX_COLUMNS, spec.vocab)
 
     def _products(self, x, names, block):

@@ -216,3 +216,16 @@ def test_decode_loop_caches_values(G, name, kind):
                 x = x + bf(o).reshape(m, -1) @ w["o"].T
                 h = norm(x, block["mlp_norm"])
                 x = x + bf(torch.nn.functional.silu(h @ w["gate"].T) * (h @ w["up"].T)) @ w["down"].T
+
+
+def test_frequencies_of_the_decoder(G):
+    """The decoder's turns per position are those of 10000^(-2 i / dim) in 64 bits: to 2^-50 of each."""
+    import math
+
+    d = G.synthetic_decoder("tiny", max_requests=1, n_pages=1)
+    dim = d.spec.head_dim
+    turns = [t % 2 ** 64 for t in d.rotary.turns.tolist()]
+    for i, t in enumerate(turns):
+        want = 10000.0 ** (-2 * i / dim) / (2 * math.pi) * 2.0 ** 64
+        assert abs(t - want) <= want * 2.0 ** -50 + 1
+    assert d.freqs.shape == (dim // 2,)
