@@ -47,6 +47,13 @@ def rms_norm(x, gain):
     return (x * torch.rsqrt((x * x).mean(1, keepdim=True) + 1e-5) * gain).bfloat16()
 
 
+def rotate(x, angles):
+    """Rotary positions in plain torch: x (tokens, heads, dim), angles (tokens, dim / 2)."""
+    c, s = torch.cos(angles)[:, None], torch.sin(angles)[:, None]
+    a, b = x.chunk(2, 2)
+    return torch.cat([a * c - b * s, b * c + a * s], 2)
+
+
 class Decoder:
     """A Llama-shaped decoder over compressed layers.
 

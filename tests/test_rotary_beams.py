@@ -373,3 +373,14 @@ def test_search_refuses_powers_past_float32(monkeypatch):
     for power, steps in ((63.0, 4), (-63.0, 4), (1.0, 10 ** 6), (1e30, 1)):
         with pytest.raises(ValueError, match="under way"):
             d.beam_search([[1]], 2, steps, length_power=power)
+
+
+def test_rotate_of_the_decode_loop():
+    """generate.rotate turns numbers i and i + dim / 2 of every head by the angles, in plain torch."""
+    from paper_2609_38477_gb300 import generate
+
+    rng = np.random.RandomState(4)
+    x, angles = torch.from_numpy(rng.randn(3, 2, 10)), torch.from_numpy(rng.randn(3, 5))
+    want, _ = S.rotate(x.numpy(), np.stack([np.cos(angles.numpy()), np.sin(angles.numpy())], 2), "half")
+    got = generate.rotate(x, angles)
+    assert got.shape == x.shape and np.abs(got.numpy() - want).max() < 1e-14
