@@ -448,11 +448,12 @@ seedq_status seedq_rotary_angles(const uint64_t *turns, int32_t half, float scal
 /* Rotate every head of n_tokens tokens; computed in float32, rounded once to
  * out_dtype.  x, out: device, token t of head h at t * token_stride + h *
  * head_stride (elements), head_dim elements in a row.  out may be x itself (the
- * same type and strides); other overlaps are not allowed.  cos_sin: n_tokens x
- * rot_dim / 2 x 2, of seedq_rotary_angles.
+ * same type and strides), and may lie between the rows of x, but not on any of
+ * them.  cos_sin: n_tokens x rot_dim / 2 x 2, of seedq_rotary_angles.
  * Errors: INVALID_ARG (NULL pointer, unknown type or layout, rot_dim odd or
  * outside 2..head_dim, head_dim above SEEDQ_ROPE_MAX_DIM, n_tokens < 0, n_heads
- * outside 0..SEEDQ_ROPE_MAX_HEADS, out = x of another type or strides),
+ * outside 0..SEEDQ_ROPE_MAX_HEADS, out = x of another type or strides, rows of out
+ * on one another, on cos_sin or on x otherwise),
  * UNSUPPORTED (more than a grid takes), CUDA.  Without tokens or heads a no-op. */
 seedq_status seedq_rotate(const void *x, int32_t x_dtype, int64_t x_token_stride,
                           int64_t x_head_stride, int64_t n_tokens, int32_t n_heads,

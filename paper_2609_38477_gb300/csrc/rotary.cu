@@ -47,10 +47,12 @@ __global__ void __launch_bounds__(256) k_rotate(const __grid_constant__ RotateAr
   rotate_item<IN, OUT, N>(a, s, (int64_t)blockIdx.x * blockDim.x + threadIdx.x);
 }
 
+int64_t rotate_ctas(const RotateArgs &a, const RotateSplit &s) { return (a.n * s.pieces * s.groups + 255) / 256; }
+
 template <int IN, int OUT>
 seedq_status launch(const RotateArgs &a, cudaStream_t st) {
   const RotateSplit s = rotate_split(a, IN, OUT);
-  const int64_t ctas = (a.n * s.pieces * s.groups + 255) / 256;
+  const int64_t ctas = rotate_ctas(a, s);
   if (ctas > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
   if (s.wide == 8) k_rotate<IN, OUT, 8><<<(unsigned)ctas, 256, 0, st>>>(a, s);
   else if (s.wide == 4) k_rotate<IN, OUT, 4><<<(unsigned)ctas, 256, 0, st>>>(a, s);
@@ -96,11 +98,12 @@ seedq_status seedq_rotate(const void *x, int32_t x_dtype, int64_t x_token_stride
     return SEEDQ_ERR_INVALID_ARG;
   if (n_tokens == 0 || n_heads == 0) return SEEDQ_OK;
   if (!x || !out || !cos_sin || (uintptr_t)cos_sin % 8) return SEEDQ_ERR_INVALID_ARG;
-  // turned where it lies: a thread writes what it alone has read
   if (x == out && (x_dtype != out_dtype || x_token_stride != out_token_stride || x_head_stride != out_head_stride))
     return SEEDQ_ERR_INVALID_ARG;
   const RotateArgs a{x, out, x_token_stride, x_head_stride, out_token_stride, out_head_stride, n_tokens, n_heads, head_dim,
                      rot_dim / 2, layout, out_dtype, (const float2 *)cos_sin};
+  if (rotate_ctas(a, rotate_split(a, x_dtype, out_dtype)) > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
+  if (rotate_overlaps(a, x_dtype)) return SEEDQ_ERR_INVALID_ARG;
   return rotate_launch(a, x_dtype, (cudaStream_t)cuda_stream);
 }
 

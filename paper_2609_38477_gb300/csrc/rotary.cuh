@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "overlap.h"
 #include "serve.cuh"
 
 namespace seedq {
@@ -118,6 +119,15 @@ inline RotateSplit rotate_split(const RotateArgs &a, int32_t in, int32_t out) {
   const int each = a.n * s.pieces * a.heads >= kRotateMany && (in != SEEDQ_F32 || out != SEEDQ_F32) ? kRotateHeads : 1;
   s.groups = (a.heads + each - 1) / each;
   return s;
+}
+
+// Whether out lies on itself, on cos and sin, or on x elsewhere than where it is x: a
+// thread writes what it alone has read, or nobody.
+inline bool rotate_overlaps(const RotateArgs &a, int32_t in) {
+  const Wide ib = dtype_bytes(in), ob = dtype_bytes(a.out_dtype);
+  const ByteRows out = byte_rows(a.out, a.dim * ob, a.n, a.ot * ob, a.heads, a.oh * ob);
+  return overlaps_itself(out) || overlap(out, byte_rows(a.cs, (Wide)a.n * a.half * 8)) ||
+         (a.out != a.x && overlap(out, byte_rows(a.x, a.dim * ib, a.n, a.xt * ib, a.heads, a.xh * ib)));
 }
 
 // Enqueues the rotation (rotary.cu).

@@ -319,7 +319,7 @@ class Rotary:
                                            _stream(stream, self.device)), "seedq_rotary_angles")
 
     def rotate(self, x, cos_sin, out, stream=None):
-        """seedq_rotate: x, out (n_tokens, n_heads, head_dim); out may be x."""
+        """seedq_rotate: x, out (n_tokens, n_heads, head_dim); out may be x, or lies on no row of it."""
         xt, xs, ot, os = _turned_rows(x, out, "out")
         n, heads, dim = x.shape
         self._want_angles(cos_sin, n, x.device)

@@ -422,3 +422,23 @@ def test_sines_of_small_angles(V, base):
         want = scale * np.sin(angle)
         small = np.abs(angle) < np.pi / 4
         assert small.sum() > 100 and np.all(np.abs(got - want)[small] <= 6.1 * U * np.abs(want)[small])
+
+
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+def test_rotate_between_the_rows_of_its_input(V, layout):
+    """Out in the same buffer as x: beside it in every token, in every head, and behind it; neighbours stay."""
+    n, h, d = 33, 6, 64
+    rotary = V.Rotary(V.rotary_frequencies(d)[0], layout)
+    cs = angles_of(V, rotary, list(range(n)))
+    for place in (lambda t, i: t.view(n, 3, h, d)[:, i], lambda t, i: t.view(n, h, 3, d)[:, :, i], lambda t, i: t.view(3, n, h, d)[i],
+                  lambda t, i: t.view(h, n, 3, d)[:, :, i].transpose(0, 1)):
+        flat = torch.randn(3 * n * h * d, device="cuda")
+        before = flat.clone()
+        want = torch.empty((n, h, d), device="cuda")
+        rotary.rotate(place(before, 2).contiguous(), cs, want)
+        rotary.rotate(place(flat, 2), cs, place(flat, 1))
+        assert torch.equal(place(flat, 1), want)
+        place(flat, 1).copy_(place(before, 1))
+        assert torch.equal(flat, before)
+        with pytest.raises(V.Q.SeedQError):
+            rotary.rotate(flat[:n * h * d].view(n, h, d), cs, flat[d:d + n * h * d].view(n, h, d))
