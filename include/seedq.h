@@ -463,9 +463,12 @@ seedq_status seedq_rotate(const void *x, int32_t x_dtype, int64_t x_token_stride
 
 /* seedq_kv_append of rotated keys: k is rotated as by seedq_rotate before the
  * scales are taken (in float32: no rounding between), v is written as it is.
- * With n_heads > 0 the step's queries are rotated by the same launch: q
- * (n_tokens tokens, head_dim as the cache, the type of k) to q_out.
- * Errors: as seedq_kv_append and seedq_rotate. */
+ * With n_heads > 0 the step's queries are rotated too, by the same launch or,
+ * where they are many, by one before it: q (n_tokens tokens, head_dim as the
+ * cache, the type of k) to q_out, which may be q itself but lies on no other
+ * input.
+ * Errors: as seedq_kv_append and seedq_rotate; INVALID_ARG too for q_out over k, v
+ * or slots. */
 typedef struct {
   const float *cos_sin;
   int32_t rot_dim;

@@ -561,6 +561,12 @@ extern "C" seedq_status seedq_kv_append_rotary(const seedq_kv_cache *cache, cons
       return SEEDQ_ERR_INVALID_ARG;
     a.q = RotateArgs{args->q, args->q_out, args->q_token_stride, args->q_head_stride, args->out_token_stride, args->out_head_stride,
                      n_tokens, args->n_heads, cache->head_dim, a.half, a.layout, args->out_dtype, a.cs};
+    // keys, values and slots are read while queries are written
+    const Wide row = (Wide)cache->head_dim * size, ob = dtype_bytes(args->out_dtype);
+    const ByteRows out = byte_rows(args->q_out, cache->head_dim * ob, n_tokens, a.q.ot * ob, args->n_heads, a.q.oh * ob);
+    for (const void *x : a.x)
+      if (overlap(out, byte_rows(x, row, n_tokens, token_stride * (Wide)size, cache->n_kv_heads, head_stride * (Wide)size))) return SEEDQ_ERR_INVALID_ARG;
+    if (rotate_overlaps(a.q, dtype) || overlap(out, byte_rows(slots, (Wide)n_tokens * 8))) return SEEDQ_ERR_INVALID_ARG;
     a.split = rotate_split(a.q, dtype, args->out_dtype);
     if (n_tokens * a.split.pieces * args->n_heads >= kQueriesApart) {
       const seedq_status rc = rotate_launch(a.q, dtype, (cudaStream_t)cuda_stream);

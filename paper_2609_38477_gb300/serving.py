@@ -186,7 +186,9 @@ class KVCache:
     def append_rotary(self, k, v, slots, rotary, cos_sin, q=None, q_out=None, stream=None):
         """seedq_kv_append_rotary: k (n_tokens, n_kv_heads, head_dim) rotated as
         by rotary.rotate, then written with v at slots; q (n_tokens, n_heads,
-        head_dim) of k's type, if given, is rotated to q_out in the same launch."""
+        head_dim) of k's type, if given, is rotated to q_out, by the same launch
+        or, many of them, by one before it.  q_out may be q, and lies on no other
+        input."""
         n, dt, st = self._pair(k, v, slots)
         rotary._want_angles(cos_sin, n, self.device)
         heads, ot, qs, os, qp, op = 0, dt, (0, 0), (0, 0), 0, 0

@@ -442,3 +442,29 @@ def test_rotate_between_the_rows_of_its_input(V, layout):
         assert torch.equal(flat, before)
         with pytest.raises(V.Q.SeedQError):
             rotary.rotate(flat[:n * h * d].view(n, h, d), cs, flat[d:d + n * h * d].view(n, h, d))
+
+
+@pytest.mark.parametrize("n,h", [(6, 2), (700, 8)])
+def test_append_rotary_from_a_fused_projection(V, n, h):
+    """Queries turned in their place in rows that hold queries, keys and values; or into other rows' gaps."""
+    d, P = 128, 16
+    rotary = V.Rotary(V.rotary_frequencies(d)[0])
+    cs = angles_of(V, rotary, list(range(n)))
+    flat = torch.randn((n, 6 * h * d), device="cuda").bfloat16()
+    before = flat.clone()
+    q, k, v, gap = (flat[:, i * d:j * d].view(n, -1, d) for i, j in ((0, 3 * h), (3 * h, 4 * h), (4 * h, 5 * h), (5 * h, 6 * h)))
+    slots = torch.arange(n, device="cuda")
+    a, b = (new_cache(V, n // P + 1, h, P, d, "int8") for _ in range(2))
+    want = torch.empty_like(q)
+    both_ways(V, b, a, k, v, slots, rotary, cs, q, want)
+    for out in (gap, q):
+        x = q[:, :out.shape[1]]
+        c = new_cache(V, n // P + 1, h, P, d, "int8")
+        c.append_rotary(k, v, slots, rotary, cs, q=x, q_out=out)
+        same(c, a)
+        assert torch.equal(out, want[:, :out.shape[1]])
+    flat[:, 5 * h * d:], flat[:, :3 * h * d] = before[:, 5 * h * d:], before[:, :3 * h * d]
+    assert torch.equal(flat, before)
+    for out in (k, v):
+        with pytest.raises(V.Q.SeedQError):
+            a.append_rotary(k, v, slots, rotary, cs, q=q[:, :h], q_out=out)

@@ -120,3 +120,15 @@ def test_rotate_refuses_overlaps(Q, kw):
     a = dict(x=FAKE, dt=0, xt=256, xh=64, n=3, heads=4, dim=64, rot=32, layout=0, cs=8 * FAKE, out=2 * FAKE, odt=0, ot=256, oh=64)
     a.update(kw)
     assert Q.lib().seedq_rotate(*a.values(), None) == 1
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out=FAKE + 64 * 4), dict(out=FAKE + 2, odt=1),  # over q, moved
+    dict(out=3 * FAKE), dict(out=3 * FAKE + 4 * 128 - 4), dict(out=4 * FAKE - 512, odt=1), dict(out=4 * FAKE + 4 * 128 * 4 - 4),  # keys, values
+    dict(out=5 * FAKE - 4 * 256 * 4 + 8), dict(out=6 * FAKE + 4), dict(oh=32), dict(ot=128)])  # slots, cos and sin, itself
+def test_append_rotary_refuses_overlaps(Q, kw):
+    c = Q.KvCacheDesc(0, 2, 64, 16, 4, 10 * FAKE, 11 * FAKE, 12 * FAKE, 13 * FAKE, 2 * 16 * 64, 16 * 64, 64)
+    a = dict(cs=6 * FAKE, rot=32, layout=0, heads=4, odt=0, q=FAKE, qt=256, qh=64, out=2 * FAKE, ot=256, oh=64)
+    a.update(kw)
+    args = Q.AppendRotaryArgs(*a.values())
+    assert Q.lib().seedq_kv_append_rotary(C.byref(c), 3 * FAKE, 4 * FAKE, 0, 128, 64, 5 * FAKE, 4, C.byref(args), None) == 1
