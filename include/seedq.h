@@ -439,7 +439,8 @@ enum { SEEDQ_ROPE_HALF = 0, SEEDQ_ROPE_PAIRS = 1 };
  *   positions  device int32, n_tokens (seedq_batch_plan's).
  *   cos_sin    device, 8-byte aligned, n_tokens x half x 2 float32.
  * Errors: INVALID_ARG (NULL pointer, half outside 1..SEEDQ_ROPE_MAX_DIM/2,
- * n_tokens < 0, scale not finite), UNSUPPORTED (more than a grid takes), CUDA.
+ * n_tokens < 0, scale not finite, cos_sin over turns or positions), UNSUPPORTED
+ * (more than a grid takes), CUDA.
  * n_tokens = 0 is a no-op. */
 seedq_status seedq_rotary_angles(const uint64_t *turns, int32_t half, float scale,
                                  const int32_t *positions, int64_t n_tokens, float *cos_sin,

@@ -85,6 +85,8 @@ seedq_status seedq_rotary_angles(const uint64_t *turns, int32_t half, float scal
   if (!turns || !positions || !cos_sin || (uintptr_t)cos_sin % 8) return SEEDQ_ERR_INVALID_ARG;
   const int64_t ctas = (n_tokens * half + 255) / 256;
   if (ctas > INT32_MAX) return SEEDQ_ERR_UNSUPPORTED;
+  const ByteRows out = byte_rows(cos_sin, (Wide)n_tokens * half * 8);
+  if (overlap(out, byte_rows(positions, (Wide)n_tokens * 4)) || overlap(out, byte_rows(turns, (Wide)half * 8))) return SEEDQ_ERR_INVALID_ARG;
   k_rotary_angles<<<(unsigned)ctas, 256, 0, (cudaStream_t)cuda_stream>>>(turns, half, scale, positions, n_tokens, (float2 *)cos_sin);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? SEEDQ_OK : cuda_fail(e);

@@ -132,3 +132,10 @@ def test_append_rotary_refuses_overlaps(Q, kw):
     a.update(kw)
     args = Q.AppendRotaryArgs(*a.values())
     assert Q.lib().seedq_kv_append_rotary(C.byref(c), 3 * FAKE, 4 * FAKE, 0, 128, 64, 5 * FAKE, 4, C.byref(args), None) == 1
+
+
+@pytest.mark.parametrize("kw", [dict(cs=2 * FAKE + 8), dict(cs=2 * FAKE - 3 * 4 * 8 + 8), dict(cs=FAKE + 24), dict(cs=FAKE - 3 * 4 * 8 + 8)])
+def test_angles_refuse_overlaps(Q, kw):
+    a = dict(turns=FAKE, half=4, scale=1.0, pos=2 * FAKE, n=3, cs=3 * FAKE)
+    a.update(kw)
+    assert Q.lib().seedq_rotary_angles(*a.values(), None) == 1
