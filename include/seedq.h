@@ -594,7 +594,7 @@ seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_r
  *   scores     device, n_groups x n_beams float32.
  *   done       device, as many bytes, not 0 where the beam has ended, or NULL.
  *   weights    device, as many float32, or NULL (all 1).
- *   out_*      device, n_groups x n_out; not over scores, done or weights.
+ *   out_*      device, n_groups x n_out; not over one another or an input.
  *   workspace  device, 16-byte aligned, seedq_beam_select_workspace_bytes(n_groups,
  *              n_beams, vocab) bytes, zeroed once before its first use, good for
  *              any call that asks for no more; calls that may overlap need one each.
@@ -602,7 +602,8 @@ seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_r
  * outside 1..SEEDQ_MAX_BEAMS, n_groups x n_beams above SEEDQ_MAX_REQUESTS, vocab
  * outside 1..SEEDQ_BEAM_MAX_VOCAB, row_stride < vocab, logits not aligned to their
  * type, end_token outside the vocabulary where done is given, scale outside
- * 2^-64..2^64, outputs over inputs, workspace too small), CUDA.  n_groups = 0 is a no-op. */
+ * 2^-64..2^64, outputs over inputs or one another, workspace too small), CUDA.
+ * n_groups = 0 is a no-op. */
 #define SEEDQ_MAX_BEAMS 32
 #define SEEDQ_BEAM_MAX_VOCAB (1 << 27)
 typedef struct {

@@ -32,6 +32,7 @@
 #include "device_once.h"
 #include "f32x2.cuh"
 #include "order.cuh"
+#include "overlap.h"
 #include "serve.cuh"
 
 namespace seedq {
@@ -872,10 +873,6 @@ cudaError_t launch(SelectArgs &a, bool vec, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-bool apart(const void *a, uint64_t na, const void *b, uint64_t nb) {
-  const uint64_t x = (uint64_t)(uintptr_t)a, y = (uint64_t)(uintptr_t)b;
-  return !a || !b || x + na <= y || y + nb <= x;
-}
 bool sizes_ok(int64_t groups, int32_t beams, int64_t vocab) {
   return groups >= 0 && beams >= 1 && beams <= kMaxBeams && groups * beams <= SEEDQ_MAX_REQUESTS && groups <= SEEDQ_MAX_REQUESTS &&
          vocab >= 1 && vocab <= SEEDQ_BEAM_MAX_VOCAB;
@@ -906,10 +903,15 @@ seedq_status seedq_beam_select(const seedq_beam_select_args *args, void *cuda_st
       p.workspace_bytes < seedq_beam_select_workspace_bytes(p.n_groups, p.n_beams, p.vocab) ||
       (p.done && (p.end_token < 0 || p.end_token >= p.vocab)) || (uintptr_t)p.logits % dtype_bytes(p.dtype))
     return SEEDQ_ERR_INVALID_ARG;
-  // CTAs that begin late read the scores again.
-  const uint64_t in = (uint64_t)p.n_groups * p.n_beams, out = (uint64_t)p.n_groups * p.n_out * 4;
-  for (const void *o : {(const void *)p.out_score, (const void *)p.out_beam, (const void *)p.out_token})
-    if (!apart(o, out, p.scores, in * 4) || !apart(o, out, p.weights, in * 4) || !apart(o, out, p.done, in)) return SEEDQ_ERR_INVALID_ARG;
+  // CTAs that begin late read the scores again, and segments' logits.
+  const Wide rows_in = (Wide)p.n_groups * p.n_beams, results = (Wide)p.n_groups * p.n_out * 4;
+  const ByteRows out[] = {byte_rows(p.out_score, results), byte_rows(p.out_beam, results), byte_rows(p.out_token, results)};
+  const ByteRows x = byte_rows(p.logits, (Wide)p.vocab * dtype_bytes(p.dtype), rows_in, (Wide)p.row_stride * dtype_bytes(p.dtype));
+  if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2])) return SEEDQ_ERR_INVALID_ARG;
+  for (const ByteRows &o : out)
+    if (overlap(o, x) || overlap(o, byte_rows(p.scores, rows_in * 4)) || (p.weights && overlap(o, byte_rows(p.weights, rows_in * 4))) ||
+        (p.done && overlap(o, byte_rows(p.done, rows_in))))
+      return SEEDQ_ERR_INVALID_ARG;
   SelectArgs a{};
   a.x = p.logits, a.stride = p.row_stride, a.vocab = (int32_t)p.vocab, a.beams = p.n_beams, a.groups = (int32_t)p.n_groups;
   a.scale = p.scale, a.c = p.scale * kLog2e, a.scores = p.scores, a.weights = p.weights, a.done = p.done, a.end_token = p.end_token;

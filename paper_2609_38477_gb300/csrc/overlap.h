@@ -61,9 +61,9 @@ inline ByteRows joined_rows(ByteRows r) {
 
 // Whether two sets of rows have a byte in common.
 inline bool overlap(const ByteRows &x, const ByteRows &y) {
-  const ByteRows a = joined_rows(x), b = joined_rows(y);
   auto end = [](const ByteRows &r) { return r.at + (r.n0 - 1) * r.s0 + (r.n1 - 1) * r.s1 + r.bytes; };
-  if (end(a) <= b.at || end(b) <= a.at) return false;
+  if (end(x) <= y.at || end(y) <= x.at) return false;
+  const ByteRows a = joined_rows(x), b = joined_rows(y);
   // k in [low, high] with -a.bytes < d + k s < b.bytes
   auto meet = [&](Wide d, Wide s, Wide low, Wide high) {
     if (s == 0) return -a.bytes < d && d < b.bytes;

@@ -139,3 +139,13 @@ def test_angles_refuse_overlaps(Q, kw):
     a = dict(turns=FAKE, half=4, scale=1.0, pos=2 * FAKE, n=3, cs=3 * FAKE)
     a.update(kw)
     assert Q.lib().seedq_rotary_angles(*a.values(), None) == 1
+
+
+@pytest.mark.parametrize("kw", [
+    dict(beam=3 * FAKE), dict(token=4 * FAKE + 124), dict(score=5 * FAKE - 124), dict(beam=5 * FAKE + 4),  # one output over another
+    dict(score=7 * FAKE), dict(token=7 * FAKE - 124), dict(beam=7 * FAKE + 31 * 416 + 396), dict(score=7 * FAKE + 2 * 416 - 4)])  # over logits
+def test_select_refuses_overlaps(Q, kw):
+    a = dict(logits=7 * FAKE, stride=104, dtype=0, beams=4, groups=8, vocab=100, scale=1.0, end=3, scores=FAKE, done=FAKE, weights=None, n_out=4,
+             score=3 * FAKE, beam=4 * FAKE, token=5 * FAKE, work=FAKE, bytes=1 << 40)
+    a.update(kw)
+    assert Q.lib().seedq_beam_select(C.byref(Q.BeamSelectArgs(*a.values())), None) == 1
