@@ -661,8 +661,9 @@ seedq_status seedq_beam_select(const seedq_beam_select_args *args, void *cuda_st
  *   workspace     device, 16-byte aligned, seedq_beam_reorder_workspace_bytes
  *                 (n_groups, n_beams) bytes; calls that may overlap need one each.
  * seq_lens_out may be seq_lens and free_count_out free_count (an earlier call's
- * outputs); no other output may alias parents, seq_lens or free_count.
- * Errors: INVALID_ARG (NULL or aliased pointer, n_caches outside
+ * outputs); beyond that no output (free_pages among them) lies on another or on an
+ * input.
+ * Errors: INVALID_ARG (NULL pointer, other outputs over one another or over inputs, n_caches outside
  * 1..SEEDQ_BEAM_MAX_CACHES, caches that differ, n_beams outside
  * 1..SEEDQ_MAX_BEAMS, rows outside 1..SEEDQ_MAX_REQUESTS, table_width outside
  * 1..2^20 or above a stride, free_capacity below n_pages, workspace too small),

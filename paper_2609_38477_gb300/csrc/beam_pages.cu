@@ -25,6 +25,7 @@
 #include <type_traits>
 
 #include "device_once.h"
+#include "overlap.h"
 #include "serve.cuh"
 
 namespace cg = cooperative_groups;
@@ -364,9 +365,19 @@ seedq_status seedq_beam_reorder(const seedq_kv_cache *caches, int32_t n_caches, 
       p.free_capacity < c.n_pages || p.free_capacity == INT32_MAX)
     return SEEDQ_ERR_INVALID_ARG;
   if (p.table_out == p.block_table && p.out_stride != p.table_stride) return SEEDQ_ERR_INVALID_ARG;
-  // Lengths and count are read before any are written.
-  for (const int32_t *o : {p.seq_lens_out, p.status, p.free_count_out})
-    if (o == p.parents || (o == p.seq_lens && o != p.seq_lens_out) || (o == p.free_count && o != p.free_count_out)) return SEEDQ_ERR_INVALID_ARG;
+  // What is read and what is written lie apart, but where one is the other: lengths, count and
+  // a row's entries are read before they are written.
+  const Wide n = (Wide)p.n_groups * p.n_beams;
+  auto table = [&](const int32_t *t, int64_t stride) { return byte_rows(t, (Wide)p.table_width * 4, n, (Wide)stride * 4); };
+  const ByteRows out[] = {byte_rows(p.seq_lens_out, n * 4), byte_rows(p.free_count_out, 4), table(p.table_out, p.out_stride),
+                          byte_rows(p.status, n * 4), byte_rows(p.free_pages, (Wide)p.free_capacity * 4)};
+  const ByteRows in[] = {byte_rows(p.seq_lens, n * 4), byte_rows(p.free_count, 4), table(p.block_table, p.table_stride), byte_rows(p.parents, n * 4)};
+  for (int i = 0; i < 5; ++i) {
+    for (int k = 0; k < 4; ++k)
+      if (!(i == k && k < 3 && out[i].at == in[k].at) && overlap(out[i], in[k])) return SEEDQ_ERR_INVALID_ARG;
+    for (int k = 0; k < i; ++k)
+      if (overlap(out[i], out[k])) return SEEDQ_ERR_INVALID_ARG;
+  }
   PagesArgs a{p.n_groups, p.n_beams, c.page_size, log2_of(c.page_size), p.table_width, p.free_capacity, p.table_stride, p.out_stride,
               p.parents, p.seq_lens, p.block_table, p.free_count, p.table_out, p.free_pages, p.seq_lens_out, p.status, p.free_count_out,
               (Workspace *)p.workspace};

@@ -149,3 +149,17 @@ def test_select_refuses_overlaps(Q, kw):
              score=3 * FAKE, beam=4 * FAKE, token=5 * FAKE, work=FAKE, bytes=1 << 40)
     a.update(kw)
     assert Q.lib().seedq_beam_select(C.byref(Q.BeamSelectArgs(*a.values())), None) == 1
+
+
+@pytest.mark.parametrize("kw", [
+    dict(lens_out=3 * FAKE - 28), dict(lens_out=2 * FAKE + 4), dict(lens_out=4 * FAKE), dict(lens_out=7 * FAKE),  # over inputs, moved
+    dict(status=2 * FAKE + 28), dict(status=3 * FAKE + 4), dict(status=8 * FAKE - 28), dict(left=2 * FAKE + 12), dict(left=3 * FAKE + 8),
+    dict(left=9 * FAKE + 4), dict(left=8 * FAKE + 28), dict(left=6 * FAKE + 12),  # over other outputs
+    dict(out=4 * FAKE + 4), dict(out=4 * FAKE - 32 * 7), dict(out=4 * FAKE + 4, ostride=9), dict(out=6 * FAKE - 64), dict(out=9 * FAKE), dict(out=2 * FAKE - 8),
+    dict(free=4 * FAKE + 32 * 7), dict(free=2 * FAKE), dict(free=3 * FAKE + 28), dict(free=8 * FAKE)])
+def test_reorder_refuses_overlaps(Q, kw):
+    a = dict(groups=2, beams=4, parents=2 * FAKE, lens=3 * FAKE, table=4 * FAKE, stride=8, out=4 * FAKE, ostride=8, width=8, cap=4,
+             free=6 * FAKE, count=7 * FAKE, lens_out=8 * FAKE, status=9 * FAKE, left=10 * FAKE, work=11 * FAKE, bytes=1 << 20)
+    a.update(kw)
+    caches = (Q.KvCacheDesc * 1)(Q.KvCacheDesc(0, 2, 64, 16, 4, 20 * FAKE, 21 * FAKE, 22 * FAKE, 23 * FAKE, 2 * 16 * 64, 16 * 64, 64))
+    assert Q.lib().seedq_beam_reorder(caches, 1, C.byref(Q.BeamReorderArgs(*a.values())), None) == 1
