@@ -123,8 +123,7 @@ __device__ __forceinline__ Lane lane_of(const AppendArgs &a, int u) {
   return {d, d + (D - 2 * a.half) / 2, 0, 0, 0, 0};
 }
 
-// cos and sin of the lane's pairs of token t; 1 and 0 where it has none, which leaves
-// numbers as they are (one that is not finite makes its page's scale a NaN anyway).
+// cos and sin of the lane's pairs of token t; what it has none of is not used.
 __device__ __forceinline__ void load_angles(const AppendArgs &a, const Lane &l, int64_t t, float2 (&c)[8]) {
   const float2 *cs = a.cs + t * a.half;
   if (a.wide_cs && l.n0 == 4 && l.n1 == 4) {
@@ -154,12 +153,18 @@ __device__ __forceinline__ void turn(const AppendArgs &a, const Lane &l, const f
         y[k] = second ? z.y : z.x;
       }
     }
-  } else if (l.n0 > 0) {
+  } else if (PAIRS == kAcross ? l.n0 > 0 : l.n0 + l.n1 == 8) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int i = PAIRS == kBeside ? 2 * k : k, j = PAIRS == kBeside ? 2 * k + 1 : 8 + k;
       const float2 z = turned(y[i], y[j], c[k]);
       y[i] = z.x, y[j] = z.y;
+    }
+  } else if (PAIRS == kBeside && l.n0 > 0) {  // pairs at the end of the rotated dims
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float2 z = turned(y[2 * k], y[2 * k + 1], c[k]);
+      if (k % 4 < (k < 4 ? l.n0 : l.n1)) y[2 * k] = z.x, y[2 * k + 1] = z.y;
     }
   }
 }

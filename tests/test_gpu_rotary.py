@@ -468,3 +468,19 @@ def test_append_rotary_from_a_fused_projection(V, n, h):
     for out in (k, v):
         with pytest.raises(V.Q.SeedQError):
             a.append_rotary(k, v, slots, rotary, cs, q=q[:, :h], q_out=out)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("dim,rot", [(128, 64), (64, 40), (32, 2), (112, 90), (48, 24), (16, 14)])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+def test_append_rotary_leaves_zeros_behind_the_rotation(V, kind, layout, dim, rot):
+    """Numbers from rot_dim on go into the cache as they are, a zero's sign among them."""
+    n, h, P = 21, 3, 16
+    rotary = V.Rotary(V.rotary_frequencies(rot)[0], layout)
+    cs = angles_of(V, rotary, list(range(7, 7 + n)))
+    x = torch.randn((2, n, h, dim), generator=torch.Generator("cuda").manual_seed(dim), device="cuda")
+    x[..., rot:] = torch.where(x[..., rot:] > 0.5, x[..., rot:], torch.where(x[..., rot:] > -0.5, -0.0, 0.0))
+    a, b = (new_cache(V, 2, h, P, dim, kind) for _ in range(2))
+    both_ways(V, a, b, x[0], x[1], torch.arange(n, device="cuda"), rotary, cs)
+    code = torch.where(x[0, :P, :, rot:].signbit(), 0x80 if kind == "e4m3" else 0, 0)[x[0, :P, :, rot:] == 0]
+    assert torch.equal(a.k[0].transpose(0, 1)[..., rot:][x[0, :P, :, rot:] == 0], code.byte())
