@@ -746,3 +746,169 @@ def test_beam_search_of_a_prompt_beside_one_without_pages(G, first, n_pages):
         rows = follow(d, short, tokens)
         want = sum(row[t] for row, t in zip(rows, tokens))
         assert abs(float(scores[1, r]) - want) <= 0.02 * sum(np.abs(row).max() for row in rows)
+
+
+# ---------------------------------------------------------------- large batches (100 MB of logits and more: warps stream through them)
+
+def large_logits(dtype, rows, v, stride, gen):
+    assert rows * v * torch.empty(0, dtype=DT[dtype]).element_size() >= 96 << 20 and v >= 16384
+    flat = torch.full((rows, stride), float("nan"), dtype=DT[dtype], device="cuda")  # between rows: nothing that may be read
+    x = flat[:, :v]
+    for r in range(0, rows, 64):
+        x[r:r + 64] = 3 * torch.randn((min(64, rows - r), v), generator=gen, device="cuda")
+    return x
+
+
+@pytest.mark.parametrize("dtype,g,b,v,stride,n,scale", [("f32", 63, 8, 50003, 50008, 5, 0.7), ("bf16", 126, 8, 50003, 50008, 8, 1.0),
+                                                        ("f16", 100, 4, 128256, 128256, 3, 1.5), ("bf16", 30, 32, 56001, 56008, 32, 1.0),
+                                                        ("f32", 1501, 1, 16777, 16780, 2, 1.0)])
+def test_select_large(V, dtype, g, b, v, stride, n, scale):
+    """Every request of a large batch against the oracle: masked tokens and rows, finished and empty beams, weights,
+    and requests spoiled by a logit, a score or a weight."""
+    def check(seed):
+        rng, gen = np.random.RandomState(g + b + 1000 * seed), torch.Generator("cuda").manual_seed(v + seed)
+        x = large_logits(dtype, g * b, v, stride, gen)
+        for r in rng.randint(0, g * b, g):
+            x[r, rng.randint(0, v, v // 3)] = -float("inf")
+        x[rng.randint(0, g * b, 3)] = -float("inf")
+        scores = (-5 + 2 * rng.randn(g, b)).astype(np.float32)
+        scores[rng.rand(g, b) < 0.1] = -np.inf
+        done = rng.rand(g, b) < 0.2
+        weights = (rng.randint(3, 30, (g, b)) ** -0.7).astype(np.float32)
+        scores[:5, 0], done[:5, 0] = -1.0, False
+        x[0, v - 1], x[b, 4096] = float("nan"), float("inf")
+        scores[2, 0], weights[3, 0], scores[4, 0] = np.nan, 0.0, np.inf
+        return check_select(V, x, scores, n, scale, done, int(rng.randint(v)), weights)
+
+    some(check)
+
+
+@pytest.mark.parametrize("dtype,rows", [("f32", 200), ("bf16", 400), ("f16", 400)])
+def test_select_equal_rows_of_a_large_batch(V, dtype, rows):
+    """Equal rows, dealt to the SMs at other places each: scores that are each token's log probability and equal to the
+    bit, ties by beam and token."""
+    v, b, n = 128256, 5, 12
+    g = rows // b
+    row = (3 * torch.randn(v, generator=torch.Generator("cuda").manual_seed(7), device="cuda")).to(DT[dtype])
+    x = row.expand(rows, v).contiguous()
+    assert x.nbytes >= 96 << 20
+    scores = torch.zeros((g, b), device="cuda")
+    scores[7], scores[8, :4], scores[9, 0] = -float("inf"), -float("inf"), -float("inf")
+    score, beam, token = select(V, x, scores, n)
+    logp = torch.log_softmax(row.double(), 0)
+    order = torch.sort(row.float(), descending=True, stable=True)
+    ties = [order.indices[order.values == y].tolist() for y in torch.unique(order.values).flip(0)[:n]]
+    of_token = {}
+    for i in range(g):
+        beams = [] if i == 7 else [4] if i == 8 else [1, 2, 3, 4] if i == 9 else list(range(b))
+        want = [(k, t) for same in ties for k in beams for t in same][:n] or [(-1, -1)] * n
+        assert list(zip(beam[i].tolist(), token[i].tolist())) == want
+        for t, s in zip(token[i].tolist(), score[i].tolist()):
+            if t < 0:
+                assert s == -float("inf")
+                continue
+            assert abs(s - float(logp[t])) <= OFF + abs(s) * U
+            assert of_token.setdefault(float(row[t]), s) == s
+
+
+def test_select_nothing_alive_in_a_batch_that_streams(V):
+    """Requests of finished, empty and masked beams between live ones, 100 MB of logits; the workspace stays good."""
+    g, b, v = 260, 3, 32768
+    x = torch.randn((g * b, v), device="cuda")
+    assert x.nbytes >= 96 << 20
+    done = torch.zeros((g, b), dtype=torch.bool, device="cuda")
+    done[::3] = True
+    scores = torch.randn((g, b), device="cuda")
+    scores[::5] = -float("inf")
+    x[3:6] = -float("inf")
+    x[9:12] = float("nan")  # request 3: finished, so nothing of it is read
+    work = V.beam_workspace(g, b, v)
+    for _ in range(3):
+        score, beam, token = (t.tolist() for t in select(V, x, scores, 2, done=done, end=9, work=work))
+        for i in range(g):
+            if i % 5 == 0 or i == 1:
+                assert beam[i] == token[i] == [-1, -1] and score[i] == [-float("inf")] * 2
+            elif i % 3 == 0:
+                assert token[i] == [9, 9] and score[i] == torch.sort(scores[i], descending=True).values[:2].tolist()
+                assert score[i] == [float(scores[i, k]) for k in beam[i]]
+            else:
+                assert min(beam[i]) >= 0 and score[i][0] >= score[i][1] > -20
+    scores[:] = -float("inf")  # nobody's
+    got = select(V, x, scores, 2, done=done, end=9, work=work)
+    assert bool((got[0] == -float("inf")).all()) and bool((got[1] == -1).all()) and bool((got[2] == -1).all())
+    assert int(work[:2 * 8192 * 4 + 16].max()) == 0
+
+
+# ---------------------------------------------------------------- pages of models of real size (copies by a launch of their own)
+
+LARGE = [(32, 8, 16, 600, 40, 2, 8, 128, "head"), (120, 4, 16, 1400, 90, 1, 2, 64, "token"), (60, 6, 48, 4000, 84, 3, 2, 80, "token"),
+         (9, 32, 32, 2000, 63, 70, 1, 64, "head")]
+
+
+def copies_apart(g, b, page, layers, heads, dim, width):
+    """More than 1 MB may have to be copied, and the lists take more CTAs than one."""
+    return g * b * layers * 2 * heads * (page - 1) * dim > 1 << 20 and g * -(-width // 32) > 16
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("g,b,page,most,width,layers,heads,dim,order", LARGE)
+def test_reorder_large(V, in_place, g, b, page, most, width, layers, heads, dim, order):
+    assert copies_apart(g, b, page, layers, heads, dim, width)
+    rng = np.random.RandomState(g + b)
+    gen = torch.Generator("cuda").manual_seed(g)
+    for kind in range(3):
+        spare = g * b if kind < 2 else g  # a stack that runs out
+        lens, table, free, n = beams_state(rng, g, b, page, most, width, spare, first=kind == 0)
+        parents = np.zeros((g, b), np.int32) if kind == 0 else np.minimum(rng.geometric(0.5, (g, b)) - 1, b - 1).astype(np.int32)
+        if kind:
+            parents[rng.rand(g) < 0.1] = -1
+            parents[rng.rand(g, b) < 0.05] = -1
+        caches = make_caches(V, layers, n, heads, page, dim, order, gen)
+        want = check_reorder(V, caches, parents, lens, table, free, spare, in_place)
+        assert len(want[5]) > 8
+        del caches
+
+
+def test_reorder_large_captured_and_replayed(V):
+    """Both launches in a graph, replayed with other parents, each against the oracle; and the graph beside calls on another stream."""
+    g, b, page, most, width, layers, heads, dim, order = LARGE[0]
+    rng = np.random.RandomState(11)
+    i32 = lambda x: torch.as_tensor(np.asarray(x, np.int32)).cuda()  # noqa: E731
+    lens, table, free, n = beams_state(rng, g, b, page, most, width, g * b)
+    caches, others = (make_caches(V, layers, n, heads, page, dim, order, torch.Generator("cuda").manual_seed(3)) for _ in range(2))
+    start = [t.clone() for c in caches for t in (c.k, c.v, c.k_scale, c.v_scale)]
+    state = lambda cs: [t for c in cs for t in (c.k, c.v, c.k_scale, c.v_scale)]  # noqa: E731
+    pages, beside = V.BeamPages(caches, g, b), V.BeamPages(others, g, b)
+    parents, t, f, cnt, ln = i32(np.zeros((g, b))), i32(table), i32(free), i32([g * b]), i32(lens)
+    to = torch.full_like(t, -9)
+    s, other = torch.cuda.Stream(), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        pages.reorder(parents, ln, t, f, cnt, out=to)
+    for _ in range(3):
+        p = np.minimum(rng.geometric(0.5, (g, b)) - 1, b - 1).astype(np.int32)
+        p2 = p[::-1].copy()
+        parents.copy_(i32(p))
+        f.copy_(i32(free))
+        to.fill_(-9)
+        f2, to2, parents2 = i32(free), torch.full_like(t, -9), i32(p2)
+        for now in (caches, others):
+            for x, y in zip(state(now), start):
+                x.copy_(y)
+        torch.cuda.synchronize()
+        graph.replay()
+        beside.reorder(parents2, ln, t, f2, cnt, out=to2, stream=other)
+        torch.cuda.synchronize()
+        for q, now, got_to, got_f, obj in ((p, caches, to, f, pages), (p2, others, to2, f2, beside)):
+            want = S.beam_reorder(q, lens, table, np.full_like(table, -9), free, g * b, page)
+            for x, y in ((got_to, want[0]), (obj.seq_lens, want[1]), (obj.status, want[2]), (got_f, want[3]), (obj.free_count[0], want[4])):
+                assert np.array_equal(x.cpu().numpy(), y)
+            model = [x.clone() for x in start]
+            for src, dst, used in want[5]:
+                for i, x in enumerate(model):
+                    if i % 4 < 2:
+                        x[dst, :, :used] = x[src, :, :used]
+                    else:
+                        x[dst] = x[src]
+            assert all(torch.equal(x, y) for x, y in zip(state(now), model))

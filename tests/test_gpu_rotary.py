@@ -484,3 +484,97 @@ def test_append_rotary_leaves_zeros_behind_the_rotation(V, kind, layout, dim, ro
     both_ways(V, a, b, x[0], x[1], torch.arange(n, device="cuda"), rotary, cs)
     code = torch.where(x[0, :P, :, rot:].signbit(), 0x80 if kind == "e4m3" else 0, 0)[x[0, :P, :, rot:] == 0]
     assert torch.equal(a.k[0].transpose(0, 1)[..., rot:][x[0, :P, :, rot:] == 0], code.byte())
+
+
+# ---------------------------------------------------------------- large calls
+
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("ti,to,n,heads,dim,rot", [("bf16", "bf16", 4099, 41, 128, 128), ("f16", "f32", 4099, 38, 128, 64), ("bf16", "f16", 3001, 37, 96, 24),
+                                                   ("f16", "f16", 701, 39, 100, 50)])
+def test_rotate_large(V, layout, ti, to, n, heads, dim, rot):
+    """Heads four to a thread, numbers of them that four does not divide; out of place and in it."""
+    rng = np.random.RandomState(n + heads)
+    rotary = V.Rotary(V.rotary_frequencies(rot)[0], layout)
+    cs = angles_of(V, rotary, rng.randint(0, 131072, n).tolist())
+    x = torch.randn((n, heads, dim), generator=torch.Generator("cuda").manual_seed(n), device="cuda").to(DT[ti])
+    out = torch.full((n, heads, dim), 9.0, dtype=DT[to], device="cuda")
+    check_rotate(V, x, cs, rotary, layout, out)
+    if ti == to:
+        wide = torch.full((n, heads + 1, dim), 4.0, dtype=DT[ti], device="cuda")  # a head more, which stays
+        wide[:, :heads] = x
+        rotary.rotate(wide[:, :heads], cs, wide[:, :heads])
+        assert torch.equal(wide[:, :heads], out) and bool((wide[:, heads] == 4.0).all())
+
+
+@pytest.mark.parametrize("kind,dtype,layout,heads,q_heads,page,dim,rot,order,lens", [
+    ("int8", "bf16", "half", 8, 32, 16, 128, 128, "head", (1024, 1024, 1024, 1024)),
+    ("e4m3", "bf16", "half", 32, 32, 16, 128, 128, "head", (1024, 1024, 1024, 1024)),
+    ("int8", "f32", "pairs", 8, 9, 64, 128, 128, "token", (1500, 1, 700, 33)),
+    ("e4m3", "f16", "pairs", 32, 33, 256, 128, 64, "head", (1024, 300, 777)),
+    ("int8", "f16", "half", 9, 0, 256, 64, 64, "token", (2000, 1, 1, 1, 511)),
+    ("e4m3", "f32", "half", 11, 11, 240, 256, 64, "head", (900, 241)),
+    ("int8", "bf16", "half", 17, 0, 48, 96, 24, "token", (333, 1000)),
+    ("e4m3", "bf16", "pairs", 10, 40, 128, 112, 112, "head", (1025,)),
+    ("int8", "f32", "half", 64, 64, 256, 16, 6, "head", (600, 600))])
+def test_append_rotary_prompts(V, kind, dtype, layout, heads, q_heads, page, dim, rot, order, lens):
+    """Prompts whose heads a CTA takes several of, three times, on from where the last ended within a page (the first pieces small
+    numbers, the next ones larger, so that pages' scales grow): codes, scales and queries as of the rotation and the plain append."""
+    rng = np.random.RandomState(heads + dim)
+    most = [-(-3 * n // page) + 1 for n in lens]
+    pages = [p.tolist() for p in np.split(rng.permutation(sum(most)), np.cumsum(most)[:-1])]
+    a, b = (new_cache(V, sum(most), heads, page, dim, kind, order) for _ in range(2))
+    rotary = V.Rotary(V.rotary_frequencies(rot)[0], layout)
+    gen = torch.Generator("cuda").manual_seed(heads)
+    at = [int(x) for x in rng.randint(0, page, len(lens))]  # in the middle of a page, which holds what it held
+    for step, size in enumerate((0.01, 1.0, 30.0)):
+        slots = []
+        for i, n in enumerate(lens):
+            n = n if step != 1 else max(n - 5, 1)
+            slots += [pages[i][p // page] * page + p % page for p in range(at[i], at[i] + n)]
+            at[i] += n
+            if step == 2:
+                slots.append(-1)  # an unused token between requests
+        n = len(slots)
+        assert 2 * n * heads > 8192
+        odd = step if dtype != "f32" else 0  # rows that do not allow wide loads
+        flat = torch.zeros(2 * n * heads * dim + odd, dtype=DT[dtype], device="cuda")
+        x = flat[odd:].view(2, n, heads, dim)
+        x.copy_(size * torch.randn((2, n, heads, dim), generator=gen, device="cuda"))
+        x[:, ::7] *= 4
+        cs = angles_of(V, rotary, rng.randint(0, 100000, n).tolist())
+        q = torch.randn((n, q_heads, dim), generator=gen, device="cuda").to(DT[dtype]) if q_heads else None
+        q_out = torch.full((n, q_heads, dim), 5.0, dtype=DT[dtype if step else "bf16"], device="cuda") if q_heads else None
+        both_ways(V, a, b, x[0], x[1], torch.tensor(slots, device="cuda"), rotary, cs, q, q_out)
+        if q_heads and step:  # the same in place
+            turned = q.clone()
+            a.append_rotary(x[0], x[1], torch.full((n,), -1, device="cuda"), rotary, cs, q=turned, q_out=turned)
+            assert torch.equal(turned, q_out)
+            same(a, b)
+
+
+def test_append_rotary_prompts_captured_and_replayed(V):
+    """A prompts' write with its queries' own launch in a graph, replayed with other positions, numbers and slots."""
+    n, h, d, P = 1100, 8, 128, 16
+    rotary = V.Rotary(V.rotary_frequencies(d)[0])
+    a, b = (new_cache(V, 3 * (n // P + 1), h, P, d, "int8") for _ in range(2))
+    pos, slots = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int64, device="cuda")
+    x, q = torch.randn((2, n, h, d), device="cuda").bfloat16(), torch.randn((n, 5 * h, d), device="cuda").bfloat16()
+    cs, q_out = torch.empty((n, d // 2, 2), device="cuda"), torch.empty_like(q)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        rotary.angles(pos, cs)
+        a.append_rotary(x[0], x[1], slots, rotary, cs, q=q, q_out=q_out)
+    for i in range(3):
+        pos.copy_(torch.randint(0, 50000, (n,)))
+        slots.copy_(torch.arange(n) + i * (n + 3))
+        x.normal_()
+        q.normal_()
+        graph.replay()
+        want, turned = torch.empty_like(q), torch.empty((n, h, d), device="cuda")
+        rotary.rotate(q, cs, want)
+        rotary.rotate(x[0], cs, turned)
+        b.append(turned, x[1].float(), slots)
+        assert torch.equal(q_out, want)
+        same(a, b)
