@@ -912,3 +912,57 @@ def test_reorder_large_captured_and_replayed(V):
                     else:
                         x[dst] = x[src]
             assert all(torch.equal(x, y) for x, y in zip(state(now), model))
+
+
+# ---------------------------------------------------------------- the largest sizes
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_select_of_the_largest_vocabulary(V, dtype, odd):
+    """2^27 tokens, by streaming warps and (rows that do not allow wide loads) by a CTA per chunk: tokens exactly, the score
+    to the roundings of 2^14 sums of sums that an eighth of a row's chunks join (2^15 u at most, u = 2^-24; 2^13 sums of
+    2048 logits or more in order, and a term's own)."""
+    v, n = 1 << 27, 20
+    x = torch.randn(v + odd, generator=torch.Generator("cuda").manual_seed(odd), device="cuda").to(DT[dtype])[odd:].view(1, v)
+    x[0, [5, v // 2, v - 1]] = torch.tensor([9.0, 8.0, 10.0], device="cuda").to(DT[dtype])
+    score, beam, token = select(V, x, torch.zeros((1, 1), device="cuda"), n)
+    top = torch.topk(x[0].float(), 4 * n)
+    order = sorted(zip((-top.values).tolist(), top.indices.tolist()))[:n]
+    assert order[-1][0] < -float(top.values[-1])  # no ties at the end
+    assert token[0].tolist() == [t for _, t in order] and token[0, :3].tolist() == [v - 1, 5, v // 2] and bool((beam == 0).all())
+    lse = float(torch.logsumexp(x[0].double(), 0))
+    for s, (z, _) in zip(score[0].tolist(), order):
+        assert abs(s - (-z - lse)) <= 2.0 ** -9 + abs(s) * U
+
+
+@pytest.mark.parametrize("g,b,v", [(8192, 1, 16384), (256, 32, 16384), (8192, 1, 200), (256, 32, 300)])
+def test_select_of_the_most_rows(V, g, b, v):
+    """8192 rows, streaming and not, two thirds of whose requests bring nothing or one finished beam: as in smaller batches."""
+    x = (3 * torch.randn((g * b, v), generator=torch.Generator("cuda").manual_seed(b), device="cuda")).half()
+    scores = torch.rand((g, b), generator=torch.Generator("cuda").manual_seed(v), device="cuda") - 3
+    done = torch.zeros((g, b), dtype=torch.bool, device="cuda")
+    scores[1::3], done[2::3] = -float("inf"), True
+    work = V.beam_workspace(g, b, v)
+    for _ in range(2):
+        score, beam, token = select(V, x, scores, 3, done=done, end=7, work=work)
+        assert bool((token[1::3] == -1).all()) and bool((score[1::3] == -float("inf")).all())
+        best = scores[2::3].topk(min(b, 3), 1)
+        assert torch.equal(score[2::3, :min(b, 3)], best.values) and bool((token[2::3, :min(b, 3)] == 7).all())
+        live = torch.arange(0, g, 3, device="cuda")
+        total = torch.log_softmax(x.double().view(g, b, v)[live], 2) + scores[live].double()[..., None]
+        want = total.flatten(1).topk(4, 1)
+        apart = (want.values[:, :3] - want.values[:, 1:] > 2 * OFF).all(1)  # no neighbours too close to tell, and no ties
+        assert float(apart.double().mean()) > 0.7
+        got = (beam[live].long() * v + token[live])[apart]
+        assert torch.equal(got, want.indices[:, :3][apart])
+        assert bool(((score[live].double() - want.values[:, :3]).abs() <= OFF + want.values[:, :3].abs() * U).all())
+    assert int(work[:2 * 8192 * 4 + 16].max()) == 0
+
+
+@pytest.mark.parametrize("g,b,page,most,width", [(8192, 1, 16, 40, 3), (256, 32, 16, 60, 4), (1, 4, 16, 300000, 18750), (2, 32, 16, 20000, 1250)])
+def test_reorder_of_the_most_rows_and_the_longest_lists(V, g, b, page, most, width):
+    rng = np.random.RandomState(g + width)
+    for in_place in (True, False):
+        lens, table, free, n = beams_state(rng, g, b, page, most, width, g * b)
+        parents = rng.randint(-1, b, (g, b)).astype(np.int32)
+        check_reorder(V, make_caches(V, 1, n, 1, page, 16, "head", torch.Generator("cuda").manual_seed(g)), parents, lens, table, free, g * b, in_place)

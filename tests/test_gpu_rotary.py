@@ -578,3 +578,42 @@ def test_append_rotary_prompts_captured_and_replayed(V):
         b.append(turned, x[1].float(), slots)
         assert torch.equal(q_out, want)
         same(a, b)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("heads,dim,page,reps", [(2, 32, 32, 1), (40, 128, 64, 60)])
+def test_append_rotary_runs_of_a_page_in_any_order(V, kind, heads, dim, page, reps):
+    """Runs of one page's slots that go back, meet or repeat a slot: as calls of their own, one after the other."""
+    rng = np.random.RandomState(heads)
+    rotary = V.Rotary(V.rotary_frequencies(dim)[0])
+    once = [[5, 6, 7], [5], [5], [3, 4], [0, 1], [30, 31], [2], [2, 3, 4, 5, 6, 7, 8], [9], list(range(page))[10:], [0]]
+    a, b, c = (new_cache(V, reps, heads, page, dim, kind) for _ in range(3))
+    slots = [p * page + s for p in range(reps) for run in once for s in run]
+    x = torch.from_numpy((2.0 ** rng.randint(-6, 6, (2, len(slots), 1, 1)) * rng.randn(2, len(slots), heads, dim)).astype(np.float32)).cuda()
+    cs = angles_of(V, rotary, rng.randint(0, 9999, len(slots)).tolist())
+    both_ways(V, a, b, x[0], x[1], torch.tensor(slots, device="cuda"), rotary, cs)
+    cuts = [0] + [i for i in range(1, len(slots)) if slots[i] != slots[i - 1] + 1] + [len(slots)]  # what follows on is one run
+    for at, to in zip(cuts, cuts[1:]):
+        if slots[at] < 5 * page:
+            c.append_rotary(x[0, at:to], x[1, at:to], torch.tensor(slots[at:to], device="cuda"), rotary, cs[at:to])
+    for y, z in ((a.k, c.k), (a.v, c.v), (a.k_scale, c.k_scale), (a.v_scale, c.v_scale)):
+        assert torch.equal(y[:5], z[:5])
+
+
+def test_append_rotary_of_the_most_heads(V):
+    """1024 heads of 16 dims, a few tokens and some prompts' worth."""
+    rotary = V.Rotary(V.rotary_frequencies(16)[0])
+    for n in (3, 200):
+        a, b = (new_cache(V, 20, 1024, 16, 16, "int8") for _ in range(2))
+        x = torch.randn((2, n, 1024, 16), device="cuda").half()
+        q = torch.randn((n, 3000, 16), device="cuda").half()
+        cs = angles_of(V, rotary, list(range(n)))
+        both_ways(V, a, b, x[0], x[1], torch.arange(n, device="cuda") + 7, rotary, cs, q, torch.empty_like(q))
+
+
+def test_rotate_the_most_heads_and_the_widest(V):
+    for n, heads, dim, rot in ((2, 65536, 2, 2), (1, 65536, 16, 10), (5, 3, 1024, 1024)):
+        for layout in ("half", "pairs"):
+            rotary = V.Rotary(V.rotary_frequencies(rot)[0], layout)
+            x = torch.randn((n, heads, dim), device="cuda")
+            check_rotate(V, x, angles_of(V, rotary, list(range(n))), rotary, layout, torch.empty_like(x))
