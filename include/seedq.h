@@ -586,8 +586,8 @@ seedq_status seedq_token_logprobs(const void *logits, int32_t dtype, int64_t n_r
  *   out_score[g][i]  the total, not weighted; out_beam[g][i] the beam b;
  *   out_token[g][i]  the token.  Past the candidates -inf, -1 and -1.
  * Beams are compared at 46 bits, their log sums are float32's.  A request with a
- * score of NaN or +inf, a weight that is not positive and finite (both only of
- * beams that bring anything) or a NaN or +inf among a live beam's logits gets NaN,
+ * score of NaN or +inf, a weight that is not positive and finite (of a beam whose
+ * score is not -inf) or a NaN or +inf among a live beam's logits gets NaN,
  * -1 and -1 everywhere.  Logits of done beams and of those with score -inf are not
  * read.
  *   logits     device, row r at r * row_stride elements of type dtype.

@@ -13,7 +13,7 @@
 // The copies are units of one head and tensor of one layer and page, dealt to all
 // warps: of a second launch, or, where they are small, of the first.
 //
-// Measured: 4 requests of 4 beams of 600 tokens, 32 layers of 8 heads of 128, 8.5 us
+// Measured: 4 requests of 4 beams of 600 tokens, 32 layers of 8 heads of 128, 8.4 us
 // (the lists 6: launch, six dependent trips to memory and two barriers of the
 // cluster); 32 requests of 8 beams, 8 layers, 22 us, of which the copies (67 MB) take
 // 11 to 12 (5.8 TB/s).
@@ -35,7 +35,7 @@ namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32;
 constexpr int kMaxBeams = SEEDQ_MAX_BEAMS;
-constexpr int kMaxCluster = 8;  // one CTA takes 33 us instead of 23 for 32 requests of 8 beams
+constexpr int kMaxCluster = 8;  // one CTA takes 27.5 us instead of 21.8 for 32 requests of 8 beams
 constexpr int kAtOnce = 8;      // rows of a tile under way
 constexpr int kLayersAtOnce = 64;  // whose pointers go in a launch's parameters
 // What may have to be copied, up to which the first launch does it: a fork of 2 small
@@ -71,7 +71,7 @@ struct CopyArgs {
   uint8_t *codes[kLayersAtOnce][2];
   float *scales[kLayersAtOnce][2];
 };
-constexpr int kCopyAhead = 8;  // loads of 16 bytes that a lane has under way (4: 25.4 us instead of 23.5)
+constexpr int kCopyAhead = 8;  // loads of 16 bytes that a lane has under way (4: 23.7 us instead of 21.8, 16: 34)
 
 // What warp `me` of `warps` copies of the first n entries of the list.
 __device__ __forceinline__ void copy_pages(const CopyArgs &a, int n, int64_t me, int64_t warps) {

@@ -15,13 +15,19 @@
 // again, and chooses from their logits.  Each choice is by a float32 bound that at
 // least n reach, then by counting, for each of the few that do, how many precede it.
 //
-// Measured, n = twice the beams: a request of 4 beams of 32000 logits 8.5 us, 4
-// requests of 4 beams of 128256 10.4 (the pass over the logits 3.9: launch, one trip
-// to memory, an arrival), 64 of 8 beams of 128256 bfloat16 35 us (the pass 24, 4.4
-// TB/s).  The join is a chain of about fifteen trips to L2 or shared memory and
-// barriers of one CTA, 5 to 7 us (sorted lists of 32 took 9 to 19), and many requests'
-// joins fall at the end.  Segments of 256: what is read again is 1 KB a candidate, and
-// a row of 128256 has 501 maxima, one look of a CTA at 4 beams.
+// Measured, n = twice the beams (the first: as many): a request of 4 beams of 32000
+// logits 8.8 us, 4 requests of 4 beams of 128256 10.3 (the pass over the logits 3.9:
+// launch, one trip to memory, an arrival), 64 of 8 beams of 128256 bfloat16 35 us (the
+// pass 24, 4.4 TB/s).  The join is a chain of about fifteen trips to L2 or shared memory
+// and barriers of one CTA, 5 to 7 us alone and 8.3 beside sixty others (sorted lists of
+// 32 took 9 to 19), and many requests' joins fall at the end.  Segments of 256: what is
+// read again is 1 KB a candidate, and a row of 128256 has 501 maxima, one look of a CTA
+// at 4 beams.
+//
+// Where live beams have fewer segments than candidates are wanted, nothing bounds the
+// chosen segments' logits; more than 256 of them are chosen one after another (one live
+// beam of 300 logits, 4 chosen: 27 us; of 1000, 8 chosen: 44; 32 of 300, 32 chosen:
+// 129), as are about equal totals and numbers whose bounds float32 does not hold.
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <stdint.h>
@@ -278,9 +284,9 @@ __device__ __forceinline__ void push(Join &s, int b, float x, int index) {
   if (at < kMaxFound) s.found_x[at] = x, s.found_at[at] = (uint32_t)b << kTokenBits | (uint32_t)index;
 }
 
-// For rows in which more than fit are about equal, or numbers too large for the
-// bounds: the n first one after another.  each(f) calls f(beam, logit, index) for
-// all that the thread sees.
+// For rows in which more than fit are about equal or nothing bounds them, or numbers
+// too large or small for the bounds: the n first one after another.  each(f) calls
+// f(beam, logit, index) for all that the thread sees.
 template <typename Each>
 __device__ __forceinline__ void choose_slowly(const SelectArgs &a, Join &s, Each each) {
   Item last = {~0ull, ~0ull};
