@@ -26,8 +26,9 @@
 //
 // Where live beams have fewer segments than candidates are wanted, nothing bounds the
 // chosen segments' logits; more than 256 of them are chosen one after another (one live
-// beam of 300 logits, 4 chosen: 27 us; of 1000, 8 chosen: 44; 32 of 300, 32 chosen:
-// 129), as are about equal totals and numbers whose bounds float32 does not hold.
+// beam of 300 logits, 4 chosen: 27 us; of 1000, 8 chosen: 44; of 7900, 32 chosen: 769,
+// and 8000 10.9), as are about equal totals and numbers whose bounds float32 does not
+// hold.
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <stdint.h>
