@@ -663,8 +663,8 @@ seedq_status seedq_beam_select(const seedq_beam_select_args *args, void *cuda_st
  * seq_lens_out may be seq_lens and free_count_out free_count (an earlier call's
  * outputs); beyond that no output (free_pages among them) lies on another or on an
  * input.
- * Errors: INVALID_ARG (NULL pointer, other outputs over one another or over inputs, n_caches outside
- * 1..SEEDQ_BEAM_MAX_CACHES, caches that differ, n_beams outside
+ * Errors: INVALID_ARG (NULL pointer, other outputs over one another or over inputs,
+ * n_caches outside 1..SEEDQ_BEAM_MAX_CACHES, caches that differ, n_beams outside
  * 1..SEEDQ_MAX_BEAMS, rows outside 1..SEEDQ_MAX_REQUESTS, table_width outside
  * 1..2^20 or above a stride, free_capacity below n_pages, workspace too small),
  * UNSUPPORTED (as the cache calls), CUDA. */

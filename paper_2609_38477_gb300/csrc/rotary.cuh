@@ -122,7 +122,7 @@ inline RotateSplit rotate_split(const RotateArgs &a, int32_t in, int32_t out) {
 }
 
 // Whether out lies on itself, on cos and sin, or on x elsewhere than where it is x: a
-// thread writes what it alone has read, or nobody.
+// thread may write only what no other reads.
 inline bool rotate_overlaps(const RotateArgs &a, int32_t in) {
   const Wide ib = dtype_bytes(in), ob = dtype_bytes(a.out_dtype);
   const ByteRows out = byte_rows(a.out, a.dim * ob, a.n, a.ot * ob, a.heads, a.oh * ob);
